@@ -308,8 +308,8 @@ def _softmax_parts(scores, seen):
 def _run_paged(s):
     c = s["case"]
     if own:
-        rr, ws = _keep(s, **({"routes": s["routes"]} if c["k"] else {}))
         more = dict(routes=s["routes"], n_sink=c["sinks"], n_recent=c["recent"]) if c["k"] else {}
+        rr, ws = _keep(s, **more)
         return rr.paged_attention(s["Q"], s["K_cache"], s["V_cache"], s["table"], s["lengths"], workspace=ws,
                                   k_scale=s["k_scale"], v_scale=s["v_scale"], **more)
     if c["k"]:
