@@ -56,7 +56,8 @@ typedef enum {
     RR_ERR_UNSUPPORTED = -5  /* valid but outside the shapes the library supports */
 } rr_status;
 
-typedef enum { RR_F32 = 0, RR_BF16 = 1 } rr_dtype;
+/* (RR_E4M3, eight bits of the OCP e4m3 form, is a type of paged caches only.) */
+typedef enum { RR_F32 = 0, RR_BF16 = 1, RR_E4M3 = 2 } rr_dtype;
 
 /* Shape and rule parameters.  Supported: d in {32, 64, 128} (and 256 for
  * bf16); 1 <= k <= n_k; k + m <= 128; k + m + r + n_sink + n_recent <= 256;
@@ -251,7 +252,10 @@ typedef enum {
     RR_KERNEL_POOL = 5,     /* chunk pooling */
     RR_KERNEL_EXPAND = 6,   /* token expansion */
     RR_KERNEL_ATTENTION = 7, /* sparse attention over routed chunks */
-    RR_KERNEL_KINDS = 8
+    RR_KERNEL_APPEND = 8,   /* new tokens into the paged cache */
+    RR_KERNEL_PAGED = 9,    /* attention over the paged cache */
+    RR_KERNEL_JOIN = 10,    /* its parts joined */
+    RR_KERNEL_KINDS = 11
 } rr_kernel_kind;
 
 rr_status rr_profile_start(void);
@@ -335,6 +339,128 @@ typedef struct {
 
 rr_status rr_sparse_attention(const rr_attn_config *cfg, const void *Q, const void *K, const void *V,
                               const int32_t *routes, void *O, void *hip_stream);
+
+/* ------------------------------------------------------------------------
+ * The paged cache: keys and values of a batch of sequences that grow a few
+ * tokens at a time, and attention of their newest tokens.
+ *
+ * A cache is two pools K_cache and V_cache, [n_pages, n_kv_heads, page, d]
+ * each: page p holds `page` consecutive tokens of one sequence (or of several
+ * that begin alike).  Token u of sequence b lies in page page_table[b][u /
+ * page] at place u % page; page_table is [n_seqs, max_pages] int32.  A page is
+ * a chunk: rr_pool_chunks over a pool taken as [n_pages * n_kv_heads, page, d]
+ * gives the representations of whole pages, and rr_full_route with n_q = 1
+ * and the batch folded into the heads routes over them.
+ *
+ * lengths [n_seqs] int32 counts each sequence's tokens, those new in this
+ * step included, for the append and for the attention after it.  Entries of
+ * page_table outside [0, n_pages) hold no page: nothing is written there and
+ * no query sees their tokens.  Lengths are taken between 0 and max_pages *
+ * page.  Sequences may share pages that none of them writes.
+ *
+ * Types: dtype RR_BF16 with cache_dtype RR_BF16 or RR_E4M3, or RR_F32 with
+ * RR_F32.  An RR_E4M3 cache holds x / scale of key head g, k_scale[g] for
+ * keys and v_scale[g] for values ([n_kv_heads] binary32, positive), rounded
+ * to nearest even, past the largest finite value (448) clamped to it.  The
+ * scales are NULL for other caches.
+ *
+ * Pointers to vectors that the attention reads (Q, the pools) or writes (O)
+ * and the workspace are 16-byte aligned (RR_ERR_INVALID otherwise).
+ * ---------------------------------------------------------------------- */
+
+typedef struct {
+    int32_t n_heads;      /* of Q; not read where Q is NULL */
+    int32_t n_kv_heads;
+    int32_t d;            /* a multiple of 8, at most 1024 */
+    int32_t page;         /* tokens a page */
+    int32_t n_pages;      /* pages of each pool */
+    int32_t max_pages;    /* page_table entries of a sequence */
+    int32_t n_seqs;
+    int32_t n_tokens;     /* new tokens, all sequences' (0: nothing to do) */
+    int32_t rot;          /* leading features of a head that are rotated: even, 0 .. d */
+    int32_t interleaved;  /* partners: 1: features 2j and 2j + 1; 0: j and j + rot / 2 */
+    int32_t dtype;        /* of K, V, Q and Q_out */
+    int32_t cache_dtype;
+    int64_t ldq, ldk, ldv;       /* elements from one token's rows to the next one's: >= heads * d, or 0 (one token's
+                                    rows for all) */
+    const float *k_scale, *v_scale;
+} rr_append_config;
+
+/* Appends new tokens: K and V [n_tokens, n_kv_heads, d] go into the pools,
+ * keys rotated by their positions; queries Q [n_tokens, n_heads, d] (or NULL)
+ * get the same rotation into Q_out [n_tokens, n_heads, d], which may be Q
+ * itself where ldq = n_heads * d and must not overlap it otherwise.  Tokens
+ * are packed: those of sequence b are tokens seq_start[b] .. seq_start[b+1] - 1
+ * ([n_seqs + 1] int32, ascending); NULL: n_tokens / n_seqs each.  The last one
+ * of sequence b is token lengths[b] - 1 of the sequence.  Tokens outside
+ * every sequence, and those that would lie before a sequence's first token
+ * or past its page table, are left out: their rows of Q_out keep what they
+ * held.  Position p turns partners (x, y) into (x cos a - y sin a, y cos a +
+ * x sin a), a = p * freqs[j], freqs [rot / 2] binary64 radians; angles are
+ * reduced in binary64, the rotation is computed in binary32 and rounded
+ * once.  Two new tokens must not lie in the same place.
+ * Returns RR_ERR_INVALID for bad sizes, types or NULL pointers. */
+rr_status rr_cache_append(const rr_append_config *cfg, const void *K, const void *V, const void *Q,
+                          const int32_t *seq_start, const int32_t *lengths, const int32_t *page_table,
+                          const double *freqs, void *K_cache, void *V_cache, void *Q_out, void *hip_stream);
+
+typedef struct {
+    int32_t n_heads;
+    int32_t n_kv_heads;
+    int32_t d;           /* 64, 128, or 256 for bf16 */
+    int32_t page;
+    int32_t n_pages;
+    int32_t max_pages;
+    int32_t n_seqs;
+    int32_t n_q;         /* query tokens of each sequence: its newest */
+    int32_t k;           /* route slots (0: no routes) */
+    int32_t n_sink;      /* with routes: first pages ... */
+    int32_t n_recent;    /* ... and last pages that every query sees besides */
+    int32_t n_prefix;    /* rr_prefix_attention: tokens that all sequences begin with (otherwise 0) */
+    int32_t dtype;       /* of Q and O */
+    int32_t cache_dtype;
+    float scale;         /* softmax scale; 0: 1/sqrt(d) */
+    int32_t reserved;    /* must be 0 */
+    const float *k_scale, *v_scale;
+} rr_paged_config;
+
+/* Bytes of workspace that rr_paged_attention and rr_prefix_attention need for
+ * a config (0: the config is not valid, see rr_last_error).  A workspace needs
+ * no initial contents; calls that may run at the same time need one each. */
+size_t rr_paged_workspace_bytes(const rr_paged_config *cfg);
+
+/* Attention of the newest n_q tokens of every sequence over its cache (Sec.
+ * 2.2 Eq. (3) where a token is all that is new): query t of Q [n_seqs, n_q,
+ * n_heads, d] stands at position p = lengths[b] - n_q + t of sequence b and
+ * attends, with one softmax scaled by `scale`, to the sequence's tokens u <= p;
+ * query head h reads key head h / (n_heads / n_kv_heads).  A query that sees
+ * no token (p < 0) gets a zero output.
+ *   routes  NULL with k = 0: every token; else [n_seqs * n_heads * n_q, k]
+ *           int32 (row (b * n_heads + h) * n_q + t) page indices within the
+ *           sequence: the query sees the tokens u <= p of those pages, of its
+ *           first n_sink and of the n_recent up to the one that holds p, each
+ *           once; other slots (-1, or a page that begins after p) are skipped.
+ *           k + n_sink + n_recent <= 256, any of them may be 0.
+ *   O       [n_seqs, n_q, n_heads, d] of dtype.
+ *   lse     optional [n_seqs, n_q, n_heads] binary32: the logarithm of the sum
+ *           of exp(scaled score), -INFINITY where no token is seen.
+ * Scores, softmax and sums in binary32; with bf16 queries the softmax weights
+ * enter the value product as the sum of two bf16 numbers.  Tokens that a
+ * query does not see have no part in its output, whatever their rows hold.
+ * Returns RR_ERR_INVALID for bad sizes, NULL or unaligned pointers or a
+ * workspace too small, RR_ERR_UNSUPPORTED for other types or d. */
+rr_status rr_paged_attention(const rr_paged_config *cfg, const void *Q, const void *K_cache, const void *V_cache,
+                             const int32_t *page_table, const int32_t *lengths, const int32_t *routes, void *O,
+                             float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The same without routes for sequences whose first n_prefix tokens are the
+ * same: prefix_pages [ceil(n_prefix / page)] int32 holds their pages (in the
+ * last one the first n_prefix % page places, if any), which are read for the
+ * whole batch at once; page_table serves the tokens from n_prefix on (its
+ * earlier entries are not read, n_prefix may lie inside a page). */
+rr_status rr_prefix_attention(const rr_paged_config *cfg, const void *Q, const void *K_cache, const void *V_cache,
+                              const int32_t *page_table, const int32_t *lengths, const int32_t *prefix_pages, void *O,
+                              float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -3,7 +3,7 @@
 Each HIP source is compiled to an object under ``_build/`` in parallel and the
 objects are linked into ``paper_2609_07306_amd/librouterelay.so``.  Packed
 binary32 VALU instructions are disabled (``-packed-fp32-ops``); device
-code is compiled with ``-fno-honor-nans``.
+code is compiled with ``-fno-honor-nans``, except for the paged cache's.
 """
 from __future__ import annotations
 
@@ -17,7 +17,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "librouterelay.so")
-SOURCES = ["rr_api.hip", "rr_route.hip", "rr_rescore.hip", "rr_rescore_dense.hip", "rr_consumer.hip"] + [
+SOURCES = ["rr_api.hip", "rr_route.hip", "rr_rescore.hip", "rr_rescore_dense.hip", "rr_consumer.hip",
+           "rr_append.hip", "rr_paged.hip"] + [
     f"rr_route_{t}_{m}.hip" for t in ("f32", "bf16") for m in ("full", "anchor", "reroute", "relay")]
 # the resident-score kernel: one object per caller, input type and width, all from
 # rr_resident_inst.hip; each is listed under the name its object takes
@@ -29,6 +30,8 @@ SOURCES += RESIDENT
 # addresses: the compiler's wave-level aggregation would only add a wait for the
 # returned value right behind each of them
 NO_ATOMIC_OPT = ("-mllvm", "-amdgpu-atomic-optimizer-strategy=None")
+# caches may hold anything where no token was written yet, NaN among it
+HONOR_NANS = {"rr_append.hip", "rr_paged.hip"}
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -48,6 +51,8 @@ def _compile(name: str) -> str:
     src, more = name, ()
     if name in RESIDENT:
         src, more = "rr_resident_inst.hip", RESIDENT[name] + NO_ATOMIC_OPT
+    if name in HONOR_NANS:
+        more = ("-Xarch_device", "-fhonor-nans")
     cmd = [HIPCC, *FLAGS, *more, "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

@@ -12,6 +12,7 @@
 
 #include "routerelay.h"
 #include "rr_internal.hpp"
+#include "rr_paged.hpp"
 #include "rr_rescore.hpp"
 
 struct rr_ledger {
@@ -943,4 +944,182 @@ rr_status rr_sparse_attention(const rr_attn_config *cfg, const void *Q, const vo
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     hipError_t e = timed(RR_KERNEL_ATTENTION, stream, [&] { return rr::launch_attention(a, stream); });
     return e == hipSuccess ? RR_OK : hip_fail(e, "attention launch");
+}
+
+// -------------------------------------------------------- the paged cache
+
+namespace {
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// What the append and the attention ask of a cache alike.
+rr_status check_cache(int32_t n_kv_heads, int32_t page, int32_t n_pages, int32_t max_pages, int32_t n_seqs, int32_t dtype,
+                      int32_t cache_dtype, const float *k_scale, const float *v_scale)
+{
+    if (n_kv_heads < 1 || page < 1 || n_pages < 1 || max_pages < 1 || n_seqs < 1)
+        return fail(RR_ERR_INVALID, "n_kv_heads, page, n_pages, max_pages and n_seqs must be >= 1");
+    if ((int64_t)max_pages * page > (1 << 30)) return fail(RR_ERR_INVALID, "max_pages * page must be at most 2^30");
+    if (dtype != RR_F32 && dtype != RR_BF16) return fail(RR_ERR_INVALID, "dtype must be RR_F32 or RR_BF16");
+    if (cache_dtype != dtype && !(dtype == RR_BF16 && cache_dtype == RR_E4M3))
+        return fail(RR_ERR_INVALID, "cache_dtype must be dtype, or RR_E4M3 with RR_BF16");
+    if ((k_scale != nullptr) != (cache_dtype == RR_E4M3) || (v_scale != nullptr) != (cache_dtype == RR_E4M3))
+        return fail(RR_ERR_INVALID, "k_scale and v_scale are given for RR_E4M3 caches, and for them only");
+    return RR_OK;
+}
+
+// The launch arguments of an attention call, its pointers apart.
+rr_status paged_args(const rr_paged_config *cfg, rr::PagedArgs *out)
+{
+    if (!cfg) return fail(RR_ERR_INVALID, "config is NULL");
+    const rr_paged_config &c = *cfg;
+    rr_status st = check_cache(c.n_kv_heads, c.page, c.n_pages, c.max_pages, c.n_seqs, c.dtype, c.cache_dtype, c.k_scale, c.v_scale);
+    if (st != RR_OK) return st;
+    if (c.n_heads < 1 || c.n_heads % c.n_kv_heads != 0)
+        return fail(RR_ERR_INVALID, "n_heads must be a positive multiple of n_kv_heads");
+    if (c.n_q < 1) return fail(RR_ERR_INVALID, "n_q must be >= 1");
+    if (c.k < 0 || c.n_sink < 0 || c.n_recent < 0 || (int64_t)c.k + c.n_sink + c.n_recent > rr::kMaxAttnSlots)
+        return fail(RR_ERR_INVALID, "k, n_sink and n_recent must be >= 0 and 256 together at most");
+    if (c.n_prefix < 0 || c.n_prefix > (1 << 30)) return fail(RR_ERR_INVALID, "n_prefix must lie in [0, 2^30]");
+    if (c.n_prefix > 0 && c.k + c.n_sink + c.n_recent > 0) return fail(RR_ERR_INVALID, "a shared prefix takes no routes");
+    if (c.reserved != 0) return fail(RR_ERR_INVALID, "rr_paged_config.reserved must be 0");
+    if (!(c.scale >= 0.f) || std::isinf(c.scale)) return fail(RR_ERR_INVALID, "scale must be finite and >= 0");
+    if (!rr::paged_supported(c.dtype, c.cache_dtype, c.d))
+        return fail(RR_ERR_UNSUPPORTED, "attention over a paged cache supports d = 64 and 128, and 256 for bf16 queries");
+    if ((int64_t)c.n_seqs * c.n_q > INT32_MAX / c.n_heads) return fail(RR_ERR_UNSUPPORTED, "too many query rows");
+    rr::PagedArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.k_scale = c.k_scale;
+    a.v_scale = c.v_scale;
+    a.n_heads = c.n_heads;
+    a.n_kv_heads = c.n_kv_heads;
+    a.group = c.n_heads / c.n_kv_heads;
+    a.n_pages = c.n_pages;
+    a.max_pages = c.max_pages;
+    a.n_seqs = c.n_seqs;
+    a.n_q = c.n_q;
+    a.capacity = c.max_pages * c.page;
+    a.k = c.k;
+    a.n_sink = c.n_sink;
+    a.n_recent = c.n_recent;
+    a.n_prefix = c.n_prefix;
+    a.pd = rr::page_div(c.page);
+    a.scale = c.scale > 0.f ? c.scale : 1.f / std::sqrt((float)c.d);
+    rr::paged_schedule(a, c.cache_dtype, c.d);
+    *out = a;
+    return RR_OK;
+}
+
+rr_status paged_call(const rr_paged_config *cfg, const void *Q, const void *K_cache, const void *V_cache,
+                     const int32_t *page_table, const int32_t *lengths, const int32_t *routes,
+                     const int32_t *prefix_pages, void *O, float *lse, void *workspace, size_t workspace_bytes,
+                     void *hip_stream)
+{
+    rr::PagedArgs a;
+    rr_status st = paged_args(cfg, &a);
+    if (st != RR_OK) return st;
+    if (!Q || !K_cache || !V_cache || !page_table || !lengths || !O || !workspace)
+        return fail(RR_ERR_INVALID, "Q, the caches, page_table, lengths, O and workspace must be device pointers");
+    if (!aligned16(Q) || !aligned16(K_cache) || !aligned16(V_cache) || !aligned16(O) || !aligned16(workspace))
+        return fail(RR_ERR_INVALID, "Q, the caches, O and workspace must be 16-byte aligned");
+    const size_t need = rr::paged_workspace_bytes(a, cfg->d);
+    if (workspace_bytes < need)
+        return fail(RR_ERR_INVALID, "the workspace has " + std::to_string(workspace_bytes) + " bytes of " + std::to_string(need));
+    a.Q = Q;
+    a.K = K_cache;
+    a.V = V_cache;
+    a.O = O;
+    a.lse = lse;
+    a.table = page_table;
+    a.lengths = lengths;
+    a.routes = routes;
+    a.prefix_pages = prefix_pages;
+    rr::paged_layout(a, cfg->d, workspace);
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    hipError_t e = timed(RR_KERNEL_PAGED, stream, [&] { return rr::launch_paged(a, cfg->cache_dtype, cfg->d, stream); });
+    if (e == hipSuccess)
+        e = timed(RR_KERNEL_JOIN, stream, [&] { return rr::launch_paged_join(a, cfg->cache_dtype, cfg->d, stream); });
+    return e == hipSuccess ? RR_OK : hip_fail(e, "paged attention launch");
+}
+
+}  // namespace
+
+rr_status rr_cache_append(const rr_append_config *cfg, const void *K, const void *V, const void *Q,
+                          const int32_t *seq_start, const int32_t *lengths, const int32_t *page_table,
+                          const double *freqs, void *K_cache, void *V_cache, void *Q_out, void *hip_stream)
+{
+    if (!cfg) return fail(RR_ERR_INVALID, "config is NULL");
+    const rr_append_config &c = *cfg;
+    rr_status st = check_cache(c.n_kv_heads, c.page, c.n_pages, c.max_pages, c.n_seqs, c.dtype, c.cache_dtype, c.k_scale, c.v_scale);
+    if (st != RR_OK) return st;
+    if (c.d < 8 || c.d > 1024 || c.d % 8 != 0) return fail(RR_ERR_INVALID, "d must be a multiple of 8 in [8, 1024]");
+    if (c.rot < 0 || c.rot > c.d || c.rot % 2 != 0) return fail(RR_ERR_INVALID, "rot must be even and lie in [0, d]");
+    if (c.interleaved != 0 && c.interleaved != 1) return fail(RR_ERR_INVALID, "interleaved must be 0 or 1");
+    if (c.n_tokens < 0) return fail(RR_ERR_INVALID, "n_tokens must be >= 0");
+    if (c.ldk < 0 || c.ldv < 0 || (Q && c.ldq < 0)) return fail(RR_ERR_INVALID, "ldq, ldk and ldv must be >= 0");
+    if (!lengths || !page_table || !K_cache || !V_cache)
+        return fail(RR_ERR_INVALID, "lengths, page_table and the caches must be device pointers");
+    if (c.n_tokens > 0 && (!K || !V)) return fail(RR_ERR_INVALID, "K and V must be device pointers");
+    if (c.rot > 0 && !freqs) return fail(RR_ERR_INVALID, "freqs must hold rot / 2 frequencies");
+    if ((Q != nullptr) != (Q_out != nullptr)) return fail(RR_ERR_INVALID, "Q and Q_out go together");
+    if (Q && c.n_heads < 1) return fail(RR_ERR_INVALID, "n_heads must be >= 1");
+    if (Q && Q == Q_out && c.n_tokens > 1 && c.ldq != (int64_t)c.n_heads * c.d)
+        return fail(RR_ERR_INVALID, "Q_out may be Q only where ldq is n_heads * d");
+    if (!seq_start && c.n_tokens % c.n_seqs != 0)
+        return fail(RR_ERR_INVALID, "n_tokens must be a multiple of n_seqs where seq_start is NULL");
+    if (c.n_tokens == 0) return RR_OK;
+    rr::AppendArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.Q = Q;
+    a.K = K;
+    a.V = V;
+    a.Kc = K_cache;
+    a.Vc = V_cache;
+    a.Q_out = Q_out;
+    a.seq_start = seq_start;
+    a.lengths = lengths;
+    a.table = page_table;
+    a.freqs = freqs;
+    a.k_scale = c.k_scale;
+    a.v_scale = c.v_scale;
+    a.ldq = c.ldq;
+    a.ldk = c.ldk;
+    a.ldv = c.ldv;
+    a.n_heads = c.n_heads;
+    a.n_kv_heads = c.n_kv_heads;
+    a.d = c.d;
+    a.n_pages = c.n_pages;
+    a.max_pages = c.max_pages;
+    a.n_seqs = c.n_seqs;
+    a.n_tokens = c.n_tokens;
+    a.rot = c.rot;
+    a.per_seq = seq_start ? 0 : c.n_tokens / c.n_seqs;
+    a.pd = rr::page_div(c.page);
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    hipError_t e = timed(RR_KERNEL_APPEND, stream,
+                         [&] { return rr::launch_append(a, c.dtype, c.cache_dtype, c.interleaved != 0, stream); });
+    return e == hipSuccess ? RR_OK : hip_fail(e, "append launch");
+}
+
+size_t rr_paged_workspace_bytes(const rr_paged_config *cfg)
+{
+    rr::PagedArgs a;
+    return paged_args(cfg, &a) == RR_OK ? rr::paged_workspace_bytes(a, cfg->d) : 0;
+}
+
+rr_status rr_paged_attention(const rr_paged_config *cfg, const void *Q, const void *K_cache, const void *V_cache,
+                             const int32_t *page_table, const int32_t *lengths, const int32_t *routes, void *O,
+                             float *lse, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (cfg && cfg->n_prefix != 0) return fail(RR_ERR_INVALID, "n_prefix is rr_prefix_attention's");
+    if (cfg && (routes != nullptr) != (cfg->k > 0)) return fail(RR_ERR_INVALID, "routes and k go together");
+    return paged_call(cfg, Q, K_cache, V_cache, page_table, lengths, routes, nullptr, O, lse, workspace, workspace_bytes, hip_stream);
+}
+
+rr_status rr_prefix_attention(const rr_paged_config *cfg, const void *Q, const void *K_cache, const void *V_cache,
+                              const int32_t *page_table, const int32_t *lengths, const int32_t *prefix_pages, void *O,
+                              float *lse, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (cfg && cfg->n_prefix < 1) return fail(RR_ERR_INVALID, "n_prefix must be >= 1");
+    if (!prefix_pages) return fail(RR_ERR_INVALID, "prefix_pages must be a device pointer");
+    return paged_call(cfg, Q, K_cache, V_cache, page_table, lengths, nullptr, prefix_pages, O, lse, workspace, workspace_bytes, hip_stream);
 }

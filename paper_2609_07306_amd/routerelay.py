@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librouterelay.so")
 
 RR_OK, RR_ERR_INVALID, RR_ERR_OOM, RR_ERR_HIP, RR_ERR_STATE, RR_ERR_UNSUPPORTED = 0, -1, -2, -3, -4, -5
-RR_F32, RR_BF16 = 0, 1
+RR_F32, RR_BF16, RR_E4M3 = 0, 1, 2
 RR_OPT_SPLIT_RELAY, RR_OPT_ONE_PASS_RELAY = 1, 2
 
 EXPORTED = (
@@ -25,9 +25,11 @@ EXPORTED = (
     "rr_ledger_routes", "rr_ledger_export", "rr_ledger_import", "rr_ledger_relay_stats",
     "rr_ledger_index_bytes", "rr_status_string", "rr_last_error", "rr_profile_start",
     "rr_profile_stop", "rr_unconverged_rows", "rr_set_sweep_cap", "rr_relay_layer_static",
-    "rr_pool_chunks", "rr_expand_tokens", "rr_sparse_attention",
+    "rr_pool_chunks", "rr_expand_tokens", "rr_sparse_attention", "rr_cache_append",
+    "rr_paged_workspace_bytes", "rr_paged_attention", "rr_prefix_attention",
 )
-KERNEL_KINDS = ("full", "anchor", "reroute", "rescore", "relay", "pool", "expand", "attention")
+KERNEL_KINDS = ("full", "anchor", "reroute", "rescore", "relay", "pool", "expand", "attention", "append",
+                "paged", "join")
 
 
 class RRError(RuntimeError):
@@ -53,6 +55,20 @@ class _AttnConfig(ctypes.Structure):
         ("d", ctypes.c_int32), ("chunk", ctypes.c_int32), ("k", ctypes.c_int32), ("causal", ctypes.c_int32),
         ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
     ]
+
+
+class _AppendConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_heads", "n_kv_heads", "d", "page", "n_pages", "max_pages", "n_seqs", "n_tokens", "rot", "interleaved", "dtype",
+        "cache_dtype")] + [("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64),
+                           ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class _PagedConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_heads", "n_kv_heads", "d", "page", "n_pages", "max_pages", "n_seqs", "n_q", "k", "n_sink", "n_recent",
+        "n_prefix", "dtype", "cache_dtype")] + [("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                                                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
 def _load():
@@ -81,6 +97,10 @@ def _load():
         "rr_pool_chunks": (ctypes.c_int, [vp, i32, i32, i32, i32, i32, vp, vp]),
         "rr_expand_tokens": (ctypes.c_int, [vp, ctypes.c_int64, i32, i32, i32, vp, vp]),
         "rr_sparse_attention": (ctypes.c_int, [ctypes.POINTER(_AttnConfig), vp, vp, vp, vp, vp, vp]),
+        "rr_cache_append": (ctypes.c_int, [ctypes.POINTER(_AppendConfig)] + [vp] * 11),
+        "rr_paged_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(_PagedConfig)]),
+        "rr_paged_attention": (ctypes.c_int, [ctypes.POINTER(_PagedConfig)] + [vp] * 9 + [ctypes.c_size_t, vp]),
+        "rr_prefix_attention": (ctypes.c_int, [ctypes.POINTER(_PagedConfig)] + [vp] * 9 + [ctypes.c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -380,3 +400,205 @@ def sparse_attention(Q, K, V, routes, chunk: int, causal: bool, scale: float = 0
                                    _out(out, (H, n, d), torch.bfloat16), _stream(stream)))
     return out
 
+
+
+# -------------------------------------------------------- the paged cache
+
+_E4M3 = torch.float8_e4m3fn
+_DTYPES = {torch.float32: RR_F32, torch.bfloat16: RR_BF16, _E4M3: RR_E4M3}
+
+
+def _device_of(first, *others):
+    """The device of the tensors of a call; they have to share one."""
+    dev = first.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}: a call takes one device's")
+    return dev
+
+
+class _On:
+    """The device of a call made current for it, and the stream it goes to: the
+    given one, or the device's current one."""
+
+    def __init__(self, dev, stream):
+        if dev.type != "cuda":
+            raise ValueError("tensor must be on the GPU")
+        self.guard = torch.cuda.device(dev)
+        self.dev, self.stream = dev, stream
+
+    def __enter__(self):
+        self.guard.__enter__()
+        if self.stream is None:
+            self.stream = torch.cuda.current_stream(self.dev)
+        elif self.stream.device != self.dev:
+            self.guard.__exit__(None, None, None)
+            raise ValueError(f"the stream is of {self.stream.device}, the tensors are on {self.dev}")
+        return self.stream
+
+    def __exit__(self, *exc):
+        return self.guard.__exit__(*exc)
+
+
+def _empty(shape, dtype, dev, stream):
+    """Memory for a call on the given stream (None: the current one), of that
+    stream's own: freed, only what the stream does later can take it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _of(name, t, shape, dtype):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} of shape {list(shape)}")
+    return _ptr(t)
+
+
+def _cache_of(K_cache, V_cache, dtype, k_scale, v_scale):
+    """The pools' sizes (n_pages, n_kv_heads, page, d), their type and the scales."""
+    if K_cache.dim() != 4 or K_cache.dtype not in _DTYPES or V_cache.dtype != K_cache.dtype:
+        raise TypeError("K_cache and V_cache must be [n_pages, H_kv, page, d] tensors of one type of "
+                        "float32, bfloat16 and float8_e4m3fn")
+    if V_cache.shape != K_cache.shape:
+        raise ValueError("K_cache and V_cache must have one shape")
+    if K_cache.dtype != dtype and not (dtype == torch.bfloat16 and K_cache.dtype == _E4M3):
+        raise TypeError("the cache must have the queries' type, or float8_e4m3fn with bfloat16")
+    scales = []
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        if (t is not None) != (K_cache.dtype == _E4M3):
+            raise ValueError("k_scale and v_scale are given for float8_e4m3fn caches, and for them only")
+        scales.append(None if t is None else _of(name, t, (K_cache.shape[1],), torch.float32))
+    return tuple(K_cache.shape), _DTYPES[K_cache.dtype], scales
+
+
+def _rows_of(name, t, n, heads, d, dtype):
+    """Elements between one token's rows and the next one's: the rows of a token
+    lie together, tokens may lie apart (views of a fused projection)."""
+    if t.dim() != 3 or tuple(t.shape) != (n, heads, d) or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} of shape {[n, heads, d]}")
+    if not t.is_cuda:
+        raise ValueError("tensor must be on the GPU")
+    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: the rows of a token must be contiguous")
+    return t.stride(0) if n > 1 else heads * d
+
+
+def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, freqs=None, interleaved=False, Q=None,
+                 Q_out=None, k_scale=None, v_scale=None, stream=None):
+    """rr_cache_append: new tokens' keys and values K, V [n_tokens, H_kv, d]
+    into the pages of their sequences (K_cache, V_cache [n_pages, H_kv, page,
+    d], page_table [B, max_pages] and lengths [B] int32, the new tokens counted
+    in; seq_start [B + 1] int32, None: n_tokens / B each).  With freqs [rot / 2]
+    float64 the first rot features of keys are rotated by position, and of
+    queries Q [n_tokens, H, d] (returned, in Q_out if given).  K, V and Q may
+    be views whose tokens lie apart."""
+    if K.dim() != 3 or K.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("K must be a [n_tokens, H_kv, d] float32 or bfloat16 tensor")
+    dev = _device_of(K, V, K_cache, V_cache, page_table, lengths, seq_start, freqs, Q, Q_out, k_scale, v_scale)
+    (n_pages, Hkv, page, d), cache, (ks, vs) = _cache_of(K_cache, V_cache, K.dtype, k_scale, v_scale)
+    n = K.shape[0]
+    ldk, ldv = (_rows_of(name, t, n, Hkv, d, K.dtype) for name, t in (("K", K), ("V", V)))
+    if page_table.dim() != 2 or lengths.dim() != 1:
+        raise ValueError("page_table must be [B, max_pages] and lengths [B]")
+    B, most = page_table.shape
+    H, ldq, rot = 0, 0, 0
+    if freqs is not None:
+        if freqs.dim() != 1 or freqs.dtype != torch.float64:
+            raise TypeError("freqs must be a [rot / 2] float64 tensor")
+        rot = 2 * freqs.shape[0]
+    if Q is not None:
+        if Q.dim() != 3:
+            raise TypeError("Q must be a [n_tokens, H, d] tensor")
+        H = Q.shape[1]
+        ldq = _rows_of("Q", Q, n, H, d, K.dtype)
+    elif Q_out is not None:
+        raise ValueError("Q_out without Q")
+    with _On(dev, stream) as s:
+        if Q is not None and Q_out is None:
+            Q_out = _empty((n, H, d), Q.dtype, dev, stream)
+        cfg = _AppendConfig(H, Hkv, d, page, n_pages, most, B, n, rot, int(interleaved), _DTYPES[K.dtype], cache, ldq,
+                            ldk, ldv, ks, vs)
+        _check(lib.rr_cache_append(
+            ctypes.byref(cfg), K.data_ptr(), V.data_ptr(), None if Q is None else Q.data_ptr(),
+            None if seq_start is None else _of("seq_start", seq_start, (B + 1,), torch.int32),
+            _of("lengths", lengths, (B,), torch.int32), _of("page_table", page_table, (B, most), torch.int32),
+            _ptr(freqs) if rot else None, _ptr(K_cache), _ptr(V_cache),
+            None if Q is None else _of("Q_out", Q_out, (n, H, d), K.dtype), s.cuda_stream))
+    return Q_out
+
+
+def _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, n_prefix, scale, k_scale, v_scale):
+    if Q.dim() != 4 or Q.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("Q must be a [B, n_q, H, d] float32 or bfloat16 tensor")
+    (n_pages, Hkv, page, d), cache, (ks, vs) = _cache_of(K_cache, V_cache, Q.dtype, k_scale, v_scale)
+    B, nq, H, dq = Q.shape
+    if dq != d:
+        raise ValueError(f"Q has rows of {dq} features, the cache of {d}")
+    if page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError("page_table must be [B, max_pages]")
+    k = 0
+    if routes is not None:
+        if routes.dim() != 2 or routes.shape[0] != B * H * nq:
+            raise ValueError("routes must be [B * H * n_q, k]")
+        k = routes.shape[1]
+    return _PagedConfig(H, Hkv, d, page, n_pages, page_table.shape[1], B, nq, k, n_sink, n_recent, n_prefix,
+                        _DTYPES[Q.dtype], cache, float(scale), 0, ks, vs)
+
+
+def paged_workspace(Q, K_cache, page_table, routes=None, n_sink=0, n_recent=0, n_prefix=0):
+    """A workspace (uint8 device tensor) for paged_attention and
+    prefix_attention calls of these shapes.  Calls that may run at the same
+    time, captured graphs that are replayed side by side among them, need one
+    each."""
+    one = torch.empty(K_cache.shape[1] if K_cache.dim() == 4 else 0, dtype=torch.float32, device=K_cache.device)
+    scale = one if K_cache.dtype == _E4M3 else None
+    cfg = _paged_config(Q, K_cache, K_cache, page_table, routes, n_sink, n_recent, n_prefix, 0.0, scale, scale)
+    n = lib.rr_paged_workspace_bytes(ctypes.byref(cfg))
+    if n == 0:
+        raise RRError(RR_ERR_INVALID, lib.rr_last_error().decode())
+    return torch.empty(n, dtype=torch.uint8, device=Q.device)
+
+
+def _paged_call(call, cfg, Q, K_cache, V_cache, page_table, lengths, pages, pages_shape, out, lse, workspace, stream, dev):
+    B, nq, H, d = Q.shape
+    with _On(dev, stream) as s:
+        if out is None:
+            out = _empty((B, nq, H, d), Q.dtype, dev, stream)
+        if workspace is None:
+            n = lib.rr_paged_workspace_bytes(ctypes.byref(cfg))
+            workspace = _empty((n,), torch.uint8, dev, stream)
+        elif workspace.dtype != torch.uint8 or workspace.dim() != 1:
+            raise ValueError("workspace must be a one-dimensional uint8 tensor")
+        _check(call(ctypes.byref(cfg), _ptr(Q), _ptr(K_cache), _ptr(V_cache),
+                    _of("page_table", page_table, page_table.shape, torch.int32), _of("lengths", lengths, (B,), torch.int32),
+                    None if pages is None else _of(*pages, pages_shape, torch.int32), _out(out, (B, nq, H, d), Q.dtype),
+                    _out(lse, (B, nq, H), torch.float32), _ptr(workspace), workspace.numel(), s.cuda_stream))
+    return out
+
+
+def paged_attention(Q, K_cache, V_cache, page_table, lengths, routes=None, n_sink=0, n_recent=0, scale=0.0, k_scale=None,
+                    v_scale=None, out=None, lse=None, workspace=None, stream=None):
+    """rr_paged_attention: the newest n_q tokens' queries Q [B, n_q, H, d] over
+    their sequences' caches (as in cache_append) -> O [B, n_q, H, d].  routes
+    [B * H * n_q, k] int32 page indices: each query over those pages, its first
+    n_sink and its last n_recent ones.  lse: optional float32 output [B, n_q,
+    H].  workspace: paged_workspace(...), or None for one of this call's own."""
+    dev = _device_of(Q, K_cache, V_cache, page_table, lengths, routes, k_scale, v_scale, out, lse, workspace)
+    cfg = _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, 0, scale, k_scale, v_scale)
+    if cfg.k == 0:
+        routes = None
+    return _paged_call(lib.rr_paged_attention, cfg, Q, K_cache, V_cache, page_table, lengths,
+                       None if routes is None else ("routes", routes), None if routes is None else routes.shape, out, lse,
+                       workspace, stream, dev)
+
+
+def prefix_attention(Q, K_cache, V_cache, page_table, lengths, prefix_pages, n_prefix, scale=0.0, k_scale=None,
+                     v_scale=None, out=None, lse=None, workspace=None, stream=None):
+    """rr_prefix_attention: paged_attention (without routes) for sequences that
+    begin with the same n_prefix tokens, which are read once for the batch from
+    prefix_pages [ceil(n_prefix / page)] int32."""
+    dev = _device_of(Q, K_cache, V_cache, page_table, lengths, prefix_pages, k_scale, v_scale, out, lse, workspace)
+    cfg = _paged_config(Q, K_cache, V_cache, page_table, None, 0, 0, n_prefix, scale, k_scale, v_scale)
+    return _paged_call(lib.rr_prefix_attention, cfg, Q, K_cache, V_cache, page_table, lengths,
+                       ("prefix_pages", prefix_pages), (n_chunks(n_prefix, cfg.page),), out, lse, workspace, stream, dev)
