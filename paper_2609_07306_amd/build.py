@@ -25,13 +25,17 @@ SOURCES = ["rr_api.hip", "rr_route.hip", "rr_rescore.hip", "rr_rescore_dense.hip
 RESIDENT = {f"rr_resident_inst_{mode}_{dt}_{d}.hip": (f"-DRR_MODE={mode}", f"-DRR_DT={dt}", f"-DRR_D={d}")
             for mode in ("MODE_FULL", "MODE_ANCHOR", "MODE_RELAY")
             for dt, widths in (("float", (32, 64, 128)), ("bf16_t", (32, 64, 128, 256))) for d in widths}
-SOURCES += RESIDENT
+# the paged cache's attention, likewise, per cache type and width
+PAGED = {f"rr_paged_inst_{ty}_{d}.hip": (f"-DRR_TY={ty}", f"-DRR_D={d}")
+         for ty, widths in (("CACHE_F32", (64, 128)), ("CACHE_BF16", (64, 128, 256)), ("CACHE_E4M3", (64, 128, 256)))
+         for d in widths}
+SOURCES += [*RESIDENT, *PAGED]
 # ... whose atomics come from one lane per wave or from lanes with different
 # addresses: the compiler's wave-level aggregation would only add a wait for the
 # returned value right behind each of them
 NO_ATOMIC_OPT = ("-mllvm", "-amdgpu-atomic-optimizer-strategy=None")
 # caches may hold anything where no token was written yet, NaN among it
-HONOR_NANS = {"rr_append.hip", "rr_paged.hip"}
+HONOR_NANS = {"rr_append.hip", "rr_paged.hip", *PAGED}
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -51,8 +55,10 @@ def _compile(name: str) -> str:
     src, more = name, ()
     if name in RESIDENT:
         src, more = "rr_resident_inst.hip", RESIDENT[name] + NO_ATOMIC_OPT
+    if name in PAGED:
+        src, more = "rr_paged_inst.hip", PAGED[name]
     if name in HONOR_NANS:
-        more = ("-Xarch_device", "-fhonor-nans")
+        more += ("-Xarch_device", "-fhonor-nans")
     cmd = [HIPCC, *FLAGS, *more, "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

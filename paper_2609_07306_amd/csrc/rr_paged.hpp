@@ -68,6 +68,9 @@ __host__ __device__ __forceinline__ int32_t sequence_of(const int32_t *start, in
     return start[lo] <= i && i < start[lo + 1] ? lo : -1;
 }
 
+constexpr int kPagedUnit = 128;  // keys of a unit of the attention's work
+constexpr int kPagedGrid = 512;  // workgroups of an attention launch: two a compute unit
+
 enum CacheType : int32_t { CACHE_F32 = 0, CACHE_BF16 = 1, CACHE_E4M3 = 2 };
 
 struct AppendArgs {
@@ -98,15 +101,17 @@ struct PagedArgs {
     float scale;
     // schedule (paged_schedule)
     int32_t rows;           // query rows of a (sequence, key head): n_q * group; routes: 1
-    int32_t row_tiles;      // ... in tiles of 16 * row_blocks
+    int32_t own_tile, row_tiles;  // ... in tiles of so many
     int32_t items_per_seq;  // H_kv * row_tiles; routes: H * n_q
     int32_t route_units;    // routes: units of every item
-    int32_t prefix_rows, prefix_tiles, prefix_items, prefix_units;
-    int32_t row_blocks, grid, min_units, batch_keys;
+    int32_t prefix_rows, prefix_tile, prefix_tiles, prefix_items, prefix_units;  // of the batch against the prefix
+    bool own_wide, prefix_wide;        // which body takes them
+    int32_t narrow_tile, wide_tile;    // rows of a body's parts
+    int32_t grid, min_units, batch_keys;
     // workspace
-    float *parts;    // [2 * grid] parts of items that several workgroups share
+    float *parts, *wide_parts;  // [2 * grid] parts of each body's items that several workgroups share
     float *whole;    // prefix: [2][rows of the call] parts of items that one workgroup held
-    int4 *heads;     // per item: its first part, its first workgroup, its parts
+    int4 *heads;     // per item: its first part, its first workgroup, its parts, its body
 };
 
 size_t paged_workspace_bytes(const PagedArgs &a, int d);

@@ -1,0 +1,1171 @@
+// Attention of the newest tokens of a batch of sequences over a paged cache
+// (all of it, along routes of pages, or behind a shared prefix), for gfx950.
+//
+//   o = sum_u 2^(c q.k_u - m) v_u / l,  l = sum_u 2^(c q.k_u - m),  c = scale log2 e
+//
+// One pass over the keys with a running maximum m per query.  A call's work
+// is cut into items: the query rows of one (sequence, key head) -- n_q tokens
+// times the heads that share the key head -- in tiles of rows; with routes one
+// query head's row, which has its own pages; with a shared prefix also tiles
+// over the rows of the whole batch against the prefix, which is what reads it
+// once for many sequences.  Every item is a number of units of 128 keys, and
+// the units of all items, in order, are cut into equal runs, one per
+// workgroup: lengths that differ a hundredfold leave no compute unit idle, and
+// one long sequence is spread over the card.  Lengths live on the device, so
+// every workgroup sums them to find its run.  An item that lies in several
+// runs leaves a part (m, l, sum) per run in the workspace; a second launch
+// joins them.
+//
+// Two bodies share this.  The narrow one is for items of up to 16 rows (32),
+// where memory is the bound: each of four waves takes its own 32-key tiles of
+// the run, so that no barrier stands between loads and products, and a tile's
+// keys and values are requested while the tile before it is still in its
+// softmax.  The wide one is for items of more rows, where the products are:
+// a wave holds 32 rows, and the four share tiles of 64 keys through LDS.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <climits>
+#include <cmath>
+
+#include "rr_device.hpp"
+#include "rr_internal.hpp"
+#include "rr_paged.hpp"
+
+namespace rr {
+namespace paged {
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef short short8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kT = 256;             // threads of a workgroup
+constexpr int kW = kT / 64;         // waves
+constexpr int kStagedPages = 512;   // page numbers held in LDS at a time
+constexpr float kLazy = 8.f;        // log2 headroom of the running softmax maximum
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int32_t kNoToken = INT_MAX;
+
+// Four bf16 of a transposed LDS read (ds_read_b64_tr_b16): lane i of each
+// 16-lane group receives column i of the four rows that its lanes address,
+// lane j the 8 bytes of row j / 4 at columns 4 (j % 4).
+__device__ __forceinline__ short4_t lds_read_tr16(const unsigned char *p)
+{
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t *)p);
+}
+
+__device__ __forceinline__ bf16x8_t as_bf16x8(u32x4_t x) { return __builtin_bit_cast(bf16x8_t, x); }
+
+__device__ __forceinline__ bf16x8_t join8(short4_t x, short4_t y)
+{
+    return __builtin_bit_cast(bf16x8_t, (short8_t){x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
+}
+
+// Eight e4m3 values, exactly, as bf16.
+__device__ __forceinline__ bf16x8_t e4m3_to_bf16(uint32_t lo, uint32_t hi)
+{
+    const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
+    const bf16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+    const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
+    const bf16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+    return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// A weight as the sum of two bf16 numbers, 2^-17 off: rounded to one, it would
+// add as much error as the rounding of the output.
+__device__ __forceinline__ void split_weight(float x, __bf16 &hi, __bf16 &lo)
+{
+    hi = (__bf16)x;
+    lo = (__bf16)(x - (float)hi);
+}
+
+// Where some rows of a product see a token and others don't, a value that is
+// not finite would reach the others as 0 * inf.  It is taken out of the
+// operand, and `odd` marks it: a product of the marks with "the row sees the
+// token" then tells which outputs it belongs to.
+__device__ __forceinline__ void take_odd(bf16x8_t &v, bf16x8_t &odd)
+{
+    // (bits of the whole vector: a bit cast of one of its elements takes the first one's)
+    const short8_t bits = __builtin_bit_cast(short8_t, v);
+    short8_t kept, marks;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const bool is = (bits[e] & 0x7F80) == 0x7F80;
+        marks[e] = is ? (short)0x3F80 : (short)0;  // 1
+        kept[e] = is ? (short)0 : bits[e];
+    }
+    v = __builtin_bit_cast(bf16x8_t, kept);
+    odd = __builtin_bit_cast(bf16x8_t, marks);
+}
+
+// ------------------------------------------------------------- the runs
+
+struct Item {
+    bool prefix;
+    int32_t b;      // sequence
+    int32_t j;      // item within the sequence (or within the prefix)
+    int32_t units;  // its units
+    int64_t first;  // its first unit
+    int64_t index;  // its number (of its head)
+};
+
+struct Run {
+    int64_t at, end, per_wg;  // units [at, end) of the body's
+    Item it;
+};
+
+// LDS that both bodies use.
+struct Common {
+    int32_t phys[kStagedPages];
+    int32_t chunk[kMaxAttnSlots];
+    int64_t sum[kW];
+    int64_t at[3];
+    int32_t b;
+    int32_t count[kW];
+    int32_t lo[kW], hi[kW], bad[kW];
+    int32_t lim[128];
+    float m[kW][32], l[kW][32];
+};
+
+__device__ __forceinline__ int32_t seq_units(const PagedArgs &a, int32_t b)
+{
+    if (a.route_units) return a.route_units;
+    const int32_t n = held_tokens(a.lengths[b], a.capacity) - a.n_prefix;
+    return n <= kPagedUnit ? 1 : (n + kPagedUnit - 1) / kPagedUnit;
+}
+
+// This workgroup's run of the items that a body takes: the prefix's, the
+// sequences', or one after the other.  False where it has none.
+__device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, bool pre, bool own, Run &r)
+{
+    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
+    const int64_t prefix_total = pre ? (int64_t)a.prefix_items * a.prefix_units : 0;
+    const int per = (a.n_seqs + kT - 1) / kT;
+    const int b0 = own ? min(tid * per, a.n_seqs) : 0, b1 = own ? min(b0 + per, a.n_seqs) : 0;
+    int64_t sum = 0;
+    for (int b = b0; b < b1; ++b) sum += seq_units(a, b);
+    int64_t inc = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t v = (int64_t)shfl_u64((uint64_t)inc, max(lane - o, 0));
+        inc += lane >= o ? v : 0;
+    }
+    __syncthreads();  // (an earlier body's readers of LDS are done)
+    if (lane == 63) sh.sum[w] = inc;
+    if (tid == 0) {
+        sh.b = 0;
+        sh.at[2] = 0;
+    }
+    __syncthreads();
+    int64_t before = inc - sum, all = 0;
+    for (int v = 0; v < kW; ++v) {
+        before += v < w ? sh.sum[v] : 0;
+        all += sh.sum[v];
+    }
+    const int64_t total = prefix_total + all * a.items_per_seq;
+    const int64_t share = (total + a.grid - 1) / a.grid;
+    r.per_wg = share > a.min_units ? share : a.min_units;
+    r.at = blockIdx.x * r.per_wg;
+    r.end = min(r.at + r.per_wg, total);
+    if (r.at >= r.end) return false;  // (uniform)
+    // the sequence that the run begins in
+    const int64_t u = (r.at - prefix_total) / a.items_per_seq;
+    if (own && r.at >= prefix_total && u >= before && u < before + sum) {
+        int b = b0;
+        int64_t base = before;
+        for (;;) {
+            const int32_t n = seq_units(a, b);
+            if (u < base + n) break;
+            base += n;
+            ++b;
+        }
+        sh.b = b;
+        sh.at[2] = base;
+    }
+    __syncthreads();
+    Item &it = r.it;
+    it.b = sh.b;
+    it.prefix = r.at < prefix_total;
+    if (it.prefix) {
+        it.units = a.prefix_units;
+        it.j = (int32_t)(r.at / it.units);
+        it.index = it.j;
+        it.first = it.index * it.units;
+    } else {
+        const int64_t base = prefix_total + sh.at[2] * a.items_per_seq;
+        it.units = seq_units(a, it.b);
+        it.j = (int32_t)((r.at - base) / it.units);
+        it.index = a.prefix_items + (int64_t)it.b * a.items_per_seq + it.j;
+        it.first = base + (int64_t)it.j * it.units;
+    }
+    return true;
+}
+
+__device__ __forceinline__ void next_item(const PagedArgs &a, Item &it)
+{
+    it.first += it.units;
+    ++it.index;
+    ++it.j;
+    if (it.prefix) {
+        if (it.j == a.prefix_items) {
+            it.prefix = false;
+            it.j = it.b = 0;
+            it.units = seq_units(a, 0);
+        }
+    } else if (it.j == a.items_per_seq) {
+        it.j = 0;
+        ++it.b;
+        it.units = seq_units(a, it.b);
+    }
+}
+
+// The query rows of an item: of key head g, from row0 on.
+struct Rows {
+    bool prefix;
+    int b, g, row0, n;
+
+    // sequence, query token and head of row r
+    __device__ __forceinline__ void of(const PagedArgs &a, int r, int &b_, int &t, int &h) const
+    {
+        int x = row0 + r;
+        b_ = b;
+        if (prefix) {
+            b_ = x / a.rows;
+            x -= b_ * a.rows;
+        }
+        t = x / a.group;
+        h = g * a.group + (x - t * a.group);
+    }
+    // the last token that row r sees, -1 for none
+    __device__ __forceinline__ int last(const PagedArgs &a, int r) const
+    {
+        int b_, t, h;
+        of(a, r, b_, t, h);
+        const int p = held_tokens(a.lengths[b_], a.capacity) - a.n_q + t;
+        return max(prefix ? min(p, a.n_prefix - 1) : p, -1);
+    }
+};
+
+__device__ __forceinline__ Rows rows_of(const PagedArgs &a, const Item &it)
+{
+    Rows r;
+    r.prefix = it.prefix;
+    r.b = it.b;
+    if (it.prefix) {
+        r.g = it.j / a.prefix_tiles;
+        r.row0 = (it.j - r.g * a.prefix_tiles) * a.prefix_tile;
+        r.n = min(a.prefix_tile, a.prefix_rows - r.row0);
+    } else if (a.route_units) {
+        // item = head * n_q + query token: row t * group + j of its key head
+        const int h = it.j / a.n_q, t = it.j - h * a.n_q;
+        r.g = h / a.group;
+        r.row0 = t * a.group + (h - r.g * a.group);
+        r.n = 1;
+    } else {
+        r.g = it.j / a.row_tiles;
+        r.row0 = (it.j - r.g * a.row_tiles) * a.own_tile;
+        r.n = min(a.own_tile, a.rows - r.row0);
+    }
+    return r;
+}
+
+// Where a body writes an item's result: the output itself where no other item
+// or workgroup has a part in its rows, else a part of D sums, the maximum and
+// the sum of weights.
+struct Sink {
+    bool last_word, entire, prefix;
+    float *cut;  // parts of this run's cut item, D + 4 floats a row
+
+    __device__ __forceinline__ float *part(const PagedArgs &a, int D, int r, int64_t orow) const
+    {
+        const int64_t half = prefix ? 0 : (int64_t)a.n_seqs * a.n_q * a.n_heads;
+        return entire ? a.whole + (half + orow) * (D + 4) : cut + (int64_t)r * (D + 4);
+    }
+};
+
+// ... and the item's head, by the workgroup that holds its first unit: the
+// slot of its first part, its first workgroup, its parts, and the body.
+__device__ __forceinline__ Sink sink_of(const PagedArgs &a, int D, const Run &r, int u0, int u1, bool first, bool wide)
+{
+    Sink s;
+    s.prefix = r.it.prefix;
+    s.entire = u0 == 0 && u1 == r.it.units;
+    s.last_word = s.entire && a.prefix_items == 0;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (first ? 0 : 1);
+    s.cut = (wide ? a.wide_parts : a.parts) + slot * (wide ? a.wide_tile : a.narrow_tile) * (D + 4);
+    if (u0 == 0 && threadIdx.x == 0) {
+        const int64_t last_wg = (r.it.first + r.it.units - 1) / r.per_wg;
+        a.heads[r.it.index] = int4{(int)slot, (int)blockIdx.x, (int)(last_wg - blockIdx.x) + 1, wide ? 1 : 0};
+    }
+    return s;
+}
+
+__device__ __forceinline__ float inverse_sum(float sum, float scale)
+{
+    return sum > 0.f ? scale / sum : sum == 0.f ? 0.f : sum;  // (a sum that is NaN stays)
+}
+
+__device__ __forceinline__ float log_sum(float m, float sum) { return m == -INFINITY ? -INFINITY : (m + log2f(sum)) * kLn2; }
+
+// ------------------------------------------------------------- narrow body
+//
+// S^T = K Q^T on 16x16 MFMA tiles with the keys as rows, so K goes from memory
+// to the operand registers as it lies (a lane holds 16 bytes of one key); a
+// lane then has four scores of one query per tile, which are just the keys
+// that its part of the operand of O^T = V^T P^T takes.  V is transposed on the
+// way: row-major into a buffer of the wave's own in LDS, read with the LDS
+// transpose read; in binary32, where an operand holds one key per lane,
+// straight from memory.
+
+// What a cache type's tiles look like.
+//   KT  keys of a wave's tile
+//   KR  rows (keys) of a tile that a lane loads 16-byte pieces of
+//   PK  such pieces of a row and lane: piece c of lane group kg holds the
+//       row's elements from (4 c + kg) * (16 / SIZE) on
+template <int TY, int D>
+struct Shape {
+    static constexpr int SIZE = TY == CACHE_F32 ? 4 : TY == CACHE_BF16 ? 2 : 1;
+    static constexpr int KT = TY == CACHE_F32 ? 16 : 32;
+    static constexpr int KR = KT / 16;
+    static constexpr int PK = D * SIZE / 64;
+    static constexpr int VRS = 2 * D + 64;  // bytes of a row of the V buffer
+    static constexpr int ORS = D + 4;       // floats of a row of the output buffer
+    static constexpr int VBYTES = TY == CACHE_F32 ? 0 : KT * VRS;
+    static constexpr int OBYTES = 16 * ORS * 4;
+    static constexpr int WAVE = VBYTES > OBYTES ? VBYTES : OBYTES;
+    static constexpr int LDS = kW * WAVE;
+};
+
+// The feature that element i of value accumulator v belongs to, for lane
+// group kg.
+template <int TY>
+__device__ __forceinline__ int feature_of(int v, int i, int kg)
+{
+    if constexpr (TY == CACHE_F32)
+        return 64 * (v >> 2) + 16 * kg + 4 * i + (v & 3);  // (rows of V^T are 4 features apart)
+    else
+        return 16 * v + 4 * kg + i;
+}
+
+template <int TY, int D, int NR>
+__device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsigned char *smem, bool pre, bool own)
+{
+    using S = Shape<TY, D>;
+    constexpr bool F32 = TY == CACHE_F32;
+    constexpr int NV = D / 16;  // value accumulators of a row block
+    Run run;
+    if (!find_run(a, sh, pre, own, run)) return;
+    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, l16 = lane & 15, kg = lane >> 4;
+    unsigned char *vbuf = smem + w * S::WAVE;
+    const int64_t run0 = run.at;
+
+    for (;;) {
+        const Item &it = run.it;
+        const int u0 = (int)(run.at - it.first), u1 = (int)min((int64_t)it.units, run.end - it.first);
+        const Rows rows = rows_of(a, it);
+        const int g = rows.g, blocks = (rows.n + 15) >> 4;
+
+        // query operands; lim: the last token that a row sees (-1: none);
+        // lo and hi: the least and the largest of them that is one
+        bf16x8_t fq[F32 ? 1 : NR][F32 ? 1 : D / 32];
+        f32x4_t fqf[F32 ? NR : 1][F32 ? D / 16 : 1];
+        int lim[NR], lo = kNoToken, hi = -1;
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            int b, t, h;
+            const int r = min(16 * n + l16, rows.n - 1);
+            rows.of(a, r, b, t, h);
+            lim[n] = rows.last(a, r);
+            if (lim[n] >= 0) {
+                lo = min(lo, lim[n]);
+                hi = max(hi, lim[n]);
+            }
+            const int64_t q = (((int64_t)b * a.n_q + t) * a.n_heads + h) * D;
+            if constexpr (F32) {
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c)
+                    fqf[n][c] = *reinterpret_cast<const f32x4_t *>(static_cast<const float *>(a.Q) + q + 16 * c + 4 * kg);
+            } else {
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    // (e4m3 keys come 16 to a piece, two operands of 8)
+                    const int f = TY == CACHE_E4M3 ? 64 * (c >> 1) + 16 * kg + 8 * (c & 1) : 32 * c + 8 * kg;
+                    fq[n][c] = as_bf16x8(*reinterpret_cast<const u32x4_t *>(static_cast<const bf16_t *>(a.Q) + q + f));
+                }
+            }
+        }
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) {
+            lo = min(lo, __shfl_xor(lo, o, 64));
+            hi = max(hi, __shfl_xor(hi, o, 64));
+        }
+
+        float m_run[NR], l_run[NR];
+        f32x4_t acc[NR][NV];
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            m_run[n] = -INFINITY;
+            l_run[n] = 0.f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) acc[n][v] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        const float c2 = a.scale * 1.4426950408889634f * (a.k_scale ? a.k_scale[g] : 1.f);
+
+        // Key positions: tokens from `base` on, or, along routes, the places
+        // of the listed pages one after the other.
+        const int base = it.prefix ? 0 : a.n_prefix;
+        int n_pos;
+        __syncthreads();  // (the last item's readers of LDS are done)
+        if (a.route_units) {
+            // the pages that the row sees, each once: a slot is dropped if an
+            // earlier one names its page
+            const int64_t row = ((int64_t)it.b * a.items_per_seq + it.j) * a.k;
+            const int here = hi >= 0 ? a.pd.div(hi) : -1, slots = a.n_sink + a.n_recent + a.k;
+            static_assert(kMaxAttnSlots <= kT, "a slot per thread");
+            int id = -1;
+            if (tid < a.n_sink)
+                id = tid;
+            else if (tid < a.n_sink + a.n_recent)
+                id = here - (tid - a.n_sink);
+            else if (tid < slots)
+                id = a.routes[row + tid - a.n_sink - a.n_recent];
+            bool ok = tid < slots && id >= 0 && id <= here;
+            if (tid < kMaxAttnSlots) sh.phys[tid] = ok ? id : -1;
+            __syncthreads();
+            if (ok)
+                for (int s = 0; s < tid; ++s) ok = ok && sh.phys[s] != id;
+            const uint64_t mk = __ballot(ok);
+            if (lane == 0) sh.count[w] = __popcll(mk);
+            __syncthreads();
+            int before = __popcll(mk & ((1ull << lane) - 1ull)), all = 0;
+            for (int v = 0; v < kW; ++v) {
+                before += v < w ? sh.count[v] : 0;
+                all += sh.count[v];
+            }
+            if (ok) {
+                sh.chunk[before] = id;
+                sh.phys[before] = pool_page(a.table[(int64_t)it.b * a.max_pages + id], a.n_pages);
+            }
+            n_pos = all * a.pd.page;
+        } else {
+            n_pos = hi < base ? 0 : hi - base + 1;
+        }
+        const int p0 = (int)min((int64_t)u0 * kPagedUnit, (int64_t)n_pos);
+        const int p1 = (int)min((int64_t)u1 * kPagedUnit, (int64_t)n_pos);
+
+        for (int pa = p0; pa < p1; pa += a.batch_keys) {
+            const int pb = min(p1 - pa, a.batch_keys) + pa;
+            const int ch0 = a.route_units ? 0 : a.pd.div(base + pa);
+            if (!a.route_units) {  // (routes: a list of at most 256 pages is there whole)
+                if (pa != p0) __syncthreads();
+                const int ch1 = a.pd.div(base + pb - 1);
+                const int32_t *src = it.prefix ? a.prefix_pages : a.table + (int64_t)it.b * a.max_pages;
+                for (int c = ch0 + tid; c <= ch1; c += kT) sh.phys[c - ch0] = pool_page(src[c], a.n_pages);
+            }
+            __syncthreads();
+
+            // where position p lies: its token and page, kNoToken where the
+            // page is none or p is past the run
+            auto locate = [&](int p, int &phys, int &place) -> int32_t {
+                const bool in = p < pb;
+                p = min(p, pb - 1);
+                int tok;
+                if (a.route_units) {
+                    const int s = a.pd.div(p);
+                    place = p - s * a.pd.page;
+                    phys = sh.phys[s];
+                    tok = sh.chunk[s] * a.pd.page + place;
+                } else {
+                    tok = base + p;
+                    const int c = a.pd.div(tok);
+                    place = tok - c * a.pd.page;
+                    phys = sh.phys[c - ch0];
+                }
+                const bool ok = in && phys >= 0 && tok <= hi;
+                if (!ok) phys = place = 0;  // (row 0 of the pool is there)
+                return ok ? tok : kNoToken;
+            };
+
+            u32x4_t kr[S::KR][S::PK], vr[S::KR][S::PK];
+            int32_t tok[S::KR];
+            const unsigned char *Kb = static_cast<const unsigned char *>(a.K);
+            const unsigned char *Vb = static_cast<const unsigned char *>(a.V);
+            auto load = [&](int p) {
+                int64_t off[S::KR];
+#pragma unroll
+                for (int r = 0; r < S::KR; ++r) {
+                    int phys, place;
+                    tok[r] = locate(p + 16 * r + l16, phys, place);
+                    off[r] = pool_row(phys, a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE;
+                }
+#pragma unroll
+                for (int r = 0; r < S::KR; ++r)
+#pragma unroll
+                    for (int c = 0; c < S::PK; ++c)
+                        kr[r][c] = *reinterpret_cast<const u32x4_t *>(Kb + off[r] + 64 * c + 16 * kg);
+                if constexpr (F32) {
+                    // V^T operands: lane (l16, kg) takes features 64 c + 4 l16 ..
+                    // of key 4 kg + s: vr[0][4 c + s]
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        const int64_t o = (int64_t)shfl_u64((uint64_t)off[0], 4 * kg + s);
+#pragma unroll
+                        for (int c = 0; c < D / 64; ++c)
+                            vr[0][4 * c + s] = *reinterpret_cast<const u32x4_t *>(Vb + o + 256 * c + 16 * l16);
+                    }
+                } else {
+#pragma unroll
+                    for (int r = 0; r < S::KR; ++r)
+#pragma unroll
+                        for (int c = 0; c < S::PK; ++c)
+                            vr[r][c] = *reinterpret_cast<const u32x4_t *>(Vb + off[r] + 64 * c + 16 * kg);
+                }
+            };
+
+            int p = pa + w * S::KT;
+            if (p < pb) load(p);
+            for (; p < pb; p += kW * S::KT) {
+                // (wave-uniform) all_seen: every key of the tile is seen by
+                // every row; mixed: some key by some rows and not by others
+                bool all_seen = true, mixed = false;
+#pragma unroll
+                for (int r = 0; r < S::KR; ++r) {
+                    all_seen = all_seen && tok[r] <= lo;
+                    mixed = mixed || (tok[r] > lo && tok[r] != kNoToken);
+                }
+                all_seen = __ballot(all_seen) == ~0ull;
+                mixed = __ballot(mixed) != 0ull;
+
+                // rows that no query sees become zeros: their weights are 0,
+                // but memory that was never written may hold NaN
+                if constexpr (F32) {
+                    if (!all_seen) {
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) {
+                            const bool keep = __shfl(tok[0], 4 * kg + s, 64) != kNoToken;
+#pragma unroll
+                            for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) vr[0][4 * c + s][e] = keep ? vr[0][4 * c + s][e] : 0u;
+                        }
+                    }
+                } else {
+                    __builtin_amdgcn_wave_barrier();  // (the buffer's readers are this wave's, and in order)
+#pragma unroll
+                    for (int r = 0; r < S::KR; ++r) {
+                        const bool keep = tok[r] != kNoToken;
+#pragma unroll
+                        for (int c = 0; c < S::PK; ++c) {
+                            if (!all_seen) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) vr[r][c][e] = keep ? vr[r][c][e] : 0u;
+                            }
+                            unsigned char *dst = vbuf + (16 * r + l16) * S::VRS;
+                            if constexpr (TY == CACHE_BF16) {
+                                *reinterpret_cast<u32x4_t *>(dst + 64 * c + 16 * kg) = vr[r][c];
+                            } else {
+                                *reinterpret_cast<bf16x8_t *>(dst + 128 * c + 32 * kg) = e4m3_to_bf16(vr[r][c][0], vr[r][c][1]);
+                                *reinterpret_cast<bf16x8_t *>(dst + 128 * c + 32 * kg + 16) = e4m3_to_bf16(vr[r][c][2], vr[r][c][3]);
+                            }
+                        }
+                    }
+                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+                    __builtin_amdgcn_wave_barrier();
+                }
+
+                // S^T = K Q^T: s[n][r] of lane (l16, kg): keys 16 r + 4 kg + i
+                // of the tile, query row 16 n + l16
+                f32x4_t s[NR][S::KR];
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int r = 0; r < S::KR; ++r) s[n][r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int r = 0; r < S::KR; ++r) {
+#pragma unroll
+                    for (int c = 0; c < S::PK; ++c) {
+                        if constexpr (F32) {
+                            const f32x4_t k4 = __builtin_bit_cast(f32x4_t, kr[r][c]);
+#pragma unroll
+                            for (int n = 0; n < NR; ++n)
+                                if (NR == 1 || n < blocks)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        s[n][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], fqf[n][c][e], s[n][r], 0, 0, 0);
+                        } else if constexpr (TY == CACHE_BF16) {
+                            const bf16x8_t kf = as_bf16x8(kr[r][c]);
+#pragma unroll
+                            for (int n = 0; n < NR; ++n)
+                                if (NR == 1 || n < blocks)
+                                    s[n][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, fq[n][c], s[n][r], 0, 0, 0);
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                const bf16x8_t kf = e4m3_to_bf16(kr[r][c][2 * q], kr[r][c][2 * q + 1]);
+#pragma unroll
+                                for (int n = 0; n < NR; ++n)
+                                    if (NR == 1 || n < blocks)
+                                        s[n][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, fq[n][2 * c + q], s[n][r], 0, 0, 0);
+                            }
+                        }
+                    }
+                }
+                int32_t of_key[S::KR][4];  // token of key 16 r + 4 kg + i
+                if (!all_seen) {
+#pragma unroll
+                    for (int r = 0; r < S::KR; ++r)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) of_key[r][i] = __shfl(tok[r], 4 * kg + i, 64);
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) {
+                        const int last = lim[n] < 0 ? hi : lim[n];
+#pragma unroll
+                        for (int r = 0; r < S::KR; ++r)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) s[n][r][i] = of_key[r][i] <= last ? s[n][r][i] : -INFINITY;
+                    }
+                }
+                f32x4_t vf[F32 ? D / 16 : 1];
+                if constexpr (F32) {
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c) vf[c] = __builtin_bit_cast(f32x4_t, vr[0][c]);
+                }
+                if (p + kW * S::KT < pb) load(p + kW * S::KT);
+
+                // the running maximum moves only when a score exceeds it by
+                // more than kLazy (weights are then at most 2^kLazy), so that
+                // lanes compare notes and rescale rarely
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    if (NR > 1 && n >= blocks) continue;
+                    float mx = s[n][0][0];
+#pragma unroll
+                    for (int r = 0; r < S::KR; ++r)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[n][r][i]);
+                    mx *= c2;
+                    if (__ballot(mx > m_run[n] + kLazy) != 0ull) {
+                        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+                        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                        const float m_new = fmaxf(m_run[n], mx);
+                        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[n] - m_new);
+                        l_run[n] *= alpha;
+#pragma unroll
+                        for (int v = 0; v < NV; ++v)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[n][v][i] *= alpha;
+                        m_run[n] = m_new;
+                    }
+                    const float m_use = m_run[n] == -INFINITY ? 0.f : m_run[n];
+#pragma unroll
+                    for (int r = 0; r < S::KR; ++r)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            s[n][r][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r][i], c2, -m_use));
+                            l_run[n] += s[n][r][i];
+                        }
+                }
+
+                // O^T += V^T P^T
+                if constexpr (F32) {
+                    auto values = [&](auto odd_tile) {
+#pragma unroll
+                        for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    float x = vf[4 * c + i][e], odd = 0.f;
+                                    if constexpr (decltype(odd_tile)::value) {
+                                        const bool is = (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u;
+                                        odd = is ? 1.f : 0.f;
+                                        x = is ? 0.f : x;
+                                    }
+#pragma unroll
+                                    for (int n = 0; n < NR; ++n) {
+                                        if (NR > 1 && n >= blocks) continue;
+                                        f32x4_t &o = acc[n][4 * c + e];
+                                        o = __builtin_amdgcn_mfma_f32_16x16x4f32(x, s[n][0][i], o, 0, 0, 0);
+                                        if constexpr (decltype(odd_tile)::value) {
+                                            const float sees = of_key[0][i] <= (lim[n] < 0 ? hi : lim[n]) ? 1.f : 0.f;
+                                            const f32x4_t z = {0.f, 0.f, 0.f, 0.f};
+                                            const f32x4_t k = __builtin_amdgcn_mfma_f32_16x16x4f32(odd, sees, z, 0, 0, 0);
+#pragma unroll
+                                            for (int y = 0; y < 4; ++y) o[y] = k[y] > 0.f ? NAN : o[y];
+                                        }
+                                    }
+                                }
+                    };
+                    if (mixed)
+                        values(std::true_type());
+                    else
+                        values(std::false_type());
+                } else {
+                    bf16x8_t ph[NR], pl[NR];
+#pragma unroll
+                    for (int n = 0; n < NR; ++n)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                __bf16 x, y;
+                                split_weight(s[n][r % S::KR][i], x, y);
+                                ph[n][4 * r + i] = x;
+                                pl[n][4 * r + i] = y;
+                            }
+                    auto values = [&](auto odd_tile) {
+#pragma unroll
+                        for (int v = 0; v < NV; ++v) {
+                            const unsigned char *vp = vbuf + (4 * kg + (l16 >> 2)) * S::VRS + 2 * (16 * v + 4 * (l16 & 3));
+                            bf16x8_t vt = join8(lds_read_tr16(vp), lds_read_tr16(vp + 16 * S::VRS)), odd;
+                            if constexpr (decltype(odd_tile)::value) take_odd(vt, odd);
+#pragma unroll
+                            for (int n = 0; n < NR; ++n) {
+                                if (NR > 1 && n >= blocks) continue;
+                                f32x4_t &o = acc[n][v];
+                                o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, ph[n], o, 0, 0, 0);
+                                o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pl[n], o, 0, 0, 0);
+                                if constexpr (decltype(odd_tile)::value) {
+                                    bf16x8_t sees;
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e)
+                                        sees[e] = of_key[(e >> 2) % S::KR][e & 3] <= (lim[n] < 0 ? hi : lim[n]) ? (__bf16)1.f : (__bf16)0.f;
+                                    const f32x4_t z = {0.f, 0.f, 0.f, 0.f};
+                                    const f32x4_t k = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, sees, z, 0, 0, 0);
+#pragma unroll
+                                    for (int y = 0; y < 4; ++y) o[y] = k[y] > 0.f ? NAN : o[y];
+                                }
+                            }
+                        }
+                    };
+                    if (mixed)
+                        values(std::true_type());
+                    else
+                        values(std::false_type());
+                }
+            }
+        }
+
+        // ------------------------- the waves' sums joined, the result written
+        const Sink sink = sink_of(a, D, run, u0, u1, run.at == run0, false);
+        const float vs = a.v_scale ? a.v_scale[g] : 1.f;
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            if (n >= blocks) continue;  // (uniform)
+            __syncthreads();
+            float *ob = reinterpret_cast<float *>(smem + w * S::WAVE);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                if constexpr (F32) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ob[l16 * S::ORS + feature_of<TY>(v, i, kg)] = acc[n][v][i];
+                } else {
+                    *reinterpret_cast<f32x4_t *>(ob + l16 * S::ORS + feature_of<TY>(v, 0, kg)) = acc[n][v];
+                }
+            }
+            float l = l_run[n];
+            l += __shfl_xor(l, 16, 64);
+            l += __shfl_xor(l, 32, 64);
+            if (kg == 0) {
+                const bool none = lim[n] < 0;
+                // (scores that are all NaN leave no maximum, but their sum counts)
+                sh.m[w][l16] = none ? -INFINITY : l != l ? 0.f : m_run[n];
+                sh.l[w][l16] = none ? 0.f : l;
+            }
+            __syncthreads();
+            // 16 threads a row, D / 16 features each in pieces of four
+            const int q = tid >> 4, r = 16 * n + q;
+            if (r < rows.n) {
+                float m = -INFINITY, sum = 0.f, wt[kW];
+#pragma unroll
+                for (int v = 0; v < kW; ++v) m = fmaxf(m, sh.m[v][q]);
+#pragma unroll
+                for (int v = 0; v < kW; ++v) {
+                    wt[v] = sh.m[v][q] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sh.m[v][q] - m);
+                    sum += wt[v] * sh.l[v][q];
+                }
+                int b, t, h;
+                rows.of(a, r, b, t, h);
+                const int64_t orow = ((int64_t)b * a.n_q + t) * a.n_heads + h;
+                const float inv = inverse_sum(sum, vs);
+                float *part = sink.part(a, D, r, orow);
+#pragma unroll
+                for (int f0 = 0; f0 < D / 64; ++f0) {
+                    const int f = 64 * f0 + 4 * (tid & 15);
+                    f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int v = 0; v < kW; ++v) {
+                        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(reinterpret_cast<float *>(smem + v * S::WAVE) + q * S::ORS + f);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = wt[v] != 0.f ? __builtin_fmaf(wt[v], y[i], x[i]) : x[i];
+                    }
+                    if (sink.last_word) {
+                        if constexpr (F32) {
+                            *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.O) + orow * D + f) = x * inv;
+                        } else {
+                            bf16x4_t y;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) y[i] = (__bf16)(x[i] * inv);
+                            *reinterpret_cast<bf16x4_t *>(static_cast<__bf16 *>(a.O) + orow * D + f) = y;
+                        }
+                    } else {
+                        *reinterpret_cast<f32x4_t *>(part + f) = x;
+                    }
+                }
+                if ((tid & 15) == 0) {
+                    if (!sink.last_word) {
+                        part[D] = m;
+                        part[D + 1] = sum;
+                    } else if (a.lse) {
+                        a.lse[orow] = log_sum(m, sum);
+                    }
+                }
+            }
+        }
+        run.at = it.first + u1;
+        if (run.at >= run.end) return;
+        next_item(a, run.it);
+    }
+}
+
+// --------------------------------------------------------------- wide body
+//
+// S^T = K Q^T on 32x32 MFMA tiles: a lane owns one query row and 16 keys of a
+// 32-key block, which is the order in which O^T = V^T P^T takes them.  Up to
+// four row blocks, one a wave; items of fewer rows give two waves to a row
+// block, each with every other key block.
+
+template <int TY, int D>
+struct WideShape {
+    static constexpr int SIZE = TY == CACHE_BF16 ? 2 : 1;
+    static constexpr int KB = D <= 128 ? 64 : 32;  // keys of a staged tile
+    static constexpr int NB = KB / 32;
+    static constexpr int KRS = 2 * D + 16;  // bytes of a row of the K tile (odd in units of 16: rows in distinct banks)
+    static constexpr int VRS = 2 * D + 64;  // ... of the V tile (its transposed reads cover 4 rows x 32 bytes)
+    static constexpr int BUF = KB * (KRS + VRS);
+    static constexpr int OBYTES = 2 * 64 * (D / 32) * 16 * 4;  // two waves' accumulators
+    static constexpr int LDS = 2 * BUF > OBYTES ? 2 * BUF : OBYTES;
+    static constexpr int PPR = D * SIZE / 16;    // 16-byte pieces of a row
+    static constexpr int PT = KB * PPR / kT;     // pieces of a thread
+};
+
+template <int TY, int D>
+__device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsigned char *smem, bool pre, bool own)
+{
+    using S = WideShape<TY, D>;
+    constexpr int NMB = D / 32;
+    Run run;
+    if (!find_run(a, sh, pre, own, run)) return;
+    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+    const int64_t run0 = run.at;
+
+    for (;;) {
+        const Item &it = run.it;
+        const int u0 = (int)(run.at - it.first), u1 = (int)min((int64_t)it.units, run.end - it.first);
+        const Rows rows = rows_of(a, it);
+        const int g = rows.g;
+        // row blocks (1, 2 or 4), waves of a row block, this wave's of each
+        const int wr = rows.n <= 32 ? 1 : rows.n <= 64 ? 2 : 4, wk = min(S::NB, kW / wr);
+        const int rb = w & (wr - 1), kp = w / wr;
+        const bool on = kp < wk && 32 * rb < rows.n;
+
+        __syncthreads();  // (the last item's readers of LDS are done)
+        {
+            const int last = tid < rows.n ? rows.last(a, tid) : -1;
+            if (tid < 128) sh.lim[tid] = last;
+            int lo = last < 0 ? kNoToken : last, hi = last;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                lo = min(lo, __shfl_xor(lo, o, 64));
+                hi = max(hi, __shfl_xor(hi, o, 64));
+            }
+            if (lane == 0) {
+                sh.lo[w] = lo;
+                sh.hi[w] = hi;
+            }
+        }
+        Frag<bf16_t, D> fq;
+        {
+            int b, t, h;
+            rows.of(a, min(32 * rb + l32, rows.n - 1), b, t, h);
+            fq.load(static_cast<const bf16_t *>(a.Q) + (((int64_t)b * a.n_q + t) * a.n_heads + h) * D, hh);
+        }
+        __syncthreads();
+        const int lo = min(sh.lo[0], sh.lo[1]), hi = max(sh.hi[0], sh.hi[1]);  // (rows past 127 there are none)
+        const int lim = sh.lim[(32 * rb + l32) & 127], last = lim < 0 ? hi : lim;
+
+        float m_run = -INFINITY, l_run = 0.f;
+        f32x16_t acc[NMB];
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb) acc[mb] = f32x16_t{};
+        const float c2 = a.scale * 1.4426950408889634f * (a.k_scale ? a.k_scale[g] : 1.f);
+
+        const int base = it.prefix ? 0 : a.n_prefix;
+        const int n_pos = hi < base ? 0 : hi - base + 1;
+        const int p0 = (int)min((int64_t)u0 * kPagedUnit, (int64_t)n_pos);
+        const int p1 = (int)min((int64_t)u1 * kPagedUnit, (int64_t)n_pos);
+
+        for (int pa = p0; pa < p1; pa += a.batch_keys) {
+            const int pb = min(p1 - pa, a.batch_keys) + pa;
+            const int ch0 = a.pd.div(base + pa), ch1 = a.pd.div(base + pb - 1);
+            __syncthreads();
+            {
+                const int32_t *src = it.prefix ? a.prefix_pages : a.table + (int64_t)it.b * a.max_pages;
+                bool bad = false;
+                for (int c = ch0 + tid; c <= ch1; c += kT) {
+                    const int x = pool_page(src[c], a.n_pages);
+                    sh.phys[c - ch0] = x;
+                    bad = bad || x < 0;
+                }
+                const uint64_t any = __ballot(bad);
+                if (lane == 0) sh.bad[w] = any != 0ull;
+            }
+            __syncthreads();
+            const bool holes = (sh.bad[0] | sh.bad[1] | sh.bad[2] | sh.bad[3]) != 0;  // (uniform)
+            auto there = [&](int tok) { return sh.phys[a.pd.div(tok) - ch0] >= 0; };
+
+            u32x4_t kr[S::PT], vr[S::PT];
+            bool keep[S::PT];
+            auto load = [&](int p) {
+#pragma unroll
+                for (int q = 0; q < S::PT; ++q) {
+                    const int x = tid + q * kT, key = x / S::PPR, c = x % S::PPR;
+                    const int tok = base + min(p + key, pb - 1);
+                    const int ch = a.pd.div(tok);
+                    int phys = sh.phys[ch - ch0], place = tok - ch * a.pd.page;
+                    keep[q] = p + key < pb && phys >= 0;
+                    if (phys < 0) phys = place = 0;  // (row 0 of the pool is there)
+                    const int64_t off = pool_row(phys, a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE + 16 * c;
+                    kr[q] = *reinterpret_cast<const u32x4_t *>(static_cast<const unsigned char *>(a.K) + off);
+                    vr[q] = *reinterpret_cast<const u32x4_t *>(static_cast<const unsigned char *>(a.V) + off);
+                }
+            };
+            auto store = [&](unsigned char *buf) {
+#pragma unroll
+                for (int q = 0; q < S::PT; ++q) {
+                    const int x = tid + q * kT, key = x / S::PPR, c = x % S::PPR;
+                    unsigned char *kd = buf + key * S::KRS, *vd = buf + S::KB * S::KRS + key * S::VRS;
+                    // (a value that no row sees is 0: memory that was never written may hold NaN)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) vr[q][e] = keep[q] ? vr[q][e] : 0u;
+                    if constexpr (TY == CACHE_BF16) {
+                        *reinterpret_cast<u32x4_t *>(kd + 16 * c) = kr[q];
+                        *reinterpret_cast<u32x4_t *>(vd + 16 * c) = vr[q];
+                    } else {
+                        *reinterpret_cast<bf16x8_t *>(kd + 32 * c) = e4m3_to_bf16(kr[q][0], kr[q][1]);
+                        *reinterpret_cast<bf16x8_t *>(kd + 32 * c + 16) = e4m3_to_bf16(kr[q][2], kr[q][3]);
+                        *reinterpret_cast<bf16x8_t *>(vd + 32 * c) = e4m3_to_bf16(vr[q][0], vr[q][1]);
+                        *reinterpret_cast<bf16x8_t *>(vd + 32 * c + 16) = e4m3_to_bf16(vr[q][2], vr[q][3]);
+                    }
+                }
+            };
+            load(pa);
+            store(smem);
+            __syncthreads();
+            int cur = 0;
+            for (int p = pa; p < pb; p += S::KB, cur ^= 1) {
+                const bool more = p + S::KB < pb;
+                if (more) load(p + S::KB);
+                const unsigned char *kt = smem + cur * S::BUF, *vt = kt + S::KB * S::KRS;
+#pragma unroll 1
+                for (int kb = kp; kb < S::NB; kb += wk) {
+                    const int k0 = p + 32 * kb;
+                    if (!on || k0 >= pb) break;  // (wave-uniform)
+                    f32x16_t s = {};
+#pragma unroll
+                    for (int q = 0; q < D / 16; ++q) {
+                        const bf16x8_t kf = *reinterpret_cast<const bf16x8_t *>(kt + (32 * kb + l32) * S::KRS + hh * D + 16 * q);
+                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, fq.v[q], s, 0, 0, 0);
+                    }
+                    // (wave-uniform) every key of the block is seen by every row;
+                    // else bit r of `seen`: this lane's row sees key acc_row(r, hh)
+                    const bool open = k0 + 31 < pb && base + k0 + 31 <= lo && !holes;
+                    uint32_t seen = 0u;
+                    if (!open) {
+#pragma unroll 1
+                        for (int r = 0; r < 16; ++r) {
+                            const int x = k0 + acc_row(r, hh), tok = base + x;
+                            const bool is = x < pb && tok <= last && (!holes || there(tok));
+                            seen |= (uint32_t)is << r;
+                        }
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[r] = (seen >> r) & 1u ? s[r] : -INFINITY;
+                    }
+                    float mx = s[0];
+#pragma unroll
+                    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+                    mx *= c2;
+                    if (__ballot(mx > m_run + kLazy) != 0ull) {  // (the maximum moves rarely, as in the narrow body)
+                        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                        const float m_new = fmaxf(m_run, mx);
+                        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+                        l_run *= alpha;
+#pragma unroll
+                        for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) acc[mb][r] *= alpha;
+                        m_run = m_new;
+                    }
+                    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+                    bf16x8_t ph[2], pl[2];
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, -m_use));
+                        l_run += x;
+                        __bf16 y, z;
+                        split_weight(x, y, z);
+                        ph[r >> 3][r & 7] = y;
+                        pl[r >> 3][r & 7] = z;
+                    }
+                    auto values = [&](auto odd_tile) {
+#pragma unroll
+                        for (int mb = 0; mb < NMB; ++mb) {
+#pragma unroll
+                            for (int s2 = 0; s2 < 2; ++s2) {
+                                // keys 16 s2 + 4 hh + 0..3 and + 8..11 of the block, the order of the accumulator
+                                const int j = lane & 15;
+                                const unsigned char *vp = vt + (32 * kb + 16 * s2 + 4 * hh + (j >> 2)) * S::VRS +
+                                                          2 * (32 * mb + 16 * (l32 >> 4) + 4 * (j & 3));
+                                bf16x8_t vf = join8(lds_read_tr16(vp), lds_read_tr16(vp + 8 * S::VRS)), odd;
+                                if constexpr (decltype(odd_tile)::value) take_odd(vf, odd);
+                                acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph[s2], acc[mb], 0, 0, 0);
+                                acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[s2], acc[mb], 0, 0, 0);
+                                if constexpr (decltype(odd_tile)::value) {
+                                    bf16x8_t see;
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) see[e] = (seen >> (8 * s2 + e)) & 1u ? (__bf16)1.f : (__bf16)0.f;
+                                    const f32x16_t z = {};
+                                    const f32x16_t k = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd, see, z, 0, 0, 0);
+#pragma unroll
+                                    for (int r = 0; r < 16; ++r) acc[mb][r] = k[r] > 0.f ? NAN : acc[mb][r];
+                                }
+                            }
+                        }
+                    };
+                    if (!open && lo < hi && base + k0 + 31 > lo)
+                        values(std::true_type());
+                    else
+                        values(std::false_type());
+                }
+                if (more) store(smem + (cur ^ 1) * S::BUF);
+                __syncthreads();
+            }
+        }
+
+        // ------------------------------------------------- the result written
+        const Sink sink = sink_of(a, D, run, u0, u1, run.at == run0, true);
+        l_run += __shfl_xor(l_run, 32, 64);
+        // (scores that are all NaN leave no maximum, but their sum counts)
+        m_run = lim < 0 ? -INFINITY : l_run != l_run ? 0.f : m_run;
+        l_run = lim < 0 ? 0.f : l_run;
+        __syncthreads();
+        if (wk == 2) {  // (uniform) the second wave of a row block hands its sums to the first
+            f32x4_t *ob = reinterpret_cast<f32x4_t *>(smem) + rb * (64 * NMB * 4) + lane;
+            if (on && kp == 1) {
+#pragma unroll
+                for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        ob[(4 * mb + q) * 64] = f32x4_t{acc[mb][4 * q], acc[mb][4 * q + 1], acc[mb][4 * q + 2], acc[mb][4 * q + 3]};
+                if (hh == 0) {
+                    sh.m[rb][l32] = m_run;
+                    sh.l[rb][l32] = l_run;
+                }
+            }
+            __syncthreads();
+            if (on && kp == 0) {
+                const float m1 = sh.m[rb][l32], m = fmaxf(m_run, m1);
+                const float w0 = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m);
+                const float w1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 - m);
+#pragma unroll
+                for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4_t y = ob[(4 * mb + q) * 64];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = w0 != 0.f ? w0 * acc[mb][4 * q + i] : 0.f;
+                            acc[mb][4 * q + i] = w1 != 0.f ? __builtin_fmaf(w1, y[i], x) : x;
+                        }
+                    }
+                l_run = w0 * l_run + w1 * sh.l[rb][l32];
+                m_run = m;
+            }
+        }
+        const int r = 32 * rb + l32;
+        if (on && kp == 0 && r < rows.n) {
+            int b, t, h;
+            rows.of(a, r, b, t, h);
+            const int64_t orow = ((int64_t)b * a.n_q + t) * a.n_heads + h;
+            const float inv = inverse_sum(l_run, a.v_scale ? a.v_scale[g] : 1.f);
+            float *part = sink.part(a, D, r, orow);
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int f = 32 * mb + 8 * q + 4 * hh;
+                    if (sink.last_word) {
+                        bf16x4_t y;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] = (__bf16)(acc[mb][4 * q + i] * inv);
+                        *reinterpret_cast<bf16x4_t *>(static_cast<__bf16 *>(a.O) + orow * D + f) = y;
+                    } else {
+                        *reinterpret_cast<f32x4_t *>(part + f) =
+                            f32x4_t{acc[mb][4 * q], acc[mb][4 * q + 1], acc[mb][4 * q + 2], acc[mb][4 * q + 3]};
+                    }
+                }
+            }
+            if (hh == 0) {
+                if (!sink.last_word) {
+                    part[D] = m_run;
+                    part[D + 1] = l_run;
+                } else if (a.lse) {
+                    a.lse[orow] = log_sum(m_run, l_run);
+                }
+            }
+        }
+        run.at = it.first + u1;
+        if (run.at >= run.end) return;
+        next_item(a, run.it);
+    }
+}
+
+// The bodies of a launch one after the other: WIDE for the items of many
+// rows, NR > 0 (16-row blocks) for the others.
+template <int TY, int D, bool WIDE, int NR>
+__global__ __launch_bounds__(kT, D <= 128 && NR <= 1 ? 2 : 1) void paged_kernel(PagedArgs a)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ Common sh;
+    if constexpr (WIDE) wide_body<TY, D>(a, sh, smem, a.prefix_wide, a.own_wide);
+    if constexpr (NR > 0) narrow_body<TY, D, NR>(a, sh, smem, !a.prefix_wide && a.prefix_items > 0, !a.own_wide);
+}
+
+template <int TY, int D, bool WIDE, int NR>
+hipError_t launch_one(const PagedArgs &a, hipStream_t stream)
+{
+    constexpr int narrow = NR > 0 ? Shape<TY, D>::LDS : 0;
+    constexpr int lds = WIDE && WideShape<TY, D>::LDS > narrow ? WideShape<TY, D>::LDS : narrow;
+    static LdsLimit seen;
+    const void *fn = reinterpret_cast<const void *>(&paged_kernel<TY, D, WIDE, NR>);
+    hipError_t e = raise_lds_limit(fn, lds + sizeof(Common), seen);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((paged_kernel<TY, D, WIDE, NR>), dim3((unsigned)a.grid), dim3(kT), lds, stream, a);
+    return hipGetLastError();
+}
+
+template <int TY, int D>
+hipError_t launch_d(const PagedArgs &a, hipStream_t stream)
+{
+    if constexpr (TY == CACHE_F32) {
+        return a.narrow_tile == 16 ? launch_one<TY, D, false, 1>(a, stream) : launch_one<TY, D, false, 2>(a, stream);
+    } else {
+        if (a.own_wide) return launch_one<TY, D, true, 0>(a, stream);
+        return a.prefix_wide ? launch_one<TY, D, true, 1>(a, stream) : launch_one<TY, D, false, 1>(a, stream);
+    }
+}
+
+}  // namespace paged
+}  // namespace rr
