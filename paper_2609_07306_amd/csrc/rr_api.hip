@@ -1004,7 +1004,8 @@ rr_status paged_args(const rr_paged_config *cfg, rr::PagedArgs *out)
     a.n_prefix = c.n_prefix;
     a.pd = rr::page_div(c.page);
     a.scale = c.scale > 0.f ? c.scale : 1.f / std::sqrt((float)c.d);
-    rr::paged_schedule(a, c.cache_dtype, c.d);
+    if (!rr::paged_schedule(a, c.cache_dtype, c.d))
+        return fail(RR_ERR_UNSUPPORTED, "n_seqs * max_pages * page * n_kv_heads is too large: 2^31 times 128 keys at most");
     *out = a;
     return RR_OK;
 }

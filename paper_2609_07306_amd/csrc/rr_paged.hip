@@ -6,9 +6,10 @@ namespace rr {
 namespace {
 
 using paged::f32x4_t;
-using paged::kLn2;
-using paged::kT;
-using paged::kW;
+using paged::inverse_sum;
+using paged::log_sum;
+
+constexpr int kT = 256;  // threads of a joining workgroup
 
 // -------------------------------------------------------------------- join
 //
@@ -20,10 +21,9 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
 {
     constexpr int PL = D / 4;      // lanes of a part, four features each
     constexpr int NP = kT / PL;    // parts in flight
-    __shared__ float s_w[2 * kPagedGrid + 2];
-    __shared__ float s_red[kW];
+    __shared__ float s_m[NP], s_l[NP];
     __shared__ float s_acc[NP][D];
-    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
+    const int tid = threadIdx.x;
     const int64_t orow = blockIdx.x;  // (b, t, h)
     const int h = (int)(orow % a.n_heads);
     const int64_t bt = orow / a.n_heads;
@@ -42,11 +42,18 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
     const int4 own = a.heads[a.prefix_items + (int64_t)b * a.items_per_seq + item];
     int n_own = own.z, n_pre = 0, pre_row = 0;
     int4 pre = {0, 0, 0, 0};
+    const float *pre_part = nullptr;  // of a wide prefix: its splits lie a.prefix_tiles slots apart
     if (a.prefix_items) {
-        const int r = b * a.rows + t * a.group + j;
-        pre = a.heads[g * a.prefix_tiles + r / a.prefix_tile];
-        pre_row = r % a.prefix_tile;
-        n_pre = pre.z;
+        const int r = b * a.rows + t * a.group + j, x = r / a.prefix_tile;
+        pre_row = r - x * a.prefix_tile;
+        if (a.prefix_wide) {
+            n_pre = a.prefix_splits;
+            const int slot = g * a.prefix_splits * a.prefix_tiles + x;
+            pre_part = a.prefix_parts + ((int64_t)slot * a.prefix_tile + pre_row) * (D + 4);
+        } else {
+            pre = a.heads[g * a.prefix_tiles + x];
+            n_pre = pre.z;
+        }
     } else if (n_own == 1) {
         return;  // (uniform) its workgroup wrote the result
     }
@@ -55,58 +62,62 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
         const bool p = i >= n_own;
         const int4 &hd = p ? pre : own;
         i = p ? i - n_own : i;
+        if (p && pre_part) return pre_part + (int64_t)i * a.prefix_tiles * a.prefix_tile * (D + 4);
         if (hd.z == 1) return a.whole + ((p ? 0 : n_rows) + orow) * (D + 4);
         const int64_t slot = i == 0 ? hd.x : 2 * (int64_t)(hd.y + i);
-        return (hd.w ? a.wide_parts : a.parts) + (slot * (hd.w ? a.wide_tile : a.narrow_tile) + (p ? pre_row : own_row)) * (D + 4);
+        return (hd.w ? a.wide_parts : a.parts) + (slot * (hd.w ? a.own_tile : a.narrow_tile) + (p ? pre_row : own_row)) * (D + 4);
     };
     const int n = n_own + n_pre;
 
-    float m = -INFINITY;
-    for (int i = tid; i < n; i += kT) {
-        const float x = part_of(i)[D];
-        s_w[i] = x;
-        m = fmaxf(m, x);
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    if (lane == 0) s_red[w] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-    __syncthreads();
-    float l = 0.f;
-    for (int i = tid; i < n; i += kT) {
-        const float x = s_w[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_w[i] - m);
-        l += x * part_of(i)[D + 1];
-        s_w[i] = x;
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o, 64);
-    if (lane == 0) s_red[w] = l;
-    __syncthreads();
-    l = (s_red[0] + s_red[1]) + (s_red[2] + s_red[3]);
-
+    // PL lanes a part, NP parts at once, kept with a running maximum like the
+    // attention's own: sums and statistics are asked for together
     const int pl = tid % PL, pg = tid / PL;
     f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 4
     for (int i = pg; i < n; i += NP) {
-        const float wt = s_w[i];
-        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(part_of(i) + 4 * pl);
+        const float *p = part_of(i);
+        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(p + 4 * pl);
+        const float mi = p[D], li = p[D + 1];
+        const float m_new = fmaxf(m, mi);
+        const float w0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+        const float w1 = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - m_new);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = wt != 0.f ? __builtin_fmaf(wt, y[e], x[e]) : x[e];
+        for (int e = 0; e < 4; ++e) {
+            const float z = w0 != 0.f ? w0 * x[e] : 0.f;
+            x[e] = w1 != 0.f ? __builtin_fmaf(w1, y[e], z) : z;
+        }
+        l = w0 * l + w1 * li;
+        m = m_new;
     }
     *reinterpret_cast<f32x4_t *>(&s_acc[pg][4 * pl]) = x;
+    if (pl == 0) {
+        s_m[pg] = m;
+        s_l[pg] = l;
+    }
     __syncthreads();
-    const float vs = a.v_scale ? a.v_scale[g] : 1.f, inv = l > 0.f ? vs / l : l == 0.f ? 0.f : l;
+    m = -INFINITY;
+    l = 0.f;
+    float wt[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) m = fmaxf(m, s_m[i]);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        wt[i] = s_m[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[i] - m);
+        l += wt[i] * s_l[i];
+    }
+    const float inv = inverse_sum(l, a.v_scale ? a.v_scale[g] : 1.f);
     for (int f = tid; f < D; f += kT) {
         float y = 0.f;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) y += s_acc[i][f];
+        for (int i = 0; i < NP; ++i) y = wt[i] != 0.f ? __builtin_fmaf(wt[i], s_acc[i][f], y) : y;
         y *= inv;
         if constexpr (F32)
             static_cast<float *>(a.O)[orow * D + f] = y;
         else
             static_cast<__bf16 *>(a.O)[orow * D + f] = (__bf16)y;
     }
-    if (tid == 0 && a.lse) a.lse[orow] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
+    if (tid == 0 && a.lse) a.lse[orow] = log_sum(m, l);
 }
 
 }  // namespace
@@ -117,7 +128,7 @@ bool paged_supported(int dtype, int cache, int d)
     return (cache == CACHE_BF16 || cache == CACHE_E4M3) && (d == 64 || d == 128 || d == 256);
 }
 
-void paged_schedule(PagedArgs &a, int cache, int d)
+bool paged_schedule(PagedArgs &a, int cache, int d)
 {
     const int per_b = a.n_q * a.group;
     const bool routed = a.k + a.n_sink + a.n_recent > 0, f32 = cache == CACHE_F32;
@@ -142,20 +153,38 @@ void paged_schedule(PagedArgs &a, int cache, int d)
     a.prefix_items = a.n_kv_heads * a.prefix_tiles;
     a.prefix_units = (a.n_prefix + kPagedUnit - 1) / kPagedUnit;
     a.narrow_tile = !a.own_wide ? a.own_tile : !a.prefix_wide && a.n_prefix ? a.prefix_tile : 0;
-    a.wide_tile = (a.own_wide ? a.own_tile : 0) > (a.prefix_wide ? a.prefix_tile : 0) ? a.own_tile : a.prefix_wide ? a.prefix_tile : 0;
     const int64_t keys = (int64_t)(paged::kStagedPages - 1) * a.pd.page / kPagedUnit * kPagedUnit;
     a.batch_keys = (int32_t)(keys < (1 << 30) ? keys : (1 << 30));
     a.min_units = 1;
     // units of the longest sequences that the page table can hold
-    int64_t most = routed ? a.route_units : (a.capacity + kPagedUnit - 1) / kPagedUnit;
-    most = most * a.items_per_seq * a.n_seqs + (int64_t)a.prefix_items * a.prefix_units;
-    const int64_t need = (most + a.min_units - 1) / a.min_units;
-    a.grid = (int32_t)(need < kPagedGrid ? need : kPagedGrid);
+    const double most_own = (double)(routed ? a.route_units : (a.capacity + kPagedUnit - 1) / kPagedUnit) * a.items_per_seq * a.n_seqs;
+    const double most = most_own + (double)a.prefix_items * a.prefix_units;
+    if (most >= (double)INT32_MAX) return false;
+    // splits of a wide prefix: the fewest that leave at most a tenth more of
+    // the card idle than the best number does, of two units at least
+    a.prefix_splits = a.prefix_slots = 0;
+    if (a.prefix_wide) {
+        const auto used = [&](int splits) {
+            const int n = a.prefix_items * splits, rounds = (n + kPagedGrid - 1) / kPagedGrid;
+            return (double)n / ((double)rounds * kPagedGrid);
+        };
+        const int most_splits = a.prefix_units / 2 < 1 ? 1 : a.prefix_units / 2 < kPagedGrid ? a.prefix_units / 2 : kPagedGrid;
+        double best = 0.;
+        for (int n = 1; n <= most_splits; ++n) best = used(n) > best ? used(n) : best;
+        a.prefix_splits = 1;
+        while (used(a.prefix_splits) < 0.9 * best) ++a.prefix_splits;
+        a.prefix_slots = a.prefix_items * a.prefix_splits;
+    }
+    const double need = a.prefix_wide ? (most_own > a.prefix_slots ? most_own : a.prefix_slots) : most;
+    a.grid = need < kPagedGrid ? (int32_t)need : kPagedGrid;
+    return true;
 }
 
 static int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
 
 static int64_t parts_bytes(const PagedArgs &a, int d, int tile) { return align256((int64_t)2 * a.grid * tile * (d + 4) * 4); }
+
+static int64_t prefix_bytes(const PagedArgs &a, int d) { return align256((int64_t)a.prefix_slots * a.prefix_tile * (d + 4) * 4); }
 
 static int64_t whole_bytes(const PagedArgs &a, int d)
 {
@@ -165,7 +194,7 @@ static int64_t whole_bytes(const PagedArgs &a, int d)
 size_t paged_workspace_bytes(const PagedArgs &a, int d)
 {
     const int64_t items = a.prefix_items + (int64_t)a.n_seqs * a.items_per_seq;
-    return (size_t)(parts_bytes(a, d, a.narrow_tile) + parts_bytes(a, d, a.wide_tile) + whole_bytes(a, d) + align256(items * 16));
+    return (size_t)(parts_bytes(a, d, a.narrow_tile) + parts_bytes(a, d, a.own_wide ? a.own_tile : 0) + prefix_bytes(a, d) + whole_bytes(a, d) + align256(items * 16));
 }
 
 void paged_layout(PagedArgs &a, int d, void *workspace)
@@ -174,7 +203,9 @@ void paged_layout(PagedArgs &a, int d, void *workspace)
     a.parts = reinterpret_cast<float *>(p);
     p += parts_bytes(a, d, a.narrow_tile);
     a.wide_parts = reinterpret_cast<float *>(p);
-    p += parts_bytes(a, d, a.wide_tile);
+    p += parts_bytes(a, d, a.own_wide ? a.own_tile : 0);
+    a.prefix_parts = reinterpret_cast<float *>(p);
+    p += prefix_bytes(a, d);
     a.whole = reinterpret_cast<float *>(p);
     p += whole_bytes(a, d);
     a.heads = reinterpret_cast<int4 *>(p);

@@ -106,17 +106,20 @@ struct PagedArgs {
     int32_t route_units;    // routes: units of every item
     int32_t prefix_rows, prefix_tile, prefix_tiles, prefix_items, prefix_units;  // of the batch against the prefix
     bool own_wide, prefix_wide;        // which body takes them
-    int32_t narrow_tile, wide_tile;    // rows of a body's parts
+    int32_t prefix_splits, prefix_slots;  // of the wide body: key splits, (key head, split, row tile) slots
+    int32_t narrow_tile;               // rows of a narrow item at most
     int32_t grid, min_units, batch_keys;
     // workspace
     float *parts, *wide_parts;  // [2 * grid] parts of each body's items that several workgroups share
-    float *whole;    // prefix: [2][rows of the call] parts of items that one workgroup held
+    float *prefix_parts;        // [prefix_slots] parts
+    float *whole;    // with a prefix: [2][rows of the call] parts of items that one workgroup held
     int4 *heads;     // per item: its first part, its first workgroup, its parts, its body
 };
 
 size_t paged_workspace_bytes(const PagedArgs &a, int d);
-// Fills in the schedule of a call whose shape is set; cache: CacheType.
-void paged_schedule(PagedArgs &a, int cache, int d);
+// Fills in the schedule of a call whose shape is set; cache: CacheType.  False
+// where it has 2^31 units of work or more.
+bool paged_schedule(PagedArgs &a, int cache, int d);
 // Lays the workspace out from its first byte.
 void paged_layout(PagedArgs &a, int d, void *workspace);
 bool paged_supported(int dtype, int cache, int d);

@@ -41,8 +41,7 @@ typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef short short8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kT = 256;             // threads of a workgroup
-constexpr int kW = kT / 64;         // waves
+constexpr int kMostWaves = 4;       // waves of a workgroup at most
 constexpr int kStagedPages = 512;   // page numbers held in LDS at a time
 constexpr float kLazy = 8.f;        // log2 headroom of the running softmax maximum
 constexpr float kLn2 = 0.6931471805599453f;
@@ -73,12 +72,21 @@ __device__ __forceinline__ bf16x8_t e4m3_to_bf16(uint32_t lo, uint32_t hi)
     return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// A weight as the sum of two bf16 numbers, 2^-17 off: rounded to one, it would
-// add as much error as the rounding of the output.
-__device__ __forceinline__ void split_weight(float x, __bf16 &hi, __bf16 &lo)
+// Eight weights as sums of two bf16 numbers each, 2^-16 off: rounded to one,
+// they would add as much error as the rounding of the output.  The first
+// number is the weight cut off after its eighth bit (a mask, no rounding), the
+// second what that leaves, rounded.
+__device__ __forceinline__ void split_weights(const float (&x)[8], bf16x8_t &hi, bf16x8_t &lo)
 {
-    hi = (__bf16)x;
-    lo = (__bf16)(x - (float)hi);
+    u32x4_t h;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t a = __float_as_uint(x[2 * q]), b = __float_as_uint(x[2 * q + 1]);
+        h[q] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // the upper halves of b and a
+        lo[2 * q] = (__bf16)(x[2 * q] - __uint_as_float(a & 0xFFFF0000u));
+        lo[2 * q + 1] = (__bf16)(x[2 * q + 1] - __uint_as_float(b & 0xFFFF0000u));
+    }
+    hi = as_bf16x8(h);
 }
 
 // Where some rows of a product see a token and others don't, a value that is
@@ -107,26 +115,28 @@ struct Item {
     int32_t b;      // sequence
     int32_t j;      // item within the sequence (or within the prefix)
     int32_t units;  // its units
-    int64_t first;  // its first unit
-    int64_t index;  // its number (of its head)
+    int32_t first;  // its first unit
+    int32_t index;  // its number (of its head)
 };
 
 struct Run {
-    int64_t at, end, per_wg;  // units [at, end) of the body's
+    int32_t at, end, per_wg;  // units [at, end) of the body's
     Item it;
 };
+
+// A value that is the same in all lanes, as the scalar that it is.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // LDS that both bodies use.
 struct Common {
     int32_t phys[kStagedPages];
     int32_t chunk[kMaxAttnSlots];
-    int64_t sum[kW];
-    int64_t at[3];
-    int32_t b;
-    int32_t count[kW];
-    int32_t lo[kW], hi[kW], bad[kW];
-    int32_t lim[128];
-    float m[kW][32], l[kW][32];
+    int32_t sum[kMostWaves];
+    int32_t at, b;
+    int32_t count[kMostWaves];
+    int32_t lo[kMostWaves], hi[kMostWaves], bad[kMostWaves];
+    int32_t lim[32 * kMostWaves];
+    float m[kMostWaves][32], l[kMostWaves][32];
 };
 
 __device__ __forceinline__ int32_t seq_units(const PagedArgs &a, int32_t b)
@@ -138,67 +148,82 @@ __device__ __forceinline__ int32_t seq_units(const PagedArgs &a, int32_t b)
 
 // This workgroup's run of the items that a body takes: the prefix's, the
 // sequences', or one after the other.  False where it has none.
+template <int NW>
 __device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, bool pre, bool own, Run &r)
 {
+    constexpr int T = 64 * NW;
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
-    const int64_t prefix_total = pre ? (int64_t)a.prefix_items * a.prefix_units : 0;
-    const int per = (a.n_seqs + kT - 1) / kT;
-    const int b0 = own ? min(tid * per, a.n_seqs) : 0, b1 = own ? min(b0 + per, a.n_seqs) : 0;
-    int64_t sum = 0;
+    // (a call has less than 2^31 units)
+    const int prefix_total = pre ? a.prefix_items * a.prefix_units : 0;
+    // per thread: its sequences, their units and those of all before them
+    const bool few = a.n_seqs <= 64;
+    const int per = few ? 1 : (a.n_seqs + T - 1) / T;
+    const int b0 = own ? min((few ? lane : tid) * per, a.n_seqs) : 0, b1 = own ? min(b0 + per, a.n_seqs) : 0;
+    int sum = 0;
     for (int b = b0; b < b1; ++b) sum += seq_units(a, b);
-    int64_t inc = sum;
+    int before = sum;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int64_t v = (int64_t)shfl_u64((uint64_t)inc, max(lane - o, 0));
-        inc += lane >= o ? v : 0;
+        const int v = __shfl_up(before, o, 64);
+        before += lane >= o ? v : 0;
     }
-    __syncthreads();  // (an earlier body's readers of LDS are done)
-    if (lane == 63) sh.sum[w] = inc;
-    if (tid == 0) {
-        sh.b = 0;
-        sh.at[2] = 0;
-    }
-    __syncthreads();
-    int64_t before = inc - sum, all = 0;
-    for (int v = 0; v < kW; ++v) {
-        before += v < w ? sh.sum[v] : 0;
-        all += sh.sum[v];
-    }
-    const int64_t total = prefix_total + all * a.items_per_seq;
-    const int64_t share = (total + a.grid - 1) / a.grid;
-    r.per_wg = share > a.min_units ? share : a.min_units;
-    r.at = blockIdx.x * r.per_wg;
-    r.end = min(r.at + r.per_wg, total);
-    if (r.at >= r.end) return false;  // (uniform)
-    // the sequence that the run begins in
-    const int64_t u = (r.at - prefix_total) / a.items_per_seq;
-    if (own && r.at >= prefix_total && u >= before && u < before + sum) {
-        int b = b0;
-        int64_t base = before;
-        for (;;) {
-            const int32_t n = seq_units(a, b);
-            if (u < base + n) break;
-            base += n;
-            ++b;
+    int all = __builtin_amdgcn_readlane(before, 63);
+    before -= sum;
+    if (!few) {  // (else each wave for itself, without a barrier)
+        __syncthreads();  // (an earlier body's readers of LDS are done)
+        if (lane == 0) sh.sum[w] = all;
+        __syncthreads();
+        all = 0;
+        for (int v = 0; v < NW; ++v) {
+            before += v < w ? sh.sum[v] : 0;
+            all += sh.sum[v];
         }
-        sh.b = b;
-        sh.at[2] = base;
+        all = uniform(all);
     }
-    __syncthreads();
+    const int total = prefix_total + all * a.items_per_seq, share = (total + a.grid - 1) / a.grid;
+    r.per_wg = max(share, a.min_units);
+    if ((int64_t)blockIdx.x * r.per_wg >= total) return false;
+    r.at = blockIdx.x * r.per_wg;
+    r.end = total - r.at < r.per_wg ? total : r.at + r.per_wg;
+    // the sequence that the run begins in, and the units before it
+    int b_at = 0, b_before = 0;
+    if (own && r.at >= prefix_total) {
+        const int u = (r.at - prefix_total) / a.items_per_seq;
+        const bool mine = u >= before && u < before + sum;
+        if (few) {
+            b_at = __ffsll((unsigned long long)__ballot(mine)) - 1;
+            b_before = __builtin_amdgcn_readlane(before, b_at);
+        } else {
+            if (mine) {
+                int b = b0, base = before;
+                for (;;) {
+                    const int n = seq_units(a, b);
+                    if (u < base + n) break;
+                    base += n;
+                    ++b;
+                }
+                sh.b = b;
+                sh.at = base;
+            }
+            __syncthreads();
+            b_at = uniform(sh.b);
+            b_before = uniform(sh.at);
+        }
+    }
     Item &it = r.it;
-    it.b = sh.b;
+    it.b = b_at;
     it.prefix = r.at < prefix_total;
     if (it.prefix) {
         it.units = a.prefix_units;
-        it.j = (int32_t)(r.at / it.units);
+        it.j = r.at / it.units;
         it.index = it.j;
-        it.first = it.index * it.units;
+        it.first = it.j * it.units;
     } else {
-        const int64_t base = prefix_total + sh.at[2] * a.items_per_seq;
-        it.units = seq_units(a, it.b);
-        it.j = (int32_t)((r.at - base) / it.units);
-        it.index = a.prefix_items + (int64_t)it.b * a.items_per_seq + it.j;
-        it.first = base + (int64_t)it.j * it.units;
+        const int base = prefix_total + b_before * a.items_per_seq;
+        it.units = uniform(seq_units(a, b_at));
+        it.j = (r.at - base) / it.units;
+        it.index = a.prefix_items + b_at * a.items_per_seq + it.j;
+        it.first = base + it.j * it.units;
     }
     return true;
 }
@@ -212,12 +237,12 @@ __device__ __forceinline__ void next_item(const PagedArgs &a, Item &it)
         if (it.j == a.prefix_items) {
             it.prefix = false;
             it.j = it.b = 0;
-            it.units = seq_units(a, 0);
+            it.units = uniform(seq_units(a, 0));
         }
     } else if (it.j == a.items_per_seq) {
         it.j = 0;
         ++it.b;
-        it.units = seq_units(a, it.b);
+        it.units = uniform(seq_units(a, it.b));
     }
 }
 
@@ -273,15 +298,15 @@ __device__ __forceinline__ Rows rows_of(const PagedArgs &a, const Item &it)
 
 // Where a body writes an item's result: the output itself where no other item
 // or workgroup has a part in its rows, else a part of D sums, the maximum and
-// the sum of weights.
+// the sum of weights: D + 4 floats a row.
 struct Sink {
-    bool last_word, entire, prefix;
-    float *cut;  // parts of this run's cut item, D + 4 floats a row
+    bool last_word;
+    float *by_row;  // parts by row of the call, or null:
+    float *cut;     // parts by row of the item
 
-    __device__ __forceinline__ float *part(const PagedArgs &a, int D, int r, int64_t orow) const
+    __device__ __forceinline__ float *part(int D, int r, int64_t orow) const
     {
-        const int64_t half = prefix ? 0 : (int64_t)a.n_seqs * a.n_q * a.n_heads;
-        return entire ? a.whole + (half + orow) * (D + 4) : cut + (int64_t)r * (D + 4);
+        return by_row ? by_row + orow * (D + 4) : cut + (int64_t)r * (D + 4);
     }
 };
 
@@ -289,15 +314,15 @@ struct Sink {
 // slot of its first part, its first workgroup, its parts, and the body.
 __device__ __forceinline__ Sink sink_of(const PagedArgs &a, int D, const Run &r, int u0, int u1, bool first, bool wide)
 {
+    const bool entire = u0 == 0 && u1 == r.it.units;
+    const int slot = 2 * (int)blockIdx.x + (first ? 0 : 1);
     Sink s;
-    s.prefix = r.it.prefix;
-    s.entire = u0 == 0 && u1 == r.it.units;
-    s.last_word = s.entire && a.prefix_items == 0;
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (first ? 0 : 1);
-    s.cut = (wide ? a.wide_parts : a.parts) + slot * (wide ? a.wide_tile : a.narrow_tile) * (D + 4);
+    s.last_word = entire && a.prefix_items == 0;
+    s.by_row = entire ? a.whole + (r.it.prefix ? 0 : (int64_t)a.n_seqs * a.n_q * a.n_heads) * (D + 4) : nullptr;
+    s.cut = (wide ? a.wide_parts : a.parts) + (int64_t)slot * (wide ? a.own_tile : a.narrow_tile) * (D + 4);
     if (u0 == 0 && threadIdx.x == 0) {
-        const int64_t last_wg = (r.it.first + r.it.units - 1) / r.per_wg;
-        a.heads[r.it.index] = int4{(int)slot, (int)blockIdx.x, (int)(last_wg - blockIdx.x) + 1, wide ? 1 : 0};
+        const int last_wg = (r.it.first + r.it.units - 1) / r.per_wg;
+        a.heads[r.it.index] = int4{slot, (int)blockIdx.x, last_wg - (int)blockIdx.x + 1, wide ? 1 : 0};
     }
     return s;
 }
@@ -335,7 +360,6 @@ struct Shape {
     static constexpr int VBYTES = TY == CACHE_F32 ? 0 : KT * VRS;
     static constexpr int OBYTES = 16 * ORS * 4;
     static constexpr int WAVE = VBYTES > OBYTES ? VBYTES : OBYTES;
-    static constexpr int LDS = kW * WAVE;
 };
 
 // The feature that element i of value accumulator v belongs to, for lane
@@ -349,23 +373,38 @@ __device__ __forceinline__ int feature_of(int v, int i, int kg)
         return 16 * v + 4 * kg + i;
 }
 
-template <int TY, int D, int NR>
+template <int TY, int D, int NR, int NW>
 __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsigned char *smem, bool pre, bool own)
 {
     using S = Shape<TY, D>;
     constexpr bool F32 = TY == CACHE_F32;
     constexpr int NV = D / 16;  // value accumulators of a row block
+    constexpr int T = 64 * NW;
     Run run;
-    if (!find_run(a, sh, pre, own, run)) return;
-    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, l16 = lane & 15, kg = lane >> 4;
+    if (!find_run<NW>(a, sh, pre, own, run)) return;
+    const int tid = threadIdx.x, w = uniform(tid >> 6), lane = tid & 63, l16 = lane & 15, kg = lane >> 4;
     unsigned char *vbuf = smem + w * S::WAVE;
-    const int64_t run0 = run.at;
+    const int run0 = run.at;
 
     for (;;) {
         const Item &it = run.it;
-        const int u0 = (int)(run.at - it.first), u1 = (int)min((int64_t)it.units, run.end - it.first);
+        const int u0 = run.at - it.first, u1 = min(it.units, run.end - it.first);
         const Rows rows = rows_of(a, it);
         const int g = rows.g, blocks = (rows.n + 15) >> 4;
+
+        // key positions: tokens from `base` on, or, along routes, the places
+        // of the listed pages one after the other.  The run's first pages (or
+        // the row's routes) are asked for here, before the lengths are there
+        const int base = it.prefix ? 0 : a.n_prefix, slots = a.n_sink + a.n_recent + a.k;
+        const int32_t *pages = it.prefix ? a.prefix_pages : a.table + (int64_t)it.b * a.max_pages;
+        const int last_page = it.prefix ? a.pd.div(a.n_prefix - 1) : a.max_pages - 1;
+        int asked = -1;
+        if (a.route_units) {
+            const int64_t row = ((int64_t)it.b * a.items_per_seq + it.j) * a.k;
+            if (tid >= a.n_sink + a.n_recent && tid < slots) asked = a.routes[row + tid - a.n_sink - a.n_recent];
+        } else {
+            asked = pages[min(a.pd.div(base + min(u0 * kPagedUnit, a.capacity)) + tid, last_page)];
+        }
 
         // query operands; lim: the last token that a row sees (-1: none);
         // lo and hi: the least and the largest of them that is one
@@ -401,6 +440,8 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
             lo = min(lo, __shfl_xor(lo, o, 64));
             hi = max(hi, __shfl_xor(hi, o, 64));
         }
+        lo = uniform(lo);
+        hi = uniform(hi);
 
         float m_run[NR], l_run[NR];
         f32x4_t acc[NR][NV];
@@ -413,24 +454,20 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
         }
         const float c2 = a.scale * 1.4426950408889634f * (a.k_scale ? a.k_scale[g] : 1.f);
 
-        // Key positions: tokens from `base` on, or, along routes, the places
-        // of the listed pages one after the other.
-        const int base = it.prefix ? 0 : a.n_prefix;
         int n_pos;
         __syncthreads();  // (the last item's readers of LDS are done)
         if (a.route_units) {
             // the pages that the row sees, each once: a slot is dropped if an
             // earlier one names its page
-            const int64_t row = ((int64_t)it.b * a.items_per_seq + it.j) * a.k;
-            const int here = hi >= 0 ? a.pd.div(hi) : -1, slots = a.n_sink + a.n_recent + a.k;
-            static_assert(kMaxAttnSlots <= kT, "a slot per thread");
+            const int here = hi >= 0 ? a.pd.div(hi) : -1;
+            static_assert(kMaxAttnSlots <= T, "a slot per thread");
             int id = -1;
             if (tid < a.n_sink)
                 id = tid;
             else if (tid < a.n_sink + a.n_recent)
                 id = here - (tid - a.n_sink);
             else if (tid < slots)
-                id = a.routes[row + tid - a.n_sink - a.n_recent];
+                id = asked;
             bool ok = tid < slots && id >= 0 && id <= here;
             if (tid < kMaxAttnSlots) sh.phys[tid] = ok ? id : -1;
             __syncthreads();
@@ -440,7 +477,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
             if (lane == 0) sh.count[w] = __popcll(mk);
             __syncthreads();
             int before = __popcll(mk & ((1ull << lane) - 1ull)), all = 0;
-            for (int v = 0; v < kW; ++v) {
+            for (int v = 0; v < NW; ++v) {
                 before += v < w ? sh.count[v] : 0;
                 all += sh.count[v];
             }
@@ -448,7 +485,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                 sh.chunk[before] = id;
                 sh.phys[before] = pool_page(a.table[(int64_t)it.b * a.max_pages + id], a.n_pages);
             }
-            n_pos = all * a.pd.page;
+            n_pos = uniform(all) * a.pd.page;
         } else {
             n_pos = hi < base ? 0 : hi - base + 1;
         }
@@ -460,9 +497,9 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
             const int ch0 = a.route_units ? 0 : a.pd.div(base + pa);
             if (!a.route_units) {  // (routes: a list of at most 256 pages is there whole)
                 if (pa != p0) __syncthreads();
-                const int ch1 = a.pd.div(base + pb - 1);
-                const int32_t *src = it.prefix ? a.prefix_pages : a.table + (int64_t)it.b * a.max_pages;
-                for (int c = ch0 + tid; c <= ch1; c += kT) sh.phys[c - ch0] = pool_page(src[c], a.n_pages);
+                const int n = a.pd.div(base + pb - 1) - ch0 + 1;
+                for (int c = tid; c < n; c += T)
+                    sh.phys[c] = pool_page(pa == p0 && c < T ? asked : pages[ch0 + c], a.n_pages);
             }
             __syncthreads();
 
@@ -526,7 +563,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
 
             int p = pa + w * S::KT;
             if (p < pb) load(p);
-            for (; p < pb; p += kW * S::KT) {
+            for (; p < pb; p += NW * S::KT) {
                 // (wave-uniform) all_seen: every key of the tile is seen by
                 // every row; mixed: some key by some rows and not by others
                 bool all_seen = true, mixed = false;
@@ -632,7 +669,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) vf[c] = __builtin_bit_cast(f32x4_t, vr[0][c]);
                 }
-                if (p + kW * S::KT < pb) load(p + kW * S::KT);
+                if (p + NW * S::KT < pb) load(p + NW * S::KT);
 
                 // the running maximum moves only when a score exceeds it by
                 // more than kLazy (weights are then at most 2^kLazy), so that
@@ -705,16 +742,12 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                 } else {
                     bf16x8_t ph[NR], pl[NR];
 #pragma unroll
-                    for (int n = 0; n < NR; ++n)
+                    for (int n = 0; n < NR; ++n) {
+                        float x[8];
 #pragma unroll
-                        for (int r = 0; r < 2; ++r)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                __bf16 x, y;
-                                split_weight(s[n][r % S::KR][i], x, y);
-                                ph[n][4 * r + i] = x;
-                                pl[n][4 * r + i] = y;
-                            }
+                        for (int e = 0; e < 8; ++e) x[e] = s[n][(e >> 2) % S::KR][e & 3];
+                        split_weights(x, ph[n], pl[n]);
+                    }
                     auto values = [&](auto odd_tile) {
 #pragma unroll
                         for (int v = 0; v < NV; ++v) {
@@ -777,12 +810,12 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
             __syncthreads();
             // 16 threads a row, D / 16 features each in pieces of four
             const int q = tid >> 4, r = 16 * n + q;
-            if (r < rows.n) {
-                float m = -INFINITY, sum = 0.f, wt[kW];
+            if (q < 16 && r < rows.n) {
+                float m = -INFINITY, sum = 0.f, wt[NW];
 #pragma unroll
-                for (int v = 0; v < kW; ++v) m = fmaxf(m, sh.m[v][q]);
+                for (int v = 0; v < NW; ++v) m = fmaxf(m, sh.m[v][q]);
 #pragma unroll
-                for (int v = 0; v < kW; ++v) {
+                for (int v = 0; v < NW; ++v) {
                     wt[v] = sh.m[v][q] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sh.m[v][q] - m);
                     sum += wt[v] * sh.l[v][q];
                 }
@@ -790,13 +823,13 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                 rows.of(a, r, b, t, h);
                 const int64_t orow = ((int64_t)b * a.n_q + t) * a.n_heads + h;
                 const float inv = inverse_sum(sum, vs);
-                float *part = sink.part(a, D, r, orow);
+                float *part = sink.part(D, r, orow);
 #pragma unroll
                 for (int f0 = 0; f0 < D / 64; ++f0) {
                     const int f = 64 * f0 + 4 * (tid & 15);
                     f32x4_t x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int v = 0; v < kW; ++v) {
+                    for (int v = 0; v < NW; ++v) {
                         const f32x4_t y = *reinterpret_cast<const f32x4_t *>(reinterpret_cast<float *>(smem + v * S::WAVE) + q * S::ORS + f);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) x[i] = wt[v] != 0.f ? __builtin_fmaf(wt[v], y[i], x[i]) : x[i];
@@ -833,48 +866,86 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
 // --------------------------------------------------------------- wide body
 //
 // S^T = K Q^T on 32x32 MFMA tiles: a lane owns one query row and 16 keys of a
-// 32-key block, which is the order in which O^T = V^T P^T takes them.  Up to
-// four row blocks, one a wave; items of fewer rows give two waves to a row
-// block, each with every other key block.
+// 32-key block, which is the order in which O^T = V^T P^T takes them.  A row
+// block is one wave's; items of half as many rows as the waves could hold, or
+// less, give two waves to a row block, each with every other key block.
 
 template <int TY, int D>
 struct WideShape {
+    static constexpr int NW = 4;
+    static constexpr int T = 64 * NW;
+    static constexpr int ROWS = 32 * NW;           // rows of an item at most
     static constexpr int SIZE = TY == CACHE_BF16 ? 2 : 1;
     static constexpr int KB = D <= 128 ? 64 : 32;  // keys of a staged tile
     static constexpr int NB = KB / 32;
     static constexpr int KRS = 2 * D + 16;  // bytes of a row of the K tile (odd in units of 16: rows in distinct banks)
     static constexpr int VRS = 2 * D + 64;  // ... of the V tile (its transposed reads cover 4 rows x 32 bytes)
     static constexpr int BUF = KB * (KRS + VRS);
-    static constexpr int OBYTES = 2 * 64 * (D / 32) * 16 * 4;  // two waves' accumulators
-    static constexpr int LDS = 2 * BUF > OBYTES ? 2 * BUF : OBYTES;
-    static constexpr int PPR = D * SIZE / 16;    // 16-byte pieces of a row
-    static constexpr int PT = KB * PPR / kT;     // pieces of a thread
+    static constexpr int LDS = 2 * BUF;
+    static constexpr int PPR = D * SIZE / 16;          // 16-byte pieces of a row
+    static constexpr int PIECES = KB * PPR;            // ... of a tile
+    static constexpr int PT = PIECES / T;              // ... of a thread
+    static_assert(PIECES % T == 0, "");
+    static constexpr int KPW = 64 / PPR;               // keys that a wave's 64 pieces hold
+    // (half the waves' accumulators pass through the tiles' memory)
+    static_assert(NB == 1 || NW / 2 * 64 * (D / 32) * 16 * 4 <= LDS, "");
 };
 
 template <int TY, int D>
-__device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsigned char *smem, bool pre, bool own)
+__device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsigned char *smem, bool own)
 {
     using S = WideShape<TY, D>;
     constexpr int NMB = D / 32;
+    const int tid = threadIdx.x, w = uniform(tid >> 6), lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+    // The prefix's length is known to the host, which cuts it into splits: slot
+    // (key head, split, row tile), the tiles of a split next to each other and
+    // so on one XCD (workgroups are dealt to the eight round-robin), where
+    // they read the same keys at about the same time from its L2.
+    const int grid8 = a.grid >> 3;
+    int slot = (a.grid & 7) == 0 ? (blockIdx.x & 7) * grid8 + (blockIdx.x >> 3) : blockIdx.x;
     Run run;
-    if (!find_run(a, sh, pre, own, run)) return;
-    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
-    const int64_t run0 = run.at;
+    run.at = run.end = -1;
+    int run0 = 0;
 
     for (;;) {
-        const Item &it = run.it;
-        const int u0 = (int)(run.at - it.first), u1 = (int)min((int64_t)it.units, run.end - it.first);
-        const Rows rows = rows_of(a, it);
+        Rows rows;
+        int u0, u1;
+        Sink sink;
+        if (slot < a.prefix_slots) {
+            const int tile = slot % a.prefix_tiles, gs = slot / a.prefix_tiles, split = gs % a.prefix_splits;
+            rows.prefix = true;
+            rows.b = 0;
+            rows.g = gs / a.prefix_splits;
+            rows.row0 = tile * a.prefix_tile;
+            rows.n = min(a.prefix_tile, a.prefix_rows - rows.row0);
+            u0 = (int)((int64_t)split * a.prefix_units / a.prefix_splits);
+            u1 = (int)((int64_t)(split + 1) * a.prefix_units / a.prefix_splits);
+            sink = Sink{false, nullptr, a.prefix_parts + (int64_t)slot * a.prefix_tile * (D + 4)};
+            slot += a.grid;
+        } else {
+            if (run.at < 0) {
+                if (!own || !find_run<S::NW>(a, sh, false, true, run)) return;
+                run0 = run.at;
+            } else {
+                if (run.at >= run.end) return;
+                next_item(a, run.it);
+            }
+            u0 = run.at - run.it.first;
+            u1 = min(run.it.units, run.end - run.it.first);
+            rows = rows_of(a, run.it);
+            sink = sink_of(a, D, run, u0, u1, run.at == run0, true);
+            run.at = run.it.first + u1;
+        }
         const int g = rows.g;
-        // row blocks (1, 2 or 4), waves of a row block, this wave's of each
-        const int wr = rows.n <= 32 ? 1 : rows.n <= 64 ? 2 : 4, wk = min(S::NB, kW / wr);
+        // row blocks (a power of two), waves of a row block, this wave's of each
+        const int wr = rows.n <= 32 ? 1 : rows.n <= 64 ? 2 : rows.n <= 128 ? 4 : 8, wk = min(S::NB, S::NW / wr);
         const int rb = w & (wr - 1), kp = w / wr;
         const bool on = kp < wk && 32 * rb < rows.n;
 
         __syncthreads();  // (the last item's readers of LDS are done)
         {
             const int last = tid < rows.n ? rows.last(a, tid) : -1;
-            if (tid < 128) sh.lim[tid] = last;
+            if (tid < S::ROWS) sh.lim[tid] = last;
             int lo = last < 0 ? kNoToken : last, hi = last;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
@@ -893,8 +964,15 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             fq.load(static_cast<const bf16_t *>(a.Q) + (((int64_t)b * a.n_q + t) * a.n_heads + h) * D, hh);
         }
         __syncthreads();
-        const int lo = min(sh.lo[0], sh.lo[1]), hi = max(sh.hi[0], sh.hi[1]);  // (rows past 127 there are none)
-        const int lim = sh.lim[(32 * rb + l32) & 127], last = lim < 0 ? hi : lim;
+        int lo = sh.lo[0], hi = sh.hi[0];
+#pragma unroll
+        for (int v = 1; v < S::ROWS / 64; ++v) {
+            lo = min(lo, sh.lo[v]);
+            hi = max(hi, sh.hi[v]);
+        }
+        lo = uniform(lo);
+        hi = uniform(hi);
+        const int lim = sh.lim[32 * rb + l32], last = lim < 0 ? hi : lim;
 
         float m_run = -INFINITY, l_run = 0.f;
         f32x16_t acc[NMB];
@@ -902,7 +980,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
         for (int mb = 0; mb < NMB; ++mb) acc[mb] = f32x16_t{};
         const float c2 = a.scale * 1.4426950408889634f * (a.k_scale ? a.k_scale[g] : 1.f);
 
-        const int base = it.prefix ? 0 : a.n_prefix;
+        const int base = rows.prefix ? 0 : a.n_prefix;
         const int n_pos = hi < base ? 0 : hi - base + 1;
         const int p0 = (int)min((int64_t)u0 * kPagedUnit, (int64_t)n_pos);
         const int p1 = (int)min((int64_t)u1 * kPagedUnit, (int64_t)n_pos);
@@ -912,9 +990,9 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             const int ch0 = a.pd.div(base + pa), ch1 = a.pd.div(base + pb - 1);
             __syncthreads();
             {
-                const int32_t *src = it.prefix ? a.prefix_pages : a.table + (int64_t)it.b * a.max_pages;
+                const int32_t *src = rows.prefix ? a.prefix_pages : a.table + (int64_t)rows.b * a.max_pages;
                 bool bad = false;
-                for (int c = ch0 + tid; c <= ch1; c += kT) {
+                for (int c = ch0 + tid; c <= ch1; c += S::T) {
                     const int x = pool_page(src[c], a.n_pages);
                     sh.phys[c - ch0] = x;
                     bad = bad || x < 0;
@@ -923,33 +1001,55 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                 if (lane == 0) sh.bad[w] = any != 0ull;
             }
             __syncthreads();
-            const bool holes = (sh.bad[0] | sh.bad[1] | sh.bad[2] | sh.bad[3]) != 0;  // (uniform)
+            int bad = 0;
+#pragma unroll
+            for (int v = 0; v < S::NW; ++v) bad |= sh.bad[v];
+            const bool holes = uniform(bad) != 0;
             auto there = [&](int tok) { return sh.phys[a.pd.div(tok) - ch0] >= 0; };
 
             u32x4_t kr[S::PT], vr[S::PT];
-            bool keep[S::PT];
-            auto load = [&](int p) {
+            uint32_t keep = 0;  // bit q: some row sees this thread's piece q
+            // The keys of a wave's pieces (KPW of them at a time) lie in one
+            // page where pages and the first token are multiples of KPW: then
+            // a page is looked up once a wave, and a lane adds its own constant
+            const bool together = a.pd.page % S::KPW == 0 && base % S::KPW == 0;
+            const unsigned char *Kb = static_cast<const unsigned char *>(a.K), *Vb = static_cast<const unsigned char *>(a.V);
+            auto load = [&](int p) __attribute__((always_inline)) {
+                keep = 0;
+                if (together) {
 #pragma unroll
-                for (int q = 0; q < S::PT; ++q) {
-                    const int x = tid + q * kT, key = x / S::PPR, c = x % S::PPR;
-                    const int tok = base + min(p + key, pb - 1);
-                    const int ch = a.pd.div(tok);
-                    int phys = sh.phys[ch - ch0], place = tok - ch * a.pd.page;
-                    keep[q] = p + key < pb && phys >= 0;
-                    if (phys < 0) phys = place = 0;  // (row 0 of the pool is there)
-                    const int64_t off = pool_row(phys, a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE + 16 * c;
-                    kr[q] = *reinterpret_cast<const u32x4_t *>(static_cast<const unsigned char *>(a.K) + off);
-                    vr[q] = *reinterpret_cast<const u32x4_t *>(static_cast<const unsigned char *>(a.V) + off);
+                    for (int q = 0; q < S::PT; ++q) {
+                        const int key0 = (w * 64 + q * S::T) / S::PPR;  // (the wave's first)
+                        const int tok = base + min(p + key0, pb - 1), ch = a.pd.div(tok), phys = uniform(sh.phys[ch - ch0]);
+                        const int place = tok - ch * a.pd.page & ~(S::KPW - 1);
+                        keep |= (uint32_t)(p + key0 + lane / S::PPR < pb && phys >= 0) << q;
+                        const int64_t off = pool_row(max(phys, 0), a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE;
+                        kr[q] = *reinterpret_cast<const u32x4_t *>(Kb + off + 16 * lane);
+                        vr[q] = *reinterpret_cast<const u32x4_t *>(Vb + off + 16 * lane);
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < S::PT; ++q) {
+                        const int x = tid + q * S::T, key = x / S::PPR, c = x % S::PPR;
+                        const int tok = base + min(p + key, pb - 1);
+                        const int ch = a.pd.div(tok);
+                        int phys = sh.phys[ch - ch0], place = tok - ch * a.pd.page;
+                        keep |= (uint32_t)(p + key < pb && phys >= 0) << q;
+                        if (phys < 0) phys = place = 0;  // (row 0 of the pool is there)
+                        const int64_t off = pool_row(phys, a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE + 16 * c;
+                        kr[q] = *reinterpret_cast<const u32x4_t *>(Kb + off);
+                        vr[q] = *reinterpret_cast<const u32x4_t *>(Vb + off);
+                    }
                 }
             };
             auto store = [&](unsigned char *buf) {
 #pragma unroll
                 for (int q = 0; q < S::PT; ++q) {
-                    const int x = tid + q * kT, key = x / S::PPR, c = x % S::PPR;
+                    const int x = tid + q * S::T, key = x / S::PPR, c = x % S::PPR;
                     unsigned char *kd = buf + key * S::KRS, *vd = buf + S::KB * S::KRS + key * S::VRS;
                     // (a value that no row sees is 0: memory that was never written may hold NaN)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) vr[q][e] = keep[q] ? vr[q][e] : 0u;
+                    for (int e = 0; e < 4; ++e) vr[q][e] = (keep >> q) & 1u ? vr[q][e] : 0u;
                     if constexpr (TY == CACHE_BF16) {
                         *reinterpret_cast<u32x4_t *>(kd + 16 * c) = kr[q];
                         *reinterpret_cast<u32x4_t *>(vd + 16 * c) = vr[q];
@@ -961,101 +1061,122 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                     }
                 }
             };
+            // one 32-key block of a staged tile; MASKED: some row does not see
+            // some key of it
+            auto block = [&](auto masked, const unsigned char *kt, int p, int kb) __attribute__((always_inline)) {
+                constexpr bool MASKED = decltype(masked)::value;
+                const unsigned char *vt = kt + S::KB * S::KRS;
+                // (operands are read two products ahead, in this order: left alone
+                // the compiler reads each right before its product, which then
+                // waits the LDS latency every time)
+                const unsigned char *kp_ = kt + (32 * kb + l32) * S::KRS + hh * D;
+                f32x16_t s = {};
+                bf16x8_t kf[3];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) kf[q] = *reinterpret_cast<const bf16x8_t *>(kp_ + 16 * q);
+#pragma unroll
+                for (int q = 0; q < D / 16; ++q) {
+                    if (q + 2 < D / 16) kf[(q + 2) % 3] = *reinterpret_cast<const bf16x8_t *>(kp_ + 16 * (q + 2));
+                    __builtin_amdgcn_sched_barrier(0);
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[q % 3], fq.v[q], s, 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                // V^T operand i = 2 mb + s2 of the block: keys 16 s2 + 4 hh + 0..3
+                // and + 8..11, the order of the score accumulator
+                const int j = lane & 15;
+                const unsigned char *vp = vt + (32 * kb + 4 * hh + (j >> 2)) * S::VRS + 2 * (16 * (l32 >> 4) + 4 * (j & 3));
+                auto value = [&](int i) {
+                    const unsigned char *x = vp + 16 * (i & 1) * S::VRS + 64 * (i >> 1);
+                    return join8(lds_read_tr16(x), lds_read_tr16(x + 8 * S::VRS));
+                };
+                bf16x8_t vf[3];
+                vf[0] = value(0);
+                vf[1] = value(1);
+                __builtin_amdgcn_sched_barrier(0);
+                uint32_t seen = 0u;  // bit r: this lane's row sees key acc_row(r, hh)
+                if constexpr (MASKED) {
+#pragma unroll 1
+                    for (int r = 0; r < 16; ++r) {
+                        const int x = p + 32 * kb + acc_row(r, hh), tok = base + x;
+                        const bool is = x < pb && tok <= last && (!holes || there(tok));
+                        seen |= (uint32_t)is << r;
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = (seen >> r) & 1u ? s[r] : -INFINITY;
+                }
+                float mx = s[0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+                mx *= c2;
+                if (__ballot(mx > m_run + kLazy) != 0ull) {  // (the maximum moves rarely, as in the narrow body)
+                    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                    const float m_new = fmaxf(m_run, mx);
+                    const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+                    l_run *= alpha;
+#pragma unroll
+                    for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[mb][r] *= alpha;
+                    m_run = m_new;
+                }
+                const float m_use = MASKED && m_run == -INFINITY ? 0.f : m_run;
+                bf16x8_t ph[2], pl[2];
+                float l = 0.f;
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * q + e], c2, -m_use));
+                        l += x[e];
+                    }
+                    split_weights(x, ph[q], pl[q]);
+                }
+                l_run += l;
+#pragma unroll
+                for (int i = 0; i < 2 * NMB; ++i) {
+                    if (i + 2 < 2 * NMB) vf[(i + 2) % 3] = value(i + 2);
+                    __builtin_amdgcn_sched_barrier(0);
+                    bf16x8_t v = vf[i % 3], odd;
+                    if constexpr (MASKED) take_odd(v, odd);
+                    f32x16_t &o = acc[i >> 1];
+                    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, ph[i & 1], o, 0, 0, 0);
+                    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pl[i & 1], o, 0, 0, 0);
+                    if constexpr (MASKED) {
+                        bf16x8_t see;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) see[e] = (seen >> (8 * (i & 1) + e)) & 1u ? (__bf16)1.f : (__bf16)0.f;
+                        const f32x16_t z = {};
+                        const f32x16_t k = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd, see, z, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) o[r] = k[r] > 0.f ? NAN : o[r];
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            // tiles that every row sees whole, then the others
+            const int open = holes ? pa : max(pa, min(pb, lo - base + 1) - (min(pb, lo - base + 1) - pa) % S::KB);
             load(pa);
             store(smem);
             __syncthreads();
-            int cur = 0;
-            for (int p = pa; p < pb; p += S::KB, cur ^= 1) {
-                const bool more = p + S::KB < pb;
-                if (more) load(p + S::KB);
-                const unsigned char *kt = smem + cur * S::BUF, *vt = kt + S::KB * S::KRS;
-#pragma unroll 1
-                for (int kb = kp; kb < S::NB; kb += wk) {
-                    const int k0 = p + 32 * kb;
-                    if (!on || k0 >= pb) break;  // (wave-uniform)
-                    f32x16_t s = {};
-#pragma unroll
-                    for (int q = 0; q < D / 16; ++q) {
-                        const bf16x8_t kf = *reinterpret_cast<const bf16x8_t *>(kt + (32 * kb + l32) * S::KRS + hh * D + 16 * q);
-                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, fq.v[q], s, 0, 0, 0);
+            int cur = 0, p = pa;
+            auto tiles = [&](auto masked, int end) __attribute__((always_inline)) {
+                for (; p < end; p += S::KB, cur ^= 1) {
+                    const bool more = p + S::KB < pb;
+                    if (more) load(p + S::KB);
+                    if (on) {
+                        const unsigned char *kt = smem + cur * S::BUF;
+                        for (int kb = kp; kb < S::NB && p + 32 * kb < pb; kb += wk) block(masked, kt, p, kb);
                     }
-                    // (wave-uniform) every key of the block is seen by every row;
-                    // else bit r of `seen`: this lane's row sees key acc_row(r, hh)
-                    const bool open = k0 + 31 < pb && base + k0 + 31 <= lo && !holes;
-                    uint32_t seen = 0u;
-                    if (!open) {
-#pragma unroll 1
-                        for (int r = 0; r < 16; ++r) {
-                            const int x = k0 + acc_row(r, hh), tok = base + x;
-                            const bool is = x < pb && tok <= last && (!holes || there(tok));
-                            seen |= (uint32_t)is << r;
-                        }
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) s[r] = (seen >> r) & 1u ? s[r] : -INFINITY;
-                    }
-                    float mx = s[0];
-#pragma unroll
-                    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-                    mx *= c2;
-                    if (__ballot(mx > m_run + kLazy) != 0ull) {  // (the maximum moves rarely, as in the narrow body)
-                        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-                        const float m_new = fmaxf(m_run, mx);
-                        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-                        l_run *= alpha;
-#pragma unroll
-                        for (int mb = 0; mb < NMB; ++mb)
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) acc[mb][r] *= alpha;
-                        m_run = m_new;
-                    }
-                    const float m_use = m_run == -INFINITY ? 0.f : m_run;
-                    bf16x8_t ph[2], pl[2];
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, -m_use));
-                        l_run += x;
-                        __bf16 y, z;
-                        split_weight(x, y, z);
-                        ph[r >> 3][r & 7] = y;
-                        pl[r >> 3][r & 7] = z;
-                    }
-                    auto values = [&](auto odd_tile) {
-#pragma unroll
-                        for (int mb = 0; mb < NMB; ++mb) {
-#pragma unroll
-                            for (int s2 = 0; s2 < 2; ++s2) {
-                                // keys 16 s2 + 4 hh + 0..3 and + 8..11 of the block, the order of the accumulator
-                                const int j = lane & 15;
-                                const unsigned char *vp = vt + (32 * kb + 16 * s2 + 4 * hh + (j >> 2)) * S::VRS +
-                                                          2 * (32 * mb + 16 * (l32 >> 4) + 4 * (j & 3));
-                                bf16x8_t vf = join8(lds_read_tr16(vp), lds_read_tr16(vp + 8 * S::VRS)), odd;
-                                if constexpr (decltype(odd_tile)::value) take_odd(vf, odd);
-                                acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph[s2], acc[mb], 0, 0, 0);
-                                acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[s2], acc[mb], 0, 0, 0);
-                                if constexpr (decltype(odd_tile)::value) {
-                                    bf16x8_t see;
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e) see[e] = (seen >> (8 * s2 + e)) & 1u ? (__bf16)1.f : (__bf16)0.f;
-                                    const f32x16_t z = {};
-                                    const f32x16_t k = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd, see, z, 0, 0, 0);
-#pragma unroll
-                                    for (int r = 0; r < 16; ++r) acc[mb][r] = k[r] > 0.f ? NAN : acc[mb][r];
-                                }
-                            }
-                        }
-                    };
-                    if (!open && lo < hi && base + k0 + 31 > lo)
-                        values(std::true_type());
-                    else
-                        values(std::false_type());
+                    if (more) store(smem + (cur ^ 1) * S::BUF);
+                    __syncthreads();
                 }
-                if (more) store(smem + (cur ^ 1) * S::BUF);
-                __syncthreads();
-            }
+            };
+            tiles(std::false_type(), open);
+            tiles(std::true_type(), pb);
         }
 
         // ------------------------------------------------- the result written
-        const Sink sink = sink_of(a, D, run, u0, u1, run.at == run0, true);
         l_run += __shfl_xor(l_run, 32, 64);
         // (scores that are all NaN leave no maximum, but their sum counts)
         m_run = lim < 0 ? -INFINITY : l_run != l_run ? 0.f : m_run;
@@ -1100,7 +1221,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             rows.of(a, r, b, t, h);
             const int64_t orow = ((int64_t)b * a.n_q + t) * a.n_heads + h;
             const float inv = inverse_sum(l_run, a.v_scale ? a.v_scale[g] : 1.f);
-            float *part = sink.part(a, D, r, orow);
+            float *part = sink.part(D, r, orow);
 #pragma unroll
             for (int mb = 0; mb < NMB; ++mb) {
 #pragma unroll
@@ -1126,33 +1247,38 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                 }
             }
         }
-        run.at = it.first + u1;
-        if (run.at >= run.end) return;
-        next_item(a, run.it);
     }
 }
 
 // The bodies of a launch one after the other: WIDE for the items of many
 // rows, NR > 0 (16-row blocks) for the others.
 template <int TY, int D, bool WIDE, int NR>
-__global__ __launch_bounds__(kT, D <= 128 && NR <= 1 ? 2 : 1) void paged_kernel(PagedArgs a)
+struct Launch {
+    static constexpr int NW = WIDE ? WideShape<TY == CACHE_F32 ? CACHE_BF16 : TY, D>::NW : 4;
+    static constexpr int NARROW = NR > 0 ? NW * Shape<TY, D>::WAVE : 0;
+    static constexpr int WIDTH = WIDE ? WideShape<TY == CACHE_F32 ? CACHE_BF16 : TY, D>::LDS : 0;
+    static constexpr int LDS = NARROW > WIDTH ? NARROW : WIDTH;
+};
+
+template <int TY, int D, bool WIDE, int NR>
+__global__ __launch_bounds__((64 * Launch<TY, D, WIDE, NR>::NW), (D <= 128 && NR <= 1 ? 2 : 1)) void paged_kernel(PagedArgs a)
 {
+    constexpr int NW = Launch<TY, D, WIDE, NR>::NW;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ Common sh;
-    if constexpr (WIDE) wide_body<TY, D>(a, sh, smem, a.prefix_wide, a.own_wide);
-    if constexpr (NR > 0) narrow_body<TY, D, NR>(a, sh, smem, !a.prefix_wide && a.prefix_items > 0, !a.own_wide);
+    if constexpr (WIDE) wide_body<TY, D>(a, sh, smem, a.own_wide);
+    if constexpr (NR > 0) narrow_body<TY, D, NR, NW>(a, sh, smem, !a.prefix_wide && a.prefix_items > 0, !a.own_wide);
 }
 
 template <int TY, int D, bool WIDE, int NR>
 hipError_t launch_one(const PagedArgs &a, hipStream_t stream)
 {
-    constexpr int narrow = NR > 0 ? Shape<TY, D>::LDS : 0;
-    constexpr int lds = WIDE && WideShape<TY, D>::LDS > narrow ? WideShape<TY, D>::LDS : narrow;
+    using L = Launch<TY, D, WIDE, NR>;
     static LdsLimit seen;
     const void *fn = reinterpret_cast<const void *>(&paged_kernel<TY, D, WIDE, NR>);
-    hipError_t e = raise_lds_limit(fn, lds + sizeof(Common), seen);
+    hipError_t e = raise_lds_limit(fn, L::LDS + sizeof(Common), seen);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((paged_kernel<TY, D, WIDE, NR>), dim3((unsigned)a.grid), dim3(kT), lds, stream, a);
+    hipLaunchKernelGGL((paged_kernel<TY, D, WIDE, NR>), dim3((unsigned)a.grid), dim3(64 * L::NW), L::LDS, stream, a);
     return hipGetLastError();
 }
 

@@ -405,83 +405,84 @@ def sparse_attention(Q, K, V, routes, chunk: int, causal: bool, scale: float = 0
 # -------------------------------------------------------- the paged cache
 
 _E4M3 = torch.float8_e4m3fn
+# (the address alone: a torch.cuda.Stream object costs as much as a launch's checks)
+_current_stream = torch._C._cuda_getCurrentRawStream
 _DTYPES = {torch.float32: RR_F32, torch.bfloat16: RR_BF16, _E4M3: RR_E4M3}
 
 
-def _device_of(first, *others):
-    """The device of the tensors of a call; they have to share one."""
-    dev = first.device
-    for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device}: a call takes one device's")
+def _device_of(tensors):
+    """The device index of the tensors of a call (None among them: not given);
+    they have to share one."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors on {tensors[0].device} and {t.device}: a call takes one device's")
+    if dev < 0:
+        raise ValueError("tensor must be on the GPU")
     return dev
 
 
-class _On:
-    """The device of a call made current for it, and the stream it goes to: the
-    given one, or the device's current one."""
-
-    def __init__(self, dev, stream):
-        if dev.type != "cuda":
-            raise ValueError("tensor must be on the GPU")
-        self.guard = torch.cuda.device(dev)
-        self.dev, self.stream = dev, stream
-
-    def __enter__(self):
-        self.guard.__enter__()
-        if self.stream is None:
-            self.stream = torch.cuda.current_stream(self.dev)
-        elif self.stream.device != self.dev:
-            self.guard.__exit__(None, None, None)
-            raise ValueError(f"the stream is of {self.stream.device}, the tensors are on {self.dev}")
-        return self.stream
-
-    def __exit__(self, *exc):
-        return self.guard.__exit__(*exc)
+def _launch(dev, stream, call, *args):
+    """call(*args, stream) with device `dev` current, on the given stream or the
+    device's current one."""
+    if stream is None:
+        s = _current_stream(dev)
+    elif stream.device_index != dev:
+        raise ValueError(f"the stream is of {stream.device}, the tensors are on cuda:{dev}")
+    else:
+        s = stream.cuda_stream
+    if torch.cuda.current_device() == dev:
+        _check(call(*args, s))
+    else:
+        with torch.cuda.device(dev):
+            _check(call(*args, s))
 
 
-def _empty(shape, dtype, dev, stream):
+def _empty(shape, dtype, like, stream):
     """Memory for a call on the given stream (None: the current one), of that
     stream's own: freed, only what the stream does later can take it."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return torch.empty(shape, dtype=dtype, device=like.device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return torch.empty(shape, dtype=dtype, device=like.device)
 
 
 def _of(name, t, shape, dtype):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} of shape {list(shape)}")
-    return _ptr(t)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 def _cache_of(K_cache, V_cache, dtype, k_scale, v_scale):
-    """The pools' sizes (n_pages, n_kv_heads, page, d), their type and the scales."""
-    if K_cache.dim() != 4 or K_cache.dtype not in _DTYPES or V_cache.dtype != K_cache.dtype:
+    """The pools' shape, their type and the scales' addresses."""
+    kind, shape = K_cache.dtype, K_cache.shape
+    if len(shape) != 4 or kind not in _DTYPES or V_cache.dtype != kind:
         raise TypeError("K_cache and V_cache must be [n_pages, H_kv, page, d] tensors of one type of "
                         "float32, bfloat16 and float8_e4m3fn")
-    if V_cache.shape != K_cache.shape:
+    if V_cache.shape != shape:
         raise ValueError("K_cache and V_cache must have one shape")
-    if K_cache.dtype != dtype and not (dtype == torch.bfloat16 and K_cache.dtype == _E4M3):
+    if kind != dtype and not (dtype == torch.bfloat16 and kind == _E4M3):
         raise TypeError("the cache must have the queries' type, or float8_e4m3fn with bfloat16")
-    scales = []
-    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-        if (t is not None) != (K_cache.dtype == _E4M3):
-            raise ValueError("k_scale and v_scale are given for float8_e4m3fn caches, and for them only")
-        scales.append(None if t is None else _of(name, t, (K_cache.shape[1],), torch.float32))
-    return tuple(K_cache.shape), _DTYPES[K_cache.dtype], scales
+    if (k_scale is not None) != (kind == _E4M3) or (v_scale is not None) != (kind == _E4M3):
+        raise ValueError("k_scale and v_scale are given for float8_e4m3fn caches, and for them only")
+    if k_scale is None:
+        return shape, _DTYPES[kind], None, None
+    heads = (shape[1],)
+    return shape, RR_E4M3, _of("k_scale", k_scale, heads, torch.float32), _of("v_scale", v_scale, heads, torch.float32)
 
 
-def _rows_of(name, t, n, heads, d, dtype):
+def _rows_of(name, t, shape, dtype):
     """Elements between one token's rows and the next one's: the rows of a token
     lie together, tokens may lie apart (views of a fused projection)."""
-    if t.dim() != 3 or tuple(t.shape) != (n, heads, d) or t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype} of shape {[n, heads, d]}")
-    if not t.is_cuda:
-        raise ValueError("tensor must be on the GPU")
-    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} of shape {list(shape)}")
+    n, heads, d = shape
+    token, head, one = t.stride()
+    if (d > 1 and one != 1) or (heads > 1 and head != d):
         raise ValueError(f"{name}: the rows of a token must be contiguous")
-    return t.stride(0) if n > 1 else heads * d
+    return token if n > 1 else heads * d
 
 
 def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, freqs=None, interleaved=False, Q=None,
@@ -493,45 +494,47 @@ def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, fr
     float64 the first rot features of keys are rotated by position, and of
     queries Q [n_tokens, H, d] (returned, in Q_out if given).  K, V and Q may
     be views whose tokens lie apart."""
-    if K.dim() != 3 or K.dtype not in (torch.float32, torch.bfloat16):
+    kind, shape = K.dtype, K.shape
+    if len(shape) != 3 or kind not in (torch.float32, torch.bfloat16):
         raise TypeError("K must be a [n_tokens, H_kv, d] float32 or bfloat16 tensor")
-    dev = _device_of(K, V, K_cache, V_cache, page_table, lengths, seq_start, freqs, Q, Q_out, k_scale, v_scale)
-    (n_pages, Hkv, page, d), cache, (ks, vs) = _cache_of(K_cache, V_cache, K.dtype, k_scale, v_scale)
-    n = K.shape[0]
-    ldk, ldv = (_rows_of(name, t, n, Hkv, d, K.dtype) for name, t in (("K", K), ("V", V)))
-    if page_table.dim() != 2 or lengths.dim() != 1:
-        raise ValueError("page_table must be [B, max_pages] and lengths [B]")
+    (n_pages, Hkv, page, d), cache, ks, vs = _cache_of(K_cache, V_cache, kind, k_scale, v_scale)
+    dev = _device_of((K, V, K_cache, V_cache, page_table, lengths, seq_start, freqs, Q, Q_out, k_scale, v_scale))
+    n = shape[0]
+    rows = (n, Hkv, d)
+    ldk, ldv = _rows_of("K", K, rows, kind), _rows_of("V", V, rows, kind)
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [B, max_pages]")
     B, most = page_table.shape
-    H, ldq, rot = 0, 0, 0
+    H = ldq = rot = 0
+    f = q = out = start = None
     if freqs is not None:
-        if freqs.dim() != 1 or freqs.dtype != torch.float64:
-            raise TypeError("freqs must be a [rot / 2] float64 tensor")
-        rot = 2 * freqs.shape[0]
+        rot = 2 * freqs.numel()
+        f = _of("freqs", freqs, (rot // 2,), torch.float64)
+    if seq_start is not None:
+        start = _of("seq_start", seq_start, (B + 1,), torch.int32)
     if Q is not None:
         if Q.dim() != 3:
             raise TypeError("Q must be a [n_tokens, H, d] tensor")
         H = Q.shape[1]
-        ldq = _rows_of("Q", Q, n, H, d, K.dtype)
+        rows = (n, H, d)
+        ldq = _rows_of("Q", Q, rows, kind)
+        if Q_out is None:
+            Q_out = _empty(rows, kind, Q, stream)
+        q, out = Q.data_ptr(), _of("Q_out", Q_out, rows, kind)
     elif Q_out is not None:
         raise ValueError("Q_out without Q")
-    with _On(dev, stream) as s:
-        if Q is not None and Q_out is None:
-            Q_out = _empty((n, H, d), Q.dtype, dev, stream)
-        cfg = _AppendConfig(H, Hkv, d, page, n_pages, most, B, n, rot, int(interleaved), _DTYPES[K.dtype], cache, ldq,
-                            ldk, ldv, ks, vs)
-        _check(lib.rr_cache_append(
-            ctypes.byref(cfg), K.data_ptr(), V.data_ptr(), None if Q is None else Q.data_ptr(),
-            None if seq_start is None else _of("seq_start", seq_start, (B + 1,), torch.int32),
-            _of("lengths", lengths, (B,), torch.int32), _of("page_table", page_table, (B, most), torch.int32),
-            _ptr(freqs) if rot else None, _ptr(K_cache), _ptr(V_cache),
-            None if Q is None else _of("Q_out", Q_out, (n, H, d), K.dtype), s.cuda_stream))
+    cfg = _AppendConfig(H, Hkv, d, page, n_pages, most, B, n, rot, 1 if interleaved else 0, _DTYPES[kind], cache, ldq, ldk,
+                        ldv, ks, vs)
+    _launch(dev, stream, lib.rr_cache_append, ctypes.byref(cfg), K.data_ptr(), V.data_ptr(), q, start,
+            _of("lengths", lengths, (B,), torch.int32), _of("page_table", page_table, (B, most), torch.int32), f if rot else None,
+            _of("K_cache", K_cache, K_cache.shape, K_cache.dtype), _of("V_cache", V_cache, K_cache.shape, K_cache.dtype), out)
     return Q_out
 
 
 def _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, n_prefix, scale, k_scale, v_scale):
     if Q.dim() != 4 or Q.dtype not in (torch.float32, torch.bfloat16):
         raise TypeError("Q must be a [B, n_q, H, d] float32 or bfloat16 tensor")
-    (n_pages, Hkv, page, d), cache, (ks, vs) = _cache_of(K_cache, V_cache, Q.dtype, k_scale, v_scale)
+    (n_pages, Hkv, page, d), cache, ks, vs = _cache_of(K_cache, V_cache, Q.dtype, k_scale, v_scale)
     B, nq, H, dq = Q.shape
     if dq != d:
         raise ValueError(f"Q has rows of {dq} features, the cache of {d}")
@@ -543,7 +546,14 @@ def _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, n_p
             raise ValueError("routes must be [B * H * n_q, k]")
         k = routes.shape[1]
     return _PagedConfig(H, Hkv, d, page, n_pages, page_table.shape[1], B, nq, k, n_sink, n_recent, n_prefix,
-                        _DTYPES[Q.dtype], cache, float(scale), 0, ks, vs)
+                        _DTYPES[Q.dtype], cache, scale, 0, ks, vs)
+
+
+def _workspace_bytes(cfg):
+    n = lib.rr_paged_workspace_bytes(ctypes.byref(cfg))
+    if n == 0:
+        raise RRError(RR_ERR_INVALID, lib.rr_last_error().decode())
+    return n
 
 
 def paged_workspace(Q, K_cache, page_table, routes=None, n_sink=0, n_recent=0, n_prefix=0):
@@ -551,29 +561,26 @@ def paged_workspace(Q, K_cache, page_table, routes=None, n_sink=0, n_recent=0, n
     prefix_attention calls of these shapes.  Calls that may run at the same
     time, captured graphs that are replayed side by side among them, need one
     each."""
-    one = torch.empty(K_cache.shape[1] if K_cache.dim() == 4 else 0, dtype=torch.float32, device=K_cache.device)
-    scale = one if K_cache.dtype == _E4M3 else None
+    scale = None
+    if K_cache.dtype == _E4M3 and K_cache.dim() == 4:  # (the scales' values play no part)
+        scale = torch.empty(K_cache.shape[1], dtype=torch.float32, device=K_cache.device)
     cfg = _paged_config(Q, K_cache, K_cache, page_table, routes, n_sink, n_recent, n_prefix, 0.0, scale, scale)
-    n = lib.rr_paged_workspace_bytes(ctypes.byref(cfg))
-    if n == 0:
-        raise RRError(RR_ERR_INVALID, lib.rr_last_error().decode())
-    return torch.empty(n, dtype=torch.uint8, device=Q.device)
+    return torch.empty(_workspace_bytes(cfg), dtype=torch.uint8, device=Q.device)
 
 
-def _paged_call(call, cfg, Q, K_cache, V_cache, page_table, lengths, pages, pages_shape, out, lse, workspace, stream, dev):
+def _paged_call(call, cfg, dev, Q, K_cache, V_cache, page_table, lengths, third, out, lse, workspace, stream):
     B, nq, H, d = Q.shape
-    with _On(dev, stream) as s:
-        if out is None:
-            out = _empty((B, nq, H, d), Q.dtype, dev, stream)
-        if workspace is None:
-            n = lib.rr_paged_workspace_bytes(ctypes.byref(cfg))
-            workspace = _empty((n,), torch.uint8, dev, stream)
-        elif workspace.dtype != torch.uint8 or workspace.dim() != 1:
-            raise ValueError("workspace must be a one-dimensional uint8 tensor")
-        _check(call(ctypes.byref(cfg), _ptr(Q), _ptr(K_cache), _ptr(V_cache),
-                    _of("page_table", page_table, page_table.shape, torch.int32), _of("lengths", lengths, (B,), torch.int32),
-                    None if pages is None else _of(*pages, pages_shape, torch.int32), _out(out, (B, nq, H, d), Q.dtype),
-                    _out(lse, (B, nq, H), torch.float32), _ptr(workspace), workspace.numel(), s.cuda_stream))
+    if out is None:
+        out = _empty(Q.shape, Q.dtype, Q, stream)
+    if workspace is None:
+        workspace = _empty((_workspace_bytes(cfg),), torch.uint8, Q, stream)
+    elif workspace.dtype != torch.uint8 or workspace.dim() != 1:
+        raise ValueError("workspace must be a one-dimensional uint8 tensor")
+    _launch(dev, stream, call, ctypes.byref(cfg), _of("Q", Q, Q.shape, Q.dtype), _of("K_cache", K_cache, K_cache.shape, K_cache.dtype),
+            _of("V_cache", V_cache, K_cache.shape, K_cache.dtype), _of("page_table", page_table, page_table.shape, torch.int32),
+            _of("lengths", lengths, (B,), torch.int32), third, _of("out", out, Q.shape, Q.dtype),
+            None if lse is None else _of("lse", lse, (B, nq, H), torch.float32),
+            _of("workspace", workspace, workspace.shape, torch.uint8), workspace.numel())
     return out
 
 
@@ -584,13 +591,11 @@ def paged_attention(Q, K_cache, V_cache, page_table, lengths, routes=None, n_sin
     [B * H * n_q, k] int32 page indices: each query over those pages, its first
     n_sink and its last n_recent ones.  lse: optional float32 output [B, n_q,
     H].  workspace: paged_workspace(...), or None for one of this call's own."""
-    dev = _device_of(Q, K_cache, V_cache, page_table, lengths, routes, k_scale, v_scale, out, lse, workspace)
     cfg = _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, 0, scale, k_scale, v_scale)
-    if cfg.k == 0:
-        routes = None
-    return _paged_call(lib.rr_paged_attention, cfg, Q, K_cache, V_cache, page_table, lengths,
-                       None if routes is None else ("routes", routes), None if routes is None else routes.shape, out, lse,
-                       workspace, stream, dev)
+    dev = _device_of((Q, K_cache, V_cache, page_table, lengths, routes, k_scale, v_scale, out, lse, workspace))
+    third = _of("routes", routes, routes.shape, torch.int32) if cfg.k else None
+    return _paged_call(lib.rr_paged_attention, cfg, dev, Q, K_cache, V_cache, page_table, lengths, third, out, lse, workspace,
+                       stream)
 
 
 def prefix_attention(Q, K_cache, V_cache, page_table, lengths, prefix_pages, n_prefix, scale=0.0, k_scale=None,
@@ -598,7 +603,8 @@ def prefix_attention(Q, K_cache, V_cache, page_table, lengths, prefix_pages, n_p
     """rr_prefix_attention: paged_attention (without routes) for sequences that
     begin with the same n_prefix tokens, which are read once for the batch from
     prefix_pages [ceil(n_prefix / page)] int32."""
-    dev = _device_of(Q, K_cache, V_cache, page_table, lengths, prefix_pages, k_scale, v_scale, out, lse, workspace)
     cfg = _paged_config(Q, K_cache, V_cache, page_table, None, 0, 0, n_prefix, scale, k_scale, v_scale)
-    return _paged_call(lib.rr_prefix_attention, cfg, Q, K_cache, V_cache, page_table, lengths,
-                       ("prefix_pages", prefix_pages), (n_chunks(n_prefix, cfg.page),), out, lse, workspace, stream, dev)
+    dev = _device_of((Q, K_cache, V_cache, page_table, lengths, prefix_pages, k_scale, v_scale, out, lse, workspace))
+    third = _of("prefix_pages", prefix_pages, (n_chunks(n_prefix, K_cache.shape[2]),), torch.int32)
+    return _paged_call(lib.rr_prefix_attention, cfg, dev, Q, K_cache, V_cache, page_table, lengths, third, out, lse, workspace,
+                       stream)
