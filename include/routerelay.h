@@ -254,7 +254,7 @@ typedef enum {
     RR_KERNEL_ATTENTION = 7, /* sparse attention over routed chunks */
     RR_KERNEL_APPEND = 8,   /* new tokens into the paged cache */
     RR_KERNEL_PAGED = 9,    /* attention over the paged cache */
-    RR_KERNEL_JOIN = 10,    /* its parts joined */
+    RR_KERNEL_JOIN = 10,    /* with a shared prefix: its parts joined */
     RR_KERNEL_KINDS = 11
 } rr_kernel_kind;
 
@@ -425,8 +425,10 @@ typedef struct {
 } rr_paged_config;
 
 /* Bytes of workspace that rr_paged_attention and rr_prefix_attention need for
- * a config (0: the config is not valid, see rr_last_error).  A workspace needs
- * no initial contents; calls that may run at the same time need one each. */
+ * a config (0: the config is not valid, see rr_last_error).  A workspace is
+ * filled with zeros before its first use; calls leave the part of it that has
+ * to be zero (the first 2048 bytes) at zero, so it serves any calls that follow
+ * one another.  Calls that may run at the same time need one each. */
 size_t rr_paged_workspace_bytes(const rr_paged_config *cfg);
 
 /* Attention of the newest n_q tokens of every sequence over its cache (Sec.
@@ -444,8 +446,11 @@ size_t rr_paged_workspace_bytes(const rr_paged_config *cfg);
  *   O       [n_seqs, n_q, n_heads, d] of dtype.
  *   lse     optional [n_seqs, n_q, n_heads] binary32: the logarithm of the sum
  *           of exp(scaled score), -INFINITY where no token is seen.
- * Scores, softmax and sums in binary32; with bf16 queries the softmax weights
- * enter the value product as the sum of two bf16 numbers.  Tokens that a
+ * Scores, softmax and sums in binary32.  With bf16 queries the softmax weights
+ * enter the value product as the sum of two bf16 numbers (2^-16 off) where at
+ * most 16 query rows are multiplied with a key head's tokens together (n_q *
+ * n_heads / n_kv_heads of a sequence, n_seqs times that of a shared prefix),
+ * rounded to bf16 (2^-8 off) where more are.  Tokens that a
  * query does not see have no part in its output, whatever their rows hold.
  * Returns RR_ERR_INVALID for bad sizes, NULL or unaligned pointers or a
  * workspace too small, RR_ERR_UNSUPPORTED for other types or d. */

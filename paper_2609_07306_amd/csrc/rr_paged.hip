@@ -5,6 +5,7 @@
 namespace rr {
 namespace {
 
+using paged::add_part;
 using paged::f32x4_t;
 using paged::inverse_sum;
 using paged::log_sum;
@@ -13,8 +14,9 @@ constexpr int kT = 256;  // threads of a joining workgroup
 
 // -------------------------------------------------------------------- join
 //
-// One workgroup per query row.  The row's parts -- of its own item, and of
-// the prefix item that holds it -- are added with weights 2^(m_i - m).
+// With a prefix: one workgroup per query row.  The row's parts -- of its own
+// item, and of the prefix item that holds it -- are added with weights
+// 2^(m_i - m).
 
 template <int D, bool F32>
 __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
@@ -30,33 +32,20 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
     const int t = (int)(bt % a.n_q), b = (int)(bt / a.n_q);
     const int g = h / a.group, j = h - g * a.group;
 
-    int own_row, item;  // row within its item's tile, item within the sequence
-    if (a.route_units) {
-        own_row = 0;
-        item = h * a.n_q + t;
-    } else {
-        const int r = t * a.group + j;
-        item = g * a.row_tiles + r / a.own_tile;
-        own_row = r % a.own_tile;
-    }
-    const int4 own = a.heads[a.prefix_items + (int64_t)b * a.items_per_seq + item];
-    int n_own = own.z, n_pre = 0, pre_row = 0;
+    const int r = t * a.group + j, own_row = r % a.own_tile;  // row within its item's tile
+    const int4 own = a.heads[a.prefix_items + (int64_t)b * a.items_per_seq + g * a.row_tiles + r / a.own_tile];
+    const int parts_tile = a.own_wide ? a.own_tile : a.narrow_tile;
     int4 pre = {0, 0, 0, 0};
     const float *pre_part = nullptr;  // of a wide prefix: its splits lie a.prefix_tiles slots apart
-    if (a.prefix_items) {
-        const int r = b * a.rows + t * a.group + j, x = r / a.prefix_tile;
-        pre_row = r - x * a.prefix_tile;
-        if (a.prefix_wide) {
-            n_pre = a.prefix_splits;
-            const int slot = g * a.prefix_splits * a.prefix_tiles + x;
-            pre_part = a.prefix_parts + ((int64_t)slot * a.prefix_tile + pre_row) * (D + 4);
-        } else {
-            pre = a.heads[g * a.prefix_tiles + x];
-            n_pre = pre.z;
-        }
-    } else if (n_own == 1) {
-        return;  // (uniform) its workgroup wrote the result
+    const int q = b * a.rows + t * a.group + j, x_tile = q / a.prefix_tile, pre_row = q - x_tile * a.prefix_tile;
+    if (a.prefix_wide) {
+        pre.z = a.prefix_splits;
+        const int slot = g * a.prefix_splits * a.prefix_tiles + x_tile;
+        pre_part = a.prefix_parts + ((int64_t)slot * a.prefix_tile + pre_row) * (D + 4);
+    } else {
+        pre = a.heads[g * a.prefix_tiles + x_tile];
     }
+    const int n_own = own.z, n = n_own + pre.z;
     const int64_t n_rows = (int64_t)a.n_seqs * a.n_q * a.n_heads;
     auto part_of = [&](int i) -> const float * {
         const bool p = i >= n_own;
@@ -65,10 +54,8 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
         if (p && pre_part) return pre_part + (int64_t)i * a.prefix_tiles * a.prefix_tile * (D + 4);
         if (hd.z == 1) return a.whole + ((p ? 0 : n_rows) + orow) * (D + 4);
         const int64_t slot = i == 0 ? hd.x : 2 * (int64_t)(hd.y + i);
-        return (hd.w ? a.wide_parts : a.parts) + (slot * (hd.w ? a.own_tile : a.narrow_tile) + (p ? pre_row : own_row)) * (D + 4);
+        return a.parts + (slot * parts_tile + (p ? pre_row : own_row)) * (D + 4);
     };
-    const int n = n_own + n_pre;
-
     // PL lanes a part, NP parts at once, kept with a running maximum like the
     // attention's own: sums and statistics are asked for together
     const int pl = tid % PL, pg = tid / PL;
@@ -77,18 +64,7 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
 #pragma unroll 4
     for (int i = pg; i < n; i += NP) {
         const float *p = part_of(i);
-        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(p + 4 * pl);
-        const float mi = p[D], li = p[D + 1];
-        const float m_new = fmaxf(m, mi);
-        const float w0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
-        const float w1 = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - m_new);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float z = w0 != 0.f ? w0 * x[e] : 0.f;
-            x[e] = w1 != 0.f ? __builtin_fmaf(w1, y[e], z) : z;
-        }
-        l = w0 * l + w1 * li;
-        m = m_new;
+        add_part(*reinterpret_cast<const f32x4_t *>(p + 4 * pl), p[D], p[D + 1], x, m, l);
     }
     *reinterpret_cast<f32x4_t *>(&s_acc[pg][4 * pl]) = x;
     if (pl == 0) {
@@ -155,7 +131,6 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     a.narrow_tile = !a.own_wide ? a.own_tile : !a.prefix_wide && a.n_prefix ? a.prefix_tile : 0;
     const int64_t keys = (int64_t)(paged::kStagedPages - 1) * a.pd.page / kPagedUnit * kPagedUnit;
     a.batch_keys = (int32_t)(keys < (1 << 30) ? keys : (1 << 30));
-    a.min_units = 1;
     // units of the longest sequences that the page table can hold
     const double most_own = (double)(routed ? a.route_units : (a.capacity + kPagedUnit - 1) / kPagedUnit) * a.items_per_seq * a.n_seqs;
     const double most = most_own + (double)a.prefix_items * a.prefix_units;
@@ -182,7 +157,10 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
 
 static int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
 
-static int64_t parts_bytes(const PagedArgs &a, int d, int tile) { return align256((int64_t)2 * a.grid * tile * (d + 4) * 4); }
+static int64_t parts_bytes(const PagedArgs &a, int d)
+{
+    return align256((int64_t)2 * a.grid * (a.own_wide ? a.own_tile : a.narrow_tile) * (d + 4) * 4);
+}
 
 static int64_t prefix_bytes(const PagedArgs &a, int d) { return align256((int64_t)a.prefix_slots * a.prefix_tile * (d + 4) * 4); }
 
@@ -191,19 +169,28 @@ static int64_t whole_bytes(const PagedArgs &a, int d)
     return a.n_prefix ? align256((int64_t)2 * a.n_seqs * a.n_q * a.n_heads * (d + 4) * 4) : 0;
 }
 
+// The counters come first, at the same place for calls of every shape, which
+// may follow each other in one workspace; heads and whole parts serve calls
+// with a prefix.
+constexpr int64_t kCounterBytes = (int64_t)kPagedGrid * sizeof(uint32_t);
+
+static int64_t heads_bytes(const PagedArgs &a)
+{
+    return a.n_prefix ? align256((a.prefix_items + (int64_t)a.n_seqs * a.items_per_seq) * (int64_t)sizeof(int4)) : 0;
+}
+
 size_t paged_workspace_bytes(const PagedArgs &a, int d)
 {
-    const int64_t items = a.prefix_items + (int64_t)a.n_seqs * a.items_per_seq;
-    return (size_t)(parts_bytes(a, d, a.narrow_tile) + parts_bytes(a, d, a.own_wide ? a.own_tile : 0) + prefix_bytes(a, d) + whole_bytes(a, d) + align256(items * 16));
+    return (size_t)(kCounterBytes + parts_bytes(a, d) + prefix_bytes(a, d) + whole_bytes(a, d) + heads_bytes(a));
 }
 
 void paged_layout(PagedArgs &a, int d, void *workspace)
 {
     unsigned char *p = static_cast<unsigned char *>(workspace);
+    a.counters = reinterpret_cast<uint32_t *>(p);
+    p += kCounterBytes;
     a.parts = reinterpret_cast<float *>(p);
-    p += parts_bytes(a, d, a.narrow_tile);
-    a.wide_parts = reinterpret_cast<float *>(p);
-    p += parts_bytes(a, d, a.own_wide ? a.own_tile : 0);
+    p += parts_bytes(a, d);
     a.prefix_parts = reinterpret_cast<float *>(p);
     p += prefix_bytes(a, d);
     a.whole = reinterpret_cast<float *>(p);

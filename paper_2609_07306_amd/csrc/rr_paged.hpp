@@ -108,12 +108,13 @@ struct PagedArgs {
     bool own_wide, prefix_wide;        // which body takes them
     int32_t prefix_splits, prefix_slots;  // of the wide body: key splits, (key head, split, row tile) slots
     int32_t narrow_tile;               // rows of a narrow item at most
-    int32_t grid, min_units, batch_keys;
+    int32_t grid, batch_keys;
     // workspace
-    float *parts, *wide_parts;  // [2 * grid] parts of each body's items that several workgroups share
-    float *prefix_parts;        // [prefix_slots] parts
-    float *whole;    // with a prefix: [2][rows of the call] parts of items that one workgroup held
-    int4 *heads;     // per item: its first part, its first workgroup, its parts, its body
+    uint32_t *counters;  // [kPagedGrid] finished parts of the item that begins in a workgroup, 0 between calls
+    float *parts;        // [2 * grid] parts of items that several workgroups share
+    float *prefix_parts; // [prefix_slots] parts
+    float *whole;        // with a prefix: [2][rows of the call] parts of items that one workgroup held
+    int4 *heads;         // with a prefix: per item its first part, its first workgroup, its parts
 };
 
 size_t paged_workspace_bytes(const PagedArgs &a, int d);

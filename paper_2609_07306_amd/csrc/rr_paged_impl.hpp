@@ -13,8 +13,9 @@
 // workgroup: lengths that differ a hundredfold leave no compute unit idle, and
 // one long sequence is spread over the card.  Lengths live on the device, so
 // every workgroup sums them to find its run.  An item that lies in several
-// runs leaves a part (m, l, sum) per run in the workspace; a second launch
-// joins them.
+// runs leaves a part (m, l, sum) per run in the workspace, and the workgroup
+// that finishes the last of them joins them (with a prefix, whose items share
+// rows with the sequences', a second launch does).
 //
 // Two bodies share this.  The narrow one is for items of up to 16 rows (32),
 // where memory is the bound: each of four waves takes its own 32-key tiles of
@@ -36,6 +37,7 @@
 namespace rr {
 namespace paged {
 
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef short short8_t __attribute__((ext_vector_type(8)));
@@ -43,6 +45,7 @@ typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kMostWaves = 4;       // waves of a workgroup at most
 constexpr int kStagedPages = 512;   // page numbers held in LDS at a time
+constexpr int kJoin = 8;            // parts in flight of a thread that joins them
 constexpr float kLazy = 8.f;        // log2 headroom of the running softmax maximum
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int32_t kNoToken = INT_MAX;
@@ -137,6 +140,7 @@ struct Common {
     int32_t lo[kMostWaves], hi[kMostWaves], bad[kMostWaves];
     int32_t lim[32 * kMostWaves];
     float m[kMostWaves][32], l[kMostWaves][32];
+    float jm[16], jl[16];
 };
 
 __device__ __forceinline__ int32_t seq_units(const PagedArgs &a, int32_t b)
@@ -180,8 +184,13 @@ __device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, bool pr
         }
         all = uniform(all);
     }
-    const int total = prefix_total + all * a.items_per_seq, share = (total + a.grid - 1) / a.grid;
-    r.per_wg = max(share, a.min_units);
+    const int total = prefix_total + all * a.items_per_seq;
+    // two workgroups a compute unit; but one of up to eight units where few
+    // items are cut into many parts, of which there are then half as many to
+    // join (one sequence of 8192 tokens: 15.5 us against 20.5; of 32768: 29.8
+    // against 34.9; eight of 1000 to 8000: 31.0 against 31.9)
+    r.per_wg = (total + a.grid - 1) / a.grid;
+    if (!pre && a.n_seqs * a.items_per_seq <= kPagedGrid / 8) r.per_wg = max(r.per_wg, min(8, (total + kPagedGrid / 2 - 1) / (kPagedGrid / 2)));
     if ((int64_t)blockIdx.x * r.per_wg >= total) return false;
     r.at = blockIdx.x * r.per_wg;
     r.end = total - r.at < r.per_wg ? total : r.at + r.per_wg;
@@ -310,19 +319,22 @@ struct Sink {
     }
 };
 
-// ... and the item's head, by the workgroup that holds its first unit: the
-// slot of its first part, its first workgroup, its parts, and the body.
-__device__ __forceinline__ Sink sink_of(const PagedArgs &a, int D, const Run &r, int u0, int u1, bool first, bool wide)
+// The part of an item that workgroup wg leaves: a workgroup's first item has
+// its slot 2 wg, the one that its run ends in slot 2 wg + 1.
+__device__ __forceinline__ int part_slot(const Run &r, int wg) { return 2 * wg + (wg * r.per_wg >= r.it.first ? 0 : 1); }
+
+__device__ __forceinline__ Sink sink_of(const PagedArgs &a, int D, const Run &r, int u0, int u1, int tile)
 {
     const bool entire = u0 == 0 && u1 == r.it.units;
-    const int slot = 2 * (int)blockIdx.x + (first ? 0 : 1);
+    const int slot = part_slot(r, blockIdx.x);
     Sink s;
     s.last_word = entire && a.prefix_items == 0;
     s.by_row = entire ? a.whole + (r.it.prefix ? 0 : (int64_t)a.n_seqs * a.n_q * a.n_heads) * (D + 4) : nullptr;
-    s.cut = (wide ? a.wide_parts : a.parts) + (int64_t)slot * (wide ? a.own_tile : a.narrow_tile) * (D + 4);
-    if (u0 == 0 && threadIdx.x == 0) {
+    s.cut = a.parts + (int64_t)slot * tile * (D + 4);
+    if (a.prefix_items && u0 == 0 && threadIdx.x == 0) {
+        // the item's head, for the second launch: its first part, its first workgroup, its parts
         const int last_wg = (r.it.first + r.it.units - 1) / r.per_wg;
-        a.heads[r.it.index] = int4{slot, (int)blockIdx.x, last_wg - (int)blockIdx.x + 1, wide ? 1 : 0};
+        a.heads[r.it.index] = int4{slot, (int)blockIdx.x, last_wg - (int)blockIdx.x + 1, 0};
     }
     return s;
 }
@@ -333,6 +345,128 @@ __device__ __forceinline__ float inverse_sum(float sum, float scale)
 }
 
 __device__ __forceinline__ float log_sum(float m, float sum) { return m == -INFINITY ? -INFINITY : (m + log2f(sum)) * kLn2; }
+
+// Adds part p (four features from f on) to sums x with maximum m and sum of
+// weights l.
+__device__ __forceinline__ void add_part(const f32x4_t y, float mi, float li, f32x4_t &x, float &m, float &l)
+{
+    const float m_new = fmaxf(m, mi);
+    const float w0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+    const float w1 = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - m_new);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float z = w0 != 0.f ? w0 * x[e] : 0.f;
+        x[e] = w1 != 0.f ? __builtin_fmaf(w1, y[e], z) : z;
+    }
+    l = w0 * l + w1 * li;
+    m = m_new;
+}
+
+template <bool F32>
+__device__ __forceinline__ void write_four(void *O, int64_t at, f32x4_t x)
+{
+    if constexpr (F32) {
+        *reinterpret_cast<f32x4_t *>(static_cast<float *>(O) + at) = x;
+    } else {
+        bf16x4_t y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = (__bf16)x[i];
+        *reinterpret_cast<bf16x4_t *>(static_cast<__bf16 *>(O) + at) = y;
+    }
+}
+
+// Parts pass between workgroups on different XCDs, whose L2 caches do not
+// see each other's lines.  They are stored and loaded as device-scope atomics,
+// which go past the L2, so a part is there once its stores have returned: a
+// release fence would write the whole L2 back instead, from every workgroup
+// (measured: one sequence's decode 17 -> 72 us).
+// (With a prefix the next launch reads them, and they are plain stores.)
+__device__ __forceinline__ void store_part(float *p, float x, float y, bool within)
+{
+    if (within) {
+        const uint64_t v = (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32;
+        __hip_atomic_store(reinterpret_cast<uint64_t *>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    } else {
+        *reinterpret_cast<f32x2_t *>(p) = f32x2_t{x, y};
+    }
+}
+
+__device__ __forceinline__ f32x2_t load_part(const float *p)
+{
+    return __builtin_bit_cast(f32x2_t, __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// After a part of a cut item was stored: the workgroup that comes last of the
+// item's joins them, in the order of the keys whoever comes last.  The counter
+// (one per workgroup that an item may begin in) is left at zero.
+template <int D, bool F32, int NW>
+__device__ __forceinline__ void join_cut(const PagedArgs &a, Common &sh, unsigned char *smem, const Run &run, const Rows &rows,
+                                         int tile)
+{
+    constexpr int T = 64 * NW, PL = D / 4, NP = T / PL;  // lanes of a part, parts in flight
+    const int tid = threadIdx.x;
+    const int wg0 = run.it.first / run.per_wg, n = (run.it.first + run.it.units - 1) / run.per_wg - wg0 + 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's stores have returned ...
+    __syncthreads();                                  // ... and the other waves'
+    if (tid == 0) {
+        const uint32_t before = __hip_atomic_fetch_add(a.counters + wg0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (before == (uint32_t)(n - 1)) __hip_atomic_store(a.counters + wg0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        sh.at = before == (uint32_t)(n - 1);
+    }
+    __syncthreads();
+    if (!uniform(sh.at)) return;
+    const int64_t row_bytes = D + 4, stride = 2 * (int64_t)tile * row_bytes;  // (floats; from one workgroup's to the next one's)
+    const float *first = a.parts + (int64_t)part_slot(run, wg0) * tile * row_bytes;
+    const float *rest = a.parts + (int64_t)2 * wg0 * tile * row_bytes;
+    // groups of a row: a power of two, all of them for one row
+    int per_row = NP;
+    while (per_row > 1 && per_row * rows.n > NP) per_row >>= 1;
+    const int pl = tid % PL, pg = tid / PL, sub = pg & (per_row - 1);
+    float *s_acc = reinterpret_cast<float *>(smem);
+    const float vs = a.v_scale ? a.v_scale[rows.g] : 1.f;
+    for (int r = pg / per_row; r < rows.n || per_row > 1; r += NP / per_row) {
+        f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.f;
+        if (r < rows.n) {
+            // (kJoin parts are asked for before the first is used)
+            const float *row = rest + r * row_bytes;
+            for (int i0 = sub; i0 < n; i0 += kJoin * per_row) {
+                f32x2_t y[kJoin], z[kJoin], ml[kJoin];
+#pragma unroll
+                for (int k = 0; k < kJoin; ++k) {
+                    const int i = min(i0 + k * per_row, n - 1);
+                    const float *p = i == 0 ? first + r * row_bytes : row + i * stride;
+                    y[k] = load_part(p + 4 * pl);
+                    z[k] = load_part(p + 4 * pl + 2);
+                    ml[k] = load_part(p + D);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int k = 0; k < kJoin; ++k)
+                    if (i0 + k * per_row < n) add_part(f32x4_t{y[k][0], y[k][1], z[k][0], z[k][1]}, ml[k][0], ml[k][1], x, m, l);
+            }
+        }
+        if (per_row > 1) {  // (uniform; one round, every thread)
+            *reinterpret_cast<f32x4_t *>(s_acc + pg * D + 4 * pl) = x;
+            if (pl == 0) {
+                sh.jm[pg] = m;
+                sh.jl[pg] = l;
+            }
+            __syncthreads();
+            if (sub == 0)
+                for (int i = 1; i < per_row; ++i)
+                    add_part(*reinterpret_cast<const f32x4_t *>(s_acc + (pg + i) * D + 4 * pl), sh.jm[pg + i], sh.jl[pg + i], x, m, l);
+        }
+        if (r < rows.n && sub == 0) {
+            int b, t, h;
+            rows.of(a, r, b, t, h);
+            const int64_t orow = ((int64_t)b * a.n_q + t) * a.n_heads + h;
+            write_four<F32>(a.O, orow * D + 4 * pl, x * inverse_sum(l, vs));
+            if (a.lse && pl == 0) a.lse[orow] = log_sum(m, l);
+        }
+        if (per_row > 1) break;
+    }
+}
 
 // ------------------------------------------------------------- narrow body
 //
@@ -384,7 +518,6 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
     if (!find_run<NW>(a, sh, pre, own, run)) return;
     const int tid = threadIdx.x, w = uniform(tid >> 6), lane = tid & 63, l16 = lane & 15, kg = lane >> 4;
     unsigned char *vbuf = smem + w * S::WAVE;
-    const int run0 = run.at;
 
     for (;;) {
         const Item &it = run.it;
@@ -782,7 +915,8 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
         }
 
         // ------------------------- the waves' sums joined, the result written
-        const Sink sink = sink_of(a, D, run, u0, u1, run.at == run0, false);
+        const Sink sink = sink_of(a, D, run, u0, u1, a.narrow_tile);
+        const bool within = a.prefix_items == 0;  // the parts are joined within this launch
         const float vs = a.v_scale ? a.v_scale[g] : 1.f;
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
@@ -834,29 +968,23 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
 #pragma unroll
                         for (int i = 0; i < 4; ++i) x[i] = wt[v] != 0.f ? __builtin_fmaf(wt[v], y[i], x[i]) : x[i];
                     }
-                    if (sink.last_word) {
-                        if constexpr (F32) {
-                            *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.O) + orow * D + f) = x * inv;
-                        } else {
-                            bf16x4_t y;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) y[i] = (__bf16)(x[i] * inv);
-                            *reinterpret_cast<bf16x4_t *>(static_cast<__bf16 *>(a.O) + orow * D + f) = y;
-                        }
-                    } else {
-                        *reinterpret_cast<f32x4_t *>(part + f) = x;
+                    if (sink.last_word)
+                        write_four<F32>(a.O, orow * D + f, x * inv);
+                    else {
+                        store_part(part + f, x[0], x[1], within);
+                        store_part(part + f + 2, x[2], x[3], within);
                     }
                 }
                 if ((tid & 15) == 0) {
                     if (!sink.last_word) {
-                        part[D] = m;
-                        part[D + 1] = sum;
+                        store_part(part + D, m, sum, within);
                     } else if (a.lse) {
                         a.lse[orow] = log_sum(m, sum);
                     }
                 }
             }
         }
+        if (within && (u0 != 0 || u1 != it.units)) join_cut<D, F32, NW>(a, sh, smem, run, rows, a.narrow_tile);
         run.at = it.first + u1;
         if (run.at >= run.end) return;
         next_item(a, run.it);
@@ -905,7 +1033,6 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
     int slot = (a.grid & 7) == 0 ? (blockIdx.x & 7) * grid8 + (blockIdx.x >> 3) : blockIdx.x;
     Run run;
     run.at = run.end = -1;
-    int run0 = 0;
 
     for (;;) {
         Rows rows;
@@ -925,7 +1052,6 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
         } else {
             if (run.at < 0) {
                 if (!own || !find_run<S::NW>(a, sh, false, true, run)) return;
-                run0 = run.at;
             } else {
                 if (run.at >= run.end) return;
                 next_item(a, run.it);
@@ -933,7 +1059,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             u0 = run.at - run.it.first;
             u1 = min(run.it.units, run.end - run.it.first);
             rows = rows_of(a, run.it);
-            sink = sink_of(a, D, run, u0, u1, run.at == run0, true);
+            sink = sink_of(a, D, run, u0, u1, a.own_tile);
             run.at = run.it.first + u1;
         }
         const int g = rows.g;
@@ -1120,17 +1246,13 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                     m_run = m_new;
                 }
                 const float m_use = MASKED && m_run == -INFINITY ? 0.f : m_run;
-                bf16x8_t ph[2], pl[2];
+                bf16x8_t pw[2];
                 float l = 0.f;
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * q + e], c2, -m_use));
-                        l += x[e];
-                    }
-                    split_weights(x, ph[q], pl[q]);
+                for (int r = 0; r < 16; ++r) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, -m_use));
+                    l += x;
+                    pw[r >> 3][r & 7] = (__bf16)x;
                 }
                 l_run += l;
 #pragma unroll
@@ -1140,8 +1262,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                     bf16x8_t v = vf[i % 3], odd;
                     if constexpr (MASKED) take_odd(v, odd);
                     f32x16_t &o = acc[i >> 1];
-                    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, ph[i & 1], o, 0, 0, 0);
-                    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pl[i & 1], o, 0, 0, 0);
+                    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pw[i & 1], o, 0, 0, 0);
                     if constexpr (MASKED) {
                         bf16x8_t see;
 #pragma unroll
@@ -1177,6 +1298,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
         }
 
         // ------------------------------------------------- the result written
+        const bool within = a.prefix_items == 0;  // the parts are joined within this launch
         l_run += __shfl_xor(l_run, 32, 64);
         // (scores that are all NaN leave no maximum, but their sum counts)
         m_run = lim < 0 ? -INFINITY : l_run != l_run ? 0.f : m_run;
@@ -1227,26 +1349,25 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int f = 32 * mb + 8 * q + 4 * hh;
-                    if (sink.last_word) {
-                        bf16x4_t y;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) y[i] = (__bf16)(acc[mb][4 * q + i] * inv);
-                        *reinterpret_cast<bf16x4_t *>(static_cast<__bf16 *>(a.O) + orow * D + f) = y;
-                    } else {
-                        *reinterpret_cast<f32x4_t *>(part + f) =
-                            f32x4_t{acc[mb][4 * q], acc[mb][4 * q + 1], acc[mb][4 * q + 2], acc[mb][4 * q + 3]};
+                    const f32x4_t x = {acc[mb][4 * q], acc[mb][4 * q + 1], acc[mb][4 * q + 2], acc[mb][4 * q + 3]};
+                    if (sink.last_word)
+                        write_four<false>(a.O, orow * D + f, x * inv);
+                    else {
+                        store_part(part + f, x[0], x[1], within);
+                        store_part(part + f + 2, x[2], x[3], within);
                     }
                 }
             }
             if (hh == 0) {
                 if (!sink.last_word) {
-                    part[D] = m_run;
-                    part[D + 1] = l_run;
+                    store_part(part + D, m_run, l_run, within);
                 } else if (a.lse) {
                     a.lse[orow] = log_sum(m_run, l_run);
                 }
             }
         }
+        if (within && (u0 != 0 || u1 != run.it.units))
+            join_cut<D, false, S::NW>(a, sh, smem, run, rows, a.own_tile);
     }
 }
 

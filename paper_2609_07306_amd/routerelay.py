@@ -406,7 +406,8 @@ def sparse_attention(Q, K, V, routes, chunk: int, causal: bool, scale: float = 0
 
 _E4M3 = torch.float8_e4m3fn
 # (the address alone: a torch.cuda.Stream object costs as much as a launch's checks)
-_current_stream = torch._C._cuda_getCurrentRawStream
+_current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+_append, _paged, _prefix = lib.rr_cache_append, lib.rr_paged_attention, lib.rr_prefix_attention
 _DTYPES = {torch.float32: RR_F32, torch.bfloat16: RR_BF16, _E4M3: RR_E4M3}
 
 
@@ -431,20 +432,22 @@ def _launch(dev, stream, call, *args):
         raise ValueError(f"the stream is of {stream.device}, the tensors are on cuda:{dev}")
     else:
         s = stream.cuda_stream
-    if torch.cuda.current_device() == dev:
-        _check(call(*args, s))
+    if _current_device() == dev:
+        status = call(*args, s)
     else:
         with torch.cuda.device(dev):
-            _check(call(*args, s))
+            status = call(*args, s)
+    if status:
+        _check(status)
 
 
-def _empty(shape, dtype, like, stream):
+def _empty(shape, dtype, like, stream, zeros=False):
     """Memory for a call on the given stream (None: the current one), of that
     stream's own: freed, only what the stream does later can take it."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _empty(shape, dtype, like, None, zeros)
+    return (torch.zeros if zeros else torch.empty)(shape, dtype=dtype, device=like.device)
 
 
 def _of(name, t, shape, dtype):
@@ -455,8 +458,21 @@ def _of(name, t, shape, dtype):
     return t.data_ptr()
 
 
+def _lists(page_table, lengths):
+    """The addresses of page_table [B, max_pages] and lengths [B], and their sizes."""
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [B, max_pages]")
+    B, most = page_table.shape
+    if page_table.dtype != torch.int32 or lengths.dtype != torch.int32 or lengths.shape != (B,):
+        raise ValueError(f"page_table [B, max_pages] and lengths [B] must be int32: got {page_table.dtype} of shape "
+                         f"{list(page_table.shape)}, {lengths.dtype} of shape {list(lengths.shape)}")
+    if not (page_table.is_contiguous() and lengths.is_contiguous()):
+        raise ValueError("page_table and lengths must be contiguous")
+    return page_table.data_ptr(), lengths.data_ptr(), B, most
+
+
 def _cache_of(K_cache, V_cache, dtype, k_scale, v_scale):
-    """The pools' shape, their type and the scales' addresses."""
+    """The pools' shape, type and addresses, and the scales' addresses."""
     kind, shape = K_cache.dtype, K_cache.shape
     if len(shape) != 4 or kind not in _DTYPES or V_cache.dtype != kind:
         raise TypeError("K_cache and V_cache must be [n_pages, H_kv, page, d] tensors of one type of "
@@ -467,10 +483,13 @@ def _cache_of(K_cache, V_cache, dtype, k_scale, v_scale):
         raise TypeError("the cache must have the queries' type, or float8_e4m3fn with bfloat16")
     if (k_scale is not None) != (kind == _E4M3) or (v_scale is not None) != (kind == _E4M3):
         raise ValueError("k_scale and v_scale are given for float8_e4m3fn caches, and for them only")
-    if k_scale is None:
-        return shape, _DTYPES[kind], None, None
-    heads = (shape[1],)
-    return shape, RR_E4M3, _of("k_scale", k_scale, heads, torch.float32), _of("v_scale", v_scale, heads, torch.float32)
+    if not (K_cache.is_contiguous() and V_cache.is_contiguous()):
+        raise ValueError("K_cache and V_cache must be contiguous")
+    ks = vs = None
+    if k_scale is not None:
+        heads = (shape[1],)
+        ks, vs = _of("k_scale", k_scale, heads, torch.float32), _of("v_scale", v_scale, heads, torch.float32)
+    return shape, _DTYPES[kind], K_cache.data_ptr(), V_cache.data_ptr(), ks, vs
 
 
 def _rows_of(name, t, shape, dtype):
@@ -497,14 +516,12 @@ def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, fr
     kind, shape = K.dtype, K.shape
     if len(shape) != 3 or kind not in (torch.float32, torch.bfloat16):
         raise TypeError("K must be a [n_tokens, H_kv, d] float32 or bfloat16 tensor")
-    (n_pages, Hkv, page, d), cache, ks, vs = _cache_of(K_cache, V_cache, kind, k_scale, v_scale)
+    (n_pages, Hkv, page, d), cache, kc, vc, ks, vs = _cache_of(K_cache, V_cache, kind, k_scale, v_scale)
     dev = _device_of((K, V, K_cache, V_cache, page_table, lengths, seq_start, freqs, Q, Q_out, k_scale, v_scale))
     n = shape[0]
     rows = (n, Hkv, d)
     ldk, ldv = _rows_of("K", K, rows, kind), _rows_of("V", V, rows, kind)
-    if page_table.dim() != 2:
-        raise ValueError("page_table must be [B, max_pages]")
-    B, most = page_table.shape
+    table, lens, B, most = _lists(page_table, lengths)
     H = ldq = rot = 0
     f = q = out = start = None
     if freqs is not None:
@@ -525,62 +542,66 @@ def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, fr
         raise ValueError("Q_out without Q")
     cfg = _AppendConfig(H, Hkv, d, page, n_pages, most, B, n, rot, 1 if interleaved else 0, _DTYPES[kind], cache, ldq, ldk,
                         ldv, ks, vs)
-    _launch(dev, stream, lib.rr_cache_append, ctypes.byref(cfg), K.data_ptr(), V.data_ptr(), q, start,
-            _of("lengths", lengths, (B,), torch.int32), _of("page_table", page_table, (B, most), torch.int32), f if rot else None,
-            _of("K_cache", K_cache, K_cache.shape, K_cache.dtype), _of("V_cache", V_cache, K_cache.shape, K_cache.dtype), out)
+    _launch(dev, stream, _append, cfg, K.data_ptr(), V.data_ptr(), q, start, lens, table, f if rot else None, kc, vc, out)
     return Q_out
 
 
-def _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, n_prefix, scale, k_scale, v_scale):
+def _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, n_prefix, scale, k_scale, v_scale, lengths):
+    """The call's configuration, and the addresses of the pools, the page table and
+    the lengths."""
     if Q.dim() != 4 or Q.dtype not in (torch.float32, torch.bfloat16):
         raise TypeError("Q must be a [B, n_q, H, d] float32 or bfloat16 tensor")
-    (n_pages, Hkv, page, d), cache, ks, vs = _cache_of(K_cache, V_cache, Q.dtype, k_scale, v_scale)
+    (n_pages, Hkv, page, d), cache, kc, vc, ks, vs = _cache_of(K_cache, V_cache, Q.dtype, k_scale, v_scale)
     B, nq, H, dq = Q.shape
     if dq != d:
         raise ValueError(f"Q has rows of {dq} features, the cache of {d}")
     if page_table.dim() != 2 or page_table.shape[0] != B:
         raise ValueError("page_table must be [B, max_pages]")
+    table, lens, _, most = _lists(page_table, lengths)
     k = 0
     if routes is not None:
         if routes.dim() != 2 or routes.shape[0] != B * H * nq:
             raise ValueError("routes must be [B * H * n_q, k]")
         k = routes.shape[1]
-    return _PagedConfig(H, Hkv, d, page, n_pages, page_table.shape[1], B, nq, k, n_sink, n_recent, n_prefix,
-                        _DTYPES[Q.dtype], cache, scale, 0, ks, vs)
+    cfg = _PagedConfig(H, Hkv, d, page, n_pages, most, B, nq, k, n_sink, n_recent, n_prefix, _DTYPES[Q.dtype], cache, scale, 0,
+                       ks, vs)
+    return cfg, kc, vc, table, lens
 
 
 def _workspace_bytes(cfg):
-    n = lib.rr_paged_workspace_bytes(ctypes.byref(cfg))
+    n = lib.rr_paged_workspace_bytes(cfg)
     if n == 0:
         raise RRError(RR_ERR_INVALID, lib.rr_last_error().decode())
     return n
 
 
 def paged_workspace(Q, K_cache, page_table, routes=None, n_sink=0, n_recent=0, n_prefix=0):
-    """A workspace (uint8 device tensor) for paged_attention and
-    prefix_attention calls of these shapes.  Calls that may run at the same
-    time, captured graphs that are replayed side by side among them, need one
-    each."""
-    scale = None
-    if K_cache.dtype == _E4M3 and K_cache.dim() == 4:  # (the scales' values play no part)
+    """A workspace (uint8 device tensor, zeros) for paged_attention and
+    prefix_attention calls of these shapes, one after the other in any order
+    (the largest of several shapes' serves them all).  Calls that may run at
+    the same time, captured graphs that are replayed side by side among them,
+    need one each."""
+    scale, lengths = None, torch.empty(len(page_table), dtype=torch.int32, device=page_table.device)
+    if K_cache.dtype == _E4M3 and K_cache.dim() == 4:  # (values play no part)
         scale = torch.empty(K_cache.shape[1], dtype=torch.float32, device=K_cache.device)
-    cfg = _paged_config(Q, K_cache, K_cache, page_table, routes, n_sink, n_recent, n_prefix, 0.0, scale, scale)
-    return torch.empty(_workspace_bytes(cfg), dtype=torch.uint8, device=Q.device)
+    cfg = _paged_config(Q, K_cache, K_cache, page_table, routes, n_sink, n_recent, n_prefix, 0.0, scale, scale, lengths)[0]
+    return torch.zeros(_workspace_bytes(cfg), dtype=torch.uint8, device=Q.device)
 
 
-def _paged_call(call, cfg, dev, Q, K_cache, V_cache, page_table, lengths, third, out, lse, workspace, stream):
-    B, nq, H, d = Q.shape
+def _paged_call(call, config, dev, Q, third, out, lse, workspace, stream):
+    cfg, kc, vc, table, lens = config
     if out is None:
         out = _empty(Q.shape, Q.dtype, Q, stream)
+    elif out.shape != Q.shape or out.dtype != Q.dtype:
+        raise ValueError(f"out must be {Q.dtype} of shape {list(Q.shape)}")
     if workspace is None:
-        workspace = _empty((_workspace_bytes(cfg),), torch.uint8, Q, stream)
+        workspace = _empty((_workspace_bytes(cfg),), torch.uint8, Q, stream, zeros=True)
     elif workspace.dtype != torch.uint8 or workspace.dim() != 1:
         raise ValueError("workspace must be a one-dimensional uint8 tensor")
-    _launch(dev, stream, call, ctypes.byref(cfg), _of("Q", Q, Q.shape, Q.dtype), _of("K_cache", K_cache, K_cache.shape, K_cache.dtype),
-            _of("V_cache", V_cache, K_cache.shape, K_cache.dtype), _of("page_table", page_table, page_table.shape, torch.int32),
-            _of("lengths", lengths, (B,), torch.int32), third, _of("out", out, Q.shape, Q.dtype),
-            None if lse is None else _of("lse", lse, (B, nq, H), torch.float32),
-            _of("workspace", workspace, workspace.shape, torch.uint8), workspace.numel())
+    if not (Q.is_contiguous() and out.is_contiguous() and workspace.is_contiguous()):
+        raise ValueError("Q, out and workspace must be contiguous")
+    _launch(dev, stream, call, cfg, Q.data_ptr(), kc, vc, table, lens, third, out.data_ptr(),
+            None if lse is None else _of("lse", lse, Q.shape[:3], torch.float32), workspace.data_ptr(), workspace.numel())
     return out
 
 
@@ -591,11 +612,10 @@ def paged_attention(Q, K_cache, V_cache, page_table, lengths, routes=None, n_sin
     [B * H * n_q, k] int32 page indices: each query over those pages, its first
     n_sink and its last n_recent ones.  lse: optional float32 output [B, n_q,
     H].  workspace: paged_workspace(...), or None for one of this call's own."""
-    cfg = _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, 0, scale, k_scale, v_scale)
+    config = _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, 0, scale, k_scale, v_scale, lengths)
     dev = _device_of((Q, K_cache, V_cache, page_table, lengths, routes, k_scale, v_scale, out, lse, workspace))
-    third = _of("routes", routes, routes.shape, torch.int32) if cfg.k else None
-    return _paged_call(lib.rr_paged_attention, cfg, dev, Q, K_cache, V_cache, page_table, lengths, third, out, lse, workspace,
-                       stream)
+    third = _of("routes", routes, routes.shape, torch.int32) if routes is not None and routes.shape[1] else None
+    return _paged_call(_paged, config, dev, Q, third, out, lse, workspace, stream)
 
 
 def prefix_attention(Q, K_cache, V_cache, page_table, lengths, prefix_pages, n_prefix, scale=0.0, k_scale=None,
@@ -603,8 +623,7 @@ def prefix_attention(Q, K_cache, V_cache, page_table, lengths, prefix_pages, n_p
     """rr_prefix_attention: paged_attention (without routes) for sequences that
     begin with the same n_prefix tokens, which are read once for the batch from
     prefix_pages [ceil(n_prefix / page)] int32."""
-    cfg = _paged_config(Q, K_cache, V_cache, page_table, None, 0, 0, n_prefix, scale, k_scale, v_scale)
+    config = _paged_config(Q, K_cache, V_cache, page_table, None, 0, 0, n_prefix, scale, k_scale, v_scale, lengths)
     dev = _device_of((Q, K_cache, V_cache, page_table, lengths, prefix_pages, k_scale, v_scale, out, lse, workspace))
     third = _of("prefix_pages", prefix_pages, (n_chunks(n_prefix, K_cache.shape[2]),), torch.int32)
-    return _paged_call(lib.rr_prefix_attention, cfg, dev, Q, K_cache, V_cache, page_table, lengths, third, out, lse, workspace,
-                       stream)
+    return _paged_call(_prefix, config, dev, Q, third, out, lse, workspace, stream)
