@@ -104,6 +104,7 @@ struct PagedArgs {
     int32_t own_tile, row_tiles;  // ... in tiles of so many
     int32_t items_per_seq;  // H_kv * row_tiles; routes: H * n_q
     int32_t route_units;    // routes: units of every item
+    int32_t item_cost;      // units that stand for what an item of a sequence costs besides its keys
     int32_t prefix_rows, prefix_tile, prefix_tiles, prefix_items, prefix_units;  // of the batch against the prefix
     bool own_wide, prefix_wide;        // which body takes them
     int32_t prefix_splits, prefix_slots;  // of the wide body: key splits, (key head, split, row tile) slots

@@ -146,8 +146,8 @@ struct Common {
 __device__ __forceinline__ int32_t seq_units(const PagedArgs &a, int32_t b)
 {
     if (a.route_units) return a.route_units;
-    const int32_t n = held_tokens(a.lengths[b], a.capacity) - a.n_prefix;
-    return n <= kPagedUnit ? 1 : (n + kPagedUnit - 1) / kPagedUnit;
+    const int32_t n = held_tokens(a.lengths[b], a.capacity) - a.n_prefix, units = n <= 0 ? 0 : (n + kPagedUnit - 1) / kPagedUnit;
+    return max(units + a.item_cost, 1);
 }
 
 // This workgroup's run of the items that a body takes: the prefix's, the
@@ -525,6 +525,8 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
         const Rows rows = rows_of(a, it);
         const int g = rows.g, blocks = (rows.n + 15) >> 4;
 
+        // (a sequence's first item_cost units stand for what an item costs besides its keys)
+        const int cost = it.prefix || a.route_units ? 0 : a.item_cost, k0 = max(u0 - cost, 0), k1 = max(u1 - cost, 0);
         // key positions: tokens from `base` on, or, along routes, the places
         // of the listed pages one after the other.  The run's first pages (or
         // the row's routes) are asked for here, before the lengths are there
@@ -536,7 +538,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
             const int64_t row = ((int64_t)it.b * a.items_per_seq + it.j) * a.k;
             if (tid >= a.n_sink + a.n_recent && tid < slots) asked = a.routes[row + tid - a.n_sink - a.n_recent];
         } else {
-            asked = pages[min(a.pd.div(base + min(u0 * kPagedUnit, a.capacity)) + tid, last_page)];
+            asked = pages[min(a.pd.div(base + min(k0 * kPagedUnit, a.capacity)) + tid, last_page)];
         }
 
         // query operands; lim: the last token that a row sees (-1: none);
@@ -622,8 +624,8 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
         } else {
             n_pos = hi < base ? 0 : hi - base + 1;
         }
-        const int p0 = (int)min((int64_t)u0 * kPagedUnit, (int64_t)n_pos);
-        const int p1 = (int)min((int64_t)u1 * kPagedUnit, (int64_t)n_pos);
+        const int p0 = (int)min((int64_t)k0 * kPagedUnit, (int64_t)n_pos);
+        const int p1 = (int)min((int64_t)k1 * kPagedUnit, (int64_t)n_pos);
 
         for (int pa = p0; pa < p1; pa += a.batch_keys) {
             const int pb = min(p1 - pa, a.batch_keys) + pa;
@@ -1062,7 +1064,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             sink = sink_of(a, D, run, u0, u1, a.own_tile);
             run.at = run.it.first + u1;
         }
-        const int g = rows.g;
+        const int g = rows.g, cost = rows.prefix ? 0 : a.item_cost;
         // row blocks (a power of two), waves of a row block, this wave's of each
         const int wr = rows.n <= 32 ? 1 : rows.n <= 64 ? 2 : rows.n <= 128 ? 4 : 8, wk = min(S::NB, S::NW / wr);
         const int rb = w & (wr - 1), kp = w / wr;
@@ -1108,8 +1110,8 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
 
         const int base = rows.prefix ? 0 : a.n_prefix;
         const int n_pos = hi < base ? 0 : hi - base + 1;
-        const int p0 = (int)min((int64_t)u0 * kPagedUnit, (int64_t)n_pos);
-        const int p1 = (int)min((int64_t)u1 * kPagedUnit, (int64_t)n_pos);
+        const int p0 = (int)min((int64_t)max(u0 - cost, 0) * kPagedUnit, (int64_t)n_pos);
+        const int p1 = (int)min((int64_t)max(u1 - cost, 0) * kPagedUnit, (int64_t)n_pos);
 
         for (int pa = p0; pa < p1; pa += a.batch_keys) {
             const int pb = min(p1 - pa, a.batch_keys) + pa;
