@@ -142,14 +142,14 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     const double most = most_own + (double)a.prefix_items * a.prefix_units;
     if (most >= (double)INT32_MAX) return false;
     // splits of a wide prefix: the fewest that leave at most a tenth more of
-    // the card idle than the best number does, of two units at least
+    // the card idle than the best number does
     a.prefix_splits = a.prefix_slots = 0;
     if (a.prefix_wide) {
         const auto used = [&](int splits) {
             const int n = a.prefix_items * splits, rounds = (n + kPagedGrid - 1) / kPagedGrid;
             return (double)n / ((double)rounds * kPagedGrid);
         };
-        const int most_splits = a.prefix_units / 2 < 1 ? 1 : a.prefix_units / 2 < kPagedGrid ? a.prefix_units / 2 : kPagedGrid;
+        const int most_splits = a.prefix_units < kPagedGrid ? a.prefix_units : kPagedGrid;
         double best = 0.;
         for (int n = 1; n <= most_splits; ++n) best = used(n) > best ? used(n) : best;
         a.prefix_splits = 1;

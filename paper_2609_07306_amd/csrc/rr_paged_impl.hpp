@@ -123,6 +123,7 @@ struct Item {
 };
 
 struct Run {
+    int32_t me;               // its number
     int32_t at, end, per_wg;  // units [at, end) of the body's
     Item it;
 };
@@ -150,11 +151,12 @@ __device__ __forceinline__ int32_t seq_units(const PagedArgs &a, int32_t b)
     return max(units + a.item_cost, 1);
 }
 
-// This workgroup's run of the items that a body takes: the prefix's, the
-// sequences', or one after the other.  False where it has none.
+// Run `me` of the items that a body takes: the prefix's, the sequences', or
+// one after the other.  False where there is none.
 template <int NW>
-__device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, bool pre, bool own, Run &r)
+__device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, int me, bool pre, bool own, Run &r)
 {
+    r.me = me;
     constexpr int T = 64 * NW;
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
     // (a call has less than 2^31 units)
@@ -191,8 +193,8 @@ __device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, bool pr
     // against 34.9; eight of 1000 to 8000: 31.0 against 31.9)
     r.per_wg = (total + a.grid - 1) / a.grid;
     if (!pre && a.n_seqs * a.items_per_seq <= kPagedGrid / 8) r.per_wg = max(r.per_wg, min(8, (total + kPagedGrid / 2 - 1) / (kPagedGrid / 2)));
-    if ((int64_t)blockIdx.x * r.per_wg >= total) return false;
-    r.at = blockIdx.x * r.per_wg;
+    if ((int64_t)me * r.per_wg >= total) return false;
+    r.at = me * r.per_wg;
     r.end = total - r.at < r.per_wg ? total : r.at + r.per_wg;
     // the sequence that the run begins in, and the units before it
     int b_at = 0, b_before = 0;
@@ -319,14 +321,14 @@ struct Sink {
     }
 };
 
-// The part of an item that workgroup wg leaves: a workgroup's first item has
-// its slot 2 wg, the one that its run ends in slot 2 wg + 1.
+// The part of an item that run wg leaves: a run's first item has its slot
+// 2 wg, the one that it ends in slot 2 wg + 1.
 __device__ __forceinline__ int part_slot(const Run &r, int wg) { return 2 * wg + (wg * r.per_wg >= r.it.first ? 0 : 1); }
 
 __device__ __forceinline__ Sink sink_of(const PagedArgs &a, int D, const Run &r, int u0, int u1, int tile)
 {
     const bool entire = u0 == 0 && u1 == r.it.units;
-    const int slot = part_slot(r, blockIdx.x);
+    const int slot = part_slot(r, r.me);
     Sink s;
     s.last_word = entire && a.prefix_items == 0;
     s.by_row = entire ? a.whole + (r.it.prefix ? 0 : (int64_t)a.n_seqs * a.n_q * a.n_heads) * (D + 4) : nullptr;
@@ -334,7 +336,7 @@ __device__ __forceinline__ Sink sink_of(const PagedArgs &a, int D, const Run &r,
     if (a.prefix_items && u0 == 0 && threadIdx.x == 0) {
         // the item's head, for the second launch: its first part, its first workgroup, its parts
         const int last_wg = (r.it.first + r.it.units - 1) / r.per_wg;
-        a.heads[r.it.index] = int4{slot, (int)blockIdx.x, last_wg - (int)blockIdx.x + 1, 0};
+        a.heads[r.it.index] = int4{slot, r.me, last_wg - r.me + 1, 0};
     }
     return s;
 }
@@ -489,7 +491,11 @@ struct Shape {
     static constexpr int KT = TY == CACHE_F32 ? 16 : 32;
     static constexpr int KR = KT / 16;
     static constexpr int PK = D * SIZE / 64;
-    static constexpr int VRS = 2 * D + 64;  // bytes of a row of the V buffer
+    // bytes of a row of the V buffer: 8 banks from one row to the next, so the
+    // transposed reads (8 rows x 32 bytes at a time) meet 64 different banks;
+    // rows 8 .. 15 of 16 hold their 16-byte pieces in swapped pairs, so the
+    // writes (16 rows x 16 bytes) do too
+    static constexpr int VRS = 2 * D + 32;
     static constexpr int ORS = D + 4;       // floats of a row of the output buffer
     static constexpr int VBYTES = TY == CACHE_F32 ? 0 : KT * VRS;
     static constexpr int OBYTES = 16 * ORS * 4;
@@ -508,14 +514,14 @@ __device__ __forceinline__ int feature_of(int v, int i, int kg)
 }
 
 template <int TY, int D, int NR, int NW>
-__device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsigned char *smem, bool pre, bool own)
+__device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsigned char *smem, int me, bool pre, bool own)
 {
     using S = Shape<TY, D>;
     constexpr bool F32 = TY == CACHE_F32;
     constexpr int NV = D / 16;  // value accumulators of a row block
     constexpr int T = 64 * NW;
     Run run;
-    if (!find_run<NW>(a, sh, pre, own, run)) return;
+    if (!find_run<NW>(a, sh, me, pre, own, run)) return;
     const int tid = threadIdx.x, w = uniform(tid >> 6), lane = tid & 63, l16 = lane & 15, kg = lane >> 4;
     unsigned char *vbuf = smem + w * S::WAVE;
 
@@ -735,11 +741,12 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                                 for (int e = 0; e < 4; ++e) vr[r][c][e] = keep ? vr[r][c][e] : 0u;
                             }
                             unsigned char *dst = vbuf + (16 * r + l16) * S::VRS;
+                            const int swap = (l16 & 8) << 1;
                             if constexpr (TY == CACHE_BF16) {
-                                *reinterpret_cast<u32x4_t *>(dst + 64 * c + 16 * kg) = vr[r][c];
+                                *reinterpret_cast<u32x4_t *>(dst + ((64 * c + 16 * kg) ^ swap)) = vr[r][c];
                             } else {
-                                *reinterpret_cast<bf16x8_t *>(dst + 128 * c + 32 * kg) = e4m3_to_bf16(vr[r][c][0], vr[r][c][1]);
-                                *reinterpret_cast<bf16x8_t *>(dst + 128 * c + 32 * kg + 16) = e4m3_to_bf16(vr[r][c][2], vr[r][c][3]);
+                                *reinterpret_cast<bf16x8_t *>(dst + ((128 * c + 32 * kg) ^ swap)) = e4m3_to_bf16(vr[r][c][0], vr[r][c][1]);
+                                *reinterpret_cast<bf16x8_t *>(dst + ((128 * c + 32 * kg + 16) ^ swap)) = e4m3_to_bf16(vr[r][c][2], vr[r][c][3]);
                             }
                         }
                     }
@@ -880,14 +887,17 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                     for (int n = 0; n < NR; ++n) {
                         float x[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = s[n][(e >> 2) % S::KR][e & 3];
+                        for (int e = 0; e < 8; ++e) x[e] = s[n][e >> 2][e & 3];
                         split_weights(x, ph[n], pl[n]);
                     }
+                    // (rows 4 kg + 0..3 of 16: swapped pieces where kg & 2)
+                    const unsigned char *vp = vbuf + (4 * kg + (l16 >> 2)) * S::VRS;
+                    const int piece = (8 * (l16 & 3)) ^ ((kg & 2) << 3);
                     auto values = [&](auto odd_tile) {
 #pragma unroll
                         for (int v = 0; v < NV; ++v) {
-                            const unsigned char *vp = vbuf + (4 * kg + (l16 >> 2)) * S::VRS + 2 * (16 * v + 4 * (l16 & 3));
-                            bf16x8_t vt = join8(lds_read_tr16(vp), lds_read_tr16(vp + 16 * S::VRS)), odd;
+                            const unsigned char *x = vp + 32 * v + piece;
+                            bf16x8_t vt = join8(lds_read_tr16(x), lds_read_tr16(x + 16 * S::VRS)), odd;
                             if constexpr (decltype(odd_tile)::value) take_odd(vt, odd);
 #pragma unroll
                             for (int n = 0; n < NR; ++n) {
@@ -899,11 +909,11 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                                     bf16x8_t sees;
 #pragma unroll
                                     for (int e = 0; e < 8; ++e)
-                                        sees[e] = of_key[(e >> 2) % S::KR][e & 3] <= (lim[n] < 0 ? hi : lim[n]) ? (__bf16)1.f : (__bf16)0.f;
+                                        sees[e] = of_key[e >> 2][e & 3] <= (lim[n] < 0 ? hi : lim[n]) ? (__bf16)1.f : (__bf16)0.f;
                                     const f32x4_t z = {0.f, 0.f, 0.f, 0.f};
-                                    const f32x4_t k = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, sees, z, 0, 0, 0);
+                                    const f32x4_t c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, sees, z, 0, 0, 0);
 #pragma unroll
-                                    for (int y = 0; y < 4; ++y) o[y] = k[y] > 0.f ? NAN : o[y];
+                                    for (int y = 0; y < 4; ++y) o[y] = c[y] > 0.f ? NAN : o[y];
                                 }
                             }
                         }
@@ -1022,17 +1032,11 @@ struct WideShape {
 };
 
 template <int TY, int D>
-__device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsigned char *smem, bool own)
+__device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsigned char *smem, int slot, int me, bool own)
 {
     using S = WideShape<TY, D>;
     constexpr int NMB = D / 32;
     const int tid = threadIdx.x, w = uniform(tid >> 6), lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
-    // The prefix's length is known to the host, which cuts it into splits: slot
-    // (key head, split, row tile), the tiles of a split next to each other and
-    // so on one XCD (workgroups are dealt to the eight round-robin), where
-    // they read the same keys at about the same time from its L2.
-    const int grid8 = a.grid >> 3;
-    int slot = (a.grid & 7) == 0 ? (blockIdx.x & 7) * grid8 + (blockIdx.x >> 3) : blockIdx.x;
     Run run;
     run.at = run.end = -1;
 
@@ -1053,7 +1057,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             slot += a.grid;
         } else {
             if (run.at < 0) {
-                if (!own || !find_run<S::NW>(a, sh, false, true, run)) return;
+                if (!own || !find_run<S::NW>(a, sh, me, false, true, run)) return;
             } else {
                 if (run.at >= run.end) return;
                 next_item(a, run.it);
@@ -1209,12 +1213,12 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[q % 3], fq.v[q], s, 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                // V^T operand i = 2 mb + s2 of the block: keys 16 s2 + 4 hh + 0..3
+                // V^T operand i = NMB s2 + mb of the block: keys 16 s2 + 4 hh + 0..3
                 // and + 8..11, the order of the score accumulator
                 const int j = lane & 15;
                 const unsigned char *vp = vt + (32 * kb + 4 * hh + (j >> 2)) * S::VRS + 2 * (16 * (l32 >> 4) + 4 * (j & 3));
                 auto value = [&](int i) {
-                    const unsigned char *x = vp + 16 * (i & 1) * S::VRS + 64 * (i >> 1);
+                    const unsigned char *x = vp + 16 * (i / NMB) * S::VRS + 64 * (i % NMB);
                     return join8(lds_read_tr16(x), lds_read_tr16(x + 8 * S::VRS));
                 };
                 bf16x8_t vf[3];
@@ -1263,12 +1267,12 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                     __builtin_amdgcn_sched_barrier(0);
                     bf16x8_t v = vf[i % 3], odd;
                     if constexpr (MASKED) take_odd(v, odd);
-                    f32x16_t &o = acc[i >> 1];
-                    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pw[i & 1], o, 0, 0, 0);
+                    f32x16_t &o = acc[i % NMB];
+                    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pw[i / NMB], o, 0, 0, 0);
                     if constexpr (MASKED) {
                         bf16x8_t see;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) see[e] = (seen >> (8 * (i & 1) + e)) & 1u ? (__bf16)1.f : (__bf16)0.f;
+                        for (int e = 0; e < 8; ++e) see[e] = (seen >> (8 * (i / NMB) + e)) & 1u ? (__bf16)1.f : (__bf16)0.f;
                         const f32x16_t z = {};
                         const f32x16_t k = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd, see, z, 0, 0, 0);
 #pragma unroll
@@ -1389,8 +1393,19 @@ __global__ __launch_bounds__((64 * Launch<TY, D, WIDE, NR>::NW), (D <= 128 && NR
     constexpr int NW = Launch<TY, D, WIDE, NR>::NW;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ Common sh;
-    if constexpr (WIDE) wide_body<TY, D>(a, sh, smem, a.own_wide);
-    if constexpr (NR > 0) narrow_body<TY, D, NR, NW>(a, sh, smem, !a.prefix_wide && a.prefix_items > 0, !a.own_wide);
+    // A wide prefix's length is known to the host, which cuts it into splits:
+    // slot (key head, split, row tile), the tiles of a split next to each
+    // other and so on one XCD (workgroups are dealt to the eight round-robin),
+    // where they read the same keys at about the same time from its L2.  Runs
+    // begin at the workgroups that the slots leave free.
+    int slot = blockIdx.x, me = blockIdx.x;
+    if constexpr (WIDE) {
+        if ((a.grid & 7) == 0) slot = (blockIdx.x & 7) * (a.grid >> 3) + (blockIdx.x >> 3);
+        me = slot - a.prefix_slots % a.grid;
+        me += me < 0 ? a.grid : 0;
+        wide_body<TY, D>(a, sh, smem, slot, me, a.own_wide);
+    }
+    if constexpr (NR > 0) narrow_body<TY, D, NR, NW>(a, sh, smem, me, !a.prefix_wide && a.prefix_items > 0, !a.own_wide);
 }
 
 template <int TY, int D, bool WIDE, int NR>
