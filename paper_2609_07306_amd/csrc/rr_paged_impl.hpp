@@ -377,6 +377,9 @@ __device__ __forceinline__ void write_four(void *O, int64_t at, f32x4_t x)
     }
 }
 
+// Waits for all of the wave's loads from memory and stores to it.
+__device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // Parts pass between workgroups on different XCDs, whose L2 caches do not
 // see each other's lines.  They are stored and loaded as device-scope atomics,
 // which go past the L2, so a part is there once its stores have returned: a
@@ -408,8 +411,8 @@ __device__ __forceinline__ void join_cut(const PagedArgs &a, Common &sh, unsigne
     constexpr int T = 64 * NW, PL = D / 4, NP = T / PL;  // lanes of a part, parts in flight
     const int tid = threadIdx.x;
     const int wg0 = run.it.first / run.per_wg, n = (run.it.first + run.it.units - 1) / run.per_wg - wg0 + 1;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's stores have returned ...
-    __syncthreads();                                  // ... and the other waves'
+    wait_vm();        // this wave's stores have returned ...
+    __syncthreads();  // ... and the other waves'
     if (tid == 0) {
         const uint32_t before = __hip_atomic_fetch_add(a.counters + wg0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (before == (uint32_t)(n - 1)) __hip_atomic_store(a.counters + wg0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -1018,9 +1021,17 @@ struct WideShape {
     static constexpr int SIZE = TY == CACHE_BF16 ? 2 : 1;
     static constexpr int KB = D <= 128 ? 64 : 32;  // keys of a staged tile
     static constexpr int NB = KB / 32;
-    static constexpr int KRS = 2 * D + 16;  // bytes of a row of the K tile (odd in units of 16: rows in distinct banks)
-    static constexpr int VRS = 2 * D + 64;  // ... of the V tile (its transposed reads cover 4 rows x 32 bytes)
+    // bf16 tiles go from memory to LDS without passing through registers, which
+    // leaves no room between rows: a row's 16-byte chunk c lies at place c ^
+    // key_swap(row), c ^ value_swap(row) instead, so that the rows that are
+    // read together (16 at one chunk; 4 at four chunks) meet different banks.
+    // e4m3 tiles are widened on the way and have padded rows
+    static constexpr bool DIRECT = TY == CACHE_BF16;
+    static constexpr int KRS = DIRECT ? 2 * D : 2 * D + 16;  // bytes of a row of the K tile
+    static constexpr int VRS = DIRECT ? 2 * D : 2 * D + 64;  // ... of the V tile
     static constexpr int BUF = KB * (KRS + VRS);
+    __device__ __forceinline__ static int key_swap(int row) { return !DIRECT ? 0 : D == 64 ? (row >> 1) & 7 : row & 15; }
+    __device__ __forceinline__ static int value_swap(int row) { return !DIRECT ? 0 : D == 64 ? (row & 2) << 1 : (row & 3) << 2; }
     static constexpr int LDS = 2 * BUF;
     static constexpr int PPR = D * SIZE / 16;          // 16-byte pieces of a row
     static constexpr int PIECES = KB * PPR;            // ... of a tile
@@ -1030,6 +1041,15 @@ struct WideShape {
     // (half the waves' accumulators pass through the tiles' memory)
     static_assert(NB == 1 || NW / 2 * 64 * (D / 32) * 16 * 4 <= LDS, "");
 };
+
+// 16 bytes from each lane's address to lane * 16 bytes from `lds` on, without
+// a register in between.  The wave waits for them by vmcnt; the compiler does
+// not know of them, and would wait for all of them before any read of LDS if
+// it did.
+__device__ __forceinline__ void load_to_lds(const unsigned char *from, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+}
 
 template <int TY, int D>
 __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsigned char *smem, int slot, int me, bool own)
@@ -1139,58 +1159,77 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             const bool holes = uniform(bad) != 0;
             auto there = [&](int tok) { return sh.phys[a.pd.div(tok) - ch0] >= 0; };
 
-            u32x4_t kr[S::PT], vr[S::PT];
-            uint32_t keep = 0;  // bit q: some row sees this thread's piece q
             // The keys of a wave's pieces (KPW of them at a time) lie in one
             // page where pages and the first token are multiples of KPW: then
             // a page is looked up once a wave, and a lane adds its own constant
             const bool together = a.pd.page % S::KPW == 0 && base % S::KPW == 0;
             const unsigned char *Kb = static_cast<const unsigned char *>(a.K), *Vb = static_cast<const unsigned char *>(a.V);
-            auto load = [&](int p) __attribute__((always_inline)) {
-                keep = 0;
-                if (together) {
+            // each(q, first byte of the piece's row, its row in the tile, its
+            // chunk, whether some row sees it) for this thread's pieces
+            auto pieces = [&](int p, auto each) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int q = 0; q < S::PT; ++q) {
+                for (int q = 0; q < S::PT; ++q) {
+                    const int x = tid + q * S::T, key = x / S::PPR, c = x % S::PPR;
+                    int64_t row;
+                    bool seen;
+                    if (together) {
                         const int key0 = (w * 64 + q * S::T) / S::PPR;  // (the wave's first)
                         const int tok = base + min(p + key0, pb - 1), ch = a.pd.div(tok), phys = uniform(sh.phys[ch - ch0]);
                         const int place = tok - ch * a.pd.page & ~(S::KPW - 1);
-                        keep |= (uint32_t)(p + key0 + lane / S::PPR < pb && phys >= 0) << q;
-                        const int64_t off = pool_row(max(phys, 0), a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE;
-                        kr[q] = *reinterpret_cast<const u32x4_t *>(Kb + off + 16 * lane);
-                        vr[q] = *reinterpret_cast<const u32x4_t *>(Vb + off + 16 * lane);
+                        row = pool_row(max(phys, 0), a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE + lane / S::PPR * (D * S::SIZE);
+                        seen = p + key < pb && phys >= 0;
+                    } else {
+                        const int tok = base + min(p + key, pb - 1), ch = a.pd.div(tok);
+                        int phys = sh.phys[ch - ch0], place = tok - ch * a.pd.page;
+                        seen = p + key < pb && phys >= 0;
+                        if (phys < 0) phys = place = 0;  // (row 0 of the pool is there)
+                        row = pool_row(phys, a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE;
                     }
+                    each(q, row, key, c, seen);
+                }
+            };
+            u32x4_t kr[S::DIRECT ? 1 : S::PT], vr[S::DIRECT ? 1 : S::PT];
+            uint32_t keep = 0;  // bit q: some row sees this thread's piece q
+            const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
+            auto load = [&](int p, int buf) __attribute__((always_inline)) {
+                keep = 0;
+                pieces(p, [&](int q, int64_t row, int key, int c, bool seen) __attribute__((always_inline)) {
+                    if constexpr (S::DIRECT) {
+                        const uint32_t at = lds0 + buf * S::BUF + (w * 64 + q * S::T) * 16;
+                        load_to_lds(Kb + row + 16 * (c ^ S::key_swap(key)), at);
+                        load_to_lds(Vb + row + 16 * (c ^ S::value_swap(key)), at + S::KB * S::KRS);
+                    } else {
+                        keep |= (uint32_t)seen << q;
+                        kr[q] = *reinterpret_cast<const u32x4_t *>(Kb + row + 16 * c);
+                        vr[q] = *reinterpret_cast<const u32x4_t *>(Vb + row + 16 * c);
+                    }
+                });
+            };
+            auto store = [&](int buf) __attribute__((always_inline)) {
+                if constexpr (S::DIRECT) {
+                    wait_vm();
                 } else {
 #pragma unroll
                     for (int q = 0; q < S::PT; ++q) {
                         const int x = tid + q * S::T, key = x / S::PPR, c = x % S::PPR;
-                        const int tok = base + min(p + key, pb - 1);
-                        const int ch = a.pd.div(tok);
-                        int phys = sh.phys[ch - ch0], place = tok - ch * a.pd.page;
-                        keep |= (uint32_t)(p + key < pb && phys >= 0) << q;
-                        if (phys < 0) phys = place = 0;  // (row 0 of the pool is there)
-                        const int64_t off = pool_row(phys, a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE + 16 * c;
-                        kr[q] = *reinterpret_cast<const u32x4_t *>(Kb + off);
-                        vr[q] = *reinterpret_cast<const u32x4_t *>(Vb + off);
-                    }
-                }
-            };
-            auto store = [&](unsigned char *buf) {
+                        unsigned char *kd = smem + buf * S::BUF + key * S::KRS, *vd = smem + buf * S::BUF + S::KB * S::KRS + key * S::VRS;
+                        // (a value that no row sees is 0: memory that was never written may hold NaN)
 #pragma unroll
-                for (int q = 0; q < S::PT; ++q) {
-                    const int x = tid + q * S::T, key = x / S::PPR, c = x % S::PPR;
-                    unsigned char *kd = buf + key * S::KRS, *vd = buf + S::KB * S::KRS + key * S::VRS;
-                    // (a value that no row sees is 0: memory that was never written may hold NaN)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) vr[q][e] = (keep >> q) & 1u ? vr[q][e] : 0u;
-                    if constexpr (TY == CACHE_BF16) {
-                        *reinterpret_cast<u32x4_t *>(kd + 16 * c) = kr[q];
-                        *reinterpret_cast<u32x4_t *>(vd + 16 * c) = vr[q];
-                    } else {
+                        for (int e = 0; e < 4; ++e) vr[q][e] = (keep >> q) & 1u ? vr[q][e] : 0u;
                         *reinterpret_cast<bf16x8_t *>(kd + 32 * c) = e4m3_to_bf16(kr[q][0], kr[q][1]);
                         *reinterpret_cast<bf16x8_t *>(kd + 32 * c + 16) = e4m3_to_bf16(kr[q][2], kr[q][3]);
                         *reinterpret_cast<bf16x8_t *>(vd + 32 * c) = e4m3_to_bf16(vr[q][0], vr[q][1]);
                         *reinterpret_cast<bf16x8_t *>(vd + 32 * c + 16) = e4m3_to_bf16(vr[q][2], vr[q][3]);
                     }
+                }
+            };
+            // ... the same where the rows are in LDS already
+            auto clear = [&](int p, int buf) {
+                const u32x4_t z = {0u, 0u, 0u, 0u};
+                for (int x = tid; x < S::KB * (D / 8); x += S::T) {
+                    const int key = x / (D / 8);
+                    if (p + key >= pb || (holes && !there(base + p + key)))
+                        *reinterpret_cast<u32x4_t *>(smem + buf * S::BUF + S::KB * S::KRS + key * S::VRS + 16 * (x % (D / 8))) = z;
                 }
             };
             // one 32-key block of a staged tile; MASKED: some row does not see
@@ -1201,14 +1240,17 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                 // (operands are read two products ahead, in this order: left alone
                 // the compiler reads each right before its product, which then
                 // waits the LDS latency every time)
-                const unsigned char *kp_ = kt + (32 * kb + l32) * S::KRS + hh * D;
+                const unsigned char *krow = kt + (32 * kb + l32) * S::KRS;
+                auto key = [&](int q) {
+                    return *reinterpret_cast<const bf16x8_t *>(krow + 16 * ((hh * (D / 16) + q) ^ S::key_swap(l32)));
+                };
                 f32x16_t s = {};
                 bf16x8_t kf[3];
 #pragma unroll
-                for (int q = 0; q < 2; ++q) kf[q] = *reinterpret_cast<const bf16x8_t *>(kp_ + 16 * q);
+                for (int q = 0; q < 2; ++q) kf[q] = key(q);
 #pragma unroll
                 for (int q = 0; q < D / 16; ++q) {
-                    if (q + 2 < D / 16) kf[(q + 2) % 3] = *reinterpret_cast<const bf16x8_t *>(kp_ + 16 * (q + 2));
+                    if (q + 2 < D / 16) kf[(q + 2) % 3] = key(q + 2);
                     __builtin_amdgcn_sched_barrier(0);
                     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[q % 3], fq.v[q], s, 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
@@ -1216,9 +1258,10 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                 // V^T operand i = NMB s2 + mb of the block: keys 16 s2 + 4 hh + 0..3
                 // and + 8..11, the order of the score accumulator
                 const int j = lane & 15;
-                const unsigned char *vp = vt + (32 * kb + 4 * hh + (j >> 2)) * S::VRS + 2 * (16 * (l32 >> 4) + 4 * (j & 3));
+                const unsigned char *vrow = vt + (32 * kb + 4 * hh + (j >> 2)) * S::VRS + 8 * (j & 1);
                 auto value = [&](int i) {
-                    const unsigned char *x = vp + 16 * (i / NMB) * S::VRS + 64 * (i % NMB);
+                    const int c = (4 * (i % NMB) + 2 * (l32 >> 4) + ((j & 3) >> 1)) ^ S::value_swap(j >> 2);
+                    const unsigned char *x = vrow + 16 * (i / NMB) * S::VRS + 16 * c;
                     return join8(lds_read_tr16(x), lds_read_tr16(x + 8 * S::VRS));
                 };
                 bf16x8_t vf[3];
@@ -1283,19 +1326,23 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             };
             // tiles that every row sees whole, then the others
             const int open = holes ? pa : max(pa, min(pb, lo - base + 1) - (min(pb, lo - base + 1) - pa) % S::KB);
-            load(pa);
-            store(smem);
+            load(pa, 0);
+            store(0);
             __syncthreads();
             int cur = 0, p = pa;
             auto tiles = [&](auto masked, int end) __attribute__((always_inline)) {
                 for (; p < end; p += S::KB, cur ^= 1) {
                     const bool more = p + S::KB < pb;
-                    if (more) load(p + S::KB);
+                    if (more) load(p + S::KB, cur ^ 1);
+                    if (S::DIRECT && decltype(masked)::value && (holes || p + S::KB > pb)) {  // (uniform)
+                        clear(p, cur);
+                        __syncthreads();
+                    }
                     if (on) {
                         const unsigned char *kt = smem + cur * S::BUF;
                         for (int kb = kp; kb < S::NB && p + 32 * kb < pb; kb += wk) block(masked, kt, p, kb);
                     }
-                    if (more) store(smem + (cur ^ 1) * S::BUF);
+                    if (more) store(cur ^ 1);
                     __syncthreads();
                 }
             };
