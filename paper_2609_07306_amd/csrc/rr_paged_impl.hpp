@@ -1048,7 +1048,7 @@ struct WideShape {
 // it did.
 __device__ __forceinline__ void load_to_lds(const unsigned char *from, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
 }
 
 template <int TY, int D>
@@ -1164,56 +1164,46 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             // a page is looked up once a wave, and a lane adds its own constant
             const bool together = a.pd.page % S::KPW == 0 && base % S::KPW == 0;
             const unsigned char *Kb = static_cast<const unsigned char *>(a.K), *Vb = static_cast<const unsigned char *>(a.V);
-            // where the rows of this thread's piece q of the tile at p begin,
-            // and (seen) whether some row of the item sees that key.  looked:
-            // look()'s answer for the tile, of the pieces q in lanes q
-            struct Place {
-                int phys, place;
-            };
-            auto look = [&](int p) __attribute__((always_inline)) {
-                const int key0 = (w * 64 + (lane & (S::PT - 1)) * S::T) / S::PPR;  // (the wave's first of piece q)
-                const int tok = base + min(p + key0, pb - 1), ch = a.pd.div(tok);
-                return Place{sh.phys[ch - ch0], (tok - ch * a.pd.page) & ~(S::KPW - 1)};
-            };
-            auto row_at = [&](int p, int q, const Place &looked, bool &seen) __attribute__((always_inline)) -> int64_t {
-                const int key = (tid + q * S::T) / S::PPR;
-                if (together) {
-                    const int phys = __builtin_amdgcn_readlane(looked.phys, q), place = __builtin_amdgcn_readlane(looked.place, q);
-                    seen = p + key < pb && phys >= 0;
-                    return pool_row(max(phys, 0), a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE + lane / S::PPR * (D * S::SIZE);
+            // each(q, first byte of the piece's row, its row in the tile, its
+            // chunk, whether some row sees it) for this thread's pieces
+            auto pieces = [&](int p, auto each) __attribute__((always_inline)) {
+#pragma unroll
+                for (int q = 0; q < S::PT; ++q) {
+                    const int x = tid + q * S::T, key = x / S::PPR, c = x % S::PPR;
+                    int64_t row;
+                    bool seen;
+                    if (together) {
+                        const int key0 = (w * 64 + q * S::T) / S::PPR;  // (the wave's first)
+                        const int tok = base + min(p + key0, pb - 1), ch = a.pd.div(tok), phys = uniform(sh.phys[ch - ch0]);
+                        const int place = tok - ch * a.pd.page & ~(S::KPW - 1);
+                        row = pool_row(max(phys, 0), a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE + lane / S::PPR * (D * S::SIZE);
+                        seen = p + key < pb && phys >= 0;
+                    } else {
+                        const int tok = base + min(p + key, pb - 1), ch = a.pd.div(tok);
+                        int phys = sh.phys[ch - ch0], place = tok - ch * a.pd.page;
+                        seen = p + key < pb && phys >= 0;
+                        if (phys < 0) phys = place = 0;  // (row 0 of the pool is there)
+                        row = pool_row(phys, a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE;
+                    }
+                    each(q, row, key, c, seen);
                 }
-                const int tok = base + min(p + key, pb - 1), ch = a.pd.div(tok);
-                int phys = sh.phys[ch - ch0], place = tok - ch * a.pd.page;
-                seen = p + key < pb && phys >= 0;
-                if (phys < 0) phys = place = 0;  // (row 0 of the pool is there)
-                return pool_row(phys, a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE;
             };
             u32x4_t kr[S::DIRECT ? 1 : S::PT], vr[S::DIRECT ? 1 : S::PT];
             uint32_t keep = 0;  // bit q: some row sees this thread's piece q
             const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
-            auto load_piece = [&](int p, int buf, int q, const Place &looked) __attribute__((always_inline)) {
-                const int x = tid + q * S::T, key = x / S::PPR, c = x % S::PPR;
-                bool seen;
-                const int64_t row = row_at(p, q, looked, seen);
-                const uint32_t at = lds0 + buf * S::BUF + (w * 64 + q * S::T) * 16;
-                load_to_lds(Kb + row + 16 * (c ^ S::key_swap(key)), at);
-                load_to_lds(Vb + row + 16 * (c ^ S::value_swap(key)), at + S::KB * S::KRS);
-            };
             auto load = [&](int p, int buf) __attribute__((always_inline)) {
-                const Place looked = look(p);
                 keep = 0;
-#pragma unroll
-                for (int q = 0; q < S::PT; ++q) {
+                pieces(p, [&](int q, int64_t row, int key, int c, bool seen) __attribute__((always_inline)) {
                     if constexpr (S::DIRECT) {
-                        load_piece(p, buf, q, looked);
+                        const uint32_t at = lds0 + buf * S::BUF + (w * 64 + q * S::T) * 16;
+                        load_to_lds(Kb + row + 16 * (c ^ S::key_swap(key)), at);
+                        load_to_lds(Vb + row + 16 * (c ^ S::value_swap(key)), at + S::KB * S::KRS);
                     } else {
-                        bool seen;
-                        const int64_t at = row_at(p, q, looked, seen) + 16 * ((tid + q * S::T) % S::PPR);
                         keep |= (uint32_t)seen << q;
-                        kr[q] = *reinterpret_cast<const u32x4_t *>(Kb + at);
-                        vr[q] = *reinterpret_cast<const u32x4_t *>(Vb + at);
+                        kr[q] = *reinterpret_cast<const u32x4_t *>(Kb + row + 16 * c);
+                        vr[q] = *reinterpret_cast<const u32x4_t *>(Vb + row + 16 * c);
                     }
-                }
+                });
             };
             auto store = [&](int buf) __attribute__((always_inline)) {
                 if constexpr (S::DIRECT) {
@@ -1244,7 +1234,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             };
             // one 32-key block of a staged tile; MASKED: some row does not see
             // some key of it
-            auto block = [&](auto masked, const unsigned char *kt, int p, int kb, auto feed) __attribute__((always_inline)) {
+            auto block = [&](auto masked, const unsigned char *kt, int p, int kb) __attribute__((always_inline)) {
                 constexpr bool MASKED = decltype(masked)::value;
                 const unsigned char *vt = kt + S::KB * S::KRS;
                 // (operands are read two products ahead, in this order: left alone
@@ -1265,7 +1255,6 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[q % 3], fq.v[q], s, 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                feed();
                 // V^T operand i = NMB s2 + mb of the block: keys 16 s2 + 4 hh + 0..3
                 // and + 8..11, the order of the score accumulator
                 const int j = lane & 15;
@@ -1315,7 +1304,6 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                     pw[r >> 3][r & 7] = (__bf16)x;
                 }
                 l_run += l;
-                feed();
 #pragma unroll
                 for (int i = 0; i < 2 * NMB; ++i) {
                     if (i + 2 < 2 * NMB) vf[(i + 2) % 3] = value(i + 2);
@@ -1345,32 +1333,15 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             auto tiles = [&](auto masked, int end) __attribute__((always_inline)) {
                 for (; p < end; p += S::KB, cur ^= 1) {
                     const bool more = p + S::KB < pb;
-                    // The next tile's pieces are asked for a few at a time,
-                    // between this one's products: all at once they keep the
-                    // wave waiting for the address units (710 of 2187 cycles
-                    // a block)
-                    Place looked = {0, 0};
-                    int q = more ? 0 : S::PT;
-                    const int at_once = max(S::PT * wk / (2 * S::NB), 1);
-                    if constexpr (S::DIRECT) {
-                        if (more) looked = look(p + S::KB);
-                    } else {
-                        if (more) load(p + S::KB, cur ^ 1);
-                    }
-                    auto feed = [&]() __attribute__((always_inline)) {
-                        if constexpr (S::DIRECT) {
-                            for (int n = 0; n < at_once && q < S::PT; ++n, ++q) load_piece(p + S::KB, cur ^ 1, q, looked);
-                        }
-                    };
+                    if (more) load(p + S::KB, cur ^ 1);
                     if (S::DIRECT && decltype(masked)::value && (holes || p + S::KB > pb)) {  // (uniform)
                         clear(p, cur);
                         __syncthreads();
                     }
                     if (on) {
                         const unsigned char *kt = smem + cur * S::BUF;
-                        for (int kb = kp; kb < S::NB && p + 32 * kb < pb; kb += wk) block(masked, kt, p, kb, feed);
+                        for (int kb = kp; kb < S::NB && p + 32 * kb < pb; kb += wk) block(masked, kt, p, kb);
                     }
-                    while (S::DIRECT && q < S::PT) feed();
                     if (more) store(cur ^ 1);
                     __syncthreads();
                 }
