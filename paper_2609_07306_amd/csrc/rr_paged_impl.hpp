@@ -1045,10 +1045,11 @@ struct WideShape {
 // 16 bytes from each lane's address to lane * 16 bytes from `lds` on, without
 // a register in between.  The wave waits for them by vmcnt; the compiler does
 // not know of them, and would wait for all of them before any read of LDS if
-// it did.
+// it did.  (M0 is set where it is used, and nothing else in these kernels
+// reads it.)
 __device__ __forceinline__ void load_to_lds(const unsigned char *from, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
 }
 
 template <int TY, int D>
