@@ -1451,9 +1451,9 @@ __global__ __launch_bounds__((64 * Launch<TY, D, WIDE, NR>::NW), (D <= 128 && NR
         if ((a.grid & 7) == 0) slot = (blockIdx.x & 7) * (a.grid >> 3) + (blockIdx.x >> 3);
         me = slot - a.prefix_slots % a.grid;
         me += me < 0 ? a.grid : 0;
-        wide_body<TY, D>(a, sh, smem, slot, me, a.own_wide);
     }
-    if constexpr (NR > 0) narrow_body<TY, D, NR, NW>(a, sh, smem, me, !a.prefix_wide && a.prefix_items > 0, !a.own_wide);
+    if constexpr (WIDE) wide_body<TY, D>(a, sh, smem, slot, me, NR == 0);
+    if constexpr (NR > 0) narrow_body<TY, D, NR, NW>(a, sh, smem, me, !WIDE && a.prefix_items > 0, true);
 }
 
 template <int TY, int D, bool WIDE, int NR>
