@@ -9,10 +9,10 @@
 // to a fraction of a turn in binary64, and its sine and cosine are taken once
 // a token and shared by all of its heads through LDS.
 //
-// A workgroup takes TOK tokens.  A thread keeps the same features of a row
-// over the heads that it goes through, so it reads its sines and cosines once
-// a token; a vector piece is 16 bytes of input (one element where rows are
-// not aligned to that).
+// A workgroup takes a token.  A thread keeps the same features of a row over
+// the heads that it goes through, so it reads its sines and cosines once; a
+// vector piece is 16 bytes of input (one element where rows are not aligned to
+// that).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -97,49 +97,32 @@ __device__ __forceinline__ void write_cache(void *pool, int64_t at, const float 
         write_piece<T, N, VEC>(static_cast<T *>(pool) + at, x);
 }
 
-template <typename T, bool E4, bool INTER, int N, bool VEC, int TOK>
+template <typename T, bool E4, bool INTER, int N, bool VEC>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
 {
-    __shared__ float s_cos[TOK * kMostRot / 2], s_sin[TOK * kMostRot / 2];
-    __shared__ int32_t s_pos[TOK], s_phys[TOK], s_place[TOK];
-    const int tid = threadIdx.x, i0 = blockIdx.x * TOK, half = a.rot >> 1;
+    __shared__ float s_cos[kMostRot / 2], s_sin[kMostRot / 2];
+    const int tid = threadIdx.x, half = a.rot >> 1;
 
-    // where the tokens go
-    if (tid < TOK) {
-        const int i = i0 + tid;
-        int pos = -1, phys = -1, place = 0;
-        if (i < a.n_tokens) {
-            int b, left;  // tokens of the sequence's new ones from this one on
-            if (a.seq_start) {
-                b = sequence_of(a.seq_start, a.n_seqs, i);
-                left = b < 0 ? 0 : a.seq_start[b + 1] - i;
-            } else {
-                b = i / a.per_seq;
-                left = (b + 1) * a.per_seq - i;
-            }
-            if (b >= 0) {
-                const int64_t p = (int64_t)a.lengths[b] - left;
-                if (p >= 0 && p < (int64_t)a.max_pages * a.pd.page) {
-                    pos = (int)p;
-                    const int c = a.pd.div(pos);
-                    place = pos - c * a.pd.page;
-                    phys = pool_page(a.table[(int64_t)b * a.max_pages + c], a.n_pages);
-                }
-            }
-        }
-        s_pos[tid] = pos;
-        s_phys[tid] = phys;
-        s_place[tid] = place;
+    // where the token goes: sequence, position, page
+    const int64_t i = blockIdx.x;
+    int b, left;  // tokens of the sequence's new ones from this one on
+    if (a.seq_start) {
+        b = sequence_of(a.seq_start, a.n_seqs, (int)i);
+        left = b < 0 ? 0 : a.seq_start[b + 1] - (int)i;
+    } else {
+        b = (int)i / a.per_seq;
+        left = a.per_seq - ((int)i - b * a.per_seq);
     }
-    __syncthreads();
+    if (b < 0) return;
+    const int64_t p = (int64_t)a.lengths[b] - left;
+    if (p < 0 || p >= (int64_t)a.max_pages * a.pd.page) return;
+    const int pos = (int)p, c = a.pd.div(pos), place = pos - c * a.pd.page;
+    const int phys = pool_page(a.table[(int64_t)b * a.max_pages + c], a.n_pages);
+
     // angles in turns: position * frequency / 2 pi, less its nearest integer
-    for (int x = tid; x < TOK * half; x += kAppendThreads) {
-        const int t = x / half, j = x - t * half;
-        const double turn = (double)s_pos[t] * a.freqs[j] * 0.15915494309189533577;
-        float s, c;
-        sincospif(2.f * (float)(turn - rint(turn)), &s, &c);
-        s_cos[x] = c;
-        s_sin[x] = s;
+    for (int x = tid; x < half; x += kAppendThreads) {
+        const double turn = (double)pos * a.freqs[x] * 0.15915494309189533577;
+        sincospif(2.f * (float)(turn - rint(turn)), &s_sin[x], &s_cos[x]);
     }
     __syncthreads();
 
@@ -149,72 +132,66 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
     const int turned = INTER ? a.rot / N : half / N, units = INTER ? a.d / N : turned + (a.d - a.rot) / N;
     const int n_rows = a.n_kv_heads + (a.Q ? a.n_heads : 0);
     const int lanes = min(units, kAppendThreads), rows_at_once = kAppendThreads / lanes;
-    for (int t = 0; t < TOK; ++t) {
-        if (s_pos[t] < 0) continue;  // (uniform)
-        const int64_t i = i0 + t;
-        const int phys = s_phys[t], place = s_place[t];
-        const float *cs = s_cos + t * half, *sn = s_sin + t * half;
-        if (tid < lanes * rows_at_once) {
-            for (int u = tid % lanes; u < units; u += lanes) {
-                const bool turn = u < turned;
-                // first element of the piece, and of its partner
-                const int f0 = INTER ? u * N : turn ? u * N : a.rot + (u - turned) * N, f1 = f0 + half;
-                float c[N], s[N];
-                if (turn) {
+    if (tid < lanes * rows_at_once) {
+        for (int u = tid % lanes; u < units; u += lanes) {
+            const bool turn = u < turned;
+            // first element of the piece, and of its partner
+            const int f0 = INTER ? u * N : turn ? u * N : a.rot + (u - turned) * N, f1 = f0 + half;
+            float c[N], s[N];
+            if (turn) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        c[e] = cs[INTER ? (f0 + e) >> 1 : f0 + e];
-                        s[e] = sn[INTER ? (f0 + e) >> 1 : f0 + e];
-                    }
+                for (int e = 0; e < N; ++e) {
+                    c[e] = s_cos[INTER ? (f0 + e) >> 1 : f0 + e];
+                    s[e] = s_sin[INTER ? (f0 + e) >> 1 : f0 + e];
                 }
-                for (int r = tid / lanes; r < n_rows; r += rows_at_once) {
-                    const bool key = r < a.n_kv_heads;
-                    if (key && phys < 0) continue;
-                    const T *src = key ? static_cast<const T *>(a.K) + i * a.ldk + r * a.d
-                                       : static_cast<const T *>(a.Q) + i * a.ldq + (r - a.n_kv_heads) * a.d;
-                    float x[N], y[N];
-                    read_piece<T, N, VEC>(src + f0, x);
-                    if (turn) {
-                        if constexpr (INTER) {
+            }
+            for (int r = tid / lanes; r < n_rows; r += rows_at_once) {
+                const bool key = r < a.n_kv_heads;
+                if (key && phys < 0) continue;
+                const T *src = key ? static_cast<const T *>(a.K) + i * a.ldk + r * a.d
+                                   : static_cast<const T *>(a.Q) + i * a.ldq + (r - a.n_kv_heads) * a.d;
+                float x[N], y[N];
+                read_piece<T, N, VEC>(src + f0, x);
+                if (turn) {
+                    if constexpr (INTER) {
 #pragma unroll
-                            for (int e = 0; e < N; e += 2) {
-                                const float p = x[e], q = x[e + 1];
-                                x[e] = p * c[e] - q * s[e];
-                                x[e + 1] = q * c[e] + p * s[e];
-                            }
-                        } else {
-                            read_piece<T, N, VEC>(src + f1, y);
+                        for (int e = 0; e < N; e += 2) {
+                            const float p = x[e], q = x[e + 1];
+                            x[e] = p * c[e] - q * s[e];
+                            x[e + 1] = q * c[e] + p * s[e];
+                        }
+                    } else {
+                        read_piece<T, N, VEC>(src + f1, y);
 #pragma unroll
-                            for (int e = 0; e < N; ++e) {
-                                const float p = x[e], q = y[e];
-                                x[e] = p * c[e] - q * s[e];
-                                y[e] = q * c[e] + p * s[e];
-                            }
+                        for (int e = 0; e < N; ++e) {
+                            const float p = x[e], q = y[e];
+                            x[e] = p * c[e] - q * s[e];
+                            y[e] = q * c[e] + p * s[e];
                         }
                     }
-                    if (key) {
-                        const int64_t at = pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d);
-                        const float scale = E4 ? a.k_scale[r] : 1.f;
-                        write_cache<T, E4, N, VEC>(a.Kc, at + f0, x, scale);
-                        if (!INTER && turn) write_cache<T, E4, N, VEC>(a.Kc, at + f1, y, scale);
-                    } else {
-                        T *dst = static_cast<T *>(a.Q_out) + (i * a.n_heads + (r - a.n_kv_heads)) * a.d;
-                        write_piece<T, N, VEC>(dst + f0, x);
-                        if (!INTER && turn) write_piece<T, N, VEC>(dst + f1, y);
-                    }
+                }
+                if (key) {
+                    const int64_t at = pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d);
+                    const float scale = E4 ? a.k_scale[r] : 1.f;
+                    write_cache<T, E4, N, VEC>(a.Kc, at + f0, x, scale);
+                    if (!INTER && turn) write_cache<T, E4, N, VEC>(a.Kc, at + f1, y, scale);
+                } else {
+                    T *dst = static_cast<T *>(a.Q_out) + (i * a.n_heads + (r - a.n_kv_heads)) * a.d;
+                    write_piece<T, N, VEC>(dst + f0, x);
+                    if (!INTER && turn) write_piece<T, N, VEC>(dst + f1, y);
                 }
             }
         }
-        // values
-        if (phys >= 0) {
-            const int pieces = a.d / N;
-            for (int x = tid; x < a.n_kv_heads * pieces; x += kAppendThreads) {
-                const int r = x / pieces, f = (x - r * pieces) * N;
-                float v[N];
-                read_piece<T, N, VEC>(static_cast<const T *>(a.V) + i * a.ldv + r * a.d + f, v);
-                write_cache<T, E4, N, VEC>(a.Vc, pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d) + f, v,
-                                      E4 ? a.v_scale[r] : 1.f);
-            }
+    }
+    // values
+    if (phys >= 0) {
+        const int pieces = a.d / N;
+        for (int x = tid; x < a.n_kv_heads * pieces; x += kAppendThreads) {
+            const int r = x / pieces, f = (x - r * pieces) * N;
+            float v[N];
+            read_piece<T, N, VEC>(static_cast<const T *>(a.V) + i * a.ldv + r * a.d + f, v);
+            write_cache<T, E4, N, VEC>(a.Vc, pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d) + f, v,
+                                  E4 ? a.v_scale[r] : 1.f);
         }
     }
 }
@@ -228,17 +205,15 @@ hipError_t launch_append(const AppendArgs &a, int dtype, int cache, bool interle
     // (cache rows of 8 values are 8 bytes in e4m3)
     const bool vec = aligned(a.K, a.ldk) && aligned(a.V, a.ldv) && aligned(a.Q, a.Q ? a.ldq : 0) && aligned(a.Q_out, 0) &&
                      aligned(a.Kc, 0) && aligned(a.Vc, 0) && a.rot % (interleaved ? n : 2 * n) == 0;
-    auto go = [&](auto kern, int tok) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)((a.n_tokens + (int64_t)tok - 1) / tok)), dim3(kAppendThreads), 0, stream, a);
-    };
+    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)a.n_tokens), dim3(kAppendThreads), 0, stream, a); };
     auto any = [&](auto type, auto e4, auto width) {
         typedef decltype(type) T;
         constexpr bool E4 = decltype(e4)::value;
         constexpr int W = decltype(width)::value;
         if (vec)
-            interleaved ? go(append_kernel<T, E4, true, W, true, 1>, 1) : go(append_kernel<T, E4, false, W, true, 1>, 1);
+            interleaved ? go(append_kernel<T, E4, true, W, true>) : go(append_kernel<T, E4, false, W, true>);
         else  // (interleaved partners go together)
-            interleaved ? go(append_kernel<T, E4, true, 2, false, 1>, 1) : go(append_kernel<T, E4, false, 1, false, 1>, 1);
+            interleaved ? go(append_kernel<T, E4, true, 2, false>) : go(append_kernel<T, E4, false, 1, false>);
     };
     if (dtype == 0)
         any(float(), std::false_type(), std::integral_constant<int, 4>());
