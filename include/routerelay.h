@@ -376,13 +376,12 @@ typedef struct {
     int32_t n_pages;      /* pages of each pool */
     int32_t max_pages;    /* page_table entries of a sequence */
     int32_t n_seqs;
-    int32_t n_tokens;     /* new tokens, all sequences' (0: nothing to do) */
+    int32_t n_tokens;     /* new tokens, all sequences' (0: nothing to do), below 2^24 */
     int32_t rot;          /* leading features of a head that are rotated: even, 0 .. d */
     int32_t interleaved;  /* partners: 1: features 2j and 2j + 1; 0: j and j + rot / 2 */
     int32_t dtype;        /* of K, V, Q and Q_out */
     int32_t cache_dtype;
-    int64_t ldq, ldk, ldv;       /* elements from one token's rows to the next one's: >= heads * d, or 0 (one token's
-                                    rows for all) */
+    int64_t ldq, ldk, ldv;  /* elements from one token's rows to the next one's, >= 0 (0: one token's rows for all) */
     const float *k_scale, *v_scale;
 } rr_append_config;
 
@@ -399,7 +398,8 @@ typedef struct {
  * x sin a), a = p * freqs[j], freqs [rot / 2] binary64 radians; angles are
  * reduced in binary64, the rotation is computed in binary32 and rounded
  * once.  Two new tokens must not lie in the same place.
- * Returns RR_ERR_INVALID for bad sizes, types or NULL pointers. */
+ * Returns RR_ERR_INVALID for bad sizes, types or NULL pointers,
+ * RR_ERR_UNSUPPORTED for 2^24 tokens or more. */
 rr_status rr_cache_append(const rr_append_config *cfg, const void *K, const void *V, const void *Q,
                           const int32_t *seq_start, const int32_t *lengths, const int32_t *page_table,
                           const double *freqs, void *K_cache, void *V_cache, void *Q_out, void *hip_stream);
@@ -451,9 +451,12 @@ size_t rr_paged_workspace_bytes(const rr_paged_config *cfg);
  * most 16 query rows are multiplied with a key head's tokens together (n_q *
  * n_heads / n_kv_heads of a sequence, n_seqs times that of a shared prefix),
  * rounded to bf16 (2^-8 off) where more are.  Tokens that a
- * query does not see have no part in its output, whatever their rows hold.
+ * query does not see have no part in its output, whatever their rows hold;
+ * where it sees a value that is not finite, that feature of its output is
+ * infinite or NaN.
  * Returns RR_ERR_INVALID for bad sizes, NULL or unaligned pointers or a
- * workspace too small, RR_ERR_UNSUPPORTED for other types or d. */
+ * workspace too small, RR_ERR_UNSUPPORTED for other types or d, or for 2^31
+ * query rows (n_seqs * n_q * n_heads; 2^24 with a prefix) or more. */
 rr_status rr_paged_attention(const rr_paged_config *cfg, const void *Q, const void *K_cache, const void *V_cache,
                              const int32_t *page_table, const int32_t *lengths, const int32_t *routes, void *O,
                              float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);

@@ -952,6 +952,8 @@ namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+constexpr int32_t kMostGroups = (1 << 24) - 1;  // workgroups of 256 threads that a launch can have
+
 // What the append and the attention ask of a cache alike.
 rr_status check_cache(int32_t n_kv_heads, int32_t page, int32_t n_pages, int32_t max_pages, int32_t n_seqs, int32_t dtype,
                       int32_t cache_dtype, const float *k_scale, const float *v_scale)
@@ -985,7 +987,9 @@ rr_status paged_args(const rr_paged_config *cfg, rr::PagedArgs *out)
     if (!(c.scale >= 0.f) || std::isinf(c.scale)) return fail(RR_ERR_INVALID, "scale must be finite and >= 0");
     if (!rr::paged_supported(c.dtype, c.cache_dtype, c.d))
         return fail(RR_ERR_UNSUPPORTED, "attention over a paged cache supports d = 64 and 128, and 256 for bf16 queries");
-    if ((int64_t)c.n_seqs * c.n_q > INT32_MAX / c.n_heads) return fail(RR_ERR_UNSUPPORTED, "too many query rows");
+    // (with a prefix a row is a workgroup of 256 threads, and a launch has less than 2^32)
+    if ((int64_t)c.n_seqs * c.n_q > (c.n_prefix ? kMostGroups : INT32_MAX) / c.n_heads)
+        return fail(RR_ERR_UNSUPPORTED, "n_seqs * n_q * n_heads is too large: 2^31 - 1 query rows, 2^24 - 1 with a prefix, at most");
     rr::PagedArgs a;
     std::memset(&a, 0, sizeof(a));
     a.k_scale = c.k_scale;
@@ -1056,6 +1060,7 @@ rr_status rr_cache_append(const rr_append_config *cfg, const void *K, const void
     if (c.rot < 0 || c.rot > c.d || c.rot % 2 != 0) return fail(RR_ERR_INVALID, "rot must be even and lie in [0, d]");
     if (c.interleaved != 0 && c.interleaved != 1) return fail(RR_ERR_INVALID, "interleaved must be 0 or 1");
     if (c.n_tokens < 0) return fail(RR_ERR_INVALID, "n_tokens must be >= 0");
+    if (c.n_tokens > kMostGroups) return fail(RR_ERR_UNSUPPORTED, "n_tokens must be below 2^24");
     if (c.ldk < 0 || c.ldv < 0 || (Q && c.ldq < 0)) return fail(RR_ERR_INVALID, "ldq, ldk and ldv must be >= 0");
     if (!lengths || !page_table || !K_cache || !V_cache)
         return fail(RR_ERR_INVALID, "lengths, page_table and the caches must be device pointers");

@@ -34,7 +34,6 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
 
     const int r = t * a.group + j, own_row = r % a.own_tile;  // row within its item's tile
     const int4 own = a.heads[a.prefix_items + (int64_t)b * a.items_per_seq + g * a.row_tiles + r / a.own_tile];
-    const int parts_tile = a.own_wide ? a.own_tile : a.narrow_tile;
     int4 pre = {0, 0, 0, 0};
     const float *pre_part = nullptr;  // of a wide prefix: its splits lie a.prefix_tiles slots apart
     const int q = b * a.rows + t * a.group + j, x_tile = q / a.prefix_tile, pre_row = q - x_tile * a.prefix_tile;
@@ -54,7 +53,7 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
         if (p && pre_part) return pre_part + (int64_t)i * a.prefix_tiles * a.prefix_tile * (D + 4);
         if (hd.z == 1) return a.whole + ((p ? 0 : n_rows) + orow) * (D + 4);
         const int64_t slot = i == 0 ? hd.x : 2 * (int64_t)(hd.y + i);
-        return a.parts + (slot * parts_tile + (p ? pre_row : own_row)) * (D + 4);
+        return a.parts + (slot * a.own_tile + (p ? pre_row : own_row)) * (D + 4);
     };
     // PL lanes a part, NP parts at once, kept with a running maximum like the
     // attention's own: sums and statistics are asked for together
@@ -113,8 +112,9 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     // more than 16 rows go to the wide body (binary32: to 32-row tiles)
     a.own_wide = !f32 && a.rows > 16;
     a.prefix_wide = !f32 && a.prefix_rows > 16;
-    if (a.own_wide && a.n_prefix) a.prefix_wide = true;
-    const auto tile = [&](bool wide, int rows) { return !wide ? (f32 && (a.rows > 16 || a.prefix_rows > 16) ? 32 : 16) : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; };
+    // (of a narrow prefix and the sequences behind it the tiles are alike)
+    const int narrow = f32 && (a.rows > 16 || a.prefix_rows > 16) ? 32 : 16;
+    const auto tile = [&](bool wide, int rows) { return !wide ? narrow : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; };
     a.own_tile = tile(a.own_wide, a.rows);
     a.prefix_tile = tile(a.prefix_wide, a.prefix_rows);
     a.row_tiles = (a.rows + a.own_tile - 1) / a.own_tile;
@@ -128,10 +128,8 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     a.prefix_tiles = (a.prefix_rows + a.prefix_tile - 1) / a.prefix_tile;
     a.prefix_items = a.n_kv_heads * a.prefix_tiles;
     a.prefix_units = (a.n_prefix + kPagedUnit - 1) / kPagedUnit;
-    a.narrow_tile = !a.own_wide ? a.own_tile : !a.prefix_wide && a.n_prefix ? a.prefix_tile : 0;
     const int64_t keys = (int64_t)(paged::kStagedPages - 1) * a.pd.page / kPagedUnit * kPagedUnit;
     a.batch_keys = (int32_t)(keys < (1 << 30) ? keys : (1 << 30));
-    // units of the longest sequences that the page table can hold
     // an item's rows, page numbers and result take about as long as 128 keys: it
     // counts where workgroups take several items, whose lengths may differ (160
     // sequences of 64 to 2048 tokens: 110 us without, 92 with)
@@ -146,7 +144,7 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     a.prefix_splits = a.prefix_slots = 0;
     if (a.prefix_wide) {
         const auto used = [&](int splits) {
-            const int n = a.prefix_items * splits, rounds = (n + kPagedGrid - 1) / kPagedGrid;
+            const int64_t n = (int64_t)a.prefix_items * splits, rounds = (n + kPagedGrid - 1) / kPagedGrid;
             return (double)n / ((double)rounds * kPagedGrid);
         };
         const int most_splits = a.prefix_units < kPagedGrid ? a.prefix_units : kPagedGrid;
@@ -165,7 +163,7 @@ static int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
 
 static int64_t parts_bytes(const PagedArgs &a, int d)
 {
-    return align256((int64_t)2 * a.grid * (a.own_wide ? a.own_tile : a.narrow_tile) * (d + 4) * 4);
+    return align256((int64_t)2 * a.grid * a.own_tile * (d + 4) * 4);
 }
 
 static int64_t prefix_bytes(const PagedArgs &a, int d) { return align256((int64_t)a.prefix_slots * a.prefix_tile * (d + 4) * 4); }

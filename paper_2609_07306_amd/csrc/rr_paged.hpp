@@ -108,14 +108,14 @@ struct PagedArgs {
     int32_t prefix_rows, prefix_tile, prefix_tiles, prefix_items, prefix_units;  // of the batch against the prefix
     bool own_wide, prefix_wide;        // which body takes them
     int32_t prefix_splits, prefix_slots;  // of the wide body: key splits, (key head, split, row tile) slots
-    int32_t narrow_tile;               // rows of a narrow item at most
-    int32_t grid, batch_keys;
+    int32_t grid;
+    int32_t batch_keys;  // keys whose page numbers a workgroup holds at a time
     // workspace
     uint32_t *counters;  // [kPagedGrid] finished parts of the item that begins in a workgroup, 0 between calls
     float *parts;        // [2 * grid] parts of items that several workgroups share
     float *prefix_parts; // [prefix_slots] parts
     float *whole;        // with a prefix: [2][rows of the call] parts of items that one workgroup held
-    int4 *heads;         // with a prefix: per item its first part, its first workgroup, its parts
+    int4 *heads;         // with a prefix: per item its first part, its first workgroup, its parts, 0
 };
 
 size_t paged_workspace_bytes(const PagedArgs &a, int d);

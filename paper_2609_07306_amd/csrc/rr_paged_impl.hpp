@@ -930,7 +930,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
         }
 
         // ------------------------- the waves' sums joined, the result written
-        const Sink sink = sink_of(a, D, run, u0, u1, a.narrow_tile);
+        const Sink sink = sink_of(a, D, run, u0, u1, a.own_tile);
         const bool within = a.prefix_items == 0;  // the parts are joined within this launch
         const float vs = a.v_scale ? a.v_scale[g] : 1.f;
 #pragma unroll
@@ -999,7 +999,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                 }
             }
         }
-        if (within && (u0 != 0 || u1 != it.units)) join_cut<D, F32, NW>(a, sh, smem, run, rows, a.narrow_tile);
+        if (within && (u0 != 0 || u1 != it.units)) join_cut<D, F32, NW>(a, sh, smem, run, rows, a.own_tile);
         run.at = it.first + u1;
         if (run.at >= run.end) return;
         next_item(a, run.it);
@@ -1038,7 +1038,7 @@ struct WideShape {
     static constexpr int PT = PIECES / T;              // ... of a thread
     static_assert(PIECES % T == 0, "");
     static constexpr int KPW = 64 / PPR;               // keys that a wave's 64 pieces hold
-    // (half the waves' accumulators pass through the tiles' memory)
+    // (half the waves' sums pass through the tiles' memory)
     static_assert(NB == 1 || NW / 2 * 64 * (D / 32) * 16 * 4 <= LDS, "");
 };
 
@@ -1091,7 +1091,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
         }
         const int g = rows.g, cost = rows.prefix ? 0 : a.item_cost;
         // row blocks (a power of two), waves of a row block, this wave's of each
-        const int wr = rows.n <= 32 ? 1 : rows.n <= 64 ? 2 : rows.n <= 128 ? 4 : 8, wk = min(S::NB, S::NW / wr);
+        const int wr = rows.n <= 32 ? 1 : rows.n <= 64 ? 2 : 4, wk = min(S::NB, S::NW / wr);
         const int rb = w & (wr - 1), kp = w / wr;
         const bool on = kp < wk && 32 * rb < rows.n;
 
@@ -1295,7 +1295,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                         for (int r = 0; r < 16; ++r) acc[mb][r] *= alpha;
                     m_run = m_new;
                 }
-                const float m_use = MASKED && m_run == -INFINITY ? 0.f : m_run;
+                const float m_use = m_run == -INFINITY ? 0.f : m_run;
                 bf16x8_t pw[2];
                 float l = 0.f;
 #pragma unroll
@@ -1472,7 +1472,7 @@ template <int TY, int D>
 hipError_t launch_d(const PagedArgs &a, hipStream_t stream)
 {
     if constexpr (TY == CACHE_F32) {
-        return a.narrow_tile == 16 ? launch_one<TY, D, false, 1>(a, stream) : launch_one<TY, D, false, 2>(a, stream);
+        return a.own_tile == 16 ? launch_one<TY, D, false, 1>(a, stream) : launch_one<TY, D, false, 2>(a, stream);
     } else {
         if (a.own_wide) return launch_one<TY, D, true, 0>(a, stream);
         return a.prefix_wide ? launch_one<TY, D, true, 1>(a, stream) : launch_one<TY, D, false, 1>(a, stream);

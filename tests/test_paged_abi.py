@@ -161,6 +161,20 @@ def test_paged_attention_rejects_bad_pointers():
         assert b"workspace" in rr.lib.rr_last_error()
 
 
+def test_limits_of_a_launch():
+    """Tokens of an append and query rows behind a prefix take a workgroup each,
+    and a launch has less than 2^24."""
+    rr = _rr()
+    assert _append_call(rr, _append(rr, n_tokens=1 << 24)) == -5
+    assert rr.lib.rr_last_error()
+    rows = dict(n_heads=8, n_kv_heads=2, n_seqs=1 << 10)
+    for n_q, prefix, ok in ((1 << 11, 8, False), ((1 << 11) - 1, 8, True), (1 << 11, 0, True)):
+        c = _paged(rr, n_q=n_q, n_prefix=prefix, **rows)
+        assert (rr.lib.rr_paged_workspace_bytes(ctypes.byref(c)) > 0) is ok
+        if not ok:
+            assert _paged_call(rr, c, prefix=True) == -5
+
+
 def test_workspace_is_bounded():
     """A workspace holds parts of a fixed number of workgroups, whatever the
     lengths that the page table allows."""
