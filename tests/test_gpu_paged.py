@@ -730,3 +730,173 @@ def test_profiled_kinds():
     got = rr.profile_stop()
     assert got["append"][1] == 1 and got["paged"][1] == 1 and got["join"][1] <= 1
     assert got["append"][0] > 0 and got["paged"][0] > 0
+
+
+# ------------------------------------------------------- batches and long runs
+
+MANY = [
+    # name, H, Hkv, d, dtype, cache, page, sequences, n_q, longest, prefix
+    ("seventy", 8, 2, 128, "bf16", "bf16", 16, 70, 1, 300, 0),
+    ("many_items", 8, 2, 64, "bf16", "bf16", 32, 300, 1, 400, 0),
+    ("many_items_e4m3", 8, 2, 128, "bf16", "e4m3", 16, 300, 2, 200, 0),
+    ("many_items_f32", 8, 4, 64, "f32", "f32", 16, 260, 1, 200, 0),
+    ("many_rows", 16, 2, 128, "bf16", "bf16", 16, 300, 4, 200, 0),
+    ("many_rows_e4m3", 16, 2, 64, "bf16", "e4m3", 16, 70, 4, 300, 0),
+    ("prefix_seventy", 8, 2, 64, "bf16", "bf16", 16, 70, 1, 150, 200),
+    ("prefix_many_items", 8, 2, 128, "bf16", "bf16", 16, 300, 1, 150, 333),
+    ("prefix_many_rows", 16, 2, 128, "bf16", "bf16", 16, 70, 5, 150, 333),
+    ("prefix_many_rows_items", 16, 2, 64, "bf16", "e4m3", 16, 300, 5, 100, 130),
+    ("prefix_d256_rows", 8, 1, 256, "bf16", "bf16", 16, 70, 3, 100, 200),
+    ("prefix_f32", 8, 2, 64, "f32", "f32", 16, 70, 2, 150, 200),
+    ("prefix_rounds", 32, 8, 64, "bf16", "bf16", 16, 130, 16, 60, 200),
+    ("prefix_rounds_narrow", 32, 8, 64, "bf16", "bf16", 16, 520, 4, 40, 150),
+]
+
+
+@pytest.mark.parametrize("case", MANY, ids=[c[0] for c in MANY])
+def test_many_sequences(case):
+    """More sequences than a wave has lanes or a workgroup threads, more items
+    than workgroups, more splits of a prefix than workgroups: outputs of some
+    sequences against the oracle, of all of them against a call for each."""
+    rr = rrmod()
+    name, H, Hkv, d, dtype, cache, page, B, nq, longest, prefix = case
+    note(f"many sequences {case}")
+    rng = np.random.default_rng(B + d + nq)
+    lens = rng.integers(0, longest, size=B)
+    lens[rng.random(B) < 0.2] = 0
+    lens[-1], lens[B // 2] = longest, 1
+    kw = {}
+    if prefix:
+        c, pages = _prefix_cache(rng, Hkv, d, page, cache, prefix, lens.tolist())
+        kw = dict(prefix_pages=pages, n_prefix=prefix)
+    else:
+        c = Cache(rng, lens.tolist(), Hkv, d, page, cache)
+    Q = _values(rng, (B, nq, H, d), dtype, 2.0)
+    lse = torch.empty((B, nq, H), device=DEV)
+    Kc, Vc, table, lengths = c.args()
+
+    def call(sel, lse=None):
+        if prefix:
+            return rr.prefix_attention(Q[sel], Kc, Vc, table[sel], lengths[sel], _i32(pages), prefix, lse=lse, **c.kw())
+        return rr.paged_attention(Q[sel], Kc, Vc, table[sel], lengths[sel], lse=lse, **c.kw())
+
+    O = call(slice(0, B), lse=lse)
+    torch.cuda.synchronize()
+    some = sorted({0, 1, B // 2, B - 1, *rng.integers(0, B, size=4).tolist()})
+    whole = c.table, c.lens
+    c.table, c.lens = c.table[some], [c.lens[b] for b in some]
+    ref = c.oracle(Q[some], **kw)
+    c.table, c.lens = whole
+    rows = nq * H // Hkv * (B if prefix else 1)
+    _check(O[some], lse[some], ref, d, max(c.lens), dtype, rows)
+    # one call for each part of the batch: other runs and splits.  Both are off
+    # by (err + 2^-8) * W + 2^-8 |o| at most for bf16, W and |o| <= max |v| < 6;
+    # err (scores of at most 100, 350 tokens) stays below 2^-9
+    parts = torch.cat([call(slice(b, min(b + 61, B))) for b in range(0, B, 61)])
+    torch.cuda.synchronize()
+    loose = 2 * (2.0 ** -9 + (2.0 ** -7 if dtype == "bf16" else 0.0))
+    assert float((O.double() - parts.double()).abs().max()) <= loose * 6
+
+
+LONG = [
+    # name, H, Hkv, d, dtype, cache, lengths, n_q, prefix (pages of one token)
+    ("narrow", 4, 4, 64, "bf16", "bf16", [22000, 21000, 22001], 1, 0),
+    ("wide", 16, 4, 64, "bf16", "bf16", [22000, 21000, 22001], 5, 0),
+    ("wide_e4m3", 16, 4, 64, "bf16", "e4m3", [22000, 300, 42001], 5, 0),
+    ("prefix", 8, 4, 64, "bf16", "bf16", [7 * i for i in range(40)], 4, 40000),
+    ("prefix_f32", 4, 2, 64, "f32", "f32", [7, 0, 30], 2, 70000),
+]
+
+
+@pytest.mark.parametrize("case", LONG, ids=[c[0] for c in LONG])
+def test_more_pages_than_are_held_at_a_time(case):
+    """Pages of one token, and runs of more of them than a workgroup holds the
+    numbers of."""
+    rr = rrmod()
+    name, H, Hkv, d, dtype, cache, lens, nq, prefix = case
+    note(f"many pages {case}")
+    rng = np.random.default_rng(len(name))
+    B = len(lens)
+    Q = _values(rng, (B, nq, H, d), dtype, 2.0)
+    if prefix:
+        c, pages = _prefix_cache(rng, Hkv, d, 1, cache, prefix, lens)
+        O = rr.prefix_attention(Q, *c.args(), _i32(pages), prefix, **c.kw())
+    else:
+        c, pages = Cache(rng, lens, Hkv, d, 1, cache), None
+        O = rr.paged_attention(Q, *c.args(), **c.kw())
+    torch.cuda.synchronize()
+    some = [0, B - 1]
+    c.table, c.lens = c.table[some], [c.lens[b] for b in some]
+    ref = c.oracle(Q[some], prefix_pages=pages, n_prefix=prefix)
+    _check(O[some], None, ref, d, max(c.lens), dtype, nq * H // Hkv * (B if prefix else 1))
+
+
+@pytest.mark.parametrize("cache,nq", [("bf16", 6), ("e4m3", 1), ("e4m3", 6)])
+def test_offsets_past_32_bits_of_other_bodies(cache, nq):
+    """The last pages of pools of more than 2^31 elements, for more query rows
+    and for 8-bit caches."""
+    rr = rrmod()
+    note(f"large pools {cache} {nq}")
+    Hkv, d, page = 2, 128, 64
+    n_pages = (1 << 31) // (Hkv * page * d) + 30
+    rng = np.random.default_rng(2)
+    kw = {}
+    if cache == "e4m3":
+        Kc, Vc = (torch.zeros((n_pages, Hkv, page, d), dtype=torch.uint8, device=DEV).view(E4M3) for _ in range(2))
+        scales = [np.array([0.01, 0.02], np.float32), np.array([0.03, 0.01], np.float32)]
+        kw = dict(k_scale=torch.from_numpy(scales[0]).to(DEV), v_scale=torch.from_numpy(scales[1]).to(DEV))
+    else:
+        Kc, Vc = (torch.zeros((n_pages, Hkv, page, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    lens = [200, 70]
+    table = np.array([[n_pages - 1, 5, n_pages - 3, n_pages - 2], [n_pages - 20, n_pages - 21, 0, 0]])
+    K, V = (_values(rng, (270, Hkv, d), "bf16") for _ in range(2))
+    rr.cache_append(K, V, Kc, Vc, _i32(table), _i32(lens), seq_start=_i32([0, 200, 270]), **kw)
+    Q = _values(rng, (2, nq, 8, d), "bf16", 2.0)
+    O = rr.paged_attention(Q, Kc, Vc, _i32(table), _i32(lens), **kw)
+    torch.cuda.synchronize()
+    used = sorted(set(table.flatten().tolist()))
+    small = np.searchsorted(used, table)
+    at = torch.tensor(used, device=DEV)
+    pick = (lambda x: _np(x.view(torch.uint8)[at].view(E4M3))) if cache == "e4m3" else (lambda x: _np(x[at]))
+    okw = dict(k_scale=scales[0], v_scale=scales[1]) if kw else {}
+    ref = op.attention(_np(Q), pick(Kc), pick(Vc), small, lens, **okw)
+    _check(O, None, ref, d, 200, "bf16", nq * 4)
+
+
+def test_captured_prefix_and_routes():
+    """Calls with a prefix and along routes, captured and replayed with later
+    lengths, eager calls in the same workspace between the replays."""
+    rr = rrmod()
+    note("captured prefix and routes")
+    rng = np.random.default_rng(31)
+    H, Hkv, d, page, prefix, B, nq = 8, 2, 128, 16, 150, 9, 2
+    c, pages = _prefix_cache(rng, Hkv, d, page, "bf16", prefix, [60 + 13 * i for i in range(B)])
+    full = list(c.lens)
+    table = c.table.copy()
+    table[:, :prefix // page] = pages[:prefix // page]
+    c.table = table
+    Kc, Vc, tab, lengths = c.args()
+    Q = _values(rng, (B, nq, H, d), "bf16", 2.0)
+    pg = _i32(pages)
+    R = rng.integers(0, 12, size=(B * H * nq, 5))
+    routes = _i32(R)
+    ws = rr.paged_workspace(Q, Kc, tab, n_prefix=prefix)
+    if rr.paged_workspace(Q, Kc, tab, routes=routes, n_recent=1).numel() > ws.numel():
+        ws = rr.paged_workspace(Q, Kc, tab, routes=routes, n_recent=1)
+    O1, O2 = (torch.empty_like(Q) for _ in range(2))
+    rr.prefix_attention(Q, Kc, Vc, tab, lengths, pg, prefix, out=O1, workspace=ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        rr.prefix_attention(Q, Kc, Vc, tab, lengths, pg, prefix, out=O1, workspace=ws)
+        rr.paged_attention(Q, Kc, Vc, tab, lengths, routes=routes, n_recent=1, out=O2, workspace=ws)
+    for i in range(4):
+        c.lens = [n - 7 * i for n in full]
+        lengths.copy_(_i32(c.lens))
+        Q.copy_(_values(rng, tuple(Q.shape), "bf16", 2.0))
+        g.replay()
+        torch.cuda.synchronize()
+        _check(O1, None, c.oracle(Q, prefix_pages=pages, n_prefix=prefix), d, max(full), "bf16", B * nq * 4)
+        _check(O2, None, c.oracle(Q, routes=R, n_recent=1), d, max(full), "bf16")
+        assert torch.equal(rr.prefix_attention(Q, Kc, Vc, tab, lengths, pg, prefix, workspace=ws), O1)
+        assert torch.equal(rr.paged_attention(Q, Kc, Vc, tab, lengths, routes=routes, n_recent=1, workspace=ws), O2)
