@@ -11,12 +11,16 @@ using paged::inverse_sum;
 using paged::log_sum;
 
 constexpr int kT = 256;  // threads of a joining workgroup
+constexpr int kAtOnce = 4;  // parts of a thread in flight
 
 // -------------------------------------------------------------------- join
 //
 // With a prefix: one workgroup per query row.  The row's parts -- of its own
 // item, and of the prefix item that holds it -- are added with weights
-// 2^(m_i - m).
+// 2^(m_i - m).  Bound by the parts, which it reads once: 10 us for 2048 rows
+// of 33 parts (36 MB, 3.6 TB/s; the whole call 56.9 us with four parts of a
+// thread asked for before the first is used, 58.5 without, the same with
+// eight), 22 us for 10240 rows of 7 to 17.
 
 template <int D, bool F32>
 __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
@@ -60,10 +64,20 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
     const int pl = tid % PL, pg = tid / PL;
     f32x4_t x = {0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-#pragma unroll 4
-    for (int i = pg; i < n; i += NP) {
-        const float *p = part_of(i);
-        add_part(*reinterpret_cast<const f32x4_t *>(p + 4 * pl), p[D], p[D + 1], x, m, l);
+    for (int i0 = pg; i0 < n; i0 += kAtOnce * NP) {
+        f32x4_t y[kAtOnce];
+        float mi[kAtOnce], li[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const float *p = part_of(min(i0 + k * NP, n - 1));
+            y[k] = *reinterpret_cast<const f32x4_t *>(p + 4 * pl);
+            mi[k] = p[D];
+            li[k] = p[D + 1];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            if (i0 + k * NP < n) add_part(y[k], mi[k], li[k], x, m, l);
     }
     *reinterpret_cast<f32x4_t *>(&s_acc[pg][4 * pl]) = x;
     if (pl == 0) {
