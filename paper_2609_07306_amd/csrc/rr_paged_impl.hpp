@@ -197,13 +197,14 @@ __device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, int me,
     r.at = me * r.per_wg;
     r.end = total - r.at < r.per_wg ? total : r.at + r.per_wg;
     // the sequence that the run begins in, and the units before it
-    int b_at = 0, b_before = 0;
+    int b_at = 0, b_before = 0, b_units = 0;
     if (own && r.at >= prefix_total) {
         const int u = (r.at - prefix_total) / a.items_per_seq;
         const bool mine = u >= before && u < before + sum;
         if (few) {
             b_at = __ffsll((unsigned long long)__ballot(mine)) - 1;
             b_before = __builtin_amdgcn_readlane(before, b_at);
+            b_units = __builtin_amdgcn_readlane(sum, b_at);
         } else {
             if (mine) {
                 int b = b0, base = before;
@@ -219,6 +220,7 @@ __device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, int me,
             __syncthreads();
             b_at = uniform(sh.b);
             b_before = uniform(sh.at);
+            b_units = uniform(seq_units(a, b_at));
         }
     }
     Item &it = r.it;
@@ -231,7 +233,7 @@ __device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, int me,
         it.first = it.j * it.units;
     } else {
         const int base = prefix_total + b_before * a.items_per_seq;
-        it.units = uniform(seq_units(a, b_at));
+        it.units = b_units;
         it.j = (r.at - base) / it.units;
         it.index = a.prefix_items + b_at * a.items_per_seq + it.j;
         it.first = base + it.j * it.units;
