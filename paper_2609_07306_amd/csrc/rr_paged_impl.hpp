@@ -37,7 +37,7 @@
 namespace rr {
 namespace paged {
 
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef short short8_t __attribute__((ext_vector_type(8)));
@@ -383,24 +383,28 @@ __device__ __forceinline__ void write_four(void *O, int64_t at, f32x4_t x)
 __device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Parts pass between workgroups on different XCDs, whose L2 caches do not
-// see each other's lines.  They are stored and loaded as device-scope atomics,
-// which go past the L2, so a part is there once its stores have returned: a
-// release fence would write the whole L2 back instead, from every workgroup
-// (measured: one sequence's decode 17 -> 72 us).
+// see each other's lines.  They are stored and loaded at device scope (sc1, as
+// a device-scope atomic is), which goes past the L2, so a part is there once
+// its stores have returned: a release fence would write the whole L2 back
+// instead, from every workgroup (measured: one sequence's decode 17 -> 72 us).
 // (With a prefix the next launch reads them, and they are plain stores.)
-__device__ __forceinline__ void store_part(float *p, float x, float y, bool within)
+constexpr int kDeviceScope = 16;  // sc1 of a buffer instruction
+
+template <int D>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t parts_of(const PagedArgs &a)
 {
-    if (within) {
-        const uint64_t v = (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32;
-        __hip_atomic_store(reinterpret_cast<uint64_t *>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    } else {
-        *reinterpret_cast<f32x2_t *>(p) = f32x2_t{x, y};
-    }
+    return __builtin_amdgcn_make_buffer_rsrc(a.parts, 0, 2 * a.grid * a.own_tile * (D + 4) * (int)sizeof(float), 0x00020000);
 }
 
-__device__ __forceinline__ f32x2_t load_part(const float *p)
+// Four sums (or the maximum and the sum of weights, and two that nothing
+// reads) at p, which lies in a.parts where they are joined within the launch.
+template <int D>
+__device__ __forceinline__ void store_part(const PagedArgs &a, float *p, f32x4_t x, bool within)
 {
-    return __builtin_bit_cast(f32x2_t, __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    if (within)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), parts_of<D>(a), (int)((p - a.parts) * sizeof(float)), 0, kDeviceScope);
+    else
+        *reinterpret_cast<f32x4_t *>(p) = x;
 }
 
 // After a part of a cut item was stored: the workgroup that comes last of the
@@ -422,9 +426,10 @@ __device__ __forceinline__ void join_cut(const PagedArgs &a, Common &sh, unsigne
     }
     __syncthreads();
     if (!uniform(sh.at)) return;
-    const int64_t row_bytes = D + 4, stride = 2 * (int64_t)tile * row_bytes;  // (floats; from one workgroup's to the next one's)
-    const float *first = a.parts + (int64_t)part_slot(run, wg0) * tile * row_bytes;
-    const float *rest = a.parts + (int64_t)2 * wg0 * tile * row_bytes;
+    // (bytes; at most 2 * 512 parts of 128 rows)
+    constexpr int ROW = (D + 4) * (int)sizeof(float);
+    const int stride = 2 * tile * ROW, first = part_slot(run, wg0) * tile * ROW, rest = wg0 * stride;
+    const __amdgpu_buffer_rsrc_t parts = parts_of<D>(a);
     // groups of a row: a power of two, all of them for one row
     int per_row = NP;
     while (per_row > 1 && per_row * rows.n > NP) per_row >>= 1;
@@ -436,21 +441,20 @@ __device__ __forceinline__ void join_cut(const PagedArgs &a, Common &sh, unsigne
         float m = -INFINITY, l = 0.f;
         if (r < rows.n) {
             // (kJoin parts are asked for before the first is used)
-            const float *row = rest + r * row_bytes;
             for (int i0 = sub; i0 < n; i0 += kJoin * per_row) {
-                f32x2_t y[kJoin], z[kJoin], ml[kJoin];
+                u32x4_t y[kJoin];
+                u32x2_t ml[kJoin];
 #pragma unroll
                 for (int k = 0; k < kJoin; ++k) {
-                    const int i = min(i0 + k * per_row, n - 1);
-                    const float *p = i == 0 ? first + r * row_bytes : row + i * stride;
-                    y[k] = load_part(p + 4 * pl);
-                    z[k] = load_part(p + 4 * pl + 2);
-                    ml[k] = load_part(p + D);
+                    const int i = min(i0 + k * per_row, n - 1), at = (i == 0 ? first : rest + i * stride) + r * ROW;
+                    y[k] = __builtin_amdgcn_raw_buffer_load_b128(parts, at + 16 * pl, 0, kDeviceScope);
+                    ml[k] = __builtin_amdgcn_raw_buffer_load_b64(parts, at + 4 * D, 0, kDeviceScope);
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int k = 0; k < kJoin; ++k)
-                    if (i0 + k * per_row < n) add_part(f32x4_t{y[k][0], y[k][1], z[k][0], z[k][1]}, ml[k][0], ml[k][1], x, m, l);
+                    if (i0 + k * per_row < n)
+                        add_part(__builtin_bit_cast(f32x4_t, y[k]), __uint_as_float(ml[k][0]), __uint_as_float(ml[k][1]), x, m, l);
             }
         }
         if (per_row > 1) {  // (uniform; one round, every thread)
@@ -987,14 +991,12 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                     }
                     if (sink.last_word)
                         write_four<F32>(a.O, orow * D + f, x * inv);
-                    else {
-                        store_part(part + f, x[0], x[1], within);
-                        store_part(part + f + 2, x[2], x[3], within);
-                    }
+                    else
+                        store_part<D>(a, part + f, x, within);
                 }
                 if ((tid & 15) == 0) {
                     if (!sink.last_word) {
-                        store_part(part + D, m, sum, within);
+                        store_part<D>(a, part + D, f32x4_t{m, sum, 0.f, 0.f}, within);
                     } else if (a.lse) {
                         a.lse[orow] = log_sum(m, sum);
                     }
@@ -1408,15 +1410,13 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                     const f32x4_t x = {acc[mb][4 * q], acc[mb][4 * q + 1], acc[mb][4 * q + 2], acc[mb][4 * q + 3]};
                     if (sink.last_word)
                         write_four<false>(a.O, orow * D + f, x * inv);
-                    else {
-                        store_part(part + f, x[0], x[1], within);
-                        store_part(part + f + 2, x[2], x[3], within);
-                    }
+                    else
+                        store_part<D>(a, part + f, x, within);
                 }
             }
             if (hh == 0) {
                 if (!sink.last_word) {
-                    store_part(part + D, m_run, l_run, within);
+                    store_part<D>(a, part + D, f32x4_t{m_run, l_run, 0.f, 0.f}, within);
                 } else if (a.lse) {
                     a.lse[orow] = log_sum(m_run, l_run);
                 }
