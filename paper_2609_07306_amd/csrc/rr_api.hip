@@ -1041,7 +1041,7 @@ rr_status paged_call(const rr_paged_config *cfg, const void *Q, const void *K_ca
     rr::paged_layout(a, cfg->d, workspace);
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     hipError_t e = timed(RR_KERNEL_PAGED, stream, [&] { return rr::launch_paged(a, cfg->cache_dtype, cfg->d, stream); });
-    if (e == hipSuccess && a.n_prefix > 0)
+    if (e == hipSuccess && (a.n_prefix > 0 || a.join_apart))
         e = timed(RR_KERNEL_JOIN, stream, [&] { return rr::launch_paged_join(a, cfg->cache_dtype, cfg->d, stream); });
     return e == hipSuccess ? RR_OK : hip_fail(e, "paged attention launch");
 }

@@ -15,9 +15,9 @@ constexpr int kAtOnce = 4;  // parts of a thread in flight
 
 // -------------------------------------------------------------------- join
 //
-// With a prefix: one workgroup per query row.  The row's parts -- of its own
-// item, and of the prefix item that holds it -- are added with weights
-// 2^(m_i - m).  Bound by the parts, which it reads once: 10 us for 2048 rows
+// Where a call takes a second launch: one workgroup per query row.  The row's
+// parts -- of its own item, and of the prefix item that holds it -- are added
+// with weights 2^(m_i - m).  Bound by the parts, which it reads once: 10 us for 2048 rows
 // of 33 parts (36 MB, 3.6 TB/s; the whole call 56.9 us with four parts of a
 // thread asked for before the first is used, 58.5 without, the same with
 // eight), 22 us for 10240 rows of 7 to 17.
@@ -41,7 +41,9 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
     int4 pre = {0, 0, 0, 0};
     const float *pre_part = nullptr;  // of a wide prefix: its splits lie a.prefix_tiles slots apart
     const int q = b * a.rows + t * a.group + j, x_tile = q / a.prefix_tile, pre_row = q - x_tile * a.prefix_tile;
-    if (a.prefix_wide) {
+    if (a.prefix_items == 0) {
+        if (own.z == 1) return;  // (its workgroup wrote the output itself)
+    } else if (a.prefix_wide) {
         pre.z = a.prefix_splits;
         const int slot = g * a.prefix_splits * a.prefix_tiles + x_tile;
         pre_part = a.prefix_parts + ((int64_t)slot * a.prefix_tile + pre_row) * (D + 4);
@@ -123,16 +125,33 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     const bool routed = a.k + a.n_sink + a.n_recent > 0, f32 = cache == CACHE_F32;
     a.rows = routed ? 1 : per_b;
     a.prefix_rows = a.n_prefix ? a.n_seqs * per_b : 0;
-    // more than 16 rows go to the wide body (binary32: to 32-row tiles)
-    a.own_wide = !f32 && a.rows > 16;
+    // more than 16 rows go to the wide body, where few items are cut into many
+    // parts more than 32: narrow tiles of 32 rows read K and V with all four
+    // waves (32 rows on 32768 tokens: 36.5 us against 37.5; on 4 times 8192:
+    // 37.7 against 56; but 32 sequences of 500 to 4000 tokens: 87 against 67).
+    // binary32 has the narrow body alone
+    const bool few = (int64_t)a.n_seqs * a.n_kv_heads <= kPagedGrid / 8 && d <= 128 && a.n_prefix == 0;
+    a.own_wide = !f32 && a.rows > (few ? 32 : 16);
     a.prefix_wide = !f32 && a.prefix_rows > 16;
     // (of a narrow prefix and the sequences behind it the tiles are alike)
-    const int narrow = f32 && (a.rows > 16 || a.prefix_rows > 16) ? 32 : 16;
+    const int narrow = a.rows > 16 || (f32 && a.prefix_rows > 16) ? 32 : 16;
     const auto tile = [&](bool wide, int rows) { return !wide ? narrow : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; };
     a.own_tile = tile(a.own_wide, a.rows);
     a.prefix_tile = tile(a.prefix_wide, a.prefix_rows);
     a.row_tiles = (a.rows + a.own_tile - 1) / a.own_tile;
     a.items_per_seq = routed ? a.n_heads * a.n_q : a.n_kv_heads * a.row_tiles;
+    // (kernels of 32-row narrow tiles and of 256 features take a compute unit
+    // for one workgroup)
+    const int most_wg = d == 256 || (!a.own_wide && !a.prefix_wide && narrow == 32) ? kPagedGrid / 2 : kPagedGrid;
+    // Without a prefix the workgroup that finishes an item's last part joins
+    // its parts, which takes it about 7 us for 300 rows of parts; a second
+    // launch takes about as long, and 1 us for 1300 rows of the batch.  (One
+    // sequence of 8192 tokens, 4 rows: 15.8 us with one launch, 17.9 with two;
+    // 16 rows: 21.4 and 19.0; 128 rows: 86 and 34; 8 of 2048 with 512: 81
+    // and 106.)  So a call that takes two has less than 2^23 rows
+    const int64_t items = (int64_t)a.n_seqs * a.items_per_seq;
+    a.join_apart = a.n_prefix == 0 &&
+                   (most_wg / items + 1) * (a.rows < a.own_tile ? a.rows : a.own_tile) * d / 128 >= 300 + (int64_t)a.n_seqs * a.n_q * a.n_heads / 32;
     a.route_units = 0;
     if (routed) {
         const int64_t slots = (int64_t)a.k + a.n_sink + a.n_recent;
@@ -158,10 +177,10 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     a.prefix_splits = a.prefix_slots = 0;
     if (a.prefix_wide) {
         const auto used = [&](int splits) {
-            const int64_t n = (int64_t)a.prefix_items * splits, rounds = (n + kPagedGrid - 1) / kPagedGrid;
-            return (double)n / ((double)rounds * kPagedGrid);
+            const int64_t n = (int64_t)a.prefix_items * splits, rounds = (n + most_wg - 1) / most_wg;
+            return (double)n / ((double)rounds * most_wg);
         };
-        const int most_splits = a.prefix_units < kPagedGrid ? a.prefix_units : kPagedGrid;
+        const int most_splits = a.prefix_units < most_wg ? a.prefix_units : most_wg;
         double best = 0.;
         for (int n = 1; n <= most_splits; ++n) best = used(n) > best ? used(n) : best;
         a.prefix_splits = 1;
@@ -169,7 +188,7 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
         a.prefix_slots = a.prefix_items * a.prefix_splits;
     }
     const double need = a.prefix_wide ? (most_own > a.prefix_slots ? most_own : a.prefix_slots) : most;
-    a.grid = need < kPagedGrid ? (int32_t)need : kPagedGrid;
+    a.grid = need < most_wg ? (int32_t)need : most_wg;
     return true;
 }
 
@@ -188,13 +207,13 @@ static int64_t whole_bytes(const PagedArgs &a, int d)
 }
 
 // The counters come first, at the same place for calls of every shape, which
-// may follow each other in one workspace; heads and whole parts serve calls
-// with a prefix.
+// may follow each other in one workspace; heads serve calls that take a second
+// launch, whole parts those with a prefix.
 constexpr int64_t kCounterBytes = (int64_t)kPagedGrid * sizeof(uint32_t);
 
 static int64_t heads_bytes(const PagedArgs &a)
 {
-    return a.n_prefix ? align256((a.prefix_items + (int64_t)a.n_seqs * a.items_per_seq) * (int64_t)sizeof(int4)) : 0;
+    return a.n_prefix || a.join_apart ? align256((a.prefix_items + (int64_t)a.n_seqs * a.items_per_seq) * (int64_t)sizeof(int4)) : 0;
 }
 
 size_t paged_workspace_bytes(const PagedArgs &a, int d)

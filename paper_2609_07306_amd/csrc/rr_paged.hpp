@@ -109,13 +109,14 @@ struct PagedArgs {
     bool own_wide, prefix_wide;        // which body takes them
     int32_t prefix_splits, prefix_slots;  // of the wide body: key splits, (key head, split, row tile) slots
     int32_t grid;
+    bool join_apart;     // without a prefix: the parts are joined by a second launch
     int32_t batch_keys;  // keys whose page numbers a workgroup holds at a time
     // workspace
     uint32_t *counters;  // [kPagedGrid] finished parts of the item that begins in a workgroup, 0 between calls
     float *parts;        // [2 * grid] parts of items that several workgroups share
     float *prefix_parts; // [prefix_slots] parts
     float *whole;        // with a prefix: [2][rows of the call] parts of items that one workgroup held
-    int4 *heads;         // with a prefix: per item its first part, its first workgroup, its parts, 0
+    int4 *heads;         // with a second launch: per item its first part, its first workgroup, its parts, 0
 };
 
 size_t paged_workspace_bytes(const PagedArgs &a, int d);

@@ -14,11 +14,12 @@
 // one long sequence is spread over the card.  Lengths live on the device, so
 // every workgroup sums them to find its run.  An item that lies in several
 // runs leaves a part (m, l, sum) per run in the workspace, and the workgroup
-// that finishes the last of them joins them (with a prefix, whose items share
-// rows with the sequences', a second launch does).
+// that finishes the last of them joins them.  A second launch does where that
+// is faster (paged_schedule), and with a prefix, whose items share rows with
+// the sequences'.
 //
-// Two bodies share this.  The narrow one is for items of up to 16 rows (32),
-// where memory is the bound: each of four waves takes its own 32-key tiles of
+// Two bodies share this.  The narrow one is for items of up to 16 rows (32 of
+// few items and in binary32), where memory is the bound: each of four waves takes its own 32-key tiles of
 // the run, so that no barrier stands between loads and products, and a tile's
 // keys and values are requested while the tile before it is still in its
 // softmax.  The wide one is for items of more rows, where the products are:
@@ -188,11 +189,12 @@ __device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, int me,
     }
     const int total = prefix_total + all * a.items_per_seq;
     // two workgroups a compute unit; but one of up to eight units where few
-    // items are cut into many parts, of which there are then half as many to
-    // join (one sequence of 8192 tokens: 15.5 us against 20.5; of 32768: 29.8
-    // against 34.9; eight of 1000 to 8000: 31.0 against 31.9)
+    // items are cut into many parts and one workgroup joins them, of which
+    // there are then half as many (one sequence of 8192 tokens: 15.5 us
+    // against 20.5; of 32768: 29.8 against 34.9; eight of 1000 to 8000: 31.0
+    // against 31.9)
     r.per_wg = (total + a.grid - 1) / a.grid;
-    if (!pre && a.n_seqs * a.items_per_seq <= kPagedGrid / 8) r.per_wg = max(r.per_wg, min(8, (total + kPagedGrid / 2 - 1) / (kPagedGrid / 2)));
+    if (!pre && !a.join_apart && a.n_seqs * a.items_per_seq <= kPagedGrid / 8) r.per_wg = max(r.per_wg, min(8, (total + kPagedGrid / 2 - 1) / (kPagedGrid / 2)));
     if ((int64_t)me * r.per_wg >= total) return false;
     r.at = me * r.per_wg;
     r.end = total - r.at < r.per_wg ? total : r.at + r.per_wg;
@@ -335,8 +337,8 @@ __device__ __forceinline__ Sink sink_of(const PagedArgs &a, int D, const Run &r,
     s.last_word = entire && a.prefix_items == 0;
     s.by_row = entire ? a.whole + (r.it.prefix ? 0 : (int64_t)a.n_seqs * a.n_q * a.n_heads) * (D + 4) : nullptr;
     s.cut = a.parts + (int64_t)slot * tile * (D + 4);
-    if (a.prefix_items && u0 == 0 && threadIdx.x == 0) {
-        // the item's head, for the second launch: its first part, its first workgroup, its parts
+    if ((a.prefix_items || a.join_apart) && u0 == 0 && threadIdx.x == 0) {
+        // the item's head, for a second launch: its first part, its first workgroup, its parts
         const int last_wg = (r.it.first + r.it.units - 1) / r.per_wg;
         a.heads[r.it.index] = int4{slot, r.me, last_wg - r.me + 1, 0};
     }
@@ -387,7 +389,7 @@ __device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(0)" ::
 // a device-scope atomic is), which goes past the L2, so a part is there once
 // its stores have returned: a release fence would write the whole L2 back
 // instead, from every workgroup (measured: one sequence's decode 17 -> 72 us).
-// (With a prefix the next launch reads them, and they are plain stores.)
+// (Where a second launch reads them they are plain stores.)
 constexpr int kDeviceScope = 16;  // sc1 of a buffer instruction
 
 template <int D>
@@ -937,7 +939,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
 
         // ------------------------- the waves' sums joined, the result written
         const Sink sink = sink_of(a, D, run, u0, u1, a.own_tile);
-        const bool within = a.prefix_items == 0;  // the parts are joined within this launch
+        const bool within = a.prefix_items == 0 && !a.join_apart;  // the parts are joined within this launch
         const float vs = a.v_scale ? a.v_scale[g] : 1.f;
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
@@ -1356,7 +1358,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
         }
 
         // ------------------------------------------------- the result written
-        const bool within = a.prefix_items == 0;  // the parts are joined within this launch
+        const bool within = a.prefix_items == 0 && !a.join_apart;  // the parts are joined within this launch
         l_run += __shfl_xor(l_run, 32, 64);
         // (scores that are all NaN leave no maximum, but their sum counts)
         m_run = lim < 0 ? -INFINITY : l_run != l_run ? 0.f : m_run;
@@ -1477,7 +1479,8 @@ hipError_t launch_d(const PagedArgs &a, hipStream_t stream)
         return a.own_tile == 16 ? launch_one<TY, D, false, 1>(a, stream) : launch_one<TY, D, false, 2>(a, stream);
     } else {
         if (a.own_wide) return launch_one<TY, D, true, 0>(a, stream);
-        return a.prefix_wide ? launch_one<TY, D, true, 1>(a, stream) : launch_one<TY, D, false, 1>(a, stream);
+        if (a.prefix_wide) return launch_one<TY, D, true, 1>(a, stream);
+        return a.own_tile == 16 ? launch_one<TY, D, false, 1>(a, stream) : launch_one<TY, D, false, 2>(a, stream);
     }
 }
 

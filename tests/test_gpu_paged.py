@@ -863,6 +863,52 @@ def test_offsets_past_32_bits_of_other_bodies(cache, nq):
     _check(O, None, ref, d, 200, "bf16", nq * 4)
 
 
+CUT = [
+    # name, H, Hkv, d, dtype, cache, page, lengths, n_q
+    ("rows_16", 16, 1, 128, "bf16", "bf16", 16, [3000], 1),
+    ("rows_17", 17, 1, 128, "bf16", "bf16", 16, [2000, 0, 40], 1),
+    ("rows_32", 32, 1, 64, "bf16", "bf16", 64, [5000, 1], 1),
+    ("rows_32_e4m3", 16, 2, 128, "bf16", "e4m3", 16, [2500, 700, 3], 4),
+    ("rows_24_e4m3_d64", 12, 1, 64, "bf16", "e4m3", 16, [2500], 2),
+    ("rows_33", 33, 1, 128, "bf16", "bf16", 16, [1800, 100], 1),
+    ("rows_90", 6, 2, 128, "bf16", "bf16", 48, [1500, 20, 300], 30),
+    ("rows_128_e4m3", 8, 1, 128, "bf16", "e4m3", 64, [2000], 16),
+    ("rows_200", 8, 2, 64, "bf16", "bf16", 64, [1000, 700], 50),
+    ("rows_40_d256", 8, 1, 256, "bf16", "bf16", 32, [1600, 900], 5),
+    ("rows_12_d256", 12, 1, 256, "bf16", "e4m3", 32, [3000], 1),
+    ("rows_15_f32", 6, 2, 64, "f32", "f32", 48, [3000, 900, 2], 5),
+    ("rows_32_f32", 16, 2, 128, "f32", "f32", 16, [1500, 700], 4),
+    ("rows_70_f32", 14, 1, 64, "f32", "f32", 16, [900, 80], 5),
+]
+
+
+@pytest.mark.parametrize("case", CUT, ids=[c[0] for c in CUT])
+def test_few_items_cut_into_many_parts(case):
+    """Parts joined by the last workgroup or by a second launch, some items
+    whole; newest tokens that are not finite reach their own rows alone."""
+    rr = rrmod()
+    name, H, Hkv, d, dtype, cache, page, lens, nq = case
+    note(f"cut {case}")
+    rng = np.random.default_rng(sum(lens) + H)
+    c = Cache(rng, lens, Hkv, d, page, cache)
+    Q = _values(rng, (len(lens), nq, H, d), dtype, 2.0)
+    lse = torch.empty((len(lens), nq, H), device=DEV)
+    args = c.args()
+    ws = rr.paged_workspace(Q, args[0], args[2])
+    O = rr.paged_attention(Q, *args, lse=lse, workspace=ws, **c.kw())
+    torch.cuda.synchronize()
+    want = c.oracle(Q)
+    _check(O, lse, want, d, max(lens), dtype, nq * H // Hkv)
+    assert not ws[:2048].any()
+    assert torch.equal(rr.paged_attention(Q, *args, workspace=ws, **c.kw()), O)
+    if nq > 1:
+        c.put(0, lens[0] - 1, *(np.full((1, Hkv, d), math.nan) for _ in range(2)))
+        P = rr.paged_attention(Q, *args, workspace=ws, **c.kw())
+        torch.cuda.synchronize()
+        _check(P[:, :nq - 1], None, tuple(x[:, :nq - 1] for x in want), d, max(lens), dtype, nq * H // Hkv)
+        assert not P[0, nq - 1].isfinite().any()
+
+
 def test_captured_prefix_and_routes():
     """Calls with a prefix and along routes, captured and replayed with later
     lengths, eager calls in the same workspace between the replays."""
