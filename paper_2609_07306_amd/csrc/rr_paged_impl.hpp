@@ -490,6 +490,12 @@ __device__ __forceinline__ void join_cut(const PagedArgs &a, Common &sh, unsigne
 // way: row-major into a buffer of the wave's own in LDS, read with the LDS
 // transpose read; in binary32, where an operand holds one key per lane,
 // straight from memory.
+//
+// Bound by the reads of K and V: 64 sequences of 300 to 32768 tokens (32 heads
+// on 8, d = 128) 342 us, 5.75 TB/s; 128 of 100 to 16384 in an 8-bit cache 174
+// us, 4.9 TB/s; along routes 187 us, 5.6 TB/s.  One sequence of 8192 tokens
+// (33 MB, 6.6 us of reads) takes 15.7 us: the chain length, page, tile before
+// the reads, and after them the parts that pass between workgroups.
 
 // What a cache type's tiles look like.
 //   KT  keys of a wave's tile
@@ -1018,6 +1024,16 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
 // 32-key block, which is the order in which O^T = V^T P^T takes them.  A row
 // block is one wave's; items of half as many rows as the waves could hold, or
 // less, give two waves to a row block, each with every other key block.
+//
+// Bound by the products and the softmax's vector instructions, which overlap
+// little, and by the tiles' way from the L2 to LDS: 2048 new tokens behind
+// 6144 (d = 128, 32 heads on 8) 311 us, 1280 rows a key head on a prefix of
+// 32768 tokens 235 us, 730 TFLOP/s.  Without the loads it would take 195 us.
+// Measured and not kept: the next tile's loads between the products (274 us
+// for the call where this takes 267), the softmax of one block between the
+// products of the next one (291 against 262), eight waves that share tiles in
+// three stages (257 against 268 there, but 69 against 59 for 256 rows on 8192
+// tokens, 27 against 23 for 32 rows on 4096).
 
 template <int TY, int D>
 struct WideShape {

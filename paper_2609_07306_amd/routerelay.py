@@ -625,5 +625,5 @@ def prefix_attention(Q, K_cache, V_cache, page_table, lengths, prefix_pages, n_p
     prefix_pages [ceil(n_prefix / page)] int32."""
     config = _paged_config(Q, K_cache, V_cache, page_table, None, 0, 0, n_prefix, scale, k_scale, v_scale, lengths)
     dev = _device_of((Q, K_cache, V_cache, page_table, lengths, prefix_pages, k_scale, v_scale, out, lse, workspace))
-    third = _of("prefix_pages", prefix_pages, (n_chunks(n_prefix, K_cache.shape[2]),), torch.int32)
+    third = _of("prefix_pages", prefix_pages, (n_chunks(n_prefix, max(K_cache.shape[2], 1)),), torch.int32)
     return _paged_call(_prefix, config, dev, Q, third, out, lse, workspace, stream)
