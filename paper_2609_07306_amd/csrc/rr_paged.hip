@@ -125,16 +125,14 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     const bool routed = a.k + a.n_sink + a.n_recent > 0, f32 = cache == CACHE_F32;
     a.rows = routed ? 1 : per_b;
     a.prefix_rows = a.n_prefix ? a.n_seqs * per_b : 0;
-    // more than 16 rows go to the wide body, where few items are cut into many
-    // parts more than 32: narrow tiles of 32 rows read K and V with all four
-    // waves (32 rows on 32768 tokens: 36.5 us against 37.5; on 4 times 8192:
-    // 37.7 against 56; but 32 sequences of 500 to 4000 tokens: 87 against 67).
-    // binary32 has the narrow body alone
-    const bool few = (int64_t)a.n_seqs * a.n_kv_heads <= kPagedGrid / 8 && d <= 128 && a.n_prefix == 0;
-    a.own_wide = !f32 && a.rows > (few ? 32 : 16);
+    // more than 16 rows go to the wide body; binary32 has the narrow one alone,
+    // with tiles of 32 rows (such tiles for bf16 too, of which a compute unit
+    // holds one workgroup: 32 rows on 8192 tokens 23.4 us against 25.4, but on 8
+    // times 32768 in an 8-bit cache 164 against 129)
+    a.own_wide = !f32 && a.rows > 16;
     a.prefix_wide = !f32 && a.prefix_rows > 16;
     // (of a narrow prefix and the sequences behind it the tiles are alike)
-    const int narrow = a.rows > 16 || (f32 && a.prefix_rows > 16) ? 32 : 16;
+    const int narrow = f32 && (a.rows > 16 || a.prefix_rows > 16) ? 32 : 16;
     const auto tile = [&](bool wide, int rows) { return !wide ? narrow : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; };
     a.own_tile = tile(a.own_wide, a.rows);
     a.prefix_tile = tile(a.prefix_wide, a.prefix_rows);
@@ -142,7 +140,7 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     a.items_per_seq = routed ? a.n_heads * a.n_q : a.n_kv_heads * a.row_tiles;
     // (kernels of 32-row narrow tiles and of 256 features take a compute unit
     // for one workgroup)
-    const int most_wg = d == 256 || (!a.own_wide && !a.prefix_wide && narrow == 32) ? kPagedGrid / 2 : kPagedGrid;
+    const int most_wg = d == 256 || narrow == 32 ? kPagedGrid / 2 : kPagedGrid;
     // Without a prefix the workgroup that finishes an item's last part joins
     // its parts, which takes it about 7 us for 300 rows of parts; a second
     // launch takes about as long, and 1 us for 1300 rows of the batch.  (One

@@ -18,8 +18,8 @@
 // is faster (paged_schedule), and with a prefix, whose items share rows with
 // the sequences'.
 //
-// Two bodies share this.  The narrow one is for items of up to 16 rows (32 of
-// few items and in binary32), where memory is the bound: each of four waves takes its own 32-key tiles of
+// Two bodies share this.  The narrow one is for items of up to 16 rows (in
+// binary32 of any number, 32 at a time), where memory is the bound: each of four waves takes its own 32-key tiles of
 // the run, so that no barrier stands between loads and products, and a tile's
 // keys and values are requested while the tile before it is still in its
 // softmax.  The wide one is for items of more rows, where the products are:
@@ -1495,8 +1495,7 @@ hipError_t launch_d(const PagedArgs &a, hipStream_t stream)
         return a.own_tile == 16 ? launch_one<TY, D, false, 1>(a, stream) : launch_one<TY, D, false, 2>(a, stream);
     } else {
         if (a.own_wide) return launch_one<TY, D, true, 0>(a, stream);
-        if (a.prefix_wide) return launch_one<TY, D, true, 1>(a, stream);
-        return a.own_tile == 16 ? launch_one<TY, D, false, 1>(a, stream) : launch_one<TY, D, false, 2>(a, stream);
+        return a.prefix_wide ? launch_one<TY, D, true, 1>(a, stream) : launch_one<TY, D, false, 1>(a, stream);
     }
 }
 
