@@ -142,14 +142,19 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     // for one workgroup)
     const int most_wg = d == 256 || narrow == 32 ? kPagedGrid / 2 : kPagedGrid;
     // Without a prefix the workgroup that finishes an item's last part joins
-    // its parts, which takes it about 7 us for 300 rows of parts; a second
-    // launch takes about as long, and 1 us for 1300 rows of the batch.  (One
-    // sequence of 8192 tokens, 4 rows: 15.8 us with one launch, 17.9 with two;
-    // 16 rows: 21.4 and 19.0; 128 rows: 86 and 34; 8 of 2048 with 512: 81
-    // and 106.)  So a call that takes two has less than 2^23 rows
+    // its parts alone, row after row; a second launch has all of the card for
+    // it, but costs some 3 us and more with the rows of the batch.  It is taken
+    // where an item may have that many rows of parts (they count by their
+    // features).  32 heads on 8, d = 128, one launch and two:
+    //   1 sequence of 8192 tokens, 4 rows: 15.6 and 17.9 us; 16 rows: 21.4 and
+    //   19.0; 128 rows: 86 and 34; 8 sequences of 1000 to 8000, 32 rows: 58.7
+    //   and 42.9; 16 of them, 64 rows: 76.9 and 68.2; 8 of 2048, 512 rows: 81
+    //   and 106.
+    // So a call that takes two has less than 2^23 rows
     const int64_t items = (int64_t)a.n_seqs * a.items_per_seq;
-    a.join_apart = a.n_prefix == 0 &&
-                   (most_wg / items + 1) * (a.rows < a.own_tile ? a.rows : a.own_tile) * d / 128 >= 300 + (int64_t)a.n_seqs * a.n_q * a.n_heads / 32;
+    const int64_t parts = (items <= kPagedGrid / 8 ? kPagedGrid / 2 : most_wg) / items + 1;  // (as the runs are cut, find_run)
+    a.join_apart = a.n_prefix == 0 && parts * (a.rows < a.own_tile ? a.rows : a.own_tile) * d / 128 >=
+                                          (a.own_wide ? 80 : 140) + (int64_t)a.n_seqs * a.n_q * a.n_heads / 64;
     a.route_units = 0;
     if (routed) {
         const int64_t slots = (int64_t)a.k + a.n_sink + a.n_recent;
