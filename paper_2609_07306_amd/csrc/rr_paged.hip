@@ -17,10 +17,10 @@ constexpr int kAtOnce = 4;  // parts of a thread in flight
 //
 // Where a call takes a second launch: one workgroup per query row.  The row's
 // parts -- of its own item, and of the prefix item that holds it -- are added
-// with weights 2^(m_i - m).  Bound by the parts, which it reads once: 10 us for 2048 rows
-// of 33 parts (36 MB, 3.6 TB/s; the whole call 56.9 us with four parts of a
-// thread asked for before the first is used, 58.5 without, the same with
-// eight), 22 us for 10240 rows of 7 to 17.
+// with weights 2^(m_i - m).  Bound by the parts, which it reads once: 9 us for
+// 2048 rows of 33 parts (36 MB, 4 TB/s; the whole call 56.9 us with four parts
+// of a thread asked for before the first is used, 58.5 without, the same with
+// eight), 23 us for 10240 rows of 7 to 9.
 
 template <int D, bool F32>
 __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
@@ -153,7 +153,7 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     // So a call that takes two has less than 2^23 rows
     const int64_t items = (int64_t)a.n_seqs * a.items_per_seq;
     const int64_t parts = (items <= kPagedGrid / 8 ? kPagedGrid / 2 : most_wg) / items + 1;  // (as the runs are cut, find_run)
-    a.join_apart = a.n_prefix == 0 && parts * (a.rows < a.own_tile ? a.rows : a.own_tile) * d / 128 >=
+    a.join_apart = a.n_prefix == 0 && !routed && parts * (a.rows < a.own_tile ? a.rows : a.own_tile) * d / 128 >=
                                           (a.own_wide ? 80 : 140) + (int64_t)a.n_seqs * a.n_q * a.n_heads / 64;
     a.route_units = 0;
     if (routed) {

@@ -438,6 +438,9 @@ ROUTED = [
     ("sinks_alone", 4, 1, 256, "bf16", "bf16", 20, [400, 1, 90], 1, 0, 2, 0),
     ("f32", 6, 2, 64, "f32", "f32", 48, [900, 10, 96], 2, 7, 1, 1),
     ("f32_d128", 2, 2, 128, "f32", "f32", 16, [500], 1, 20, 2, 2),
+    ("one_head", 1, 1, 128, "bf16", "bf16", 64, [4000], 1, 60, 1, 1),
+    ("two_heads_d256", 2, 1, 256, "bf16", "bf16", 128, [8000], 1, 70, 1, 1),
+    ("two_tokens_d256", 1, 1, 256, "bf16", "e4m3", 128, [8000], 2, 70, 1, 1),
 ]
 
 
