@@ -1,5 +1,7 @@
 // The paged attention's schedule and launches, and the join of the parts that
 // its workgroups leave (the attention itself is in rr_paged_impl.hpp).
+#include <type_traits>
+
 #include "rr_paged_impl.hpp"
 
 namespace rr {
@@ -15,22 +17,25 @@ constexpr int kAtOnce = 4;  // parts of a thread in flight
 
 // -------------------------------------------------------------------- join
 //
-// Where a call takes a second launch: one workgroup per query row.  The row's
-// parts -- of its own item, and of the prefix item that holds it -- are added
-// with weights 2^(m_i - m).  Bound by the parts, which it reads once: 9 us for
-// 2048 rows of 33 parts (36 MB, 4 TB/s; the whole call 56.9 us with four parts
-// of a thread asked for before the first is used, 58.5 without, the same with
-// eight), 23 us for 10240 rows of 7 to 9.
+// Where a call takes a second launch: a query row's parts -- of its own item,
+// and of the prefix item that holds it -- are added with weights 2^(m_i - m), by
+// a workgroup or (ROWS = 4) a wave of one.  Bound by the parts, which it reads
+// once (2048 rows of 33 parts, 36 MB: 4.5 TB/s), with four parts of a thread
+// asked for before the first is used (the whole call 56.9 us, without 58.5, as
+// long with eight).
 
-template <int D, bool F32>
+template <int D, bool F32, int ROWS>
 __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
 {
-    constexpr int PL = D / 4;      // lanes of a part, four features each
-    constexpr int NP = kT / PL;    // parts in flight
-    __shared__ float s_m[NP], s_l[NP];
-    __shared__ float s_acc[NP][D];
-    const int tid = threadIdx.x;
-    const int64_t orow = blockIdx.x;  // (b, t, h)
+    constexpr int PL = D / 4;          // lanes of a part, four features each
+    constexpr int T = kT / ROWS;       // threads of a row
+    constexpr int NP = T / PL;         // its parts in flight
+    __shared__ float s_m[ROWS][NP], s_l[ROWS][NP];
+    __shared__ float s_acc[ROWS][NP][D];
+    const int tid = threadIdx.x % T, w = threadIdx.x / T;
+    const int64_t n_rows = (int64_t)a.n_seqs * a.n_q * a.n_heads;
+    const int64_t orow = min((int64_t)blockIdx.x * ROWS + w, n_rows - 1);  // (b, t, h)
+    bool live = (int64_t)blockIdx.x * ROWS + w < n_rows;
     const int h = (int)(orow % a.n_heads);
     const int64_t bt = orow / a.n_heads;
     const int t = (int)(bt % a.n_q), b = (int)(bt / a.n_q);
@@ -42,7 +47,7 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
     const float *pre_part = nullptr;  // of a wide prefix: its splits lie a.prefix_tiles slots apart
     const int q = b * a.rows + t * a.group + j, x_tile = q / a.prefix_tile, pre_row = q - x_tile * a.prefix_tile;
     if (a.prefix_items == 0) {
-        if (own.z == 1) return;  // (its workgroup wrote the output itself)
+        live = live && own.z != 1;  // (else its workgroup wrote the output itself)
     } else if (a.prefix_wide) {
         pre.z = a.prefix_splits;
         const int slot = g * a.prefix_splits * a.prefix_tiles + x_tile;
@@ -50,8 +55,7 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
     } else {
         pre = a.heads[g * a.prefix_tiles + x_tile];
     }
-    const int n_own = own.z, n = n_own + pre.z;
-    const int64_t n_rows = (int64_t)a.n_seqs * a.n_q * a.n_heads;
+    const int n_own = own.z, n = live ? n_own + pre.z : 0;
     auto part_of = [&](int i) -> const float * {
         const bool p = i >= n_own;
         const int4 &hd = p ? pre : own;
@@ -81,27 +85,28 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
         for (int k = 0; k < kAtOnce; ++k)
             if (i0 + k * NP < n) add_part(y[k], mi[k], li[k], x, m, l);
     }
-    *reinterpret_cast<f32x4_t *>(&s_acc[pg][4 * pl]) = x;
+    *reinterpret_cast<f32x4_t *>(&s_acc[w][pg][4 * pl]) = x;
     if (pl == 0) {
-        s_m[pg] = m;
-        s_l[pg] = l;
+        s_m[w][pg] = m;
+        s_l[w][pg] = l;
     }
     __syncthreads();
+    if (!live) return;
     m = -INFINITY;
     l = 0.f;
     float wt[NP];
 #pragma unroll
-    for (int i = 0; i < NP; ++i) m = fmaxf(m, s_m[i]);
+    for (int i = 0; i < NP; ++i) m = fmaxf(m, s_m[w][i]);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-        wt[i] = s_m[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[i] - m);
-        l += wt[i] * s_l[i];
+        wt[i] = s_m[w][i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][i] - m);
+        l += wt[i] * s_l[w][i];
     }
     const float inv = inverse_sum(l, a.v_scale ? a.v_scale[g] : 1.f);
-    for (int f = tid; f < D; f += kT) {
+    for (int f = tid; f < D; f += T) {
         float y = 0.f;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) y = wt[i] != 0.f ? __builtin_fmaf(wt[i], s_acc[i][f], y) : y;
+        for (int i = 0; i < NP; ++i) y = wt[i] != 0.f ? __builtin_fmaf(wt[i], s_acc[w][i][f], y) : y;
         y *= inv;
         if constexpr (F32)
             static_cast<float *>(a.O)[orow * D + f] = y;
@@ -143,18 +148,18 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     const int most_wg = d == 256 || narrow == 32 ? kPagedGrid / 2 : kPagedGrid;
     // Without a prefix the workgroup that finishes an item's last part joins
     // its parts alone, row after row; a second launch has all of the card for
-    // it, but costs some 3 us and more with the rows of the batch.  It is taken
-    // where an item may have that many rows of parts (they count by their
-    // features).  32 heads on 8, d = 128, one launch and two:
+    // it, but costs some 3 us and a little more with the rows of the batch.  It
+    // is taken where an item may have that many rows of parts (they count by
+    // their features).  32 heads on 8, d = 128, one launch and two:
     //   1 sequence of 8192 tokens, 4 rows: 15.6 and 17.9 us; 16 rows: 21.4 and
     //   19.0; 128 rows: 86 and 34; 8 sequences of 1000 to 8000, 32 rows: 58.7
-    //   and 42.9; 16 of them, 64 rows: 76.9 and 68.2; 8 of 2048, 512 rows: 81
-    //   and 106.
-    // So a call that takes two has less than 2^23 rows
+    //   and 42; 32 of 1000 to 4000, 64 rows: 93 and 81; 1 of 2048, all of them
+    //   new: 83 and 99
+    // (So a call that takes two has less than 2^25 rows.)
     const int64_t items = (int64_t)a.n_seqs * a.items_per_seq;
     const int64_t parts = (items <= kPagedGrid / 8 ? kPagedGrid / 2 : most_wg) / items + 1;  // (as the runs are cut, find_run)
     a.join_apart = a.n_prefix == 0 && !routed && parts * (a.rows < a.own_tile ? a.rows : a.own_tile) * d / 128 >=
-                                          (a.own_wide ? 80 : 140) + (int64_t)a.n_seqs * a.n_q * a.n_heads / 64;
+                                          (a.own_wide ? 80 : 140) + (int64_t)a.n_seqs * a.n_q * a.n_heads / 256;
     a.route_units = 0;
     if (routed) {
         const int64_t slots = (int64_t)a.k + a.n_sink + a.n_recent;
@@ -261,12 +266,26 @@ hipError_t launch_paged(const PagedArgs &a, int cache, int d, hipStream_t stream
 
 hipError_t launch_paged_join(const PagedArgs &a, int cache, int d, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((int64_t)a.n_seqs * a.n_q * a.n_heads)), th(kT);
-    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, th, 0, stream, a); };
+    const int64_t rows = (int64_t)a.n_seqs * a.n_q * a.n_heads;
+    auto go = [&](auto kern, int at_once) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)((rows + at_once - 1) / at_once)), dim3(kT), 0, stream, a);
+    };
+    // four rows a workgroup where that leaves one for each half of a compute unit
+    // (10240 rows of 7 to 9 parts: 11 us against 23; 2048 of 33: 8.2 against 9; but
+    // one sequence of 8192 tokens, 16 rows of one key head: the call 20.1 against
+    // 14.9)
+    const bool many = rows >= 4 * kPagedGrid;
+    auto width = [&](auto f32, auto width) {
+        constexpr bool F32 = decltype(f32)::value;
+        constexpr int D = decltype(width)::value;
+        many ? go(paged_join_kernel<D, F32, 4>, 4) : go(paged_join_kernel<D, F32, 1>, 1);
+    };
     if (cache == CACHE_F32)
-        d == 64 ? go(paged_join_kernel<64, true>) : go(paged_join_kernel<128, true>);
+        d == 64 ? width(std::true_type(), std::integral_constant<int, 64>()) : width(std::true_type(), std::integral_constant<int, 128>());
     else
-        d == 64 ? go(paged_join_kernel<64, false>) : d == 128 ? go(paged_join_kernel<128, false>) : go(paged_join_kernel<256, false>);
+        d == 64    ? width(std::false_type(), std::integral_constant<int, 64>())
+        : d == 128 ? width(std::false_type(), std::integral_constant<int, 128>())
+                   : width(std::false_type(), std::integral_constant<int, 256>());
     return hipGetLastError();
 }
 
