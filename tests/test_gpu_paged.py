@@ -751,6 +751,8 @@ MANY = [
     ("prefix_many_rows_items", 16, 2, 64, "bf16", "e4m3", 16, 300, 5, 100, 130),
     ("prefix_d256_rows", 8, 1, 256, "bf16", "bf16", 16, 70, 3, 100, 200),
     ("prefix_f32", 8, 2, 64, "f32", "f32", 16, 70, 2, 150, 200),
+    ("prefix_many_rows_f32", 8, 2, 64, "f32", "f32", 16, 70, 4, 60, 100),
+    ("prefix_many_rows_d256", 16, 2, 256, "bf16", "bf16", 16, 70, 2, 60, 300),
     ("prefix_rounds", 32, 8, 64, "bf16", "bf16", 16, 130, 16, 60, 200),
     ("prefix_rounds_narrow", 32, 8, 64, "bf16", "bf16", 16, 520, 4, 40, 150),
 ]
@@ -882,6 +884,9 @@ CUT = [
     ("rows_15_f32", 6, 2, 64, "f32", "f32", 48, [3000, 900, 2], 5),
     ("rows_32_f32", 16, 2, 128, "f32", "f32", 16, [1500, 700], 4),
     ("rows_70_f32", 14, 1, 64, "f32", "f32", 16, [900, 80], 5),
+    ("rows_in_all_2560", 32, 4, 64, "bf16", "bf16", 16, [700, 3, 400, 520, 0], 16),
+    ("rows_in_all_2064_d256", 16, 2, 256, "bf16", "e4m3", 16, [500, 30, 260], 43),
+    ("rows_in_all_2048_f32", 16, 2, 128, "f32", "f32", 48, [400, 333, 18, 1], 32),
 ]
 
 
