@@ -262,6 +262,36 @@ def test_append_leaves_out_what_has_no_place():
     assert torch.equal(Kc, want) and torch.equal(Qo, wantq)
 
 
+@pytest.mark.parametrize("B", [1, 63, 64, 65, 300])
+def test_append_finds_a_tokens_sequence(B):
+    """Sequences without new tokens among others, rows before the first one's
+    and after the last one's, starts that begin past 0: values go where they
+    should and nowhere else."""
+    rr = rrmod()
+    note(f"append to {B} sequences")
+    rng = np.random.default_rng(B)
+    Hkv, d, page = 1, 8, 4
+    new = rng.integers(0, 4, size=B) * (rng.random(B) < 0.7)
+    new[B // 2] = 5
+    lens = new + rng.integers(0, 9, size=B)
+    start = 2 + np.concatenate([[0], np.cumsum(new)])
+    n = int(start[-1]) + 3
+    width = -(-int(lens.max()) // page)
+    n_pages = B * width
+    table = rng.permutation(n_pages).reshape(B, width)
+    K, V = (_values(rng, (n, Hkv, d), "f32") for _ in range(2))
+    Kc, Vc = (torch.full((n_pages, Hkv, page, d), 7.0, device=DEV) for _ in range(2))
+    want_k, want_v = Kc.clone(), Vc.clone()
+    rr.cache_append(K, V, Kc, Vc, _i32(table), _i32(lens), seq_start=_i32(start))
+    torch.cuda.synchronize()
+    for b in range(B):
+        for j in range(new[b]):
+            u, i = int(lens[b] - new[b] + j), int(start[b] + j)
+            want_k[table[b, u // page], :, u % page] = K[i]
+            want_v[table[b, u // page], :, u % page] = V[i]
+    assert torch.equal(Kc, want_k) and torch.equal(Vc, want_v)
+
+
 def test_append_starts_past_the_tokens():
     """seq_start may count more tokens than the call brings: those alone count."""
     rr = rrmod()
