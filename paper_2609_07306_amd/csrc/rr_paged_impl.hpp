@@ -112,6 +112,17 @@ __device__ __forceinline__ void take_odd(bf16x8_t &v, bf16x8_t &odd)
     odd = __builtin_bit_cast(bf16x8_t, marks);
 }
 
+// Adds to `found` whether one of the values in x (a cache's bits) is not finite:
+// an exponent of ones (e4m3: NaN, all ones) and one more reaches the sign's bit.
+template <int TY>
+__device__ __forceinline__ void find_odd(uint32_t x, uint32_t &found)
+{
+    constexpr uint32_t ones = TY == CACHE_F32 ? 0x7F800000u : TY == CACHE_BF16 ? 0x7F807F80u : 0x7F7F7F7Fu;
+    constexpr uint32_t one = TY == CACHE_F32 ? 0x00800000u : TY == CACHE_BF16 ? 0x00800080u : 0x01010101u;
+    constexpr uint32_t sign = TY == CACHE_F32 ? 0x80000000u : TY == CACHE_BF16 ? 0x80008000u : 0x80808080u;
+    found |= ((x & ones) + one) & sign;
+}
+
 // ------------------------------------------------------------- the runs
 
 struct Item {
@@ -734,7 +745,9 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                 mixed = __ballot(mixed) != 0ull;
 
                 // rows that no query sees become zeros: their weights are 0,
-                // but memory that was never written may hold NaN
+                // but memory that was never written may hold NaN.  Of a mixed
+                // tile's other rows it matters whether all are finite
+                uint32_t found = 0;
                 if constexpr (F32) {
                     if (!all_seen) {
 #pragma unroll
@@ -743,7 +756,10 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
 #pragma unroll
                             for (int c = 0; c < D / 64; ++c)
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) vr[0][4 * c + s][e] = keep ? vr[0][4 * c + s][e] : 0u;
+                                for (int e = 0; e < 4; ++e) {
+                                    vr[0][4 * c + s][e] = keep ? vr[0][4 * c + s][e] : 0u;
+                                    find_odd<TY>(vr[0][4 * c + s][e], found);
+                                }
                         }
                     }
                 } else {
@@ -755,7 +771,10 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                         for (int c = 0; c < S::PK; ++c) {
                             if (!all_seen) {
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) vr[r][c][e] = keep ? vr[r][c][e] : 0u;
+                                for (int e = 0; e < 4; ++e) {
+                                    vr[r][c][e] = keep ? vr[r][c][e] : 0u;
+                                    find_odd<TY>(vr[r][c][e], found);
+                                }
                             }
                             unsigned char *dst = vbuf + (16 * r + l16) * S::VRS;
                             const int swap = (l16 & 8) << 1;
@@ -770,6 +789,8 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
                     __builtin_amdgcn_wave_barrier();
                 }
+
+                mixed = mixed && __ballot(found != 0) != 0ull;
 
                 // S^T = K Q^T: s[n][r] of lane (l16, kg): keys 16 r + 4 kg + i
                 // of the tile, query row 16 n + l16
