@@ -506,7 +506,8 @@ __device__ __forceinline__ void join_cut(const PagedArgs &a, Common &sh, unsigne
 //
 // Bound by the reads of K and V: 64 sequences of 300 to 32768 tokens (32 heads
 // on 8, d = 128) 342 us, 5.75 TB/s; 128 of 100 to 16384 in an 8-bit cache 174
-// us, 4.9 TB/s; along routes 187 us, 5.6 TB/s.  One sequence of 8192 tokens
+// us, 4.9 TB/s (each item begins with a chain of loads; 64 of 8192: 5.7); along
+// routes 187 us, 5.6 TB/s.  One sequence of 8192 tokens
 // (33 MB, 6.6 us of reads) takes 15.7 us: the chain length, page, tile before
 // the reads, and after them the parts that pass between workgroups.
 
