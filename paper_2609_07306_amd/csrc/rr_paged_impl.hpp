@@ -1415,6 +1415,14 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
         // (scores that are all NaN leave no maximum, but their sum counts)
         m_run = lim < 0 ? -INFINITY : l_run != l_run ? 0.f : m_run;
         l_run = lim < 0 ? 0.f : l_run;
+        // a row that sees no token went along as one that sees all of the item's,
+        // of which some may not be finite: 0 times those would not be 0
+        if (__ballot(lim < 0) != 0ull) {
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[mb][r] = lim < 0 ? 0.f : acc[mb][r];
+        }
         __syncthreads();
         if (wk == 2) {  // (uniform) the second wave of a row block hands its sums to the first
             f32x4_t *ob = reinterpret_cast<f32x4_t *>(smem) + rb * (64 * NMB * 4) + lane;
