@@ -453,7 +453,7 @@ size_t rr_paged_workspace_bytes(const rr_paged_config *cfg);
  * rounded to bf16 (2^-8 off) at worst where more are.  Tokens that a
  * query does not see have no part in its output, whatever their rows hold;
  * where it sees a value that is not finite, that feature of its output is
- * infinite or NaN.
+ * infinite or NaN, however low the score.
  * Returns RR_ERR_INVALID for bad sizes, NULL or unaligned pointers or a
  * workspace too small, RR_ERR_UNSUPPORTED for other types or d, or for 2^31
  * query rows (n_seqs * n_q * n_heads; 2^24 with a prefix) or more. */

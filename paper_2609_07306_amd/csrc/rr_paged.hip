@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kT) void paged_join_kernel(PagedArgs a)
     for (int f = tid; f < D; f += T) {
         float y = 0.f;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) y = wt[i] != 0.f ? __builtin_fmaf(wt[i], s_acc[w][i][f], y) : y;
+        for (int i = 0; i < NP; ++i) y = __builtin_fmaf(wt[i], s_acc[w][i][f], y);
         y *= inv;
         if constexpr (F32)
             static_cast<float *>(a.O)[orow * D + f] = y;

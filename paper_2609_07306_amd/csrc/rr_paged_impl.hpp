@@ -365,18 +365,17 @@ __device__ __forceinline__ float inverse_sum(float sum, float scale)
 
 __device__ __forceinline__ float log_sum(float m, float sum) { return m == -INFINITY ? -INFINITY : (m + log2f(sum)) * kLn2; }
 
-// Adds part p (four features from f on) to sums x with maximum m and sum of
-// weights l.
+// Adds a part (four features y, maximum mi, sum of weights li) to sums x with
+// maximum m and sum of weights l.  A part of weight 0 is added too: its sums are
+// NaN or infinite where its rows see a value that is, and stay so.  (A part whose
+// row sees nothing holds zeros.)
 __device__ __forceinline__ void add_part(const f32x4_t y, float mi, float li, f32x4_t &x, float &m, float &l)
 {
     const float m_new = fmaxf(m, mi);
     const float w0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
     const float w1 = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - m_new);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float z = w0 != 0.f ? w0 * x[e] : 0.f;
-        x[e] = w1 != 0.f ? __builtin_fmaf(w1, y[e], z) : z;
-    }
+    for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(w1, y[e], w0 * x[e]);
     l = w0 * l + w1 * li;
     m = m_new;
 }
@@ -976,6 +975,15 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
             if (n >= blocks) continue;  // (uniform)
             __syncthreads();
             float *ob = reinterpret_cast<float *>(smem + w * S::WAVE);
+            const bool none = lim[n] < 0;
+            // (it went along as a row that sees all of the item's tokens, of which
+            // some may not be finite)
+            if (__ballot(none) != 0ull) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[n][v][i] = none ? 0.f : acc[n][v][i];
+            }
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 if constexpr (F32) {
@@ -989,7 +997,6 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
             l += __shfl_xor(l, 16, 64);
             l += __shfl_xor(l, 32, 64);
             if (kg == 0) {
-                const bool none = lim[n] < 0;
                 // (scores that are all NaN leave no maximum, but their sum counts)
                 sh.m[w][l16] = none ? -INFINITY : l != l ? 0.f : m_run[n];
                 sh.l[w][l16] = none ? 0.f : l;
@@ -1019,7 +1026,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                     for (int v = 0; v < NW; ++v) {
                         const f32x4_t y = *reinterpret_cast<const f32x4_t *>(reinterpret_cast<float *>(smem + v * S::WAVE) + q * S::ORS + f);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x[i] = wt[v] != 0.f ? __builtin_fmaf(wt[v], y[i], x[i]) : x[i];
+                        for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(wt[v], y[i], x[i]);  // (0 times NaN stays, as in add_part)
                     }
                     if (sink.last_word)
                         write_four<F32>(a.O, orow * D + f, x * inv);
@@ -1448,10 +1455,8 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                     for (int q = 0; q < 4; ++q) {
                         const f32x4_t y = ob[(4 * mb + q) * 64];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float x = w0 != 0.f ? w0 * acc[mb][4 * q + i] : 0.f;
-                            acc[mb][4 * q + i] = w1 != 0.f ? __builtin_fmaf(w1, y[i], x) : x;
-                        }
+                        for (int i = 0; i < 4; ++i)
+                            acc[mb][4 * q + i] = __builtin_fmaf(w1, y[i], w0 * acc[mb][4 * q + i]);
                     }
                 l_run = w0 * l_run + w1 * sh.l[rb][l32];
                 m_run = m;

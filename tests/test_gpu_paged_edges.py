@@ -1,12 +1,14 @@
-"""The paged cache at its edges: queries before their sequence's first token
-beside others that see values which are not finite."""
+"""The paged cache at its edges, against the binary64 oracle: values that are
+not finite behind scores so low that their weights are 0, and queries before
+their sequence's first token beside others that see such values.  Tolerances
+as in test_gpu_paged."""
 import math
 
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_paged import DEV, Cache, _i32, _prefix_cache, _values, note, rrmod
+from test_gpu_paged import DEV, TYPE, Cache, _check, _i32, _prefix_cache, _values, note, rrmod
 
 pytestmark = pytest.mark.gpu
 
@@ -17,6 +19,81 @@ def _gpu():
         pytest.skip("needs a GPU")
     torch.cuda.set_device(0)
     yield
+
+
+LOW = [
+    # name, H, Hkv, d, dtype, cache, page, lengths, n_q, prefix, which tokens of the first have low scores
+    ("wave_bf16", 8, 2, 128, "bf16", "bf16", 16, [128, 3], 1, 0, lambda u: u // 32 == 1),
+    ("wave_e4m3", 8, 2, 64, "bf16", "e4m3", 16, [128, 3], 1, 0, lambda u: u // 32 == 1),
+    ("wave_f32", 4, 2, 64, "f32", "f32", 16, [64, 3], 1, 0, lambda u: u // 32 == 1),
+    ("blocks_bf16", 32, 1, 128, "bf16", "bf16", 16, [128, 3], 1, 0, lambda u: u // 32 % 2 == 1),
+    ("blocks_e4m3", 32, 1, 64, "bf16", "e4m3", 16, [128, 3], 1, 0, lambda u: u // 32 % 2 == 1),
+    ("run_bf16", 8, 2, 128, "bf16", "bf16", 64, [8000, 3], 1, 0, lambda u: u < 3000),
+    ("run_one_launch", 32, 8, 128, "bf16", "bf16", 64, [8000, 3], 1, 0, lambda u: u < 3000),
+    ("run_e4m3", 32, 8, 128, "bf16", "e4m3", 64, [8000, 3], 1, 0, lambda u: u >= 5000),
+    ("run_f32", 4, 4, 128, "f32", "f32", 48, [6000, 3], 1, 0, lambda u: u < 3000),
+    ("run_rows_one_launch", 18, 1, 64, "bf16", "bf16", 64, [300] * 100, 1, 0, lambda u: u < 128),
+    ("run_rows_two_launches", 64, 1, 128, "bf16", "bf16", 64, [6000, 3], 2, 0, lambda u: u < 3000),
+    ("run_rows_e4m3", 64, 1, 64, "bf16", "e4m3", 64, [6000, 3], 2, 0, lambda u: u < 3000),
+    ("run_rows_f32", 32, 1, 64, "f32", "f32", 64, [6000, 3], 2, 0, lambda u: u < 3000),
+    ("run_rows_d256", 24, 1, 256, "bf16", "bf16", 64, [3000, 3], 1, 0, lambda u: u < 1500),
+    ("prefix_bf16", 4, 2, 128, "bf16", "bf16", 16, [268, 3], 1, 208, lambda u: u < 208),
+    ("prefix_rows", 32, 1, 128, "bf16", "bf16", 16, [1200, 3], 2, 1008, lambda u: u < 1008),
+    ("prefix_rows_e4m3", 32, 1, 64, "bf16", "e4m3", 16, [1200, 3], 1, 1008, lambda u: u < 1008),
+    ("behind_prefix_f32", 8, 2, 64, "f32", "f32", 16, [268, 3], 1, 208, lambda u: 208 <= u < 267),
+    ("behind_prefix_rows", 32, 1, 64, "bf16", "bf16", 16, [1200, 3], 1, 1008, lambda u: u >= 1008),
+]
+
+
+@pytest.mark.parametrize("case,infinite_keys", [pytest.param(c, x, id=c[0] + ("_infinite_keys" if x else "")) for c in LOW
+                                                for x in (False, True) if not (x and c[5] == "e4m3")])
+def test_values_that_are_not_finite_behind_low_scores(case, infinite_keys):
+    """Where a query sees a value that is not finite that feature of its output
+    is not either, also if the score is more than 350 below the others, so that
+    the weight is 0 wherever it is formed: in another wave, another run, the
+    prefix or behind it.  infinite_keys: those scores are -inf (e4m3 holds none)."""
+    rr = rrmod()
+    name, H, Hkv, d, dtype, cache, page, lens, nq, prefix, low = case
+    n, B = lens[0], len(lens)
+    note(f"low scores {case[:-1]} {infinite_keys}")
+    rng = np.random.default_rng(len(name) + d)
+    kw, okw = {}, {}
+    if prefix:
+        c, pages = _prefix_cache(rng, Hkv, d, page, cache, prefix, [n - prefix, lens[1]])
+        kw, okw = dict(prefix_pages=_i32(pages), n_prefix=prefix), dict(prefix_pages=pages, n_prefix=prefix)
+    else:
+        c, pages = Cache(rng, lens, Hkv, d, page, cache), []
+    table = c.table
+    c.table = table.copy()
+    c.table[0, :len(pages)] = pages
+    at = np.flatnonzero([low(u) for u in range(n - nq + 1)])
+    for run in np.split(at, np.flatnonzero(np.diff(at) > 1) + 1):
+        # queries lie along (1, 1, ...): q.k of these keys is about -4.4 * 10 * d, that of the others 10 sqrt(d)
+        # at random; at 1 / sqrt(d) 352 (d = 64) to 704 below 0 against 10 at random
+        key = np.full((len(run), Hkv, d), -4.4)
+        if infinite_keys:
+            key[..., 5] = -math.inf
+        c.put(0, run[0], key, rng.standard_normal((len(run), Hkv, d)))
+    key, bad = np.full((1, Hkv, d), -4.4), rng.standard_normal((1, Hkv, d))
+    if infinite_keys:
+        key[..., 5] = -math.inf
+    bad[..., 3], bad[..., d - 1] = (math.nan if cache == "e4m3" else -math.inf), math.nan
+    c.put(0, at[len(at) // 2], key, bad)
+    c.table = table
+    Q = (10.0 + 0.1 * torch.from_numpy(rng.standard_normal((B, nq, H, d)))).to(TYPE[dtype]).to(DEV)
+    lse = torch.empty((B, nq, H), device=DEV)
+    call = rr.prefix_attention if prefix else rr.paged_attention
+    O = call(Q, *c.args(), lse=lse, **kw, **c.kw())
+    torch.cuda.synchronize()
+    assert not O[0, ..., [3, d - 1]].isfinite().any()
+    with np.errstate(invalid="ignore"):
+        exact, elog, W, S = c.oracle(Q, **okw)
+    keep = [f for f in range(d) if f not in (3, d - 1)]
+    if infinite_keys:  # (the largest sum of |q_i k_i| over the finite keys: theirs is at most 4.5 |q|_1)
+        S = np.minimum(S, 4.5 * 11 * d / math.sqrt(d))
+    ref = exact[..., keep], elog, W[..., keep], S
+    _check(O[..., keep], lse, ref, d, n, dtype, nq * H // Hkv * (B if prefix else 1))
+    assert prefix or O[1:].isfinite().all()
 
 
 NONE = [
