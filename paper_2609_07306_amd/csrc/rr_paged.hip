@@ -141,7 +141,7 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     const auto tile = [&](bool wide, int rows) { return !wide ? narrow : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; };
     a.own_tile = tile(a.own_wide, a.rows);
     a.prefix_tile = tile(a.prefix_wide, a.prefix_rows);
-    a.row_tiles = (a.rows + a.own_tile - 1) / a.own_tile;
+    a.row_tiles = 1 + (a.rows - 1) / a.own_tile;  // (there may be 2^31 - 1 rows)
     a.items_per_seq = routed ? a.n_heads * a.n_q : a.n_kv_heads * a.row_tiles;
     // (kernels of 32-row narrow tiles and of 256 features take a compute unit
     // for one workgroup)
