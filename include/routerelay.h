@@ -455,8 +455,10 @@ size_t rr_paged_workspace_bytes(const rr_paged_config *cfg);
  * where it sees a value that is not finite, that feature of its output is
  * infinite or NaN, however low the score.
  * Returns RR_ERR_INVALID for bad sizes, NULL or unaligned pointers or a
- * workspace too small, RR_ERR_UNSUPPORTED for other types or d, or for 2^31
- * query rows (n_seqs * n_q * n_heads; 2^24 with a prefix) or more. */
+ * workspace too small, RR_ERR_UNSUPPORTED for other types or d, for 2^31
+ * query rows (n_seqs * n_q * n_heads; 2^24 with a prefix) or more, or where
+ * 1 + max_pages * page / 128 times n_seqs, n_kv_heads and the tiles of (16 to
+ * 128) rows of a key head comes near 2^31. */
 rr_status rr_paged_attention(const rr_paged_config *cfg, const void *Q, const void *K_cache, const void *V_cache,
                              const int32_t *page_table, const int32_t *lengths, const int32_t *routes, void *O,
                              float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);

@@ -1009,7 +1009,7 @@ rr_status paged_args(const rr_paged_config *cfg, rr::PagedArgs *out)
     a.pd = rr::page_div(c.page);
     a.scale = c.scale > 0.f ? c.scale : 1.f / std::sqrt((float)c.d);
     if (!rr::paged_schedule(a, c.cache_dtype, c.d))
-        return fail(RR_ERR_UNSUPPORTED, "n_seqs * max_pages * page * n_kv_heads is too large: 2^31 times 128 keys at most");
+        return fail(RR_ERR_UNSUPPORTED, "n_seqs * n_kv_heads * tiles of query rows * max_pages * page is too large: below 2^31 - 512 units of 128 keys");
     *out = a;
     return RR_OK;
 }

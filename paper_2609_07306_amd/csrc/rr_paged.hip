@@ -181,7 +181,8 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     const double longest = routed ? a.route_units : (a.capacity + kPagedUnit - 1) / kPagedUnit + a.item_cost;
     const double most_own = longest * a.items_per_seq * a.n_seqs;
     const double most = most_own + (double)a.prefix_items * a.prefix_units;
-    if (most >= (double)INT32_MAX) return false;
+    // (rounded up to the grid's runs they still have to be a 32-bit number)
+    if (most > (double)(INT32_MAX - kPagedGrid)) return false;
     // splits of a wide prefix: the fewest that leave at most a tenth more of
     // the card idle than the best number does
     a.prefix_splits = a.prefix_slots = 0;

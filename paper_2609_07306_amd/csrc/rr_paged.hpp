@@ -121,7 +121,7 @@ struct PagedArgs {
 
 size_t paged_workspace_bytes(const PagedArgs &a, int d);
 // Fills in the schedule of a call whose shape is set; cache: CacheType.  False
-// where it has 2^31 units of work or more.
+// where it may have more than 2^31 - 1 - kPagedGrid units of work.
 bool paged_schedule(PagedArgs &a, int cache, int d);
 // Lays the workspace out from its first byte.
 void paged_layout(PagedArgs &a, int d, void *workspace);

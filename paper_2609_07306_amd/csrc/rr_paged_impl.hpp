@@ -173,7 +173,7 @@ __device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, int me,
     r.me = me;
     constexpr int T = 64 * NW;
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
-    // (a call has less than 2^31 units)
+    // (a call has less than 2^31 - kPagedGrid units)
     const int prefix_total = pre ? a.prefix_items * a.prefix_units : 0;
     // per thread: its sequences, their units and those of all before them
     const bool few = a.n_seqs <= 64;

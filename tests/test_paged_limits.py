@@ -4,7 +4,7 @@ import ctypes
 
 import pytest
 
-from test_paged_abi import _append, _append_call, _paged, _rr  # noqa: F401
+from test_paged_abi import _paged, _paged_call, _rr
 
 TOP = 2 ** 31 - 1
 
@@ -24,3 +24,16 @@ def test_query_rows_near_2_31(n_q, heads, kv, dtype, cache, d):
     # (0: refused, where tiles of rows times units of keys pass 2^31)
     assert n == 0 or 2048 < n <= 2048 + 1024 * 128 * (d + 4) * 4
     assert n > 0 or rr.lib.rr_last_error()
+
+
+def test_units_of_a_launch_stay_below_32_bits():
+    """Units of 128 keys (and one for an item's rows) times 1386 key heads:
+    2^31 - 2 of them, of which the last runs would end past 32 bits, are
+    refused; a page less of each head is taken."""
+    rr = _rr()
+    for units, ok in ((1549410, False), (1549409, True)):
+        c = _paged(rr, n_heads=1386, n_kv_heads=1386, n_seqs=1, page=128, max_pages=units)
+        assert (rr.lib.rr_paged_workspace_bytes(ctypes.byref(c)) > 0) is ok
+        if not ok:
+            assert b"too large" in rr.lib.rr_last_error()
+            assert _paged_call(rr, c) == -5
