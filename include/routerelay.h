@@ -399,7 +399,8 @@ typedef struct {
  * reduced in binary64, the rotation is computed in binary32 and rounded
  * once.  Two new tokens must not lie in the same place.
  * Returns RR_ERR_INVALID for bad sizes, types or NULL pointers,
- * RR_ERR_UNSUPPORTED for 2^24 tokens or more. */
+ * RR_ERR_UNSUPPORTED for 2^24 tokens or more, or for more than 2^30 elements of
+ * keys and queries in a token. */
 rr_status rr_cache_append(const rr_append_config *cfg, const void *K, const void *V, const void *Q,
                           const int32_t *seq_start, const int32_t *lengths, const int32_t *page_table,
                           const double *freqs, void *K_cache, void *V_cache, void *Q_out, void *hip_stream);

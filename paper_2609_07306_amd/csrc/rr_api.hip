@@ -1068,6 +1068,9 @@ rr_status rr_cache_append(const rr_append_config *cfg, const void *K, const void
     if (c.rot > 0 && !freqs) return fail(RR_ERR_INVALID, "freqs must hold rot / 2 frequencies");
     if ((Q != nullptr) != (Q_out != nullptr)) return fail(RR_ERR_INVALID, "Q and Q_out go together");
     if (Q && c.n_heads < 1) return fail(RR_ERR_INVALID, "n_heads must be >= 1");
+    // (an element of a token is found by a 32-bit offset)
+    if (((int64_t)c.n_kv_heads + (Q ? c.n_heads : 0)) * c.d > (1 << 30))
+        return fail(RR_ERR_UNSUPPORTED, "a token's keys and queries must be at most 2^30 elements together");
     if (Q && Q == Q_out && c.n_tokens > 1 && c.ldq != (int64_t)c.n_heads * c.d)
         return fail(RR_ERR_INVALID, "Q_out may be Q only where ldq is n_heads * d");
     if (!seq_start && c.n_tokens % c.n_seqs != 0)

@@ -4,7 +4,7 @@ import ctypes
 
 import pytest
 
-from test_paged_abi import _paged, _paged_call, _rr
+from test_paged_abi import _append, _append_call, _paged, _paged_call, _rr
 
 TOP = 2 ** 31 - 1
 
@@ -37,3 +37,15 @@ def test_units_of_a_launch_stay_below_32_bits():
         if not ok:
             assert b"too large" in rr.lib.rr_last_error()
             assert _paged_call(rr, c) == -5
+
+
+def test_elements_of_a_token_stay_below_32_bits():
+    """A token's rows of keys and queries are 2^30 elements together at most."""
+    rr = _rr()
+    for heads, kv, q, ok in ((2 ** 20 - 2, 2, True, True), (2 ** 20 - 1, 2, True, False), (2 ** 20 + 7, 2, False, True),
+                             (2, 2 ** 20, False, True), (2, 2 ** 20 + 1, False, False), (TOP, TOP, True, False)):
+        c = _append(rr, n_heads=heads, n_kv_heads=kv, d=1024, rot=0, n_tokens=0)
+        more = {} if q else dict(Q=None, Q_out=None)
+        assert _append_call(rr, c, **more) == (0 if ok else -5), (heads, kv, q)
+    # (nothing is launched for no tokens; with some a call of that size is refused too)
+    assert _append_call(rr, _append(rr, n_heads=2 ** 21, d=1024, rot=0)) == -5
