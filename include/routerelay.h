@@ -239,10 +239,11 @@ rr_status rr_ledger_relay_stats(const rr_ledger *ledger, float *alpha, float *be
  * events recorded on its own stream.  rr_profile_stop waits for those events
  * and returns, per kernel kind, the summed duration in milliseconds and the
  * number of launches.  total_ms and launches are caller arrays of n_kinds
- * entries (each may be NULL); RR_KERNEL_KINDS entries are written, and
- * n_kinds < RR_KERNEL_KINDS with a non-NULL array returns RR_ERR_INVALID
- * without writing anything (profiling then stays on).  Process-wide; not for
- * concurrent use from several threads. */
+ * entries (each may be NULL); RR_KERNEL_KINDS entries are written (of n_kinds
+ * = 8, the kinds before RR_KERNEL_APPEND that an earlier header had, those),
+ * and any other n_kinds < RR_KERNEL_KINDS with a non-NULL array returns
+ * RR_ERR_INVALID without writing anything (profiling then stays on).
+ * Process-wide; not for concurrent use from several threads. */
 typedef enum {
     RR_KERNEL_FULL = 0,     /* GEMM + TopK, full routing */
     RR_KERNEL_ANCHOR = 1,   /* GEMM + TopK + ledger build, every row */

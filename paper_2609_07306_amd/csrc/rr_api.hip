@@ -834,7 +834,9 @@ rr_status rr_profile_start(void)
 
 rr_status rr_profile_stop(double *total_ms, int64_t *launches, int32_t n_kinds)
 {
-    if ((total_ms || launches) && n_kinds < RR_KERNEL_KINDS)
+    // (or the kinds of the header before the paged cache's, for programs built against it)
+    const int32_t kinds = n_kinds == RR_KERNEL_APPEND ? n_kinds : RR_KERNEL_KINDS;
+    if ((total_ms || launches) && n_kinds < kinds)
         return fail(RR_ERR_INVALID, "rr_profile_stop: the arrays must hold RR_KERNEL_KINDS entries");
     g_prof.on = false;
     double ms[RR_KERNEL_KINDS] = {};
@@ -851,7 +853,7 @@ rr_status rr_profile_stop(double *total_ms, int64_t *launches, int32_t n_kinds)
         ms[r.kind] += t;
         n[r.kind] += 1;
     }
-    for (int k = 0; k < RR_KERNEL_KINDS; ++k) {
+    for (int k = 0; k < kinds; ++k) {
         if (total_ms) total_ms[k] = ms[k];
         if (launches) launches[k] = n[k];
     }
