@@ -416,8 +416,8 @@ typedef struct {
     int32_t n_seqs;
     int32_t n_q;         /* query tokens of each sequence: its newest */
     int32_t k;           /* route slots (0: no routes) */
-    int32_t n_sink;      /* with routes: first pages ... */
-    int32_t n_recent;    /* ... and last pages that every query sees besides */
+    int32_t n_sink;      /* first pages ... */
+    int32_t n_recent;    /* ... and last pages that every query sees besides its routes */
     int32_t n_prefix;    /* rr_prefix_attention: tokens that all sequences begin with (otherwise 0) */
     int32_t dtype;       /* of Q and O */
     int32_t cache_dtype;
@@ -439,12 +439,13 @@ size_t rr_paged_workspace_bytes(const rr_paged_config *cfg);
  * attends, with one softmax scaled by `scale`, to the sequence's tokens u <= p;
  * query head h reads key head h / (n_heads / n_kv_heads).  A query that sees
  * no token (p < 0) gets a zero output.
- *   routes  NULL with k = 0: every token; else [n_seqs * n_heads * n_q, k]
- *           int32 (row (b * n_heads + h) * n_q + t) page indices within the
- *           sequence: the query sees the tokens u <= p of those pages, of its
- *           first n_sink and of the n_recent up to the one that holds p, each
- *           once; other slots (-1, or a page that begins after p) are skipped.
- *           k + n_sink + n_recent <= 256, any of them may be 0.
+ *   routes  [n_seqs * n_heads * n_q, k] int32 (row (b * n_heads + h) * n_q + t)
+ *           page indices within the sequence: the query sees the tokens u <= p
+ *           of those pages, of its first n_sink and of the n_recent up to the
+ *           one that holds p, each once; other slots (-1, or a page that begins
+ *           after p) are skipped.  NULL with k = 0: its first n_sink and last
+ *           n_recent pages alone; every token where these are 0 too.
+ *           k + n_sink + n_recent <= 256.
  *   O       [n_seqs, n_q, n_heads, d] of dtype.
  *   lse     optional [n_seqs, n_q, n_heads] binary32: the logarithm of the sum
  *           of exp(scaled score), -INFINITY where no token is seen.

@@ -563,9 +563,22 @@ def _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, n_p
         if routes.dim() != 2 or routes.shape[0] != B * H * nq:
             raise ValueError("routes must be [B * H * n_q, k]")
         k = routes.shape[1]
+        if k == n_sink == n_recent == 0:
+            k = 1  # (a slot that names no page, _some_routes: the library takes k = 0 alone for no routes)
     cfg = _PagedConfig(H, Hkv, d, page, n_pages, most, B, nq, k, n_sink, n_recent, n_prefix, _DTYPES[Q.dtype], cache, scale, 0,
                        ks, vs)
     return cfg, kc, vc, table, lens
+
+
+def _some_routes(routes, n_sink, n_recent, stream):
+    """The routes that the library takes: none where there are no slots but other
+    pages, and a slot without a page where a row has nothing to see."""
+    if routes.shape[1]:
+        return routes
+    if n_sink or n_recent:
+        return None
+    with torch.cuda.stream(stream):
+        return torch.full((routes.shape[0], 1), -1, dtype=torch.int32, device=routes.device)
 
 
 def _workspace_bytes(cfg):
@@ -610,11 +623,17 @@ def paged_attention(Q, K_cache, V_cache, page_table, lengths, routes=None, n_sin
     """rr_paged_attention: the newest n_q tokens' queries Q [B, n_q, H, d] over
     their sequences' caches (as in cache_append) -> O [B, n_q, H, d].  routes
     [B * H * n_q, k] int32 page indices: each query over those pages, its first
-    n_sink and its last n_recent ones.  lse: optional float32 output [B, n_q,
-    H].  workspace: paged_workspace(...), or None for one of this call's own."""
+    n_sink and its last n_recent ones (k = 0: over these alone, zeros where there
+    are none; as without routes where n_sink or n_recent is set).  lse: optional
+    float32 output [B, n_q, H].  workspace: paged_workspace(...), or None for one
+    of this call's own."""
     config = _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, 0, scale, k_scale, v_scale, lengths)
     dev = _device_of((Q, K_cache, V_cache, page_table, lengths, routes, k_scale, v_scale, out, lse, workspace))
-    third = _of("routes", routes, routes.shape, torch.int32) if routes is not None and routes.shape[1] else None
+    third = None
+    if routes is not None:
+        _of("routes", routes, routes.shape, torch.int32)
+        routes = _some_routes(routes, n_sink, n_recent, stream)  # (held to the end of the call)
+        third = None if routes is None else routes.data_ptr()
     return _paged_call(_paged, config, dev, Q, third, out, lse, workspace, stream)
 
 

@@ -144,3 +144,29 @@ def test_queries_before_the_first_token_among_others(case):
     assert not O[0, none:][..., [1, 7]].isfinite().any()
     keep = [f for f in range(d) if f not in (1, 7)]
     assert O[0][..., keep].isfinite().all()
+
+
+@pytest.mark.parametrize("H,Hkv,nq,dtype", [(8, 2, 1, "bf16"), (8, 1, 3, "bf16"), (4, 2, 2, "f32")])
+def test_routes_without_slots(H, Hkv, nq, dtype):
+    """Routes of no slots name no page: zeros, not attention over everything;
+    with first or last pages besides, those alone."""
+    rr = rrmod()
+    note(f"routes without slots {H} {Hkv} {nq} {dtype}")
+    rng = np.random.default_rng(nq)
+    c = Cache(rng, [100, 1, 0, 333], Hkv, 64, 16, dtype)
+    Q = _values(rng, (4, nq, H, 64), dtype)
+    none = torch.empty((4 * H * nq, 0), dtype=torch.int32, device=DEV)
+    lse = torch.full((4, nq, H), 7.0, device=DEV)
+    side = torch.cuda.Stream()
+    for stream in (None, side):
+        for ws in (None, rr.paged_workspace(Q, c.K, _i32(c.table), routes=none)):
+            out = torch.full_like(Q, 7.0)
+            args = c.args()
+            torch.cuda.synchronize()
+            rr.paged_attention(Q, *args, routes=none, lse=lse, out=out, workspace=ws, stream=stream)
+            torch.cuda.synchronize()
+            assert not out.any() and (lse == -math.inf).all()
+    O = rr.paged_attention(Q, *c.args(), routes=none, n_sink=1, n_recent=2, lse=lse)
+    torch.cuda.synchronize()
+    _check(O, lse, c.oracle(Q, n_sink=1, n_recent=2), 64, 333, dtype)
+    assert torch.equal(O, rr.paged_attention(Q, *c.args(), n_sink=1, n_recent=2))
