@@ -584,7 +584,10 @@ def _some_routes(routes, n_sink, n_recent, stream):
 def _workspace_bytes(cfg):
     n = lib.rr_paged_workspace_bytes(cfg)
     if n == 0:
-        raise RRError(RR_ERR_INVALID, lib.rr_last_error().decode())
+        # the status is that of a call, which refuses the config before it looks
+        # at a pointer (and would refuse these, were it not for the config)
+        call, third = (_prefix, 1) if cfg.n_prefix else (_paged, 1 if cfg.k else None)
+        _check(call(cfg, None, None, None, None, None, third, None, None, None, 0, None))
     return n
 
 
