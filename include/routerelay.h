@@ -451,8 +451,8 @@ size_t rr_paged_workspace_bytes(const rr_paged_config *cfg);
  *           of exp(scaled score), -INFINITY where no token is seen.
  * Scores, softmax and sums in binary32.  With bf16 queries the softmax weights
  * enter the value product as the sum of two bf16 numbers (2^-16 off) where at
- * most 16 query rows are multiplied with a key head's tokens together (n_q *
- * n_heads / n_kv_heads of a sequence, n_seqs times that of a shared prefix),
+ * most 64 query rows are multiplied with a key head's tokens together (n_q *
+ * n_heads / n_kv_heads of a sequence, n_seqs times that behind a shared prefix),
  * rounded to bf16 (2^-8 off) at worst where more are.  Tokens that a
  * query does not see have no part in its output, whatever their rows hold;
  * where it sees a value that is not finite, that feature of its output is

@@ -141,6 +141,15 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     const auto tile = [&](bool wide, int rows) { return !wide ? narrow : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; };
     a.own_tile = tile(a.own_wide, a.rows);
     a.prefix_tile = tile(a.prefix_wide, a.prefix_rows);
+    // Rounded to one bf16 number, a weight is 2^-8 off, as much as the output; as
+    // two, 2^-16.  Where tiles hold up to 64 rows the reads of keys take the time
+    // and the second product costs little: 8192 tokens, 32 and 64 rows 24.1 and
+    // 27.0 us with one, 25.0 and 28.1 with two; 32 sequences of 1000 to 4000, 64
+    // rows 84.0 and 85.6; 64 of 100 to 1000, 32 rows 43.7 and 47.0; six behind
+    // 2000 tokens 14.2 and 14.8.  With more the products do: 8192 tokens, 128 rows
+    // 44.2 and 49.0; 2048 new ones behind 6144 305 and 384; 1280 rows on 32768
+    // tokens 241 and 302
+    a.two_weights = (a.prefix_rows ? a.prefix_rows : a.rows) <= 64;
     a.row_tiles = 1 + (a.rows - 1) / a.own_tile;  // (there may be 2^31 - 1 rows)
     a.items_per_seq = routed ? a.n_heads * a.n_q : a.n_kv_heads * a.row_tiles;
     // (kernels of 32-row narrow tiles and of 256 features take a compute unit

@@ -107,6 +107,7 @@ struct PagedArgs {
     int32_t item_cost;      // units that stand for what an item of a sequence costs besides its keys
     int32_t prefix_rows, prefix_tile, prefix_tiles, prefix_items, prefix_units;  // of the batch against the prefix
     bool own_wide, prefix_wide;        // which body takes them
+    bool two_weights;  // in the wide body a weight is two bf16 numbers
     int32_t prefix_splits, prefix_slots;  // of the wide body: key splits, (key head, split, row tile) slots
     int32_t grid;
     bool join_apart;     // without a prefix: the parts are joined by a second launch

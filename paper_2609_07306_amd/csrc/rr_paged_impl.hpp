@@ -1060,7 +1060,10 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
 // little, and by the tiles' way from the L2 to LDS: 2048 new tokens behind
 // 6144 (d = 128, 32 heads on 8) 311 us, 1280 rows a key head on a prefix of
 // 32768 tokens 235 us, 730 TFLOP/s.  Without the loads it would take 195 us.
-// Measured and not kept: the next tile's loads between the products (274 us
+// TWO: a weight enters the value product as two bf16 numbers, as in the narrow
+// body, else rounded to one (paged_schedule says which, with the times of both).
+// Measured and not kept: which of them decided at run time (the rows of 128-row
+// tiles then take 4 to 10 % longer, the others 2 to 13 %); the next tile's loads between the products (274 us
 // for the call where this takes 267), the softmax of one block between the
 // products of the next one (291 against 262), eight waves that share tiles in
 // three stages (257 against 268 there, but 69 against 59 for 256 rows on 8192
@@ -1105,7 +1108,7 @@ __device__ __forceinline__ void load_to_lds(const unsigned char *from, uint32_t 
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
 }
 
-template <int TY, int D>
+template <int TY, int D, bool TWO>
 __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsigned char *smem, int slot, int me, bool own)
 {
     using S = WideShape<TY, D>;
@@ -1354,13 +1357,18 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                     m_run = m_new;
                 }
                 const float m_use = m_run == -INFINITY ? 0.f : m_run;
-                bf16x8_t pw[2];
+                bf16x8_t pw[2], rest[2];
                 float l = 0.f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, -m_use));
-                    l += x;
-                    pw[r >> 3][r & 7] = (__bf16)x;
+                for (int q = 0; q < 2; ++q) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * q + e], c2, -m_use));
+                        l += x[e];
+                        if constexpr (!TWO) pw[q][e] = (__bf16)x[e];
+                    }
+                    if constexpr (TWO) split_weights(x, pw[q], rest[q]);
                 }
                 l_run += l;
 #pragma unroll
@@ -1378,6 +1386,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                     }
                     f32x16_t &o = acc[i % NMB];
                     o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pw[i / NMB], o, 0, 0, 0);
+                    if constexpr (TWO) o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, rest[i / NMB], o, 0, 0, 0);
                     if (MASKED && any_odd) {
                         bf16x8_t see;
 #pragma unroll
@@ -1495,7 +1504,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
 }
 
 // The bodies of a launch one after the other: WIDE for the items of many
-// rows, NR > 0 (16-row blocks) for the others.
+// rows (TWO: with two numbers a weight), NR > 0 (16-row blocks) for the others.
 template <int TY, int D, bool WIDE, int NR>
 struct Launch {
     static constexpr int NW = WIDE ? WideShape<TY == CACHE_F32 ? CACHE_BF16 : TY, D>::NW : 4;
@@ -1504,7 +1513,7 @@ struct Launch {
     static constexpr int LDS = NARROW > WIDTH ? NARROW : WIDTH;
 };
 
-template <int TY, int D, bool WIDE, int NR>
+template <int TY, int D, bool WIDE, int NR, bool TWO>
 __global__ __launch_bounds__((64 * Launch<TY, D, WIDE, NR>::NW), (D <= 128 && NR <= 1 ? 2 : 1)) void paged_kernel(PagedArgs a)
 {
     constexpr int NW = Launch<TY, D, WIDE, NR>::NW;
@@ -1521,19 +1530,19 @@ __global__ __launch_bounds__((64 * Launch<TY, D, WIDE, NR>::NW), (D <= 128 && NR
         me = slot - a.prefix_slots % a.grid;
         me += me < 0 ? a.grid : 0;
     }
-    if constexpr (WIDE) wide_body<TY, D>(a, sh, smem, slot, me, NR == 0);
+    if constexpr (WIDE) wide_body<TY, D, TWO>(a, sh, smem, slot, me, NR == 0);
     if constexpr (NR > 0) narrow_body<TY, D, NR, NW>(a, sh, smem, me, !WIDE && a.prefix_items > 0, true);
 }
 
-template <int TY, int D, bool WIDE, int NR>
+template <int TY, int D, bool WIDE, int NR, bool TWO>
 hipError_t launch_one(const PagedArgs &a, hipStream_t stream)
 {
     using L = Launch<TY, D, WIDE, NR>;
     static LdsLimit seen;
-    const void *fn = reinterpret_cast<const void *>(&paged_kernel<TY, D, WIDE, NR>);
+    const void *fn = reinterpret_cast<const void *>(&paged_kernel<TY, D, WIDE, NR, TWO>);
     hipError_t e = raise_lds_limit(fn, L::LDS + sizeof(Common), seen);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((paged_kernel<TY, D, WIDE, NR>), dim3((unsigned)a.grid), dim3(64 * L::NW), L::LDS, stream, a);
+    hipLaunchKernelGGL((paged_kernel<TY, D, WIDE, NR, TWO>), dim3((unsigned)a.grid), dim3(64 * L::NW), L::LDS, stream, a);
     return hipGetLastError();
 }
 
@@ -1541,10 +1550,12 @@ template <int TY, int D>
 hipError_t launch_d(const PagedArgs &a, hipStream_t stream)
 {
     if constexpr (TY == CACHE_F32) {
-        return a.own_tile == 16 ? launch_one<TY, D, false, 1>(a, stream) : launch_one<TY, D, false, 2>(a, stream);
+        return a.own_tile == 16 ? launch_one<TY, D, false, 1, false>(a, stream) : launch_one<TY, D, false, 2, false>(a, stream);
     } else {
-        if (a.own_wide) return launch_one<TY, D, true, 0>(a, stream);
-        return a.prefix_wide ? launch_one<TY, D, true, 1>(a, stream) : launch_one<TY, D, false, 1>(a, stream);
+        if (!a.own_wide && !a.prefix_wide) return launch_one<TY, D, false, 1, false>(a, stream);
+        if (a.own_wide)
+            return a.two_weights ? launch_one<TY, D, true, 0, true>(a, stream) : launch_one<TY, D, true, 0, false>(a, stream);
+        return a.two_weights ? launch_one<TY, D, true, 1, true>(a, stream) : launch_one<TY, D, true, 1, false>(a, stream);
     }
 }
 

@@ -170,3 +170,39 @@ def test_routes_without_slots(H, Hkv, nq, dtype):
     torch.cuda.synchronize()
     _check(O, lse, c.oracle(Q, n_sink=1, n_recent=2), 64, 333, dtype)
     assert torch.equal(O, rr.paged_attention(Q, *c.args(), n_sink=1, n_recent=2))
+
+
+FINE = [
+    # name, H, Hkv, d, dtype, cache, page, lengths, n_q, prefix
+    ("rows_17", 17, 1, 128, "bf16", "bf16", 16, [3000, 700], 1, 0),
+    ("rows_32", 32, 1, 64, "bf16", "bf16", 16, [3000, 700], 1, 0),
+    ("rows_64", 16, 2, 128, "bf16", "bf16", 64, [3000, 700], 8, 0),
+    ("rows_40_e4m3", 8, 1, 128, "bf16", "e4m3", 64, [2000, 900, 3], 5, 0),
+    ("rows_64_d256", 8, 1, 256, "bf16", "bf16", 64, [1500], 8, 0),
+    ("rows_64_d256_e4m3", 8, 1, 256, "bf16", "e4m3", 64, [1500], 8, 0),
+    ("rows_32_many", 8, 2, 64, "bf16", "bf16", 64, [400 + i for i in range(40)], 8, 0),
+    ("prefix_rows_64", 8, 2, 128, "bf16", "bf16", 16, [1200 + 20 * i for i in range(16)], 1, 1008),
+    ("prefix_rows_60", 20, 1, 64, "bf16", "e4m3", 16, [1500, 1009, 1100], 1, 1008),
+]
+
+
+@pytest.mark.parametrize("case", FINE, ids=[c[0] for c in FINE])
+def test_weights_of_up_to_64_rows_are_not_rounded_to_one_bf16(case):
+    """Outputs of up to 64 rows a key head are as near as those of 16."""
+    rr = rrmod()
+    name, H, Hkv, d, dtype, cache, page, lens, nq, prefix = case
+    note(f"fine weights {case}")
+    rng = np.random.default_rng(len(name) + d)
+    kw, okw = {}, {}
+    if prefix:
+        c, pages = _prefix_cache(rng, Hkv, d, page, cache, prefix, [x - prefix for x in lens])
+        kw, okw = dict(prefix_pages=_i32(pages), n_prefix=prefix), dict(prefix_pages=pages, n_prefix=prefix)
+    else:
+        c = Cache(rng, lens, Hkv, d, page, cache)
+    # (scores of a standard deviation of 0.3: every token counts, and outputs are small beside the values)
+    Q = _values(rng, (len(lens), nq, H, d), dtype, 0.3)
+    lse = torch.empty((len(lens), nq, H), device=DEV)
+    call = rr.prefix_attention if prefix else rr.paged_attention
+    O = call(Q, *c.args(), lse=lse, **kw, **c.kw())
+    torch.cuda.synchronize()
+    _check(O, lse, c.oracle(Q, **okw), d, max(lens), dtype, rows=16)
