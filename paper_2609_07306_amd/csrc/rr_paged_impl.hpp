@@ -548,6 +548,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
 {
     using S = Shape<TY, D>;
     constexpr bool F32 = TY == CACHE_F32;
+    static_assert(F32 || NR == 1, "bf16 items of more than 16 rows are the wide body's");
     constexpr int NV = D / 16;  // value accumulators of a row block
     constexpr int T = 64 * NW;
     Run run;
@@ -579,7 +580,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
 
         // query operands; lim: the last token that a row sees (-1: none);
         // lo and hi: the least and the largest of them that is one
-        bf16x8_t fq[F32 ? 1 : NR][F32 ? 1 : D / 32];
+        bf16x8_t fq[F32 ? 1 : D / 32];
         f32x4_t fqf[F32 ? NR : 1][F32 ? D / 16 : 1];
         int lim[NR], lo = kNoToken, hi = -1;
 #pragma unroll
@@ -602,7 +603,7 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                 for (int c = 0; c < D / 32; ++c) {
                     // (e4m3 keys come 16 to a piece, two operands of 8)
                     const int f = TY == CACHE_E4M3 ? 64 * (c >> 1) + 16 * kg + 8 * (c & 1) : 32 * c + 8 * kg;
-                    fq[n][c] = as_bf16x8(*reinterpret_cast<const u32x4_t *>(static_cast<const bf16_t *>(a.Q) + q + f));
+                    fq[c] = as_bf16x8(*reinterpret_cast<const u32x4_t *>(static_cast<const bf16_t *>(a.Q) + q + f));
                 }
             }
         }
@@ -814,19 +815,12 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                                     for (int e = 0; e < 4; ++e)
                                         s[n][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], fqf[n][c][e], s[n][r], 0, 0, 0);
                         } else if constexpr (TY == CACHE_BF16) {
-                            const bf16x8_t kf = as_bf16x8(kr[r][c]);
-#pragma unroll
-                            for (int n = 0; n < NR; ++n)
-                                if (NR == 1 || n < blocks)
-                                    s[n][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, fq[n][c], s[n][r], 0, 0, 0);
+                            s[0][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kr[r][c]), fq[c], s[0][r], 0, 0, 0);
                         } else {
 #pragma unroll
                             for (int q = 0; q < 2; ++q) {
                                 const bf16x8_t kf = e4m3_to_bf16(kr[r][c][2 * q], kr[r][c][2 * q + 1]);
-#pragma unroll
-                                for (int n = 0; n < NR; ++n)
-                                    if (NR == 1 || n < blocks)
-                                        s[n][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, fq[n][2 * c + q], s[n][r], 0, 0, 0);
+                                s[0][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, fq[2 * c + q], s[0][r], 0, 0, 0);
                             }
                         }
                     }
@@ -922,14 +916,11 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                     else
                         values(std::false_type());
                 } else {
-                    bf16x8_t ph[NR], pl[NR];
+                    float x[8];
 #pragma unroll
-                    for (int n = 0; n < NR; ++n) {
-                        float x[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = s[n][e >> 2][e & 3];
-                        split_weights(x, ph[n], pl[n]);
-                    }
+                    for (int e = 0; e < 8; ++e) x[e] = s[0][e >> 2][e & 3];
+                    bf16x8_t ph, pl;
+                    split_weights(x, ph, pl);
                     // (rows 4 kg + 0..3 of 16: swapped pieces where kg & 2)
                     const unsigned char *vp = vbuf + (4 * kg + (l16 >> 2)) * S::VRS;
                     const int piece = (8 * (l16 & 3)) ^ ((kg & 2) << 3);
@@ -939,22 +930,18 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                             const unsigned char *x = vp + 32 * v + piece;
                             bf16x8_t vt = join8(lds_read_tr16(x), lds_read_tr16(x + 16 * S::VRS)), odd;
                             if constexpr (decltype(odd_tile)::value) take_odd(vt, odd);
+                            f32x4_t &o = acc[0][v];
+                            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, ph, o, 0, 0, 0);
+                            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pl, o, 0, 0, 0);
+                            if constexpr (decltype(odd_tile)::value) {
+                                bf16x8_t sees;
 #pragma unroll
-                            for (int n = 0; n < NR; ++n) {
-                                if (NR > 1 && n >= blocks) continue;
-                                f32x4_t &o = acc[n][v];
-                                o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, ph[n], o, 0, 0, 0);
-                                o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pl[n], o, 0, 0, 0);
-                                if constexpr (decltype(odd_tile)::value) {
-                                    bf16x8_t sees;
+                                for (int e = 0; e < 8; ++e)
+                                    sees[e] = of_key[e >> 2][e & 3] <= (lim[0] < 0 ? hi : lim[0]) ? (__bf16)1.f : (__bf16)0.f;
+                                const f32x4_t z = {0.f, 0.f, 0.f, 0.f};
+                                const f32x4_t c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, sees, z, 0, 0, 0);
 #pragma unroll
-                                    for (int e = 0; e < 8; ++e)
-                                        sees[e] = of_key[e >> 2][e & 3] <= (lim[n] < 0 ? hi : lim[n]) ? (__bf16)1.f : (__bf16)0.f;
-                                    const f32x4_t z = {0.f, 0.f, 0.f, 0.f};
-                                    const f32x4_t c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, sees, z, 0, 0, 0);
-#pragma unroll
-                                    for (int y = 0; y < 4; ++y) o[y] = c[y] > 0.f ? NAN : o[y];
-                                }
+                                for (int y = 0; y < 4; ++y) o[y] = c[y] > 0.f ? NAN : o[y];
                             }
                         }
                     };
