@@ -1,14 +1,15 @@
-"""The paged cache at its edges, against the binary64 oracle: values that are
-not finite behind scores so low that their weights are 0, and queries before
-their sequence's first token beside others that see such values.  Tolerances
-as in test_gpu_paged."""
+"""The paged cache at its edges, against binary64: values that are not finite
+behind scores so low that their weights are 0, queries before their sequence's
+first token beside others that see such values, routes without slots, the
+precision of the weights, and every row of large batches.  Tolerances as in
+test_gpu_paged."""
 import math
 
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_paged import DEV, TYPE, Cache, _check, _i32, _prefix_cache, _values, note, rrmod
+from test_gpu_paged import DEV, MANY, TYPE, Cache, _check, _i32, _prefix_cache, _values, note, rrmod
 
 pytestmark = pytest.mark.gpu
 
@@ -206,3 +207,64 @@ def test_weights_of_up_to_64_rows_are_not_rounded_to_one_bf16(case):
     O = call(Q, *c.args(), lse=lse, **kw, **c.kw())
     torch.cuda.synchronize()
     _check(O, lse, c.oracle(Q, **okw), d, max(lens), dtype, rows=16)
+
+
+def _reference(c, Q, pages, prefix):
+    """oracle.paged.attention without routes, on the device, a sequence at a time."""
+    B, nq, H, d = Q.shape
+    g, page = H // c.Hkv, c.page
+    O, W = (torch.zeros(Q.shape, dtype=torch.float64, device=DEV) for _ in range(2))
+    lse, S = torch.full((B, nq, H), -math.inf, dtype=torch.float64, device=DEV), torch.zeros((B, nq, H), device=DEV)
+    for b, n in enumerate(c.lens):
+        if n == 0:
+            continue
+        u = np.arange(n)
+        ids = c.table[b, u // page]
+        if prefix:
+            ids = np.where(u < prefix, np.asarray(pages)[np.minimum(u // page, len(pages) - 1)], ids)
+        ids, at = torch.from_numpy(ids).to(DEV), torch.from_numpy(u % page).to(DEV)
+        k, v = ((p.view(torch.uint8)[ids, :, at].view(p.dtype) if c.scales[0] is not None else p[ids, :, at]).double()
+                for p in (c.K, c.V))
+        if c.scales[0] is not None:
+            k, v = (x * torch.from_numpy(s).to(DEV).double()[:, None] for x, s in zip((k, v), c.scales))
+        k, v = k.transpose(0, 1).contiguous(), v.transpose(0, 1).contiguous()  # [H_kv, n, d]
+        q = Q[b].double().view(nq, c.Hkv, g, d).transpose(0, 1).reshape(c.Hkv, nq * g, d)
+        kt = k.transpose(1, 2).contiguous()
+        s = q @ kt / math.sqrt(d)
+        last = n - nq + torch.arange(nq, device=DEV).repeat_interleave(g)
+        seen = torch.arange(n, device=DEV) <= last[:, None]
+        s = s.masked_fill(~seen, -math.inf)
+        sums = torch.logsumexp(s, -1)
+        w = torch.where(seen, (s - sums[..., None]).exp(), 0.0)
+        size = ((q.abs() @ kt.abs()).masked_fill(~seen, 0.0)).amax(-1) / math.sqrt(d)
+
+        def rows(x):  # [H_kv, nq * g, ...] -> [nq, H, ...]
+            return x.unflatten(1, (nq, g)).transpose(0, 1).flatten(1, 2)
+
+        O[b], W[b], lse[b], S[b] = rows(w @ v), rows(w @ v.abs()), rows(sums), rows(size)
+    return tuple(x.double().cpu().numpy() for x in (O, lse, W, S))
+
+
+@pytest.mark.parametrize("case", MANY, ids=[c[0] for c in MANY])
+def test_every_row_of_large_batches(case):
+    """Every output and logarithm of batches of many sequences, items, rows and
+    splits, each within its own tolerance."""
+    rr = rrmod()
+    name, H, Hkv, d, dtype, cache, page, B, nq, longest, prefix = case
+    note(f"every row {case}")
+    rng = np.random.default_rng(B + d + nq + 1)
+    lens = rng.integers(0, longest, size=B)
+    lens[rng.random(B) < 0.2] = 0
+    lens[-1], lens[B // 2] = longest, 1
+    kw, pages = {}, None
+    if prefix:
+        c, pages = _prefix_cache(rng, Hkv, d, page, cache, prefix, lens.tolist())
+        kw = dict(prefix_pages=_i32(pages), n_prefix=prefix)
+    else:
+        c = Cache(rng, lens.tolist(), Hkv, d, page, cache)
+    Q = _values(rng, (B, nq, H, d), dtype, 2.0)
+    lse = torch.full((B, nq, H), 7.0, device=DEV)
+    call = rr.prefix_attention if prefix else rr.paged_attention
+    O = call(Q, *c.args(), lse=lse, **kw, **c.kw())
+    torch.cuda.synchronize()
+    _check(O, lse, _reference(c, Q, pages, prefix), d, max(c.lens), dtype, nq * H // Hkv * (B if prefix else 1))
