@@ -255,7 +255,8 @@ typedef enum {
     RR_KERNEL_ATTENTION = 7, /* sparse attention over routed chunks */
     RR_KERNEL_APPEND = 8,   /* new tokens into the paged cache */
     RR_KERNEL_PAGED = 9,    /* attention over the paged cache */
-    RR_KERNEL_JOIN = 10,    /* with a shared prefix: its parts joined */
+    RR_KERNEL_JOIN = 10,    /* its parts joined, where that is a launch of its own: always behind a
+                               shared prefix, otherwise for few items of many parts */
     RR_KERNEL_KINDS = 11
 } rr_kernel_kind;
 
@@ -356,8 +357,12 @@ rr_status rr_sparse_attention(const rr_attn_config *cfg, const void *Q, const vo
  * lengths [n_seqs] int32 counts each sequence's tokens, those new in this
  * step included, for the append and for the attention after it.  Entries of
  * page_table outside [0, n_pages) hold no page: nothing is written there and
- * no query sees their tokens.  Lengths are taken between 0 and max_pages *
- * page.  Sequences may share pages that none of them writes.
+ * no query sees their tokens.  A length is meant to lie between 0 and
+ * max_pages * page.  One outside is no fault: the attention takes the nearer
+ * end, and its queries as the newest tokens up to there; the append takes it as
+ * it is and leaves out the tokens without a place.  (So the queries of a
+ * sequence that has outgrown its table are off by what it lacks.)  Sequences
+ * may share pages that none of them writes.
  *
  * Types: dtype RR_BF16 with cache_dtype RR_BF16 or RR_E4M3, or RR_F32 with
  * RR_F32.  An RR_E4M3 cache holds x / scale of key head g, k_scale[g] for
@@ -438,7 +443,7 @@ size_t rr_paged_workspace_bytes(const rr_paged_config *cfg);
  * n_heads, d] stands at position p = lengths[b] - n_q + t of sequence b and
  * attends, with one softmax scaled by `scale`, to the sequence's tokens u <= p;
  * query head h reads key head h / (n_heads / n_kv_heads).  A query that sees
- * no token (p < 0) gets a zero output.
+ * no token (p < 0), or whose scores are all -INFINITY, gets a zero output.
  *   routes  [n_seqs * n_heads * n_q, k] int32 (row (b * n_heads + h) * n_q + t)
  *           page indices within the sequence: the query sees the tokens u <= p
  *           of those pages, of its first n_sink and of the n_recent up to the
@@ -468,8 +473,9 @@ rr_status rr_paged_attention(const rr_paged_config *cfg, const void *Q, const vo
 
 /* The same without routes for sequences whose first n_prefix tokens are the
  * same: prefix_pages [ceil(n_prefix / page)] int32 holds their pages (in the
- * last one the first n_prefix % page places, if any), which are read for the
- * whole batch at once; page_table serves the tokens from n_prefix on (its
+ * last one the first n_prefix % page places, if any), which are read once for
+ * up to 128 query rows of the batch on a key head (binary32: 32) in place of
+ * once a sequence; page_table serves the tokens from n_prefix on (its
  * earlier entries are not read, n_prefix may lie inside a page). */
 rr_status rr_prefix_attention(const rr_paged_config *cfg, const void *Q, const void *K_cache, const void *V_cache,
                               const int32_t *page_table, const int32_t *lengths, const int32_t *prefix_pages, void *O,

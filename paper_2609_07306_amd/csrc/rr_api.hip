@@ -955,6 +955,9 @@ namespace {
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 constexpr int32_t kMostGroups = (1 << 24) - 1;  // workgroups of 256 threads that a launch can have
+// Query rows of a call behind a prefix, which keeps two parts of each (17 GB of
+// d = 128 for so many); the join that reads them takes four rows a workgroup.
+constexpr int32_t kMostPrefixRows = (1 << 24) - 1;
 
 // What the append and the attention ask of a cache alike.
 rr_status check_cache(int32_t n_kv_heads, int32_t page, int32_t n_pages, int32_t max_pages, int32_t n_seqs, int32_t dtype,
@@ -976,7 +979,8 @@ rr_status paged_args(const rr_paged_config *cfg, rr::PagedArgs *out)
 {
     if (!cfg) return fail(RR_ERR_INVALID, "config is NULL");
     const rr_paged_config &c = *cfg;
-    rr_status st = check_cache(c.n_kv_heads, c.page, c.n_pages, c.max_pages, c.n_seqs, c.dtype, c.cache_dtype, c.k_scale, c.v_scale);
+    rr_status st = check_cache(c.n_kv_heads, c.page, c.n_pages, c.max_pages, c.n_seqs, c.dtype, c.cache_dtype, c.k_scale,
+                               c.v_scale);
     if (st != RR_OK) return st;
     if (c.n_heads < 1 || c.n_heads % c.n_kv_heads != 0)
         return fail(RR_ERR_INVALID, "n_heads must be a positive multiple of n_kv_heads");
@@ -989,9 +993,9 @@ rr_status paged_args(const rr_paged_config *cfg, rr::PagedArgs *out)
     if (!(c.scale >= 0.f) || std::isinf(c.scale)) return fail(RR_ERR_INVALID, "scale must be finite and >= 0");
     if (!rr::paged_supported(c.dtype, c.cache_dtype, c.d))
         return fail(RR_ERR_UNSUPPORTED, "attention over a paged cache supports d = 64 and 128, and 256 for bf16 queries");
-    // (with a prefix a row is a workgroup of 256 threads, and a launch has less than 2^32)
-    if ((int64_t)c.n_seqs * c.n_q > (c.n_prefix ? kMostGroups : INT32_MAX) / c.n_heads)
-        return fail(RR_ERR_UNSUPPORTED, "n_seqs * n_q * n_heads is too large: 2^31 - 1 query rows, 2^24 - 1 with a prefix, at most");
+    if ((int64_t)c.n_seqs * c.n_q > (c.n_prefix ? kMostPrefixRows : INT32_MAX) / c.n_heads)
+        return fail(RR_ERR_UNSUPPORTED,
+                    "n_seqs * n_q * n_heads is too large: 2^31 - 1 query rows, 2^24 - 1 with a prefix, at most");
     rr::PagedArgs a;
     std::memset(&a, 0, sizeof(a));
     a.k_scale = c.k_scale;
@@ -1011,7 +1015,8 @@ rr_status paged_args(const rr_paged_config *cfg, rr::PagedArgs *out)
     a.pd = rr::page_div(c.page);
     a.scale = c.scale > 0.f ? c.scale : 1.f / std::sqrt((float)c.d);
     if (!rr::paged_schedule(a, c.cache_dtype, c.d))
-        return fail(RR_ERR_UNSUPPORTED, "n_seqs * n_kv_heads * tiles of query rows * max_pages * page is too large: below 2^31 - 512 units of 128 keys");
+        return fail(RR_ERR_UNSUPPORTED, "n_seqs * n_kv_heads * tiles of query rows * max_pages * page is too large: "
+                                        "below 2^31 - 512 units of 128 keys");
     *out = a;
     return RR_OK;
 }
@@ -1056,7 +1061,8 @@ rr_status rr_cache_append(const rr_append_config *cfg, const void *K, const void
 {
     if (!cfg) return fail(RR_ERR_INVALID, "config is NULL");
     const rr_append_config &c = *cfg;
-    rr_status st = check_cache(c.n_kv_heads, c.page, c.n_pages, c.max_pages, c.n_seqs, c.dtype, c.cache_dtype, c.k_scale, c.v_scale);
+    rr_status st = check_cache(c.n_kv_heads, c.page, c.n_pages, c.max_pages, c.n_seqs, c.dtype, c.cache_dtype, c.k_scale,
+                               c.v_scale);
     if (st != RR_OK) return st;
     if (c.d < 8 || c.d > 1024 || c.d % 8 != 0) return fail(RR_ERR_INVALID, "d must be a multiple of 8 in [8, 1024]");
     if (c.rot < 0 || c.rot > c.d || c.rot % 2 != 0) return fail(RR_ERR_INVALID, "rot must be even and lie in [0, d]");
@@ -1123,7 +1129,8 @@ rr_status rr_paged_attention(const rr_paged_config *cfg, const void *Q, const vo
 {
     if (cfg && cfg->n_prefix != 0) return fail(RR_ERR_INVALID, "n_prefix is rr_prefix_attention's");
     if (cfg && (routes != nullptr) != (cfg->k > 0)) return fail(RR_ERR_INVALID, "routes and k go together");
-    return paged_call(cfg, Q, K_cache, V_cache, page_table, lengths, routes, nullptr, O, lse, workspace, workspace_bytes, hip_stream);
+    return paged_call(cfg, Q, K_cache, V_cache, page_table, lengths, routes, nullptr, O, lse, workspace, workspace_bytes,
+                      hip_stream);
 }
 
 rr_status rr_prefix_attention(const rr_paged_config *cfg, const void *Q, const void *K_cache, const void *V_cache,
@@ -1132,5 +1139,6 @@ rr_status rr_prefix_attention(const rr_paged_config *cfg, const void *Q, const v
 {
     if (cfg && cfg->n_prefix < 1) return fail(RR_ERR_INVALID, "n_prefix must be >= 1");
     if (!prefix_pages) return fail(RR_ERR_INVALID, "prefix_pages must be a device pointer");
-    return paged_call(cfg, Q, K_cache, V_cache, page_table, lengths, nullptr, prefix_pages, O, lse, workspace, workspace_bytes, hip_stream);
+    return paged_call(cfg, Q, K_cache, V_cache, page_table, lengths, nullptr, prefix_pages, O, lse, workspace,
+                      workspace_bytes, hip_stream);
 }

@@ -82,8 +82,11 @@ __device__ __forceinline__ void write_e4m3(uint8_t *p, const float (&x)[N], floa
         uint32_t o[N / 4];
 #pragma unroll
         for (int q = 0; q < N / 4; ++q) {
-            const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(clamp_e4m3(x[4 * q] / scale), clamp_e4m3(x[4 * q + 1] / scale), 0, false);
-            o[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp_e4m3(x[4 * q + 2] / scale), clamp_e4m3(x[4 * q + 3] / scale), lo, true);
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = clamp_e4m3(x[4 * q + e] / scale);
+            const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+            o[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
         }
         __builtin_memcpy(__builtin_assume_aligned(p, N), o, N);
     } else {

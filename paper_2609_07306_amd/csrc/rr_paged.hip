@@ -233,7 +233,8 @@ constexpr int64_t kCounterBytes = (int64_t)kPagedGrid * sizeof(uint32_t);
 
 static int64_t heads_bytes(const PagedArgs &a)
 {
-    return a.n_prefix || a.join_apart ? align256((a.prefix_items + (int64_t)a.n_seqs * a.items_per_seq) * (int64_t)sizeof(int4)) : 0;
+    const int64_t items = a.prefix_items + (int64_t)a.n_seqs * a.items_per_seq;
+    return a.n_prefix || a.join_apart ? align256(items * (int64_t)sizeof(int4)) : 0;
 }
 
 size_t paged_workspace_bytes(const PagedArgs &a, int d)
@@ -293,7 +294,8 @@ hipError_t launch_paged_join(const PagedArgs &a, int cache, int d, hipStream_t s
         many ? go(paged_join_kernel<D, F32, 4>, 4) : go(paged_join_kernel<D, F32, 1>, 1);
     };
     if (cache == CACHE_F32)
-        d == 64 ? width(std::true_type(), std::integral_constant<int, 64>()) : width(std::true_type(), std::integral_constant<int, 128>());
+        d == 64 ? width(std::true_type(), std::integral_constant<int, 64>())
+                : width(std::true_type(), std::integral_constant<int, 128>());
     else
         d == 64    ? width(std::false_type(), std::integral_constant<int, 64>())
         : d == 128 ? width(std::false_type(), std::integral_constant<int, 128>())

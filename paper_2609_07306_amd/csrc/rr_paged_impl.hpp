@@ -7,11 +7,14 @@
 // is cut into items: the query rows of one (sequence, key head) -- n_q tokens
 // times the heads that share the key head -- in tiles of rows; with routes one
 // query head's row, which has its own pages; with a shared prefix also tiles
-// over the rows of the whole batch against the prefix, which is what reads it
-// once for many sequences.  Every item is a number of units of 128 keys, and
-// the units of all items, in order, are cut into equal runs, one per
-// workgroup: lengths that differ a hundredfold leave no compute unit idle, and
-// one long sequence is spread over the card.  Lengths live on the device, so
+// over the rows of the whole batch against the prefix, which is so read once a
+// tile (up to 128 rows; 32 in binary32) in place of once a sequence.  Every
+// item is a number of units of 128 keys, and the units of all items, in order,
+// are cut into equal runs, one per workgroup: lengths that differ a hundredfold
+// leave no compute unit idle, and one long sequence is spread over the card.
+// (Not so along routes, where every item counts the units that its slots can
+// name, so that workgroups of short sequences end early; and of many new tokens,
+// whose row tiles all count the whole sequence.)  Lengths live on the device, so
 // every workgroup sums them to find its run.  An item that lies in several
 // runs leaves a part (m, l, sum) per run in the workspace, and the workgroup
 // that finishes the last of them joins them.  A second launch does where that
@@ -207,7 +210,8 @@ __device__ __forceinline__ bool find_run(const PagedArgs &a, Common &sh, int me,
     // against 20.5; of 32768: 29.8 against 34.9; eight of 1000 to 8000: 31.0
     // against 31.9)
     r.per_wg = (total + a.grid - 1) / a.grid;
-    if (!pre && !a.join_apart && a.n_seqs * a.items_per_seq <= kPagedGrid / 8) r.per_wg = max(r.per_wg, min(8, (total + kPagedGrid / 2 - 1) / (kPagedGrid / 2)));
+    if (!pre && !a.join_apart && a.n_seqs * a.items_per_seq <= kPagedGrid / 8)
+        r.per_wg = max(r.per_wg, min(8, (total + kPagedGrid / 2 - 1) / (kPagedGrid / 2)));
     if ((int64_t)me * r.per_wg >= total) return false;
     r.at = me * r.per_wg;
     r.end = total - r.at < r.per_wg ? total : r.at + r.per_wg;
@@ -399,8 +403,12 @@ __device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(0)" ::
 // Parts pass between workgroups on different XCDs, whose L2 caches do not
 // see each other's lines.  They are stored and loaded at device scope (sc1, as
 // a device-scope atomic is), which goes past the L2, so a part is there once
-// its stores have returned: a release fence would write the whole L2 back
-// instead, from every workgroup (measured: one sequence's decode 17 -> 72 us).
+// its stores have returned, which the storing wave waits for (vmcnt) before its
+// workgroup's relaxed atomic counts the part; the loads follow the atomic whose
+// value says that all are there.  That is what these instructions do on gfx950,
+// not what the memory model of the language promises, which asks for a release
+// and an acquire: a release fence would write the whole L2 back, from every
+// workgroup (measured: one sequence's decode 17 -> 72 us).
 // (Where a second launch reads them they are plain stores.)
 constexpr int kDeviceScope = 16;  // sc1 of a buffer instruction
 
@@ -416,7 +424,8 @@ template <int D>
 __device__ __forceinline__ void store_part(const PagedArgs &a, float *p, f32x4_t x, bool within)
 {
     if (within)
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), parts_of<D>(a), (int)((p - a.parts) * sizeof(float)), 0, kDeviceScope);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), parts_of<D>(a),
+                                               (int)((p - a.parts) * sizeof(float)), 0, kDeviceScope);
     else
         *reinterpret_cast<f32x4_t *>(p) = x;
 }
@@ -468,7 +477,8 @@ __device__ __forceinline__ void join_cut(const PagedArgs &a, Common &sh, unsigne
 #pragma unroll
                 for (int k = 0; k < kJoin; ++k)
                     if (i0 + k * per_row < n)
-                        add_part(__builtin_bit_cast(f32x4_t, y[k]), __uint_as_float(ml[k][0]), __uint_as_float(ml[k][1]), x, m, l);
+                        add_part(__builtin_bit_cast(f32x4_t, y[k]), __uint_as_float(ml[k][0]), __uint_as_float(ml[k][1]),
+                                 x, m, l);
             }
         }
         if (per_row > 1) {  // (uniform; one round, every thread)
@@ -480,7 +490,8 @@ __device__ __forceinline__ void join_cut(const PagedArgs &a, Common &sh, unsigne
             __syncthreads();
             if (sub == 0)
                 for (int i = 1; i < per_row; ++i)
-                    add_part(*reinterpret_cast<const f32x4_t *>(s_acc + (pg + i) * D + 4 * pl), sh.jm[pg + i], sh.jl[pg + i], x, m, l);
+                    add_part(*reinterpret_cast<const f32x4_t *>(s_acc + (pg + i) * D + 4 * pl), sh.jm[pg + i],
+                             sh.jl[pg + i], x, m, l);
         }
         if (r < rows.n && sub == 0) {
             int b, t, h;
@@ -521,10 +532,12 @@ struct Shape {
     static constexpr int KT = TY == CACHE_F32 ? 16 : 32;
     static constexpr int KR = KT / 16;
     static constexpr int PK = D * SIZE / 64;
-    // bytes of a row of the V buffer: 8 banks from one row to the next, so the
-    // transposed reads (8 rows x 32 bytes at a time) meet 64 different banks;
-    // rows 8 .. 15 of 16 hold their 16-byte pieces in swapped pairs, so the
-    // writes (16 rows x 16 bytes) do too
+    // bytes of a row of the V buffer: 8 banks from one row to the next; rows 8 ..
+    // 15 of 16 hold their 16-byte pieces in swapped pairs.  (Laid out so that the
+    // transposed reads, 8 rows x 32 bytes at a time, and the writes, 16 rows x 16
+    // bytes, spread over the banks; the counters show conflicts in three eighths
+    // of the cycles that LDS works all the same, which is not what these bodies
+    // wait for)
     static constexpr int VRS = 2 * D + 32;
     static constexpr int ORS = D + 4;       // floats of a row of the output buffer
     static constexpr int VBYTES = TY == CACHE_F32 ? 0 : KT * VRS;
@@ -784,8 +797,9 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                             if constexpr (TY == CACHE_BF16) {
                                 *reinterpret_cast<u32x4_t *>(dst + ((64 * c + 16 * kg) ^ swap)) = vr[r][c];
                             } else {
-                                *reinterpret_cast<bf16x8_t *>(dst + ((128 * c + 32 * kg) ^ swap)) = e4m3_to_bf16(vr[r][c][0], vr[r][c][1]);
-                                *reinterpret_cast<bf16x8_t *>(dst + ((128 * c + 32 * kg + 16) ^ swap)) = e4m3_to_bf16(vr[r][c][2], vr[r][c][3]);
+                                const int at = 128 * c + 32 * kg;
+                                *reinterpret_cast<bf16x8_t *>(dst + (at ^ swap)) = e4m3_to_bf16(vr[r][c][0], vr[r][c][1]);
+                                *reinterpret_cast<bf16x8_t *>(dst + ((at + 16) ^ swap)) = e4m3_to_bf16(vr[r][c][2], vr[r][c][3]);
                             }
                         }
                     }
@@ -1011,9 +1025,10 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
                     f32x4_t x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int v = 0; v < NW; ++v) {
-                        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(reinterpret_cast<float *>(smem + v * S::WAVE) + q * S::ORS + f);
+                        const float *ov = reinterpret_cast<const float *>(smem + v * S::WAVE);
+                        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(ov + q * S::ORS + f);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(wt[v], y[i], x[i]);  // (0 times NaN stays, as in add_part)
+                        for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(wt[v], y[i], x[i]);  // (0 * NaN stays, see add_part)
                     }
                     if (sink.last_word)
                         write_four<F32>(a.O, orow * D + f, x * inv);
@@ -1220,7 +1235,8 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                         const int key0 = (w * 64 + q * S::T) / S::PPR;  // (the wave's first)
                         const int tok = base + min(p + key0, pb - 1), ch = a.pd.div(tok), phys = uniform(sh.phys[ch - ch0]);
                         const int place = tok - ch * a.pd.page & ~(S::KPW - 1);
-                        row = pool_row(max(phys, 0), a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE + lane / S::PPR * (D * S::SIZE);
+                        row = pool_row(max(phys, 0), a.n_kv_heads, g, a.pd.page, place, D) * S::SIZE +
+                              lane / S::PPR * (D * S::SIZE);
                         seen = p + key < pb && phys >= 0;
                     } else {
                         const int tok = base + min(p + key, pb - 1), ch = a.pd.div(tok);
@@ -1256,7 +1272,8 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
 #pragma unroll
                     for (int q = 0; q < S::PT; ++q) {
                         const int x = tid + q * S::T, key = x / S::PPR, c = x % S::PPR;
-                        unsigned char *kd = smem + buf * S::BUF + key * S::KRS, *vd = smem + buf * S::BUF + S::KB * S::KRS + key * S::VRS;
+                        unsigned char *kd = smem + buf * S::BUF + key * S::KRS;
+                        unsigned char *vd = smem + buf * S::BUF + S::KB * S::KRS + key * S::VRS;
                         // (a value that no row sees is 0: memory that was never written may hold NaN)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) vr[q][e] = (keep >> q) & 1u ? vr[q][e] : 0u;
@@ -1270,10 +1287,11 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
             // ... the same where the rows are in LDS already
             auto clear = [&](int p, int buf) {
                 const u32x4_t z = {0u, 0u, 0u, 0u};
+                unsigned char *vt = smem + buf * S::BUF + S::KB * S::KRS;
                 for (int x = tid; x < S::KB * (D / 8); x += S::T) {
                     const int key = x / (D / 8);
                     if (p + key >= pb || (holes && !there(base + p + key)))
-                        *reinterpret_cast<u32x4_t *>(smem + buf * S::BUF + S::KB * S::KRS + key * S::VRS + 16 * (x % (D / 8))) = z;
+                        *reinterpret_cast<u32x4_t *>(vt + key * S::VRS + 16 * (x % (D / 8))) = z;
                 }
             };
             // one 32-key block of a staged tile; MASKED: some row does not see
@@ -1434,7 +1452,8 @@ __device__ __forceinline__ void wide_body(const PagedArgs &a, Common &sh, unsign
                 for (int mb = 0; mb < NMB; ++mb)
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        ob[(4 * mb + q) * 64] = f32x4_t{acc[mb][4 * q], acc[mb][4 * q + 1], acc[mb][4 * q + 2], acc[mb][4 * q + 3]};
+                        ob[(4 * mb + q) * 64] =
+                            f32x4_t{acc[mb][4 * q], acc[mb][4 * q + 1], acc[mb][4 * q + 2], acc[mb][4 * q + 3]};
                 if (hh == 0) {
                     sh.m[rb][l32] = m_run;
                     sh.l[rb][l32] = l_run;

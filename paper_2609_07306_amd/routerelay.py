@@ -643,7 +643,7 @@ def paged_attention(Q, K_cache, V_cache, page_table, lengths, routes=None, n_sin
 def prefix_attention(Q, K_cache, V_cache, page_table, lengths, prefix_pages, n_prefix, scale=0.0, k_scale=None,
                      v_scale=None, out=None, lse=None, workspace=None, stream=None):
     """rr_prefix_attention: paged_attention (without routes) for sequences that
-    begin with the same n_prefix tokens, which are read once for the batch from
+    begin with the same n_prefix tokens, which are read for many of them at once from
     prefix_pages [ceil(n_prefix / page)] int32."""
     config = _paged_config(Q, K_cache, V_cache, page_table, None, 0, 0, n_prefix, scale, k_scale, v_scale, lengths)
     dev = _device_of((Q, K_cache, V_cache, page_table, lengths, prefix_pages, k_scale, v_scale, out, lse, workspace))
