@@ -268,3 +268,36 @@ def test_every_row_of_large_batches(case):
     O = call(Q, *c.args(), lse=lse, **kw, **c.kw())
     torch.cuda.synchronize()
     _check(O, lse, _reference(c, Q, pages, prefix), d, max(c.lens), dtype, nq * H // Hkv * (B if prefix else 1))
+
+
+def test_calls_at_once():
+    """Calls of different shapes on two streams with a workspace each, not
+    waiting for each other, give what they give alone."""
+    rr = rrmod()
+    note("calls at once")
+    rng = np.random.default_rng(41)
+    calls = []
+    for H, Hkv, d, cache, lens, nq, prefix in ((32, 8, 128, "bf16", [20000, 3, 700], 1, 0), (16, 2, 128, "bf16", [9000] * 3, 8, 0),
+                                               (8, 2, 64, "e4m3", [1300 + i for i in range(20)], 1, 1008),
+                                               (4, 2, 64, "f32", [6000, 40], 2, 0)):
+        if prefix:
+            c, pages = _prefix_cache(rng, Hkv, d, 16, cache, prefix, [x - prefix for x in lens])
+        else:
+            c, pages = Cache(rng, lens, Hkv, d, 16, cache), None
+        Q = _values(rng, (len(lens), nq, H, d), "f32" if cache == "f32" else "bf16", 2.0)
+        more = dict(prefix_pages=_i32(pages), n_prefix=prefix) if prefix else {}
+        more.update(c.kw())
+        ws = rr.paged_workspace(Q, c.K, _i32(c.table), n_prefix=prefix)
+        call = rr.prefix_attention if prefix else rr.paged_attention
+        args = c.args()
+        calls.append((lambda call=call, Q=Q, args=args, more=more, ws=ws, **kw: call(Q, *args, workspace=ws, **more, **kw),
+                      torch.empty_like(Q)))
+    want = [call() for call, _ in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(20):
+        for (call, out), s in zip(calls, streams):
+            call(out=out, stream=s)
+    torch.cuda.synchronize()
+    for (_, out), w in zip(calls, want):
+        assert torch.equal(out, w)
