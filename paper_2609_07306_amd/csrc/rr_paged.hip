@@ -162,8 +162,8 @@ bool paged_schedule(PagedArgs &a, int cache, int d)
     // their features).  32 heads on 8, d = 128, one launch and two:
     //   1 sequence of 8192 tokens, 4 rows: 15.6 and 17.9 us; 16 rows: 21.4 and
     //   19.0; 128 rows: 86 and 34; 8 sequences of 1000 to 8000, 32 rows: 58.7
-    //   and 42; 32 of 1000 to 4000, 64 rows: 93 and 81; 1 of 2048, all of them
-    //   new: 83 and 99
+    //   and 42; 32 of 1000 to 4000, 64 rows: 93 and 81 (both with a weight in one
+    //   number, two add 1.5 us); 1 of 2048, all of them new: 83 and 99
     // (So a call that takes two has less than 2^25 rows.)
     const int64_t items = (int64_t)a.n_seqs * a.items_per_seq;
     const int64_t parts = (items <= kPagedGrid / 8 ? kPagedGrid / 2 : most_wg) / items + 1;  // (as the runs are cut, find_run)

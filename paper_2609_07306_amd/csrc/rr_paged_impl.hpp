@@ -1060,8 +1060,8 @@ __device__ __forceinline__ void narrow_body(const PagedArgs &a, Common &sh, unsi
 //
 // Bound by the products and the softmax's vector instructions, which overlap
 // little, and by the tiles' way from the L2 to LDS: 2048 new tokens behind
-// 6144 (d = 128, 32 heads on 8) 311 us, 1280 rows a key head on a prefix of
-// 32768 tokens 235 us, 730 TFLOP/s.  Without the loads it would take 195 us.
+// 6144 (d = 128, 32 heads on 8) 306 us, 1280 rows a key head on a prefix of
+// 32768 tokens 240 us, 715 TFLOP/s.  Without the loads it would take 195 us.
 // TWO: a weight enters the value product as two bf16 numbers, as in the narrow
 // body, else rounded to one (paged_schedule says which, with the times of both).
 // Measured and not kept: which of them decided at run time (the rows of 128-row
