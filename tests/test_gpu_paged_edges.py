@@ -3,6 +3,7 @@ behind scores so low that their weights are 0, queries before their sequence's
 first token beside others that see such values, routes without slots, the
 precision of the weights, and every row of large batches.  Tolerances as in
 test_gpu_paged."""
+import functools
 import math
 
 import numpy as np
@@ -46,8 +47,9 @@ LOW = [
 ]
 
 
-@pytest.mark.parametrize("case,infinite_keys", [pytest.param(c, x, id=c[0] + ("_infinite_keys" if x else "")) for c in LOW
-                                                for x in (False, True) if not (x and c[5] == "e4m3")])
+@pytest.mark.parametrize("case,infinite_keys", [
+    pytest.param(c, x, id=c[0] + ("_infinite_keys" if x else "")) for c in LOW for x in (False, True)
+    if not (x and c[5] == "e4m3")])
 def test_values_that_are_not_finite_behind_low_scores(case, infinite_keys):
     """Where a query sees a value that is not finite that feature of its output
     is not either, also if the score is more than 350 below the others, so that
@@ -277,9 +279,9 @@ def test_calls_at_once():
     note("calls at once")
     rng = np.random.default_rng(41)
     calls = []
-    for H, Hkv, d, cache, lens, nq, prefix in ((32, 8, 128, "bf16", [20000, 3, 700], 1, 0), (16, 2, 128, "bf16", [9000] * 3, 8, 0),
-                                               (8, 2, 64, "e4m3", [1300 + i for i in range(20)], 1, 1008),
-                                               (4, 2, 64, "f32", [6000, 40], 2, 0)):
+    shapes = ((32, 8, 128, "bf16", [20000, 3, 700], 1, 0), (16, 2, 128, "bf16", [9000] * 3, 8, 0),
+              (8, 2, 64, "e4m3", [1300 + i for i in range(20)], 1, 1008), (4, 2, 64, "f32", [6000, 40], 2, 0))
+    for H, Hkv, d, cache, lens, nq, prefix in shapes:
         if prefix:
             c, pages = _prefix_cache(rng, Hkv, d, 16, cache, prefix, [x - prefix for x in lens])
         else:
@@ -290,8 +292,7 @@ def test_calls_at_once():
         ws = rr.paged_workspace(Q, c.K, _i32(c.table), n_prefix=prefix)
         call = rr.prefix_attention if prefix else rr.paged_attention
         args = c.args()
-        calls.append((lambda call=call, Q=Q, args=args, more=more, ws=ws, **kw: call(Q, *args, workspace=ws, **more, **kw),
-                      torch.empty_like(Q)))
+        calls.append((functools.partial(call, Q, *args, workspace=ws, **more), torch.empty_like(Q)))
     want = [call() for call, _ in calls]
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in calls]
