@@ -240,9 +240,10 @@ rr_status rr_ledger_relay_stats(const rr_ledger *ledger, float *alpha, float *be
  * and returns, per kernel kind, the summed duration in milliseconds and the
  * number of launches.  total_ms and launches are caller arrays of n_kinds
  * entries (each may be NULL); RR_KERNEL_KINDS entries are written (of n_kinds
- * = 8, the kinds before RR_KERNEL_APPEND that an earlier header had, those),
- * and any other n_kinds < RR_KERNEL_KINDS with a non-NULL array returns
- * RR_ERR_INVALID without writing anything (profiling then stays on).
+ * = 8 or 11, the kinds before RR_KERNEL_APPEND or RR_KERNEL_ROTATE that earlier
+ * headers had, those), and any other n_kinds < RR_KERNEL_KINDS with a non-NULL
+ * array returns RR_ERR_INVALID without writing anything (profiling then stays
+ * on).
  * Process-wide; not for concurrent use from several threads. */
 typedef enum {
     RR_KERNEL_FULL = 0,     /* GEMM + TopK, full routing */
@@ -257,7 +258,11 @@ typedef enum {
     RR_KERNEL_PAGED = 9,    /* attention over the paged cache */
     RR_KERNEL_JOIN = 10,    /* its parts joined, where that is a launch of its own: always behind a
                                shared prefix, otherwise for few items of many parts */
-    RR_KERNEL_KINDS = 11
+    RR_KERNEL_ROTATE = 11,  /* rows rotated by position */
+    RR_KERNEL_VERIFY = 12,  /* drafts verified */
+    RR_KERNEL_PAGES = 13,   /* page tables: forked, resized, compacted */
+    RR_KERNEL_COPY = 14,    /* pages copied */
+    RR_KERNEL_KINDS = 15
 } rr_kernel_kind;
 
 rr_status rr_profile_start(void);
@@ -411,6 +416,51 @@ rr_status rr_cache_append(const rr_append_config *cfg, const void *K, const void
                           const int32_t *seq_start, const int32_t *lengths, const int32_t *page_table,
                           const double *freqs, void *K_cache, void *V_cache, void *Q_out, void *hip_stream);
 
+/* Positions of tokens on several axes (time, height and width of an image's or
+ * a film's token; a text token has the same one on all of them).  Frequency j
+ * takes the position on axis[j]; an axis outside [0, n_axes) takes none, and
+ * its partners stay as they are. */
+typedef struct {
+    const void *positions;  /* [n_axes, n_tokens] int32, or binary32 where real is 1 */
+    const int32_t *axis;    /* [rot / 2]; NULL: the first axis for all */
+    int32_t n_axes;         /* >= 1 */
+    int32_t real;           /* 1: positions are binary32 numbers */
+} rr_axes;
+
+/* rr_cache_append with the new tokens' own positions on several axes in place
+ * of their places in the sequences: a = position * freqs[j].  Where a token's
+ * rows go, lengths alone say, as there.  axes NULL: rr_cache_append.  Returns
+ * as rr_cache_append, RR_ERR_INVALID for bad axes (checked where rot > 0). */
+rr_status rr_cache_append_axes(const rr_append_config *cfg, const void *K, const void *V, const void *Q,
+                               const int32_t *seq_start, const int32_t *lengths, const int32_t *page_table,
+                               const double *freqs, const rr_axes *axes, void *K_cache, void *V_cache, void *Q_out,
+                               void *hip_stream);
+
+typedef struct {
+    int32_t n_heads;
+    int32_t n_tokens;     /* (0: nothing to do), below 2^24 */
+    int32_t d;            /* a multiple of 8, at most 1024 */
+    int32_t rot;          /* leading features that are rotated: even, 0 .. d */
+    int32_t interleaved;  /* partners, as in rr_append_config */
+    int32_t inverse;      /* 1: back, by -a */
+    int32_t dtype;        /* of X and Y: RR_F32 or RR_BF16 */
+    int32_t reserved;     /* must be 0 */
+    int64_t x_token, x_head;  /* elements from a token's row to the next one's, from a head's to the next one's, >= 0 */
+    int64_t y_token, y_head;  /* (of Y at least d) */
+} rr_rotate_config;
+
+/* Rotates rows of queries or keys that no cache takes: row (token i, head h) of
+ * X, at X + i * x_token + h * x_head, goes to the same place of Y, its first
+ * rot features rotated as rr_cache_append does, by the positions of `axes`
+ * (tokens in order; n_axes = 1 with axis NULL for a text's).  The other layout
+ * of this library, [n_heads, n_tokens, d], has x_head = n_tokens * d and x_token
+ * = d.  With inverse = 1 rows are turned back, which is also the gradient of
+ * the rotation.  Y may be X where its strides are X's, and must not overlap it
+ * otherwise.  Returns RR_ERR_INVALID for bad sizes, types, strides or NULL
+ * pointers, RR_ERR_UNSUPPORTED for 2^24 tokens or more. */
+rr_status rr_rotate(const rr_rotate_config *cfg, const void *X, const double *freqs, const rr_axes *axes, void *Y,
+                    void *hip_stream);
+
 typedef struct {
     int32_t n_heads;
     int32_t n_kv_heads;
@@ -480,6 +530,127 @@ rr_status rr_paged_attention(const rr_paged_config *cfg, const void *Q, const vo
 rr_status rr_prefix_attention(const rr_paged_config *cfg, const void *Q, const void *K_cache, const void *V_cache,
                               const int32_t *page_table, const int32_t *lengths, const int32_t *prefix_pages, void *O,
                               float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Which pages sequences hold.  refs [n_pages] int32 counts, for every page, the
+ * entries of page_table that hold it, and whatever else the caller counts there
+ * to keep a page (a prefix that no sequence holds at the moment, pages that are
+ * never to be used).  A page with refs 0 is free.  The calls keep the counts,
+ * and everything on the device, so that a step (fork, resize, append, attention,
+ * verification) needs no host and can be captured.  Tables and counts that do
+ * not agree give tables that do not, but no access out of bounds.
+ * ---------------------------------------------------------------------- */
+
+/* Forks, reorders and ends sequences: row b of page_table [n_seqs, max_pages]
+ * and lengths[b] become what row parent[b] and its length were before the call
+ * (all rows at once); parent[b] = b leaves it as it is, a parent outside [0,
+ * n_seqs) empties it (entries -1, length 0).  No page is copied: the sequences
+ * share them, rr_cache_resize copies the one that is written.  refs follow.
+ * Returns RR_ERR_INVALID for bad sizes or NULL pointers, RR_ERR_UNSUPPORTED for
+ * more than 4096 sequences or 2^24 entries of a row or more. */
+rr_status rr_cache_fork(int32_t n_seqs, int32_t max_pages, int32_t n_pages, const int32_t *parent, int32_t *page_table,
+                        int32_t *lengths, int32_t *refs, void *hip_stream);
+
+/* The pools of all layers that one page table serves: K and V caches of one
+ * shape [n_pages, n_kv_heads, page, d] and type. */
+typedef struct {
+    int32_t n_kv_heads;
+    int32_t d;            /* a multiple of 8, at most 1024 */
+    int32_t page;
+    int32_t n_pages;
+    int32_t cache_dtype;
+    int32_t n_pools;      /* K and V of every layer, 1 .. 4096 */
+    int32_t max_pages;
+    int32_t n_seqs;
+    int32_t n_new;        /* rr_cache_resize: new tokens of every sequence, where new_tokens is NULL */
+    int32_t reserved;     /* must be 0 */
+} rr_pages_config;
+
+/* Bytes of workspace of rr_cache_resize and rr_cache_compact (of n_pages; it
+ * need not be cleared).  0: n_pages is not valid.  Calls that may run at the
+ * same time need one each. */
+size_t rr_pages_workspace_bytes(int32_t n_pages);
+
+/* Makes the page table follow the lengths, which count the new tokens that are
+ * about to be appended, as there (and are taken between 0 and what the table
+ * can hold).  In this order:
+ *   - entries past a sequence's last page let go of theirs and become -1: of
+ *     drafts that were not taken, of a sequence that ended (length 0);
+ *   - entries of its newest tokens (new_tokens[b], or n_new, of them; fewer
+ *     than none count as none), by sequence and then by entry: one that holds
+ *     no page gets the lowest free one.  One whose page has other holders
+ *     (refs > 1 at that moment) gets the lowest free one too, lets go of the
+ *     other, and the places before its first new token are copied in all
+ *     pools; the rest of the page holds what it held.
+ * Earlier entries stay as they are.  Where no page is free the entry stays as
+ * it was and missing[b] (optional, [n_seqs] int32; written for every sequence)
+ * counts it: such a sequence must not be appended to, which could write into a
+ * page that others hold.  The call made again, once pages are free, provides
+ * for it.
+ *   pools   host array of n_pools device pointers, 16-byte aligned
+ * Returns RR_ERR_INVALID for bad sizes, types, NULL or unaligned pointers or a
+ * workspace too small, RR_ERR_UNSUPPORTED for pages of more than 2^30 bytes, or
+ * where n_seqs times the 1024 entries begun of a row are 2^24 or more. */
+rr_status rr_cache_resize(const rr_pages_config *cfg, void *const *pools, const int32_t *new_tokens, const int32_t *lengths,
+                          int32_t *page_table, int32_t *refs, int32_t *missing, void *workspace, size_t workspace_bytes,
+                          void *hip_stream);
+
+/* Moves the used pages together: with n of them used (refs not 0), those from
+ * page n on take the free ones before it, the lowest the lowest, in all pools;
+ * page_table, refs and everything held there follow.  Pages from n on are free
+ * then, what they hold is left as it is.
+ *   new_ids  [n_pages] int32: the page that each page's tokens are in now, -1
+ *            for one that was free (for what holds pages besides the table)
+ *   n_used   int32: n
+ * Returns as rr_cache_resize (n_new is not read). */
+rr_status rr_cache_compact(const rr_pages_config *cfg, void *const *pools, int32_t *page_table, int32_t *refs,
+                           int32_t *new_ids, int32_t *n_used, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Drafted tokens.
+ * ---------------------------------------------------------------------- */
+
+typedef struct {
+    int32_t n_seqs;
+    int32_t n_drafts;      /* most drafts of a sequence (0: tokens are drawn, nothing is verified) */
+    int32_t vocab;         /* below 2^24 */
+    int32_t dtype;         /* of P and Q: RR_F32 or RR_BF16 */
+    int64_t p_seq, p_row;  /* elements from a sequence's first row of P to the next one's, from a row to the next, >= 0 */
+    int64_t q_seq, q_row;
+} rr_verify_config;
+
+/* Bytes of workspace of rr_verify_drafts (0: the config is not valid).  It is
+ * filled with zeros before its first use, and calls leave the part of it that
+ * has to be zero (the first 65536 bytes) at zero, so that it serves any calls
+ * that follow one another.  Calls that may run at the same time need one each. */
+size_t rr_verify_workspace_bytes(const rr_verify_config *cfg);
+
+/* Verifies drafted tokens by rejection from given uniform numbers, so that what
+ * is kept is distributed as if drawn from the target: P [n_seqs, n_drafts + 1,
+ * vocab] holds the target's probabilities at the drafts' places and at the one
+ * behind them, Q [n_seqs, n_drafts, vocab] those that the drafts were drawn
+ * with (NULL: they were not drawn, Q is 1 at each draft), drafts [n_seqs,
+ * n_drafts] int32 the drafts, of which n_drafts[b] count (NULL: all; taken
+ * between 0 and n_drafts).
+ * Draft i of sequence b is taken, if all before it are, iff uniforms[b][i] *
+ * Q[b][i][x] < P[b][i][x] (x the draft; one outside the vocabulary is not).
+ * One more token is drawn from r = max(P[b][a] - Q[b][a], 0), with a the first
+ * draft that is not taken, or from r = P[b][a] where all a of them are or where
+ * nothing of r is above 0: the lowest v with r(v) > 0 and r(0) + ... + r(v) >
+ * uniforms[b][n_drafts] * (sum of r), or the last one with r(v) > 0 where there
+ * is none.  r need not add up to one; what is not a positive finite number
+ * counts as 0 in it, and the token is -1 where P[b][a] has no other.
+ * Products, differences and sums in binary64.
+ *   uniforms  [n_seqs, n_drafts + 1] binary32, in [0, 1)
+ *   accepted  [n_seqs] int32: drafts that were taken
+ *   tokens    [n_seqs, n_drafts + 1] int32: those, then the drawn one, then -1
+ *   lengths   optional [n_seqs] int32, changed in place: less the drafts that
+ *             were not taken (as a cache counts them to which all were appended)
+ * Returns RR_ERR_INVALID for bad sizes, types, strides, NULL pointers or a
+ * workspace too small, RR_ERR_UNSUPPORTED for a vocabulary of 2^24 or more. */
+rr_status rr_verify_drafts(const rr_verify_config *cfg, const void *P, const void *Q, const int32_t *drafts,
+                           const int32_t *n_drafts, const float *uniforms, int32_t *lengths, int32_t *accepted,
+                           int32_t *tokens, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

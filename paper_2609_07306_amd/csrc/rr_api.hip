@@ -13,7 +13,10 @@
 #include "routerelay.h"
 #include "rr_internal.hpp"
 #include "rr_paged.hpp"
+#include "rr_pages.hpp"
 #include "rr_rescore.hpp"
+#include "rr_rows.hpp"
+#include "rr_verify.hpp"
 
 struct rr_ledger {
     rr_config cfg;
@@ -834,8 +837,8 @@ rr_status rr_profile_start(void)
 
 rr_status rr_profile_stop(double *total_ms, int64_t *launches, int32_t n_kinds)
 {
-    // (or the kinds of the header before the paged cache's, for programs built against it)
-    const int32_t kinds = n_kinds == RR_KERNEL_APPEND ? n_kinds : RR_KERNEL_KINDS;
+    // (or the kinds of an earlier header, for programs built against it)
+    const int32_t kinds = n_kinds == RR_KERNEL_APPEND || n_kinds == RR_KERNEL_ROTATE ? n_kinds : RR_KERNEL_KINDS;
     if ((total_ms || launches) && n_kinds < kinds)
         return fail(RR_ERR_INVALID, "rr_profile_stop: the arrays must hold RR_KERNEL_KINDS entries");
     g_prof.on = false;
@@ -974,6 +977,19 @@ rr_status check_cache(int32_t n_kv_heads, int32_t page, int32_t n_pages, int32_t
     return RR_OK;
 }
 
+rr_status check_axes(const rr_axes *axes, int32_t n_tokens)
+{
+    if (axes->n_axes < 1) return fail(RR_ERR_INVALID, "n_axes must be >= 1");
+    if (axes->real != 0 && axes->real != 1) return fail(RR_ERR_INVALID, "rr_axes.real must be 0 or 1");
+    if (n_tokens > 0 && !axes->positions) return fail(RR_ERR_INVALID, "positions must be a device pointer");
+    return RR_OK;
+}
+
+rr::Axes axes_of(const rr_axes *axes, int32_t n_tokens)
+{
+    return rr::Axes{axes->positions, axes->axis, n_tokens, axes->n_axes, axes->real};
+}
+
 // The launch arguments of an attention call, its pointers apart.
 rr_status paged_args(const rr_paged_config *cfg, rr::PagedArgs *out)
 {
@@ -1059,6 +1075,15 @@ rr_status rr_cache_append(const rr_append_config *cfg, const void *K, const void
                           const int32_t *seq_start, const int32_t *lengths, const int32_t *page_table,
                           const double *freqs, void *K_cache, void *V_cache, void *Q_out, void *hip_stream)
 {
+    return rr_cache_append_axes(cfg, K, V, Q, seq_start, lengths, page_table, freqs, nullptr, K_cache, V_cache, Q_out,
+                                hip_stream);
+}
+
+rr_status rr_cache_append_axes(const rr_append_config *cfg, const void *K, const void *V, const void *Q,
+                               const int32_t *seq_start, const int32_t *lengths, const int32_t *page_table,
+                               const double *freqs, const rr_axes *axes, void *K_cache, void *V_cache, void *Q_out,
+                               void *hip_stream)
+{
     if (!cfg) return fail(RR_ERR_INVALID, "config is NULL");
     const rr_append_config &c = *cfg;
     rr_status st = check_cache(c.n_kv_heads, c.page, c.n_pages, c.max_pages, c.n_seqs, c.dtype, c.cache_dtype, c.k_scale,
@@ -1083,9 +1108,11 @@ rr_status rr_cache_append(const rr_append_config *cfg, const void *K, const void
         return fail(RR_ERR_INVALID, "Q_out may be Q only where ldq is n_heads * d");
     if (!seq_start && c.n_tokens % c.n_seqs != 0)
         return fail(RR_ERR_INVALID, "n_tokens must be a multiple of n_seqs where seq_start is NULL");
+    if (axes && c.rot > 0 && (st = check_axes(axes, c.n_tokens)) != RR_OK) return st;
     if (c.n_tokens == 0) return RR_OK;
     rr::AppendArgs a;
     std::memset(&a, 0, sizeof(a));
+    if (axes && c.rot > 0) a.axes = axes_of(axes, c.n_tokens);
     a.Q = Q;
     a.K = K;
     a.V = V;
@@ -1141,4 +1168,230 @@ rr_status rr_prefix_attention(const rr_paged_config *cfg, const void *Q, const v
     if (!prefix_pages) return fail(RR_ERR_INVALID, "prefix_pages must be a device pointer");
     return paged_call(cfg, Q, K_cache, V_cache, page_table, lengths, nullptr, prefix_pages, O, lse, workspace,
                       workspace_bytes, hip_stream);
+}
+
+// --------------------------------------------------- rows, pages, drafts
+
+rr_status rr_rotate(const rr_rotate_config *cfg, const void *X, const double *freqs, const rr_axes *axes, void *Y,
+                    void *hip_stream)
+{
+    if (!cfg) return fail(RR_ERR_INVALID, "config is NULL");
+    const rr_rotate_config &c = *cfg;
+    if (c.n_heads < 1) return fail(RR_ERR_INVALID, "n_heads must be >= 1");
+    if (c.n_tokens < 0) return fail(RR_ERR_INVALID, "n_tokens must be >= 0");
+    if (c.n_tokens > kMostGroups) return fail(RR_ERR_UNSUPPORTED, "n_tokens must be below 2^24");
+    if (c.d < 8 || c.d > 1024 || c.d % 8 != 0) return fail(RR_ERR_INVALID, "d must be a multiple of 8 in [8, 1024]");
+    if (c.rot < 0 || c.rot > c.d || c.rot % 2 != 0) return fail(RR_ERR_INVALID, "rot must be even and lie in [0, d]");
+    if (c.interleaved != 0 && c.interleaved != 1) return fail(RR_ERR_INVALID, "interleaved must be 0 or 1");
+    if (c.inverse != 0 && c.inverse != 1) return fail(RR_ERR_INVALID, "inverse must be 0 or 1");
+    if (c.dtype != RR_F32 && c.dtype != RR_BF16) return fail(RR_ERR_INVALID, "dtype must be RR_F32 or RR_BF16");
+    if (c.reserved != 0) return fail(RR_ERR_INVALID, "rr_rotate_config.reserved must be 0");
+    if (c.x_token < 0 || c.x_head < 0) return fail(RR_ERR_INVALID, "x_token and x_head must be >= 0");
+    if ((c.n_tokens > 1 && c.y_token < c.d) || (c.n_heads > 1 && c.y_head < c.d))
+        return fail(RR_ERR_INVALID, "rows of Y must be at least d elements apart");
+    if (c.rot > 0) {
+        if (!freqs) return fail(RR_ERR_INVALID, "freqs must hold rot / 2 frequencies");
+        if (!axes) return fail(RR_ERR_INVALID, "axes must be given");
+        rr_status st = check_axes(axes, c.n_tokens);
+        if (st != RR_OK) return st;
+    }
+    if (c.n_tokens == 0) return RR_OK;
+    if (!X || !Y) return fail(RR_ERR_INVALID, "X and Y must be device pointers");
+    if (X == Y && ((c.n_tokens > 1 && c.x_token != c.y_token) || (c.n_heads > 1 && c.x_head != c.y_head)))
+        return fail(RR_ERR_INVALID, "Y may be X only where its strides are X's");
+    rr::RotateArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.X = X;
+    a.Y = Y;
+    a.freqs = freqs;
+    if (c.rot > 0) a.axes = axes_of(axes, c.n_tokens);
+    a.x_token = c.n_tokens > 1 ? c.x_token : 0;
+    a.x_head = c.n_heads > 1 ? c.x_head : 0;
+    a.y_token = c.n_tokens > 1 ? c.y_token : 0;
+    a.y_head = c.n_heads > 1 ? c.y_head : 0;
+    a.n_heads = c.n_heads;
+    a.n_tokens = c.n_tokens;
+    a.d = c.d;
+    a.rot = c.rot;
+    a.sign = c.inverse ? -1.f : 1.f;
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    hipError_t e = timed(RR_KERNEL_ROTATE, stream, [&] { return rr::launch_rotate(a, c.dtype, c.interleaved != 0, stream); });
+    return e == hipSuccess ? RR_OK : hip_fail(e, "rotation launch");
+}
+
+rr_status rr_cache_fork(int32_t n_seqs, int32_t max_pages, int32_t n_pages, const int32_t *parent, int32_t *page_table,
+                        int32_t *lengths, int32_t *refs, void *hip_stream)
+{
+    if (n_seqs < 1 || max_pages < 1 || n_pages < 1) return fail(RR_ERR_INVALID, "n_seqs, max_pages and n_pages must be >= 1");
+    if (!parent || !page_table || !lengths || !refs)
+        return fail(RR_ERR_INVALID, "parent, page_table, lengths and refs must be device pointers");
+    if (n_seqs > rr::kForkSeqs) return fail(RR_ERR_UNSUPPORTED, "at most 4096 sequences are forked in a call");
+    if (max_pages > kMostGroups) return fail(RR_ERR_UNSUPPORTED, "max_pages must be below 2^24");
+    rr::ForkArgs a{parent, page_table, lengths, refs, n_seqs, max_pages, n_pages, 0};
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    hipError_t e = timed(RR_KERNEL_PAGES, stream, [&] { return rr::launch_fork(a, stream); });
+    return e == hipSuccess ? RR_OK : hip_fail(e, "fork launch");
+}
+
+size_t rr_pages_workspace_bytes(int32_t n_pages)
+{
+    if (n_pages >= 1 && n_pages <= (1 << 30)) return rr::pages_workspace_bytes(n_pages);
+    fail(RR_ERR_INVALID, "n_pages must lie in [1, 2^30]");
+    return 0;
+}
+
+namespace {
+
+// What the resize and the compaction ask alike; the launch arguments.
+rr_status pages_args(const rr_pages_config *cfg, void *const *pools, int32_t *page_table, int32_t *refs, void *workspace,
+                     size_t workspace_bytes, rr::PagesArgs *out)
+{
+    if (!cfg) return fail(RR_ERR_INVALID, "config is NULL");
+    const rr_pages_config &c = *cfg;
+    if (c.n_kv_heads < 1 || c.page < 1 || c.n_pages < 1 || c.max_pages < 1 || c.n_seqs < 1)
+        return fail(RR_ERR_INVALID, "n_kv_heads, page, n_pages, max_pages and n_seqs must be >= 1");
+    if (c.d < 8 || c.d > 1024 || c.d % 8 != 0) return fail(RR_ERR_INVALID, "d must be a multiple of 8 in [8, 1024]");
+    if (c.n_pages > (1 << 30)) return fail(RR_ERR_INVALID, "n_pages must be at most 2^30");
+    if ((int64_t)c.max_pages * c.page > (1 << 30)) return fail(RR_ERR_INVALID, "max_pages * page must be at most 2^30");
+    if (c.cache_dtype != RR_F32 && c.cache_dtype != RR_BF16 && c.cache_dtype != RR_E4M3)
+        return fail(RR_ERR_INVALID, "unknown cache_dtype");
+    if (c.n_pools < 1 || c.n_pools > 4096) return fail(RR_ERR_INVALID, "n_pools must lie in [1, 4096]");
+    if (c.n_new < 0) return fail(RR_ERR_INVALID, "n_new must be >= 0");
+    if (c.reserved != 0) return fail(RR_ERR_INVALID, "rr_pages_config.reserved must be 0");
+    const int64_t row_bytes = (int64_t)c.d * (c.cache_dtype == RR_F32 ? 4 : c.cache_dtype == RR_BF16 ? 2 : 1);
+    if (c.n_kv_heads > (1 << 30) / row_bytes / c.page)
+        return fail(RR_ERR_UNSUPPORTED, "a page must be at most 2^30 bytes");
+    if (rr::release_groups(c.n_seqs, c.max_pages) > kMostGroups)
+        return fail(RR_ERR_UNSUPPORTED, "n_seqs times the 1024 entries begun of a row must be below 2^24");
+    if (!pools || !page_table || !refs || !workspace)
+        return fail(RR_ERR_INVALID, "pools, page_table, refs and workspace must be pointers");
+    for (int i = 0; i < c.n_pools; ++i)
+        if (!pools[i] || !aligned16(pools[i])) return fail(RR_ERR_INVALID, "the pools must be 16-byte aligned device pointers");
+    if (!aligned16(workspace)) return fail(RR_ERR_INVALID, "the workspace must be 16-byte aligned");
+    const size_t need = rr::pages_workspace_bytes(c.n_pages);
+    if (workspace_bytes < need)
+        return fail(RR_ERR_INVALID, "the workspace has " + std::to_string(workspace_bytes) + " bytes of " + std::to_string(need));
+    rr::PagesArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.table = page_table;
+    a.refs = refs;
+    a.n_seqs = c.n_seqs;
+    a.max_pages = c.max_pages;
+    a.n_pages = c.n_pages;
+    a.n_new = c.n_new;
+    a.capacity = c.max_pages * c.page;
+    a.heads = c.n_kv_heads;
+    a.row_bytes = (int32_t)row_bytes;
+    a.pd = rr::page_div(c.page);
+    a.n_copies = static_cast<int32_t *>(workspace);
+    a.copies = reinterpret_cast<rr::PageCopy *>(static_cast<char *>(workspace) + rr::kPagesHeadBytes);
+    *out = a;
+    return RR_OK;
+}
+
+// The copies that the tables' launches have listed.
+hipError_t copy_pages(const rr::PagesArgs &a, void *const *pools, int32_t n_pools, hipStream_t stream)
+{
+    for (int i0 = 0; i0 < n_pools; i0 += rr::kPoolsAtOnce) {
+        const int n = n_pools - i0 < rr::kPoolsAtOnce ? n_pools - i0 : rr::kPoolsAtOnce;
+        rr::Pools some{};
+        for (int i = 0; i < n; ++i) some.p[i] = pools[i0 + i];
+        hipError_t e = timed(RR_KERNEL_COPY, stream, [&] { return rr::launch_copies(a, some, n, stream); });
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+rr_status rr_cache_resize(const rr_pages_config *cfg, void *const *pools, const int32_t *new_tokens, const int32_t *lengths,
+                          int32_t *page_table, int32_t *refs, int32_t *missing, void *workspace, size_t workspace_bytes,
+                          void *hip_stream)
+{
+    rr::PagesArgs a;
+    rr_status st = pages_args(cfg, pools, page_table, refs, workspace, workspace_bytes, &a);
+    if (st != RR_OK) return st;
+    if (!lengths) return fail(RR_ERR_INVALID, "lengths must be a device pointer");
+    a.lengths = lengths;
+    a.new_tokens = new_tokens;
+    a.missing = missing;
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    hipError_t e = timed(RR_KERNEL_PAGES, stream, [&] { return rr::launch_resize(a, stream); });
+    if (e == hipSuccess) e = copy_pages(a, pools, cfg->n_pools, stream);
+    return e == hipSuccess ? RR_OK : hip_fail(e, "resize launch");
+}
+
+rr_status rr_cache_compact(const rr_pages_config *cfg, void *const *pools, int32_t *page_table, int32_t *refs,
+                           int32_t *new_ids, int32_t *n_used, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    rr::PagesArgs a;
+    rr_status st = pages_args(cfg, pools, page_table, refs, workspace, workspace_bytes, &a);
+    if (st != RR_OK) return st;
+    if (!new_ids || !n_used) return fail(RR_ERR_INVALID, "new_ids and n_used must be device pointers");
+    a.new_ids = new_ids;
+    a.n_used = n_used;
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    hipError_t e = timed(RR_KERNEL_PAGES, stream, [&] { return rr::launch_compact(a, stream); });
+    if (e == hipSuccess) e = copy_pages(a, pools, cfg->n_pools, stream);
+    return e == hipSuccess ? RR_OK : hip_fail(e, "compaction launch");
+}
+
+namespace {
+
+rr_status verify_args(const rr_verify_config *cfg, rr::VerifyArgs *out)
+{
+    if (!cfg) return fail(RR_ERR_INVALID, "config is NULL");
+    const rr_verify_config &c = *cfg;
+    if (c.n_seqs < 1 || c.vocab < 1) return fail(RR_ERR_INVALID, "n_seqs and vocab must be >= 1");
+    if (c.n_drafts < 0 || c.n_drafts > (1 << 20)) return fail(RR_ERR_INVALID, "n_drafts must lie in [0, 2^20]");
+    if (c.vocab > kMostGroups) return fail(RR_ERR_UNSUPPORTED, "vocab must be below 2^24");
+    if (c.dtype != RR_F32 && c.dtype != RR_BF16) return fail(RR_ERR_INVALID, "dtype must be RR_F32 or RR_BF16");
+    if (c.p_seq < 0 || c.p_row < 0 || c.q_seq < 0 || c.q_row < 0) return fail(RR_ERR_INVALID, "strides must be >= 0");
+    rr::VerifyArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.n_seqs = c.n_seqs;
+    a.n = c.n_drafts;
+    a.vocab = c.vocab;
+    a.p_seq = c.p_seq;
+    a.p_row = c.p_row;
+    a.q_seq = c.q_seq;
+    a.q_row = c.q_row;
+    rr::verify_schedule(a);
+    *out = a;
+    return RR_OK;
+}
+
+}  // namespace
+
+size_t rr_verify_workspace_bytes(const rr_verify_config *cfg)
+{
+    rr::VerifyArgs a;
+    return verify_args(cfg, &a) == RR_OK ? rr::verify_workspace_bytes(a) : 0;
+}
+
+rr_status rr_verify_drafts(const rr_verify_config *cfg, const void *P, const void *Q, const int32_t *drafts,
+                           const int32_t *n_drafts, const float *uniforms, int32_t *lengths, int32_t *accepted,
+                           int32_t *tokens, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    rr::VerifyArgs a;
+    rr_status st = verify_args(cfg, &a);
+    if (st != RR_OK) return st;
+    if (!P || !uniforms || !accepted || !tokens || !workspace)
+        return fail(RR_ERR_INVALID, "P, uniforms, accepted, tokens and workspace must be device pointers");
+    if (cfg->n_drafts > 0 && !drafts) return fail(RR_ERR_INVALID, "drafts must be a device pointer");
+    if (!aligned16(workspace)) return fail(RR_ERR_INVALID, "the workspace must be 16-byte aligned");
+    const size_t need = rr::verify_workspace_bytes(a);
+    if (workspace_bytes < need)
+        return fail(RR_ERR_INVALID, "the workspace has " + std::to_string(workspace_bytes) + " bytes of " + std::to_string(need));
+    a.P = P;
+    a.Q = cfg->n_drafts > 0 ? Q : nullptr;
+    a.drafts = drafts;
+    a.n_drafts = n_drafts;
+    a.uniforms = uniforms;
+    a.lengths = lengths;
+    a.accepted = accepted;
+    a.tokens = tokens;
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    hipError_t e = timed(RR_KERNEL_VERIFY, stream, [&] { return rr::launch_verify(a, cfg->dtype, workspace, stream); });
+    return e == hipSuccess ? RR_OK : hip_fail(e, "verification launch");
 }

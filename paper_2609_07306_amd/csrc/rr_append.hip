@@ -25,49 +25,13 @@
 #include "rr_device.hpp"
 #include "rr_internal.hpp"
 #include "rr_paged.hpp"
+#include "rr_rows.hpp"
 
 namespace rr {
 namespace {
 
 constexpr int kAppendThreads = 256;
 constexpr int kMostRot = 1024;
-
-template <typename T, int N>
-struct Piece {
-    typedef T V __attribute__((ext_vector_type(N)));
-};
-
-__device__ __forceinline__ float widen(float x) { return x; }
-__device__ __forceinline__ float widen(__bf16 x) { return (float)x; }
-
-// N consecutive elements of a row as binary32: one vector, or (VEC = false,
-// where rows are not aligned to one) element by element.
-template <typename T, int N, bool VEC>
-__device__ __forceinline__ void read_piece(const T *p, float (&x)[N])
-{
-    if constexpr (VEC) {
-        const auto v = *reinterpret_cast<const typename Piece<T, N>::V *>(p);
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = widen(v[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = widen(p[e]);
-    }
-}
-
-template <typename T, int N, bool VEC>
-__device__ __forceinline__ void write_piece(T *p, const float (&x)[N])
-{
-    if constexpr (VEC) {
-        typename Piece<T, N>::V v;
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = (T)x[e];
-        *reinterpret_cast<typename Piece<T, N>::V *>(p) = v;
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) p[e] = (T)x[e];
-    }
-}
 
 // What e4m3 holds of x: beyond the largest finite value, that one.
 __device__ __forceinline__ float clamp_e4m3(float x)
@@ -124,7 +88,9 @@ __device__ __forceinline__ int find_sequence(const int32_t *start, int n_seqs, i
     return in_vector((begun & here) >> b & 1u ? b : -1);
 }
 
-template <typename T, bool E4, bool INTER, int N, bool VEC>
+// AXES: rotated by the token's positions on several axes, not by its place in the
+// sequence.
+template <typename T, bool E4, bool INTER, int N, bool VEC, bool AXES>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
 {
     __shared__ float s_cos[kMostRot / 2], s_sin[kMostRot / 2];
@@ -149,11 +115,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
     const int pos = (int)p, c = a.pd.div(pos), place = pos - c * a.pd.page;
     const int phys = pool_page(a.table[(int64_t)b * a.max_pages + c], a.n_pages);
 
-    // angles in turns: position * frequency / 2 pi, less its nearest integer
-    for (int x = tid; x < half; x += kAppendThreads) {
-        const double turn = (double)pos * a.freqs[x] * 0.15915494309189533577;
-        sincospif(2.f * (float)(turn - rint(turn)), &s_sin[x], &s_cos[x]);
-    }
+    for (int x = tid; x < half; x += kAppendThreads)
+        turn_of(AXES ? a.axes.at(i, x) : (double)pos, a.freqs[x], &s_cos[x], &s_sin[x]);
     __syncthreads();
 
     // Rows of queries and keys.  INTER: a piece is N / 2 pairs of neighbours;
@@ -183,22 +146,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
                 float x[N], y[N];
                 read_piece<T, N, VEC>(src + f0, x);
                 if (turn) {
-                    if constexpr (INTER) {
-#pragma unroll
-                        for (int e = 0; e < N; e += 2) {
-                            const float p = x[e], q = x[e + 1];
-                            x[e] = p * c[e] - q * s[e];
-                            x[e + 1] = q * c[e] + p * s[e];
-                        }
-                    } else {
-                        read_piece<T, N, VEC>(src + f1, y);
-#pragma unroll
-                        for (int e = 0; e < N; ++e) {
-                            const float p = x[e], q = y[e];
-                            x[e] = p * c[e] - q * s[e];
-                            y[e] = q * c[e] + p * s[e];
-                        }
-                    }
+                    if constexpr (!INTER) read_piece<T, N, VEC>(src + f1, y);
+                    turn_piece<INTER, N>(x, y, c, s);
                 }
                 if (key) {
                     const int64_t at = pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d);
@@ -236,21 +185,24 @@ hipError_t launch_append(const AppendArgs &a, int dtype, int cache, bool interle
     const bool vec = aligned(a.K, a.ldk) && aligned(a.V, a.ldv) && aligned(a.Q, a.Q ? a.ldq : 0) && aligned(a.Q_out, 0) &&
                      aligned(a.Kc, 0) && aligned(a.Vc, 0) && a.rot % (interleaved ? n : 2 * n) == 0;
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)a.n_tokens), dim3(kAppendThreads), 0, stream, a); };
-    auto any = [&](auto type, auto e4, auto width) {
+    auto any = [&](auto type, auto e4, auto width, auto axes) {
         typedef decltype(type) T;
-        constexpr bool E4 = decltype(e4)::value;
+        constexpr bool E4 = decltype(e4)::value, AX = decltype(axes)::value;
         constexpr int W = decltype(width)::value;
         if (vec)
-            interleaved ? go(append_kernel<T, E4, true, W, true>) : go(append_kernel<T, E4, false, W, true>);
+            interleaved ? go(append_kernel<T, E4, true, W, true, AX>) : go(append_kernel<T, E4, false, W, true, AX>);
         else  // (interleaved partners go together)
-            interleaved ? go(append_kernel<T, E4, true, 2, false>) : go(append_kernel<T, E4, false, 1, false>);
+            interleaved ? go(append_kernel<T, E4, true, 2, false, AX>) : go(append_kernel<T, E4, false, 1, false, AX>);
     };
-    if (dtype == 0)
-        any(float(), std::false_type(), std::integral_constant<int, 4>());
-    else if (cache == CACHE_BF16)
-        any(__bf16(), std::false_type(), std::integral_constant<int, 8>());
-    else
-        any(__bf16(), std::true_type(), std::integral_constant<int, 8>());
+    auto types = [&](auto axes) {
+        if (dtype == 0)
+            any(float(), std::false_type(), std::integral_constant<int, 4>(), axes);
+        else if (cache == CACHE_BF16)
+            any(__bf16(), std::false_type(), std::integral_constant<int, 8>(), axes);
+        else
+            any(__bf16(), std::true_type(), std::integral_constant<int, 8>(), axes);
+    };
+    a.axes.positions ? types(std::true_type()) : types(std::false_type());
     return hipGetLastError();
 }
 

@@ -8,6 +8,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "rr_rows.hpp"
+
 namespace rr {
 
 // Quotients by the page length for 0 <= n < 2^31: with s the bits of
@@ -79,6 +81,7 @@ struct AppendArgs {
     void *Q_out;            // [n_tokens, H, d]
     const int32_t *seq_start, *lengths, *table;
     const double *freqs;    // [rot / 2] radians per position
+    Axes axes;              // positions null: a token's place in its sequence
     const float *k_scale, *v_scale;
     int64_t ldq, ldk, ldv;
     int32_t n_heads, n_kv_heads, d, n_pages, max_pages, n_seqs, n_tokens, rot;

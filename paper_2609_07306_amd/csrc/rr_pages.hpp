@@ -1,0 +1,55 @@
+// Arguments of the calls that change which pages sequences hold (rr_pages.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "rr_paged.hpp"
+
+namespace rr {
+
+constexpr int kForkSeqs = 4096;    // sequences of a fork: a workgroup holds a column of all of them in LDS
+constexpr int kPoolsAtOnce = 64;   // pools that a launch copies pages of
+
+struct ForkArgs {
+    const int32_t *parent;
+    int32_t *table, *lengths, *refs;
+    int32_t n_seqs, max_pages, n_pages;
+    int32_t columns;  // of a workgroup
+};
+
+// A page's first `places` places go from page src to page dst.
+struct PageCopy {
+    int32_t src, dst, places;
+};
+
+struct PagesArgs {
+    const int32_t *lengths, *new_tokens;  // new_tokens: [n_seqs], or null: n_new
+    int32_t *table, *refs;
+    int32_t *missing;           // [n_seqs] or null
+    int32_t *new_ids, *n_used;  // compaction: [n_pages], [1]
+    int32_t n_seqs, max_pages, n_pages, n_new;
+    int32_t capacity;  // tokens a page-table row can hold
+    int32_t heads;     // of a page
+    int32_t row_bytes; // of a token of a head
+    PageDiv pd;
+    int32_t *n_copies;  // workspace: copies to make ...
+    PageCopy *copies;   // ... [n_pages]
+};
+
+// The workspace holds the number of copies, then the copies.
+constexpr size_t kPagesHeadBytes = 256;
+inline size_t pages_workspace_bytes(int32_t n_pages) { return kPagesHeadBytes + (size_t)n_pages * sizeof(PageCopy); }
+
+struct Pools {
+    void *p[kPoolsAtOnce];
+};
+
+int64_t release_groups(int32_t n_seqs, int32_t max_pages);  // workgroups of a resize's first launch
+hipError_t launch_fork(const ForkArgs &a, hipStream_t stream);
+hipError_t launch_resize(const PagesArgs &a, hipStream_t stream);   // the tables; copies to make
+hipError_t launch_compact(const PagesArgs &a, hipStream_t stream);  // the same
+hipError_t launch_copies(const PagesArgs &a, const Pools &pools, int n_pools, hipStream_t stream);
+
+}  // namespace rr

@@ -1,0 +1,108 @@
+// Rows of keys and queries in pieces of vectors, their positions on several
+// axes, and the arguments of the rotation (rr_append.hip, rr_rotate.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace rr {
+
+template <typename T, int N>
+struct Piece {
+    typedef T V __attribute__((ext_vector_type(N)));
+};
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(__bf16 x) { return (float)x; }
+
+// N consecutive elements of a row as binary32: one vector, or (VEC = false,
+// where rows are not aligned to one) element by element.
+template <typename T, int N, bool VEC>
+__device__ __forceinline__ void read_piece(const T *p, float (&x)[N])
+{
+    if constexpr (VEC) {
+        const auto v = *reinterpret_cast<const typename Piece<T, N>::V *>(p);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = widen(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = widen(p[e]);
+    }
+}
+
+template <typename T, int N, bool VEC>
+__device__ __forceinline__ void write_piece(T *p, const float (&x)[N])
+{
+    if constexpr (VEC) {
+        typename Piece<T, N>::V v;
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = (T)x[e];
+        *reinterpret_cast<typename Piece<T, N>::V *>(p) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) p[e] = (T)x[e];
+    }
+}
+
+// Rotates a piece: neighbours are partners (INTER), or x's element e and y's.
+template <bool INTER, int N>
+__device__ __forceinline__ void turn_piece(float (&x)[N], float (&y)[N], const float (&c)[N], const float (&s)[N])
+{
+    if constexpr (INTER) {
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+            const float p = x[e], q = x[e + 1];
+            x[e] = p * c[e] - q * s[e];
+            x[e + 1] = q * c[e] + p * s[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float p = x[e], q = y[e];
+            x[e] = p * c[e] - q * s[e];
+            y[e] = q * c[e] + p * s[e];
+        }
+    }
+}
+
+// Cosine and sine of position * frequency.  The product loses its low digits in
+// binary32 beyond some thousand positions, so the angle is formed and reduced
+// to a fraction of a turn in binary64.
+__device__ __forceinline__ void turn_of(double pos, double freq, float *c, float *s)
+{
+    const double turn = pos * freq * 0.15915494309189533577;
+    sincospif(2.f * (float)(turn - rint(turn)), s, c);
+}
+
+// Positions of tokens on several axes.
+struct Axes {
+    const void *positions;  // [n_axes, n] int32, or binary32 where real
+    const int32_t *axis;    // [rot / 2] axis of each frequency; null: the first one's
+    int64_t n;              // tokens
+    int32_t n_axes, real;
+
+    // Token i's position as frequency j takes it; 0, which rotates nothing, for
+    // an axis that is not there.
+    __device__ __forceinline__ double at(int64_t i, int j) const
+    {
+        const int t = axis ? axis[j] : 0;
+        if ((uint32_t)t >= (uint32_t)n_axes) return 0.0;
+        const int64_t x = t * n + i;
+        return real ? (double)static_cast<const float *>(positions)[x] : (double)static_cast<const int32_t *>(positions)[x];
+    }
+};
+
+struct RotateArgs {
+    const void *X;
+    void *Y;
+    const double *freqs;  // [rot / 2]
+    Axes axes;
+    int64_t x_token, x_head, y_token, y_head;  // elements between rows
+    int32_t n_heads, n_tokens, d, rot;
+    int32_t heads_each;  // heads that a workgroup goes through
+    float sign;          // -1: back
+};
+
+hipError_t launch_rotate(const RotateArgs &a, int dtype, bool interleaved, hipStream_t stream);
+
+}  // namespace rr

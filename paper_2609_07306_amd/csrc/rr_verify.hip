@@ -1,0 +1,300 @@
+// Verification of drafted tokens against the target's probabilities, for
+// gfx950: which drafts are taken, and the token that follows them, drawn from
+// what the target has left beside the drafts (or from the target where all were
+// taken), all from given uniform numbers.
+//
+// Draft i is taken iff u_i q_i(x_i) < p_i(x_i).  With a the first one that is
+// not, the rest is r = max(p_a - q_a, 0), and the token the first v whose sum
+// of r up to it exceeds u_n times the whole sum.  Everything is formed in
+// binary64: a product of two binary32 numbers is exact there, and sums of a
+// vocabulary are off by 2^-53 of the whole a term, so that the order of the
+// additions moves a border by less than the uniform numbers' own steps.
+//
+// Bound by the bytes of one row of each of the two (the rows of taken drafts
+// are not read).  A row is split into parts, one a wave, that sum r; the
+// workgroup of a sequence that comes last finds the part in which the border
+// lies and reads that part again.
+#include <hip/hip_runtime.h>
+
+#include "rr_device.hpp"
+#include "rr_verify.hpp"
+
+namespace rr {
+namespace {
+
+constexpr int kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
+constexpr int kStep = 256;  // elements of a wave's step: four a lane
+
+__device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ double value(float x) { return (double)x; }
+__device__ __forceinline__ double value(__bf16 x) { return (double)(float)x; }
+
+// Four elements from an address that is a multiple of an element's size.
+template <typename T>
+struct Four {
+    typedef T V __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+};
+
+enum Rest : int { REST_TARGET, REST_DIFFERENCE, REST_WITHOUT };  // p; max(p - q, 0); p but for the draft
+
+// What is drawn from.
+template <typename T>
+struct Row {
+    const T *p, *q;
+    int kind, draft, vocab;
+
+    // Not a positive number: nothing.
+    __device__ __forceinline__ double weight(double x, double y, int v) const
+    {
+        const double r = kind == REST_DIFFERENCE ? x - y : (kind == REST_WITHOUT && v == draft) ? 0.0 : x;
+        return r > 0.0 && r < (double)INFINITY ? r : 0.0;
+    }
+
+    // The weights of v .. v + 3.
+    __device__ __forceinline__ void four(int v, double (&r)[4]) const
+    {
+        if (v + 4 <= vocab) {
+            const auto x = *reinterpret_cast<const typename Four<T>::V *>(p + v);
+            typename Four<T>::V y = {};
+            if (kind == REST_DIFFERENCE) y = *reinterpret_cast<const typename Four<T>::V *>(q + v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = weight(value(x[e]), value(y[e]), v + e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                r[e] = v + e < vocab ? weight(value(p[v + e]), kind == REST_DIFFERENCE ? value(q[v + e]) : 0.0, v + e) : 0.0;
+        }
+    }
+};
+
+__device__ __forceinline__ double wave_sum(double x)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o, 64);
+    return x;
+}
+
+// Sums of x over the threads before this one, and over all of them.
+__device__ __forceinline__ double block_before(double x, double *s_wave, double *all)
+{
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    double to = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const double y = __shfl_up(to, o, 64);
+        if (lane >= o) to += y;
+    }
+    const double before = __shfl_up(to, 1, 64);
+    __syncthreads();
+    if (lane == 63) s_wave[w] = to;
+    __syncthreads();
+    double base = 0.0, sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kVerifyWaves; ++i) {
+        if (i < w) base += s_wave[i];
+        sum += s_wave[i];
+    }
+    *all = sum;
+    return base + (lane ? before : 0.0);
+}
+
+template <typename T>
+__device__ __forceinline__ double part_sum(const Row<T> &row, int part, int size)
+{
+    const int lane = threadIdx.x & 63, from = part * size, to = min(from + size, row.vocab);
+    double sum = 0.0;
+#pragma unroll 4
+    for (int v = from + 4 * lane; v < to; v += kStep) {
+        double r[4];
+        row.four(v, r);
+        sum += (r[0] + r[1]) + (r[2] + r[3]);
+    }
+    return wave_sum(sum);
+}
+
+__device__ __forceinline__ double load_sum(const double *p)
+{
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ void store_sum(double *p, double x)
+{
+    __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// What the search for a border has found so far.
+struct Found {
+    int at;         // where it lies; before it is known, the last place that has any weight; -1
+    int known;
+    double before;  // the sum before that place
+};
+
+// Of one place a thread, in order (`any`: it has some weight, `here`: the
+// border lies in it), the first that has the border, or else the last that has
+// any weight, into `f`.
+__device__ __forceinline__ void look(Found &f, bool any, bool here, int at, double before)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t some = __ballot(any), border = __ballot(here);
+    for (int w = 0; w < kVerifyWaves; ++w) {
+        if (w == wave && some && !f.known && lane == (border ? __builtin_ctzll(border) : 63 - __builtin_clzll(some))) {
+            f.at = at;
+            f.before = before;
+            f.known = border != 0;
+        }
+        __syncthreads();
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
+{
+    __shared__ double s_wave[kVerifyWaves];
+    __shared__ Found s_part, s_token;
+    __shared__ int s_last;
+    const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const T *P = static_cast<const T *>(a.P) + b * a.p_seq, *Q = a.Q ? static_cast<const T *>(a.Q) + b * a.q_seq : nullptr;
+    const int32_t *drafts = a.drafts + (int64_t)b * a.n;
+    const float *u = a.uniforms + (int64_t)b * (a.n + 1);
+
+    // the first draft that is not taken: every wave looks for itself
+    const int count = a.n_drafts ? max(0, min(a.n_drafts[b], a.n)) : a.n;
+    int took = count, draft = -1;
+    for (int i0 = 0; i0 < count; i0 += 64) {
+        const int i = i0 + lane;
+        int x = -1;
+        bool taken = false;
+        if (i < count) {
+            x = drafts[i];
+            if ((uint32_t)x < (uint32_t)a.vocab) {
+                const double p = value(P[i * a.p_row + x]), q = Q ? value(Q[i * a.q_row + x]) : 1.0;
+                taken = (double)u[i] * q < p;
+            }
+        }
+        const uint64_t missed = __ballot(i < count && !taken);
+        if (missed) {
+            const int first = __builtin_ctzll(missed);
+            took = i0 + first;
+            draft = __shfl(x, first, 64);
+            break;
+        }
+    }
+    Row<T> row{P + took * a.p_row, Q, took == count ? REST_TARGET : Q ? REST_DIFFERENCE : REST_WITHOUT, draft, a.vocab};
+    if (row.kind == REST_DIFFERENCE) row.q += took * a.q_row;
+
+    // this wave's part
+    double *sums = a.sums + (int64_t)b * a.n_parts;
+    const int own = blockIdx.x * kVerifyWaves + wave;
+    if (own < a.n_parts) {
+        const double sum = part_sum(row, own, a.part);
+        if (lane == 0) store_sum(sums + own, sum);
+    }
+    wait_vm();        // this wave's sum has been stored ...
+    __syncthreads();  // ... and the other waves'
+    if (tid == 0) {
+        const uint32_t before = __hip_atomic_fetch_add(a.counters + b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_last = before == gridDim.x - 1;
+        if (s_last) __hip_atomic_store(a.counters + b, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_part = s_token = Found{-1, 0, 0.0};
+    }
+    __syncthreads();
+    if (!s_last) return;
+
+    // the workgroup that comes last: the whole sum ...
+    double total = 0.0;
+    for (int again = 0;; ++again) {
+        double x = 0.0;
+        for (int i = tid; i < a.n_parts; i += kVerifyThreads) x += load_sum(sums + i);
+        block_before(x, s_wave, &total);
+        if (total > 0.0 || again || row.kind == REST_TARGET) break;
+        // (the drafts cover all that the target has: drawn from the target)
+        row.kind = REST_TARGET;
+        for (int i = wave; i < a.n_parts; i += kVerifyWaves) {
+            const double sum = part_sum(row, i, a.part);
+            if (lane == 0) store_sum(sums + i, sum);
+        }
+        wait_vm();
+        __syncthreads();
+    }
+    // ... the part in which the border lies (past all of them, the last one) ...
+    const double border = (double)u[a.n] * total;
+    double before = 0.0;
+    for (int i0 = 0; i0 < a.n_parts && !s_part.known; i0 += kVerifyThreads) {
+        const int i = i0 + tid;
+        const double x = i < a.n_parts ? load_sum(sums + i) : 0.0;
+        double all;
+        const double from = before + block_before(x, s_wave, &all);
+        look(s_part, x > 0.0, x > 0.0 && from + x > border, i, from);
+        before += all;
+    }
+    // ... and in it the token, in the same way
+    if (s_part.at >= 0) {
+        const int from = s_part.at * a.part, to = min(from + a.part, a.vocab);
+        before = s_part.before;
+        for (int v0 = from; v0 < to && !s_token.known; v0 += 4 * kVerifyThreads) {
+            const int v = v0 + 4 * tid;
+            double r[4] = {0.0, 0.0, 0.0, 0.0}, all;
+            if (v < to) row.four(v, r);
+            double at = before + block_before((r[0] + r[1]) + (r[2] + r[3]), s_wave, &all);
+            int here = -1, any = -1;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                at += r[e];
+                if (r[e] > 0.0) any = v + e;
+                if (r[e] > 0.0 && here < 0 && at > border) here = v + e;
+            }
+            look(s_token, any >= 0, here >= 0, here >= 0 ? here : any, 0.0);
+            before += all;
+        }
+    }
+    for (int i = tid; i <= a.n; i += kVerifyThreads)
+        a.tokens[(int64_t)b * (a.n + 1) + i] = i < took ? drafts[i] : i == took ? s_token.at : -1;
+    if (tid == 0) {
+        a.accepted[b] = took;
+        if (a.lengths) a.lengths[b] -= count - took;
+    }
+}
+
+}  // namespace
+
+void verify_schedule(VerifyArgs &a)
+{
+    // a wave's part of a row: 256 elements, or up to 2048 where that still
+    // leaves some 8192 waves
+    a.part = kStep;
+    while (a.part < 8 * kStep && (int64_t)a.n_seqs * (a.vocab / a.part) > 16384) a.part *= 2;
+    a.n_parts = (a.vocab + a.part - 1) / a.part;
+}
+
+size_t verify_workspace_bytes(const VerifyArgs &a)
+{
+    const int seqs = a.n_seqs < kVerifySeqs ? a.n_seqs : kVerifySeqs;
+    return kVerifyCounterBytes + (size_t)seqs * a.n_parts * sizeof(double);
+}
+
+hipError_t launch_verify(const VerifyArgs &args, int dtype, void *workspace, hipStream_t stream)
+{
+    VerifyArgs a = args;
+    a.counters = static_cast<uint32_t *>(workspace);
+    a.sums = reinterpret_cast<double *>(static_cast<char *>(workspace) + kVerifyCounterBytes);
+    const size_t size = dtype == 0 ? 4 : 2;
+    const unsigned groups = (unsigned)((a.n_parts + kVerifyWaves - 1) / kVerifyWaves);
+    // (as many sequences at a time as there are counters)
+    for (int left = a.n_seqs; left > 0; left -= kVerifySeqs) {
+        const int n = left < kVerifySeqs ? left : kVerifySeqs;
+        auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(groups, (unsigned)n), dim3(kVerifyThreads), 0, stream, a); };
+        dtype == 0 ? go(verify_kernel<float>) : go(verify_kernel<__bf16>);
+        a.P = static_cast<const char *>(a.P) + (int64_t)n * a.p_seq * size;
+        if (a.Q) a.Q = static_cast<const char *>(a.Q) + (int64_t)n * a.q_seq * size;
+        a.drafts += (int64_t)n * a.n;
+        if (a.n_drafts) a.n_drafts += n;
+        a.uniforms += (int64_t)n * (a.n + 1);
+        if (a.lengths) a.lengths += n;
+        a.accepted += n;
+        a.tokens += (int64_t)n * (a.n + 1);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace rr

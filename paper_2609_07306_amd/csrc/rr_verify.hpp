@@ -1,0 +1,32 @@
+// Arguments of the verification of drafted tokens (rr_verify.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace rr {
+
+constexpr int kVerifySeqs = 16384;  // sequences of a launch: each has a counter
+constexpr size_t kVerifyCounterBytes = kVerifySeqs * sizeof(uint32_t);
+
+struct VerifyArgs {
+    const void *P, *Q;  // [B, n + 1, V] and [B, n, V] with strides; Q or null
+    const int32_t *drafts, *n_drafts;  // [B, n]; [B] or null
+    const float *uniforms;             // [B, n + 1]
+    int32_t *lengths;                  // [B] or null
+    int32_t *accepted, *tokens;        // [B], [B, n + 1]
+    int64_t p_seq, p_row, q_seq, q_row;  // elements between rows
+    int32_t n_seqs, n, vocab;
+    int32_t part;     // elements that a wave sums
+    int32_t n_parts;  // of a row
+    uint32_t *counters;  // [n_seqs] finished workgroups, 0 between calls
+    double *sums;        // [n_seqs, n_parts]
+};
+
+// Fills in the split of a row, from n_seqs and vocab.
+void verify_schedule(VerifyArgs &a);
+size_t verify_workspace_bytes(const VerifyArgs &a);
+hipError_t launch_verify(const VerifyArgs &a, int dtype, void *workspace, hipStream_t stream);
+
+}  // namespace rr

@@ -26,10 +26,12 @@ EXPORTED = (
     "rr_ledger_index_bytes", "rr_status_string", "rr_last_error", "rr_profile_start",
     "rr_profile_stop", "rr_unconverged_rows", "rr_set_sweep_cap", "rr_relay_layer_static",
     "rr_pool_chunks", "rr_expand_tokens", "rr_sparse_attention", "rr_cache_append",
-    "rr_paged_workspace_bytes", "rr_paged_attention", "rr_prefix_attention",
+    "rr_paged_workspace_bytes", "rr_paged_attention", "rr_prefix_attention", "rr_cache_append_axes", "rr_rotate",
+    "rr_cache_fork", "rr_pages_workspace_bytes", "rr_cache_resize", "rr_cache_compact", "rr_verify_workspace_bytes",
+    "rr_verify_drafts",
 )
 KERNEL_KINDS = ("full", "anchor", "reroute", "rescore", "relay", "pool", "expand", "attention", "append",
-                "paged", "join")
+                "paged", "join", "rotate", "verify", "pages", "copy")
 
 
 class RRError(RuntimeError):
@@ -71,6 +73,27 @@ class _PagedConfig(ctypes.Structure):
                                                 ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
+class _Axes(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("n_axes", ctypes.c_int32),
+                ("real", ctypes.c_int32)]
+
+
+class _RotateConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_heads", "n_tokens", "d", "rot", "interleaved", "inverse", "dtype",
+                                              "reserved")] + \
+               [(n, ctypes.c_int64) for n in ("x_token", "x_head", "y_token", "y_head")]
+
+
+class _PagesConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_kv_heads", "d", "page", "n_pages", "cache_dtype", "n_pools", "max_pages",
+                                              "n_seqs", "n_new", "reserved")]
+
+
+class _VerifyConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "n_drafts", "vocab", "dtype")] + \
+               [(n, ctypes.c_int64) for n in ("p_seq", "p_row", "q_seq", "q_row")]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built: run `python -m paper_2609_07306_amd.build`")
@@ -101,6 +124,14 @@ def _load():
         "rr_paged_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(_PagedConfig)]),
         "rr_paged_attention": (ctypes.c_int, [ctypes.POINTER(_PagedConfig)] + [vp] * 9 + [ctypes.c_size_t, vp]),
         "rr_prefix_attention": (ctypes.c_int, [ctypes.POINTER(_PagedConfig)] + [vp] * 9 + [ctypes.c_size_t, vp]),
+        "rr_cache_append_axes": (ctypes.c_int, [ctypes.POINTER(_AppendConfig)] + [vp] * 7 + [ctypes.POINTER(_Axes)] + [vp] * 4),
+        "rr_rotate": (ctypes.c_int, [ctypes.POINTER(_RotateConfig), vp, vp, ctypes.POINTER(_Axes), vp, vp]),
+        "rr_cache_fork": (ctypes.c_int, [i32] * 3 + [vp] * 5),
+        "rr_pages_workspace_bytes": (ctypes.c_size_t, [i32]),
+        "rr_cache_resize": (ctypes.c_int, [ctypes.POINTER(_PagesConfig)] + [vp] * 7 + [ctypes.c_size_t, vp]),
+        "rr_cache_compact": (ctypes.c_int, [ctypes.POINTER(_PagesConfig)] + [vp] * 6 + [ctypes.c_size_t, vp]),
+        "rr_verify_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(_VerifyConfig)]),
+        "rr_verify_drafts": (ctypes.c_int, [ctypes.POINTER(_VerifyConfig)] + [vp] * 9 + [ctypes.c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -408,6 +439,8 @@ _E4M3 = torch.float8_e4m3fn
 # (the address alone: a torch.cuda.Stream object costs as much as a launch's checks)
 _current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
 _append, _paged, _prefix = lib.rr_cache_append, lib.rr_paged_attention, lib.rr_prefix_attention
+_append_axes, _rotate, _verify = lib.rr_cache_append_axes, lib.rr_rotate, lib.rr_verify_drafts
+_fork, _resize, _compact = lib.rr_cache_fork, lib.rr_cache_resize, lib.rr_cache_compact
 _DTYPES = {torch.float32: RR_F32, torch.bfloat16: RR_BF16, _E4M3: RR_E4M3}
 
 
@@ -504,20 +537,37 @@ def _rows_of(name, t, shape, dtype):
     return token if n > 1 else heads * d
 
 
+def _axes_of(positions, axis, rot, n):
+    """rr_axes of positions [n_axes, n] (or [n]) int32 or float32 and axis [rot / 2] int32."""
+    kind = positions.dtype
+    if kind not in (torch.int32, torch.float32):
+        raise TypeError("positions must be int32 or float32")
+    shape = positions.shape
+    if shape[-1:] != (n,) or len(shape) > 2 or not shape[0]:
+        raise ValueError(f"positions must be [n_axes, {n}]: got {list(shape)}")
+    if not positions.is_contiguous():
+        raise ValueError("positions must be contiguous")
+    return _Axes(positions.data_ptr(), None if axis is None else _of("axis", axis, (rot // 2,), torch.int32),
+                 shape[0] if len(shape) == 2 else 1, 1 if kind == torch.float32 else 0)
+
+
 def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, freqs=None, interleaved=False, Q=None,
-                 Q_out=None, k_scale=None, v_scale=None, stream=None):
+                 Q_out=None, k_scale=None, v_scale=None, stream=None, positions=None, axis=None):
     """rr_cache_append: new tokens' keys and values K, V [n_tokens, H_kv, d]
     into the pages of their sequences (K_cache, V_cache [n_pages, H_kv, page,
     d], page_table [B, max_pages] and lengths [B] int32, the new tokens counted
     in; seq_start [B + 1] int32, None: n_tokens / B each).  With freqs [rot / 2]
     float64 the first rot features of keys are rotated by position, and of
     queries Q [n_tokens, H, d] (returned, in Q_out if given).  K, V and Q may
-    be views whose tokens lie apart."""
+    be views whose tokens lie apart.  positions [n_axes, n_tokens] int32 or
+    float32: rotated by these, frequency j by those of axis[j] (axis [rot / 2]
+    int32, None: the first), not by place in the sequence (rr_cache_append_axes)."""
     kind, shape = K.dtype, K.shape
     if len(shape) != 3 or kind not in (torch.float32, torch.bfloat16):
         raise TypeError("K must be a [n_tokens, H_kv, d] float32 or bfloat16 tensor")
     (n_pages, Hkv, page, d), cache, kc, vc, ks, vs = _cache_of(K_cache, V_cache, kind, k_scale, v_scale)
-    dev = _device_of((K, V, K_cache, V_cache, page_table, lengths, seq_start, freqs, Q, Q_out, k_scale, v_scale))
+    dev = _device_of((K, V, K_cache, V_cache, page_table, lengths, seq_start, freqs, Q, Q_out, k_scale, v_scale, positions,
+                      axis))
     n = shape[0]
     rows = (n, Hkv, d)
     ldk, ldv = _rows_of("K", K, rows, kind), _rows_of("V", V, rows, kind)
@@ -542,8 +592,50 @@ def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, fr
         raise ValueError("Q_out without Q")
     cfg = _AppendConfig(H, Hkv, d, page, n_pages, most, B, n, rot, 1 if interleaved else 0, _DTYPES[kind], cache, ldq, ldk,
                         ldv, ks, vs)
-    _launch(dev, stream, _append, cfg, K.data_ptr(), V.data_ptr(), q, start, lens, table, f if rot else None, kc, vc, out)
+    if positions is None:
+        if axis is not None:
+            raise ValueError("axis without positions")
+        _launch(dev, stream, _append, cfg, K.data_ptr(), V.data_ptr(), q, start, lens, table, f if rot else None, kc, vc, out)
+        return Q_out
+    if freqs is None:
+        raise ValueError("positions without freqs")
+    axes = _axes_of(positions, axis, rot, n)
+    _launch(dev, stream, _append_axes, cfg, K.data_ptr(), V.data_ptr(), q, start, lens, table, f if rot else None, axes, kc, vc,
+            out)
     return Q_out
+
+
+def _strides(name, t, tokens):
+    """Elements between the rows of tokens and of heads of t, tokens in dimension `tokens`."""
+    s = t.stride()
+    if t.shape[2] > 1 and s[2] != 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    return s[tokens], s[1 - tokens]
+
+
+def rotate(X, positions, freqs, axis=None, tokens=0, interleaved=False, inverse=False, out=None, stream=None):
+    """rr_rotate: the first rot features of every row of X rotated by position, as
+    cache_append does: X [n_tokens, H, d] (tokens=0) or [H, n_tokens, d]
+    (tokens=1) float32 or bfloat16, rows contiguous, positions [n_axes, n_tokens]
+    int32 or float32, freqs [rot / 2] float64, axis as in cache_append.
+    inverse=True: back (the gradient too).  out: X itself or another tensor."""
+    kind, shape = X.dtype, X.shape
+    if len(shape) != 3 or kind not in (torch.float32, torch.bfloat16):
+        raise TypeError("X must be a 3-d float32 or bfloat16 tensor")
+    if tokens not in (0, 1):
+        raise ValueError("tokens must be 0 or 1")
+    dev = _device_of((X, positions, freqs, axis, out))
+    n, rot = shape[tokens], 2 * freqs.numel()
+    f = _of("freqs", freqs, (rot // 2,), torch.float64)
+    axes = _axes_of(positions, axis, rot, n)
+    if out is None:
+        out = _empty(shape, kind, X, stream)
+    elif out.shape != shape or out.dtype != kind:
+        raise ValueError(f"out must be {kind} of shape {list(shape)}")
+    cfg = _RotateConfig(shape[1 - tokens], n, shape[2], rot, 1 if interleaved else 0, 1 if inverse else 0, _DTYPES[kind], 0,
+                        *_strides("X", X, tokens), *_strides("out", out, tokens))
+    _launch(dev, stream, _rotate, cfg, X.data_ptr(), f, axes, out.data_ptr())
+    return out
 
 
 def _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, n_prefix, scale, k_scale, v_scale, lengths):
@@ -649,3 +741,179 @@ def prefix_attention(Q, K_cache, V_cache, page_table, lengths, prefix_pages, n_p
     dev = _device_of((Q, K_cache, V_cache, page_table, lengths, prefix_pages, k_scale, v_scale, out, lse, workspace))
     third = _of("prefix_pages", prefix_pages, (n_chunks(n_prefix, max(K_cache.shape[2], 1)),), torch.int32)
     return _paged_call(_prefix, config, dev, Q, third, out, lse, workspace, stream)
+
+
+# ------------------------------------------- which pages sequences hold
+
+class Pools:
+    """The pools of all layers that one page table serves, for cache_resize and
+    cache_compact: K_caches and V_caches, tensors or lists of them (one a layer)
+    of one shape [n_pages, H_kv, page, d] and type."""
+
+    def __init__(self, K_caches, V_caches):
+        one = isinstance(K_caches, torch.Tensor)
+        self.tensors = [K_caches, V_caches] if one else [*K_caches, *V_caches]
+        if not self.tensors or not one and len(K_caches) != len(V_caches):
+            raise ValueError("K_caches and V_caches must be as many")
+        first = self.tensors[0]
+        self.shape, self.dtype = first.shape, first.dtype
+        for t in self.tensors:
+            if t.dim() != 4 or t.dtype not in _DTYPES:
+                raise TypeError("caches must be [n_pages, H_kv, page, d] tensors of float32, bfloat16 or float8_e4m3fn")
+            if t.shape != self.shape or t.dtype != self.dtype:
+                raise ValueError("caches must have one shape and one type")
+            if not t.is_contiguous():
+                raise ValueError("caches must be contiguous")
+        self.dev = _device_of(self.tensors)
+        self._addresses = (ctypes.c_void_p * len(self.tensors))(*(t.data_ptr() for t in self.tensors))
+
+    def _config(self, max_pages, n_seqs, n_new=0):
+        n_pages, Hkv, page, d = self.shape
+        return _PagesConfig(Hkv, d, page, n_pages, _DTYPES[self.dtype], len(self.tensors), max_pages, n_seqs, n_new, 0)
+
+
+def pages_workspace(pools):
+    """A workspace (uint8 device tensor) for cache_resize and cache_compact calls
+    on these pools, one after the other.  Calls that may run at the same time,
+    captured graphs that are replayed side by side among them, need one each."""
+    n = lib.rr_pages_workspace_bytes(pools.shape[0])
+    if n == 0:
+        _check(RR_ERR_INVALID)
+    return torch.empty(n, dtype=torch.uint8, device=pools.tensors[0].device)
+
+
+def _workspace_of(workspace, make, stream):
+    """The workspace's address and bytes, and itself (one of this call's own: None given)."""
+    if workspace is None:
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                workspace = make()
+        else:
+            workspace = make()
+    elif workspace.dtype != torch.uint8 or workspace.dim() != 1 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous one-dimensional uint8 tensor")
+    return workspace.data_ptr(), workspace.numel(), workspace
+
+
+def _refs(refs, n_pages):
+    return _of("refs", refs, (n_pages,), torch.int32)
+
+
+def cache_fork(page_table, lengths, refs, parent, stream=None):
+    """rr_cache_fork: row b of page_table [B, max_pages] and lengths[b] become
+    what row parent[b] was (parent [B] int32; b itself: as it is; outside [0, B):
+    empty), and refs [n_pages] counts who holds each page.  In place."""
+    dev = _device_of((page_table, lengths, refs, parent))
+    table, lens, B, most = _lists(page_table, lengths)
+    if refs.dim() != 1:
+        raise ValueError("refs must be [n_pages]")
+    n_pages = refs.shape[0]
+    _launch(dev, stream, _fork, B, most, n_pages, _of("parent", parent, (B,), torch.int32), table, lens, _refs(refs, n_pages))
+
+
+def cache_resize(pools, page_table, lengths, refs, new_tokens, missing=None, workspace=None, stream=None):
+    """rr_cache_resize: page_table [B, max_pages] follows lengths [B], new tokens
+    counted in: pages past the end are freed, the entries of the new_tokens (an
+    int, or [B] int32) newest get pages, copies of those that others hold too.
+    refs [n_pages] counts who holds each page.  In place; returns missing [B]
+    int32, the entries for which no page was free.  workspace:
+    pages_workspace(pools), or None for one of this call's own."""
+    many = isinstance(new_tokens, torch.Tensor)
+    dev = _device_of((pools.tensors[0], page_table, lengths, refs, new_tokens if many else None, missing, workspace))
+    table, lens, B, most = _lists(page_table, lengths)
+    new = _of("new_tokens", new_tokens, (B,), torch.int32) if many else None
+    r = _refs(refs, pools.shape[0])
+    if missing is None:
+        missing = _empty((B,), torch.int32, page_table, stream)
+    out = _of("missing", missing, (B,), torch.int32)
+    ws, size, workspace = _workspace_of(workspace, lambda: pages_workspace(pools), stream)
+    _launch(dev, stream, _resize, pools._config(most, B, 0 if many else new_tokens), pools._addresses, new, lens, table, r, out,
+            ws, size)
+    return missing
+
+
+def cache_compact(pools, page_table, refs, new_ids=None, n_used=None, workspace=None, stream=None):
+    """rr_cache_compact: the n used pages (refs not 0) become pages 0 .. n - 1 of
+    all pools, page_table [B, max_pages] and refs [n_pages] follow, in place.
+    Returns (new_ids [n_pages] int32: where each page's tokens are now, -1 for a
+    free one; n_used [1] int32: n).  workspace: as in cache_resize."""
+    dev = _device_of((pools.tensors[0], page_table, refs, new_ids, n_used, workspace))
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [B, max_pages]")
+    B, most = page_table.shape
+    table = _of("page_table", page_table, (B, most), torch.int32)
+    n_pages = pools.shape[0]
+    r = _refs(refs, n_pages)
+    if new_ids is None:
+        new_ids = _empty((n_pages,), torch.int32, page_table, stream)
+    if n_used is None:
+        n_used = _empty((1,), torch.int32, page_table, stream)
+    ids, used = _of("new_ids", new_ids, (n_pages,), torch.int32), _of("n_used", n_used, (1,), torch.int32)
+    ws, size, workspace = _workspace_of(workspace, lambda: pages_workspace(pools), stream)
+    _launch(dev, stream, _compact, pools._config(most, B), pools._addresses, table, r, ids, used, ws, size)
+    return new_ids, n_used
+
+
+# --------------------------------------------------------- drafted tokens
+
+def _rows_3d(name, t, shape, dtype):
+    """The strides of rows [B, n, V] that are contiguous (views of padded ones)."""
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} of shape {list(shape)}")
+    seq, row, one = t.stride()
+    if shape[2] > 1 and one != 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    return seq, row
+
+
+def _verify_config(P, n_drafts, Q=None):
+    if P.dim() != 3 or P.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("P must be a [B, n_drafts + 1, V] float32 or bfloat16 tensor")
+    B, rows, V = P.shape
+    if rows != n_drafts + 1:
+        raise ValueError(f"P has {rows} rows a sequence, one more than the {n_drafts} drafts is wanted")
+    p = _rows_3d("P", P, P.shape, P.dtype)
+    q = (0, 0) if Q is None else _rows_3d("draft_probs", Q, (B, n_drafts, V), P.dtype)
+    return _VerifyConfig(B, n_drafts, V, _DTYPES[P.dtype], *p, *q)
+
+
+def verify_workspace(P):
+    """A workspace (uint8 device tensor, zeros) for verify_drafts calls of P's
+    shape, one after the other (the largest of several shapes' serves them all).
+    Calls that may run at the same time, captured graphs that are replayed side by
+    side among them, need one each."""
+    n = lib.rr_verify_workspace_bytes(_verify_config(P, P.shape[1] - 1))
+    if n == 0:
+        status = _verify(_verify_config(P, P.shape[1] - 1), None, None, None, None, None, None, None, None, None, 0, None)
+        _check(status)
+    return torch.zeros(n, dtype=torch.uint8, device=P.device)
+
+
+def verify_drafts(P, drafts, uniforms, draft_probs=None, n_drafts=None, lengths=None, accepted=None, tokens=None,
+                  workspace=None, stream=None):
+    """rr_verify_drafts: drafts [B, n] int32 against the target's probabilities P
+    [B, n + 1, V] (float32 or bfloat16) and those that they were drawn with,
+    draft_probs [B, n, V] of the same type (None: not drawn), by uniforms [B, n +
+    1] float32; n_drafts [B] int32: how many count.  lengths [B] int32 loses the
+    drafts that were not taken, in place.  Returns (accepted [B], tokens [B, n +
+    1]) int32: how many were taken; they, the token drawn after them, then -1.
+    P and draft_probs may be views whose rows lie apart.  workspace:
+    verify_workspace(P), or None for one of this call's own."""
+    if drafts.dim() != 2:
+        raise ValueError("drafts must be [B, n_drafts]")
+    B, n = drafts.shape
+    dev = _device_of((P, drafts, uniforms, draft_probs, n_drafts, lengths, accepted, tokens, workspace))
+    cfg = _verify_config(P, n, draft_probs)
+    i32 = torch.int32
+    d, u = _of("drafts", drafts, (P.shape[0], n), i32), _of("uniforms", uniforms, (B, n + 1), torch.float32)
+    count = None if n_drafts is None else _of("n_drafts", n_drafts, (B,), i32)
+    lens = None if lengths is None else _of("lengths", lengths, (B,), i32)
+    if accepted is None:
+        accepted = _empty((B,), i32, P, stream)
+    if tokens is None:
+        tokens = _empty((B, n + 1), i32, P, stream)
+    took, out = _of("accepted", accepted, (B,), i32), _of("tokens", tokens, (B, n + 1), i32)
+    ws, size, workspace = _workspace_of(workspace, lambda: verify_workspace(P), stream)
+    _launch(dev, stream, _verify, cfg, P.data_ptr(), None if draft_probs is None else draft_probs.data_ptr(), d, count, u, lens,
+            took, out, ws, size)
+    return accepted, tokens
