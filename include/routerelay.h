@@ -566,9 +566,11 @@ typedef struct {
     int32_t reserved;     /* must be 0 */
 } rr_pages_config;
 
-/* Bytes of workspace of rr_cache_resize and rr_cache_compact (of n_pages; it
- * need not be cleared).  0: n_pages is not valid.  Calls that may run at the
- * same time need one each. */
+/* Bytes of workspace of rr_cache_resize and rr_cache_compact, for n_pages of 1 to
+ * 2^28 (0: another).  It is filled with zeros before its first use, and calls
+ * leave the part of it that has to be zero (the first 4 bytes) at zero, so that
+ * it serves any calls that follow one another.  Calls that may run at the same
+ * time need one each. */
 size_t rr_pages_workspace_bytes(int32_t n_pages);
 
 /* Makes the page table follow the lengths, which count the new tokens that are
@@ -590,7 +592,7 @@ size_t rr_pages_workspace_bytes(int32_t n_pages);
  *   pools   host array of n_pools device pointers, 16-byte aligned
  * Returns RR_ERR_INVALID for bad sizes, types, NULL or unaligned pointers or a
  * workspace too small, RR_ERR_UNSUPPORTED for pages of more than 2^30 bytes, or
- * where n_seqs times the 1024 entries begun of a row are 2^24 or more. */
+ * where n_seqs * max_pages comes to 2^34. */
 rr_status rr_cache_resize(const rr_pages_config *cfg, void *const *pools, const int32_t *new_tokens, const int32_t *lengths,
                           int32_t *page_table, int32_t *refs, int32_t *missing, void *workspace, size_t workspace_bytes,
                           void *hip_stream);

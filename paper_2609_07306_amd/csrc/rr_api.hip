@@ -957,6 +957,7 @@ namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+constexpr int32_t kMostPages = 1 << 28;  // whose holders a resize counts
 constexpr int32_t kMostGroups = (1 << 24) - 1;  // workgroups of 256 threads that a launch can have
 // Query rows of a call behind a prefix, which keeps two parts of each (17 GB of
 // d = 128 for so many); the join that reads them takes four rows a workgroup.
@@ -1227,7 +1228,7 @@ rr_status rr_cache_fork(int32_t n_seqs, int32_t max_pages, int32_t n_pages, cons
         return fail(RR_ERR_INVALID, "parent, page_table, lengths and refs must be device pointers");
     if (n_seqs > rr::kForkSeqs) return fail(RR_ERR_UNSUPPORTED, "at most 4096 sequences are forked in a call");
     if (max_pages > kMostGroups) return fail(RR_ERR_UNSUPPORTED, "max_pages must be below 2^24");
-    rr::ForkArgs a{parent, page_table, lengths, refs, n_seqs, max_pages, n_pages, 0};
+    rr::ForkArgs a{parent, page_table, lengths, refs, n_seqs, max_pages, n_pages};
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     hipError_t e = timed(RR_KERNEL_PAGES, stream, [&] { return rr::launch_fork(a, stream); });
     return e == hipSuccess ? RR_OK : hip_fail(e, "fork launch");
@@ -1235,8 +1236,8 @@ rr_status rr_cache_fork(int32_t n_seqs, int32_t max_pages, int32_t n_pages, cons
 
 size_t rr_pages_workspace_bytes(int32_t n_pages)
 {
-    if (n_pages >= 1 && n_pages <= (1 << 30)) return rr::pages_workspace_bytes(n_pages);
-    fail(RR_ERR_INVALID, "n_pages must lie in [1, 2^30]");
+    if (n_pages >= 1 && n_pages <= kMostPages) return rr::pages_workspace_bytes(n_pages);
+    fail(RR_ERR_INVALID, "n_pages must lie in [1, 2^28]");
     return 0;
 }
 
@@ -1251,7 +1252,7 @@ rr_status pages_args(const rr_pages_config *cfg, void *const *pools, int32_t *pa
     if (c.n_kv_heads < 1 || c.page < 1 || c.n_pages < 1 || c.max_pages < 1 || c.n_seqs < 1)
         return fail(RR_ERR_INVALID, "n_kv_heads, page, n_pages, max_pages and n_seqs must be >= 1");
     if (c.d < 8 || c.d > 1024 || c.d % 8 != 0) return fail(RR_ERR_INVALID, "d must be a multiple of 8 in [8, 1024]");
-    if (c.n_pages > (1 << 30)) return fail(RR_ERR_INVALID, "n_pages must be at most 2^30");
+    if (c.n_pages > kMostPages) return fail(RR_ERR_INVALID, "n_pages must be at most 2^28");
     if ((int64_t)c.max_pages * c.page > (1 << 30)) return fail(RR_ERR_INVALID, "max_pages * page must be at most 2^30");
     if (c.cache_dtype != RR_F32 && c.cache_dtype != RR_BF16 && c.cache_dtype != RR_E4M3)
         return fail(RR_ERR_INVALID, "unknown cache_dtype");
@@ -1261,8 +1262,8 @@ rr_status pages_args(const rr_pages_config *cfg, void *const *pools, int32_t *pa
     const int64_t row_bytes = (int64_t)c.d * (c.cache_dtype == RR_F32 ? 4 : c.cache_dtype == RR_BF16 ? 2 : 1);
     if (c.n_kv_heads > (1 << 30) / row_bytes / c.page)
         return fail(RR_ERR_UNSUPPORTED, "a page must be at most 2^30 bytes");
-    if (rr::release_groups(c.n_seqs, c.max_pages) > kMostGroups)
-        return fail(RR_ERR_UNSUPPORTED, "n_seqs times the 1024 entries begun of a row must be below 2^24");
+    if (rr::resize_groups(c.n_seqs, c.max_pages) > kMostGroups / 4)  // (of 1024 threads)
+        return fail(RR_ERR_UNSUPPORTED, "n_seqs * max_pages must be below 2^34");
     if (!pools || !page_table || !refs || !workspace)
         return fail(RR_ERR_INVALID, "pools, page_table, refs and workspace must be pointers");
     for (int i = 0; i < c.n_pools; ++i)
@@ -1283,23 +1284,11 @@ rr_status pages_args(const rr_pages_config *cfg, void *const *pools, int32_t *pa
     a.heads = c.n_kv_heads;
     a.row_bytes = (int32_t)row_bytes;
     a.pd = rr::page_div(c.page);
-    a.n_copies = static_cast<int32_t *>(workspace);
+    a.counter = static_cast<uint32_t *>(workspace);
+    a.n_copies = static_cast<int32_t *>(workspace) + 1;
     a.copies = reinterpret_cast<rr::PageCopy *>(static_cast<char *>(workspace) + rr::kPagesHeadBytes);
     *out = a;
     return RR_OK;
-}
-
-// The copies that the tables' launches have listed.
-hipError_t copy_pages(const rr::PagesArgs &a, void *const *pools, int32_t n_pools, hipStream_t stream)
-{
-    for (int i0 = 0; i0 < n_pools; i0 += rr::kPoolsAtOnce) {
-        const int n = n_pools - i0 < rr::kPoolsAtOnce ? n_pools - i0 : rr::kPoolsAtOnce;
-        rr::Pools some{};
-        for (int i = 0; i < n; ++i) some.p[i] = pools[i0 + i];
-        hipError_t e = timed(RR_KERNEL_COPY, stream, [&] { return rr::launch_copies(a, some, n, stream); });
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
 }
 
 }  // namespace
@@ -1317,7 +1306,7 @@ rr_status rr_cache_resize(const rr_pages_config *cfg, void *const *pools, const 
     a.missing = missing;
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     hipError_t e = timed(RR_KERNEL_PAGES, stream, [&] { return rr::launch_resize(a, stream); });
-    if (e == hipSuccess) e = copy_pages(a, pools, cfg->n_pools, stream);
+    if (e == hipSuccess) e = timed(RR_KERNEL_COPY, stream, [&] { return rr::launch_copies(a, pools, cfg->n_pools, false, stream); });
     return e == hipSuccess ? RR_OK : hip_fail(e, "resize launch");
 }
 
@@ -1332,7 +1321,7 @@ rr_status rr_cache_compact(const rr_pages_config *cfg, void *const *pools, int32
     a.n_used = n_used;
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     hipError_t e = timed(RR_KERNEL_PAGES, stream, [&] { return rr::launch_compact(a, stream); });
-    if (e == hipSuccess) e = copy_pages(a, pools, cfg->n_pools, stream);
+    if (e == hipSuccess) e = timed(RR_KERNEL_COPY, stream, [&] { return rr::launch_copies(a, pools, cfg->n_pools, true, stream); });
     return e == hipSuccess ? RR_OK : hip_fail(e, "compaction launch");
 }
 

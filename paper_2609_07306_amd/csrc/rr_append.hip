@@ -115,8 +115,11 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
     const int pos = (int)p, c = a.pd.div(pos), place = pos - c * a.pd.page;
     const int phys = pool_page(a.table[(int64_t)b * a.max_pages + c], a.n_pages);
 
-    for (int x = tid; x < half; x += kAppendThreads)
-        turn_of(AXES ? a.axes.at(i, x) : (double)pos, a.freqs[x], &s_cos[x], &s_sin[x]);
+    for (int x = tid; x < half; x += kAppendThreads) {
+        double p[1] = {(double)pos};
+        if (AXES) a.axes.at(i, x, p);
+        turn_of(p[0], a.freqs[x], &s_cos[x], &s_sin[x]);
+    }
     __syncthreads();
 
     // Rows of queries and keys.  INTER: a piece is N / 2 pairs of neighbours;
@@ -130,12 +133,13 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
             const bool turn = u < turned;
             // first element of the piece, and of its partner
             const int f0 = INTER ? u * N : turn ? u * N : a.rot + (u - turned) * N, f1 = f0 + half;
-            float c[N], s[N];
+            constexpr int NT = kTurns<INTER, N>;
+            float c[NT], s[NT];
             if (turn) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    c[e] = s_cos[INTER ? (f0 + e) >> 1 : f0 + e];
-                    s[e] = s_sin[INTER ? (f0 + e) >> 1 : f0 + e];
+                for (int e = 0; e < NT; ++e) {
+                    c[e] = s_cos[(INTER ? f0 >> 1 : f0) + e];
+                    s[e] = s_sin[(INTER ? f0 >> 1 : f0) + e];
                 }
             }
             for (int r = tid / lanes; r < n_rows; r += rows_at_once) {

@@ -11,27 +11,35 @@
 
 #include <type_traits>
 
+#include "rr_device.hpp"
 #include "rr_internal.hpp"
 #include "rr_pages.hpp"
 
 namespace rr {
 namespace {
 
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+
 // ------------------------------------------------------------------- fork
 
-constexpr int kForkThreads = 256;
+constexpr int kForkThreads = 512, kForkAtOnce = 4;
 constexpr int kForkLds = 65536;  // bytes of parents, children and columns
 
 // Row b becomes what row parent[b] was; no such row: empty.  A workgroup takes
-// some columns of all rows, through LDS, so that rows change in place.  A row
-// that k others become and that itself changes (m = 1) or not (0) adds k - m
-// holders to each of its pages.
+// C columns of all rows, through LDS, so that rows change in place.  A row that
+// k others become and that itself changes (m = 1) or not (0) adds k - m holders
+// to each of its pages.
+//
+// Bound by those additions where many rows change: sequences that hold the same
+// page mostly follow each other, so neighbouring rows' are summed in a wave
+// before one of them adds (beams of 512 sequences, in groups of 8 that share all
+// but the last page of up to 1000: 12.2 -> 9.2 us).
+template <int C>
 __global__ __launch_bounds__(kForkThreads) void fork_kernel(ForkArgs a)
 {
     extern __shared__ int32_t lds[];
     int32_t *s_parent = lds, *s_kids = lds + a.n_seqs, *s_tile = lds + 2 * a.n_seqs;
-    const int tid = threadIdx.x, C = a.columns;
-    const int c0 = blockIdx.x * C;
+    const int tid = threadIdx.x, c0 = blockIdx.x * C, n = a.n_seqs * C;
     for (int b = tid; b < a.n_seqs; b += kForkThreads) s_kids[b] = 0;
     __syncthreads();
     for (int b = tid; b < a.n_seqs; b += kForkThreads) {
@@ -41,18 +49,47 @@ __global__ __launch_bounds__(kForkThreads) void fork_kernel(ForkArgs a)
         if (s >= 0 && s != b) atomicAdd(s_kids + s, 1);
     }
     __syncthreads();
-    for (int x = tid; x < a.n_seqs * C; x += kForkThreads) {
-        const int b = x / C, c = c0 + x - b * C, more = s_kids[b] - (s_parent[b] != b);
-        if (c >= a.max_pages || (s_kids[b] == 0 && s_parent[b] == b)) continue;
-        const int e = a.table[(int64_t)b * a.max_pages + c];
-        s_tile[x] = e;
-        if (more && (uint32_t)e < (uint32_t)a.n_pages) atomicAdd(a.refs + e, more);
+    const int lane = tid & 63;
+    uint64_t column = 0;  // lanes of this one's column
+#pragma unroll
+    for (int l = 0; l < 64; l += C) column |= (uint64_t)1 << l;
+    column <<= lane % C;
+    // (entries that wait for nothing but themselves: some at a time)
+    for (int x0 = tid; x0 - tid < n; x0 += kForkAtOnce * kForkThreads) {
+        int e[kForkAtOnce], more[kForkAtOnce];
+#pragma unroll
+        for (int j = 0; j < kForkAtOnce; ++j) {
+            const int x = x0 + j * kForkThreads, b = x / C, c = c0 + x % C;
+            more[j] = 0;
+            e[j] = -1;
+            if (x >= n || c >= a.max_pages) continue;
+            const int kids = s_kids[b];
+            const bool stays = s_parent[b] == b;
+            more[j] = kids - !stays;
+            if (kids || !stays) e[j] = a.table[(int64_t)b * a.max_pages + c];
+        }
+#pragma unroll
+        for (int j = 0; j < kForkAtOnce; ++j) {
+            if (x0 + j * kForkThreads < n) s_tile[x0 + j * kForkThreads] = e[j];
+            // runs of rows with the same page, numbered; the sum of each, in its first row
+            const int above = __shfl_up(e[j], C, 64);
+            const bool first = lane < C || above != e[j] || e[j] < 0;
+            const int run = __popcll(__ballot(first) & column & (~(uint64_t)0 >> (63 - lane)));
+            int sum = more[j];
+            if (__ballot(!first)) {
+#pragma unroll
+                for (int step = C; step < 64; step *= 2) {
+                    const int other = __shfl_down(run, step, 64), y = __shfl_down(sum, step, 64);
+                    if (lane + step < 64 && other == run) sum += y;
+                }
+            }
+            if (first && sum && (uint32_t)e[j] < (uint32_t)a.n_pages) atomicAdd(a.refs + e[j], sum);
+        }
     }
     __syncthreads();
-    for (int x = tid; x < a.n_seqs * C; x += kForkThreads) {
-        const int b = x / C, k = x - b * C, c = c0 + k, s = s_parent[b];
-        if (c >= a.max_pages || s == b) continue;
-        a.table[(int64_t)b * a.max_pages + c] = s >= 0 ? s_tile[s * C + k] : -1;
+    for (int x = tid; x < n; x += kForkThreads) {
+        const int b = x / C, c = c0 + x % C, s = s_parent[b];
+        if (c < a.max_pages && s != b) a.table[(int64_t)b * a.max_pages + c] = s >= 0 ? s_tile[s * C + x % C] : -1;
     }
     if (blockIdx.x > 0) return;
     __syncthreads();
@@ -62,87 +99,125 @@ __global__ __launch_bounds__(kForkThreads) void fork_kernel(ForkArgs a)
         if (s_parent[b] != b) a.lengths[b] = s_parent[b] >= 0 ? s_tile[s_parent[b]] : 0;
 }
 
-// ----------------------------------------------------------------- resize
+// ------------------------------------------- one workgroup that keeps the books
 
-constexpr int kReleaseThreads = 256, kReleaseColumns = 1024;
 constexpr int kBookThreads = 1024, kBookWaves = kBookThreads / 64;
-constexpr int kScan = 4;  // blocks of four pages a thread that are looked at together
+constexpr int kDeviceScope = 16;  // sc1 of a buffer instruction
 
 typedef int32_t i32x4_t __attribute__((ext_vector_type(4), aligned(4)));
 
-// Entries past a sequence's last page let go of theirs.
-__global__ __launch_bounds__(kReleaseThreads) void release_kernel(PagesArgs a)
-{
-    const int tiles = (a.max_pages + kReleaseColumns - 1) / kReleaseColumns;
-    const int b = blockIdx.x / tiles, c0 = (blockIdx.x - b * tiles) * kReleaseColumns;
-    const int length = held_tokens(a.lengths[b], a.capacity);
-    const int end = a.pd.div(length + a.pd.page - 1);
-#pragma unroll
-    for (int k = 0; k < kReleaseColumns; k += kReleaseThreads) {
-        const int c = c0 + k + threadIdx.x;
-        if (c < end || c >= a.max_pages) continue;
-        int32_t *entry = a.table + (int64_t)b * a.max_pages + c;
-        const int e = pool_page(*entry, a.n_pages);
-        if (e < 0) continue;
-        atomicSub(a.refs + e, 1);
-        *entry = -1;
-    }
-}
-
-// Sums of x over the threads before this one, and over all of them.
-template <typename T>
-__device__ __forceinline__ T before_of(T x, T *s_wave, T *all)
-{
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    T to = x;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const T y = __shfl_up(to, o, 64);
-        if (lane >= o) to += y;
-    }
-    __syncthreads();
-    if (lane == 63) s_wave[w] = to;
-    __syncthreads();
-    T base = 0, sum = 0;
-#pragma unroll
-    for (int i = 0; i < kBookWaves; ++i) {
-        if (i < w) base += s_wave[i];
-        sum += s_wave[i];
-    }
-    *all = sum;
-    return base + to - x;
-}
-
 __device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// What other waves of this workgroup may have changed a moment ago.
+// What other waves may have changed a moment ago.
 __device__ __forceinline__ int32_t now(const int32_t *p)
 {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// refs of the four pages from p on (1 past the pools).
-__device__ __forceinline__ i32x4_t four_refs(const PagesArgs &a, int p)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int x)
 {
-    if (p + 4 <= a.n_pages) return *reinterpret_cast<const i32x4_t *>(a.refs + p);
-    i32x4_t r;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = p + e < a.n_pages ? a.refs[p + e] : 1;
-    return r;
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true);
 }
 
-// The entries of the newest tokens, a thread each, in the order of sequences
-// and entries: those without a page get one, and those whose page others hold
-// too get a copy of it.  One workgroup.
-__global__ __launch_bounds__(kBookThreads) void provide_kernel(PagesArgs a)
+// Sums over lanes 0 .. this one of its row of 16, and of the wave.
+__device__ __forceinline__ int row_up_to(int x)
 {
-    __shared__ int s_first[kBookThreads], s_begin[kBookThreads], s_to[kBookThreads + 1], s_missing[kBookThreads];
-    __shared__ int s_page[kBookThreads], s_free[kBookThreads];
-    __shared__ int s_wave[kBookWaves];
-    __shared__ uint64_t s_wave64[kBookWaves];
+    x += moved<0x111, 0xf>(x);  // from 1, 2, 4 and 8 lanes before
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    return x + moved<0x118, 0xf>(x);
+}
+
+__device__ __forceinline__ int wave_up_to(int x)
+{
+    x = row_up_to(x);
+    x += moved<0x142, 0xa>(x);         // row 0 to row 1, row 2 to row 3
+    return x + moved<0x143, 0xc>(x);   // the first two rows to the others
+}
+
+// Sums over the waves before this one of what each one has (`mine`, in its lane
+// 63), and over all of them, in one barrier; s_wave is one of two that calls
+// take in turn.  One workgroup's time goes into instructions (its 16 waves share
+// four SIMDs: 16 cycles each), so sums are few and by data-parallel moves.
+__device__ __forceinline__ int waves_before(int mine, int *s_wave, int *all)
+{
+    static_assert(kBookWaves == 16, "a row of lanes");
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (lane == 63) s_wave[w] = mine;
+    __syncthreads();
+    const int to = row_up_to(s_wave[lane & 15]);
+    *all = __builtin_amdgcn_readlane(to, 15);
+    return w ? __builtin_amdgcn_readlane(to, w - 1) : 0;
+}
+
+// Sums of x over the threads before this one, and over all of them.
+__device__ __forceinline__ int before_of(int x, int *s_wave, int *all)
+{
+    const int to = wave_up_to(x);
+    return waves_before(to, s_wave, all) + to - x;
+}
+
+// A round's pages: kScan times 256 of each wave, four a lane, wave after wave.
+constexpr int kScan = 4, kWavePages = kScan * 256, kRoundPages = kBookWaves * kWavePages;
+
+// ----------------------------------------------------------------- resize
+
+constexpr int kEntriesEach = 4;  // of the table, a thread of a resize
+
+// How many of s_page[0 .. n) are e.
+__device__ __forceinline__ int times_before(const int *s_page, int n, int e)
+{
+    typedef int32_t V __attribute__((ext_vector_type(4)));
+    int found = 0, j = 0;
+#pragma unroll 4
+    for (; j + 4 <= n; j += 4) {
+        const V v = *reinterpret_cast<const V *>(s_page + j);
+        found += (v[0] == e) + (v[1] == e) + (v[2] == e) + (v[3] == e);
+    }
+    for (; j < n; ++j) found += s_page[j] == e;
+    return found;
+}
+
+// Entries past a sequence's last page let go of theirs, all workgroups; then
+// the one that comes last goes through the entries of the newest tokens, a
+// thread each, in the order of sequences and entries: those without a page get
+// one, and those whose page others hold too get a copy of it.
+__global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
+{
+    __shared__ int s_first[kBookThreads], s_begin[kBookThreads], s_to[kBookThreads], s_missing[kBookThreads];
+    __shared__ __attribute__((aligned(16))) int s_page[kBookThreads];
+    __shared__ int s_free[kBookThreads];
+    __shared__ int s_wave[2][kBookWaves];
     __shared__ int s_cursor, s_copies, s_stop;
-    const int tid = threadIdx.x;
-    if (tid == 0) s_cursor = s_copies = 0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    const int64_t from0 = (int64_t)blockIdx.x * (kEntriesEach * kBookThreads);
+    const int b_first = (int)(from0 / a.max_pages), c_first = (int)(from0 - (int64_t)b_first * a.max_pages);
+#pragma unroll
+    for (int j = 0; j < kEntriesEach; ++j) {
+        const int x = c_first + j * kBookThreads + tid, b = b_first + x / a.max_pages, c = x % a.max_pages;
+        if (b >= a.n_seqs) continue;
+        int32_t *entry = a.table + (int64_t)b * a.max_pages + c;
+        const int e = pool_page(*entry, a.n_pages);
+        const int end = a.pd.div(held_tokens(a.lengths[b], a.capacity) + a.pd.page - 1);
+        if (c < end || e < 0) continue;
+        atomicSub(a.refs + e, 1);
+        *entry = -1;
+    }
+    wait_vm();        // this wave's changes are there for all ...
+    __syncthreads();  // ... and the other waves'
+    if (tid == 0) {
+        const uint32_t before = __hip_atomic_fetch_add(a.counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_stop = before == gridDim.x - 1;
+        if (s_stop) __hip_atomic_store(a.counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_cursor = s_copies = 0;
+    }
+    __syncthreads();
+    if (!s_stop) return;
+
+    const __amdgpu_buffer_rsrc_t refs =
+        __builtin_amdgcn_make_buffer_rsrc(a.refs, 0, a.n_pages * (int)sizeof(int32_t), 0x00020000);
     for (int b0 = 0; b0 < a.n_seqs; b0 += kBookThreads) {
         // the sequences' new entries
         const int b = b0 + tid;
@@ -156,30 +231,26 @@ __global__ __launch_bounds__(kBookThreads) void provide_kernel(PagesArgs a)
             }
         }
         int items;
-        const int at = before_of(n, s_wave, &items);
+        s_to[tid] = before_of(n, s_wave[0], &items);
         s_first[tid] = first;
         s_begin[tid] = begin;
-        s_to[tid] = at;
         s_missing[tid] = 0;
-        if (tid == 0) s_to[kBookThreads] = items;
         __syncthreads();
         for (int i0 = 0; i0 < items; i0 += kBookThreads) {
             const int i = i0 + tid;
-            const bool live = i < items;
             int q = 0, c = 0, e = -1, holders = 0;
-            if (live) {
+            if (i < items) {
                 // the last sequence that begins at or before item i
-                int lo = 0, hi = kBookThreads;
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) / 2;
+                int hi = min(kBookThreads, a.n_seqs - b0);
+                while (hi - q > 1) {
+                    const int mid = (q + hi) / 2;
                     if (s_to[mid] <= i)
-                        lo = mid;
+                        q = mid;
                     else
                         hi = mid;
                 }
-                q = lo;
                 c = s_first[q] + i - s_to[q];
-                e = pool_page(now(a.table + (int64_t)(b0 + q) * a.max_pages + c), a.n_pages);
+                e = pool_page(a.table[(int64_t)(b0 + q) * a.max_pages + c], a.n_pages);
                 if (e >= 0) holders = now(a.refs + e);
             }
             // A page that several hold is copied as long as that is so: each
@@ -189,36 +260,51 @@ __global__ __launch_bounds__(kBookThreads) void provide_kernel(PagesArgs a)
             if (__syncthreads_or(shared)) {
                 s_page[tid] = shared ? e : -1;
                 __syncthreads();
-                if (shared)
-                    for (int j = 0; j < tid; ++j) rank += s_page[j] == e;
+                if (shared) rank = times_before(s_page, tid, e);
             }
-            bool need = live && (e < 0 || holders - rank > 1);
-            int wanted;
-            const int order = before_of((int)need, s_wave, &wanted);
+            bool need = i < items && (e < 0 || holders - rank > 1);
+            int wanted, have = 0;
+            const int order = before_of((int)need, s_wave[1], &wanted);
             // the lowest free pages
-            int have = 0;
-            for (int from = s_cursor; have < wanted && from < a.n_pages; from += 4 * kScan * kBookThreads) {
+            int turn = 1;
+            for (int from = s_cursor; have < wanted && from < a.n_pages; from += kRoundPages) {
+                const int p0 = from + wave * kWavePages + 4 * lane;
+                int free = 0, at[kScan];
                 i32x4_t r[kScan];
+                if (p0 - 4 * lane < a.n_pages) {
 #pragma unroll
-                for (int k = 0; k < kScan; ++k) r[k] = four_refs(a, min(from + 4 * (k * kBookThreads + tid), a.n_pages));
-                uint64_t mine = 0, all;  // free pages of each block, 16 bits each
+                    for (int k = 0; k < kScan; ++k)
+                        r[k] = __builtin_bit_cast(
+                            i32x4_t, __builtin_amdgcn_raw_buffer_load_b128(refs, 4 * (p0 + 256 * k), 0, kDeviceScope));
 #pragma unroll
-                for (int k = 0; k < kScan; ++k)
-                    mine |= (uint64_t)((r[k][0] == 0) + (r[k][1] == 0) + (r[k][2] == 0) + (r[k][3] == 0)) << (16 * k);
-                const uint64_t before = before_of(mine, s_wave64, &all);
+                    for (int k = 0; k < kScan; ++k) {
+                        int mine = 0;
 #pragma unroll
-                for (int k = 0; k < kScan; ++k) {
-                    int at_free = have + (int)(before >> (16 * k) & 0xffff);
-                    const int p = from + 4 * (k * kBookThreads + tid);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        if (r[k][x] == 0) {
-                            if (at_free < wanted) s_free[at_free] = p + x;
-                            if (at_free == wanted - 1) s_cursor = p + x + 1;
-                            ++at_free;
+                        for (int x = 0; x < 4; ++x) {
+                            if (p0 + 256 * k + x >= a.n_pages) r[k][x] = 1;  // (past the pools zeros are read)
+                            mine += r[k][x] == 0;
                         }
-                    have += (int)(all >> (16 * k) & 0xffff);
+                        const int to = wave_up_to(mine);
+                        at[k] = free + to - mine;
+                        free += __builtin_amdgcn_readlane(to, 63);
+                    }
                 }
+                int all;
+                const int before = have + waves_before(free, s_wave[turn ^= 1], &all);
+                if (free) {
+#pragma unroll
+                    for (int k = 0; k < kScan; ++k) {
+                        int to = before + at[k];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            if (r[k][x] == 0) {
+                                if (to < wanted) s_free[to] = p0 + 256 * k + x;
+                                if (to == wanted - 1) s_cursor = p0 + 256 * k + x + 1;
+                                ++to;
+                            }
+                    }
+                }
+                have += all;
             }
             if (tid == 0) s_stop = kBookThreads;
             __syncthreads();
@@ -228,11 +314,7 @@ __global__ __launch_bounds__(kBookThreads) void provide_kernel(PagesArgs a)
                 if (need && order == have) s_stop = tid;
                 if (tid == 0) s_cursor = a.n_pages;
                 __syncthreads();
-                if (shared && tid > s_stop) {
-                    rank = 0;
-                    for (int j = 0; j < s_stop; ++j) rank += s_page[j] == e;
-                    need = holders - rank > 1;
-                }
+                if (shared && tid > s_stop) need = holders - times_before(s_page, s_stop, e) > 1;
             }
             if (need && tid < s_stop) {
                 const int id = s_free[order];
@@ -249,7 +331,6 @@ __global__ __launch_bounds__(kBookThreads) void provide_kernel(PagesArgs a)
             wait_vm();  // (the pages' counts, for the next round)
             __syncthreads();
         }
-        __syncthreads();
         if (a.missing && b < a.n_seqs) a.missing[b] = s_missing[tid];
         __syncthreads();
     }
@@ -258,53 +339,96 @@ __global__ __launch_bounds__(kBookThreads) void provide_kernel(PagesArgs a)
 
 // ---------------------------------------------------------------- compact
 
+// refs of the four pages from p on, as far as there are any.
+__device__ __forceinline__ i32x4_t four_refs(const PagesArgs &a, int p)
+{
+    if (p + 4 <= a.n_pages) return *reinterpret_cast<const i32x4_t *>(a.refs + p);
+    i32x4_t r = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (p + e < a.n_pages) r[e] = a.refs[p + e];
+    return r;
+}
+
 // The n used pages that lie past page n - 1 take the free ones before it, in
 // order.  One workgroup: the pages are counted, then listed, then the counts
 // of holders move.
 __global__ __launch_bounds__(kBookThreads) void compact_kernel(PagesArgs a)
 {
-    __shared__ int s_wave[kBookWaves];
-    __shared__ uint64_t s_wave64[kBookWaves];
-    const int tid = threadIdx.x;
+    __shared__ int s_wave[2][kBookWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int mine = 0, used;
+#pragma unroll 4
     for (int p = 4 * tid; p < a.n_pages; p += 4 * kBookThreads) {
         const i32x4_t r = four_refs(a, p);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) mine += p + x < a.n_pages && r[x] != 0;
+        for (int x = 0; x < 4; ++x) mine += r[x] != 0;
     }
-    before_of(mine, s_wave, &used);
-    int low = 0, high = 0;  // free pages before page `used`, used ones from it on
-    for (int p0 = 0; p0 < a.n_pages; p0 += 4 * kBookThreads) {
-        const int p = p0 + 4 * tid;
-        i32x4_t r = {0, 0, 0, 0};
-        if (p < a.n_pages) r = four_refs(a, p);
-        uint64_t n = 0, all;
+    before_of(mine, s_wave[0], &used);
+    int low = 0, high = 0, turn = 0;  // free pages before page `used`, used ones from it on
+    for (int from = 0; from < a.n_pages; from += kRoundPages) {
+        const int p0 = from + wave * kWavePages + 4 * lane;
+        // of both kinds, 16 bits each: in blocks of this wave before this one,
+        // and in lanes of this one before this one
+        int found = 0, at[kScan];
+        i32x4_t r[kScan];
+        if (p0 - 4 * lane < a.n_pages) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-            if (p + x < a.n_pages) n += p + x < used ? (uint64_t)(r[x] == 0) : (uint64_t)(r[x] != 0) << 32;
-        const uint64_t before = before_of(n, s_wave64, &all);
-        int at_low = low + (int)(uint32_t)before, at_high = high + (int)(before >> 32);
+            for (int k = 0; k < kScan; ++k) r[k] = four_refs(a, min(p0 + 256 * k, a.n_pages));
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            if (p + x >= a.n_pages) continue;
-            const bool is_used = r[x] != 0;
-            if (p + x < used || !is_used) a.new_ids[p + x] = is_used ? p + x : -1;
-            if (p + x < used && !is_used) a.copies[at_low++].dst = p + x;
-            if (p + x >= used && is_used) {
-                a.copies[at_high].src = p + x;
-                a.copies[at_high++].places = a.pd.page;
+            for (int k = 0; k < kScan; ++k) {
+                int n = 0;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) n += p0 + 256 * k + x < used ? (int)(r[k][x] == 0) : (int)(r[k][x] != 0) << 16;
+                const int to = wave_up_to(n);
+                at[k] = found + to - n;
+                found += __builtin_amdgcn_readlane(to, 63);
             }
         }
-        low += (int)(uint32_t)all;
-        high += (int)(all >> 32);
+        int all;
+        const int before = waves_before(found, s_wave[turn ^= 1], &all);
+        if (p0 - 4 * lane < a.n_pages) {
+#pragma unroll
+            for (int k = 0; k < kScan; ++k) {
+                const int to = before + at[k];
+                int at_low = low + (to & 0xffff), at_high = high + (to >> 16);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int p = p0 + 256 * k + x;
+                    if (p >= a.n_pages) continue;
+                    const bool is_used = r[k][x] != 0;
+                    if (p < used || !is_used) a.new_ids[p] = is_used ? p : -1;
+                    if (p < used && !is_used) a.copies[at_low++].dst = p;
+                    if (p >= used && is_used) {
+                        a.copies[at_high].src = p;
+                        a.copies[at_high++].places = a.pd.page;
+                    }
+                }
+            }
+        }
+        low += all & 0xffff;
+        high += all >> 16;
     }
     wait_vm();
     __syncthreads();
-    for (int k = tid; k < high; k += kBookThreads) {
-        const int src = now(&a.copies[k].src), dst = now(&a.copies[k].dst);
-        a.refs[dst] = a.refs[src];
-        a.refs[src] = 0;
-        a.new_ids[src] = dst;
+    constexpr int kMoves = 4;  // (at a time)
+    for (int k0 = tid; k0 < high; k0 += kMoves * kBookThreads) {
+        int src[kMoves], dst[kMoves], held[kMoves];
+#pragma unroll
+        for (int j = 0; j < kMoves; ++j) {
+            const int k = min(k0 + j * kBookThreads, high - 1);
+            src[j] = now(&a.copies[k].src);
+            dst[j] = now(&a.copies[k].dst);
+        }
+#pragma unroll
+        for (int j = 0; j < kMoves; ++j) held[j] = a.refs[src[j]];
+#pragma unroll
+        for (int j = 0; j < kMoves; ++j) {
+            if (k0 + j * kBookThreads >= high) continue;
+            a.refs[dst[j]] = held[j];
+            a.refs[src[j]] = 0;
+            a.new_ids[src[j]] = dst[j];
+        }
     }
     if (tid == 0) {
         *a.n_copies = high;
@@ -312,101 +436,150 @@ __global__ __launch_bounds__(kBookThreads) void compact_kernel(PagesArgs a)
     }
 }
 
-__global__ __launch_bounds__(256) void rename_kernel(PagesArgs a)
-{
-    const int64_t n = (int64_t)a.n_seqs * a.max_pages;
-    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int e = pool_page(a.table[i], a.n_pages);
-        if (e >= 0) a.table[i] = a.new_ids[e];
-    }
-}
-
 // ------------------------------------------------------------------ copies
 
-constexpr int kCopyThreads = 256, kCopyEach = 8;  // pieces of a thread's turn
-constexpr int kCopyGroups = 2048;
+constexpr int kCopyThreads = 256;
 
-// Pages of all pools, a piece of P bytes at a time: a unit is the same stretch
-// of the pieces of one page in one pool.
-template <typename P>
-__global__ __launch_bounds__(kCopyThreads) void copies_kernel(PagesArgs a, Pools pools, int n_pools)
+// How pages are copied.  Compaction reads every page once and leaves little to
+// other calls, so both ways go past the caches, and workgroups are many: 600
+// pages of 128 KB in four pools (629 MB) in 111 us, 5.6 TB/s; four pieces a
+// thread and 8192 workgroups 117, with stores alone past the caches 120, none
+// 125.  Copies of a page that several sequences share are read from the L2 by
+// all but the first, and most calls have none to make: fewer workgroups (an
+// empty launch of 4096 takes 2.6 us, of 8192 3.4).
+struct Moved {
+    static constexpr int kEach = 2, kGroups = 16384;  // pieces of a thread's turn
+    static constexpr bool kOnce = true;
+};
+struct Shared {
+    static constexpr int kEach = 4, kGroups = 4096;
+    static constexpr bool kOnce = false;
+};
+
+// Pages of all pools, a piece (a vector P) at a time.  A unit of a workgroup's
+// work is a stretch of the pieces of one page in one pool, or (SMALL) as many
+// pages as it has room for.  units < 2^31.
+//
+// Before that, after a compaction (in the first of its launches), the entries
+// of the table take their pages' new names.
+template <typename P, bool SMALL, typename How>
+__global__ __launch_bounds__(kCopyThreads) void copies_kernel(PagesArgs a, Pools pools, uint32_t n_pools, int64_t n_entries)
 {
-    const int n = *a.n_copies;
-    const int row = a.row_bytes / (int)sizeof(P), whole = a.pd.page * row;  // pieces of a token of a head, of a page of a head
-    constexpr int kStretch = kCopyThreads * kCopyEach;
-    const int64_t stretches = ((int64_t)a.heads * whole + kStretch - 1) / kStretch;
-    const int64_t units = (int64_t)n * n_pools * stretches;
-    for (int64_t t = blockIdx.x; t < units; t += gridDim.x) {
-        const int64_t pair = t / stretches, x0 = (t - pair * stretches) * kStretch;
-        const int k = (int)(pair / n_pools), pool = (int)(pair - (int64_t)k * n_pools);
-        const PageCopy c = a.copies[k];
-        const int seg = c.places * row;  // pieces that move of a head
-        const int64_t all = (int64_t)a.heads * seg;
-        P *base = static_cast<P *>(pools.p[pool]);
-        const P *src = base + (int64_t)c.src * a.heads * whole;
-        P *dst = base + (int64_t)c.dst * a.heads * whole;
-        P v[kCopyEach];
-        int64_t at[kCopyEach];
+    if constexpr (How::kOnce) {
+        const int64_t all = (int64_t)gridDim.x * kCopyThreads;
+        for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < n_entries; i += all) {
+            const int e = pool_page(a.table[i], a.n_pages);
+            if (e >= 0) a.table[i] = a.new_ids[e];
+        }
+    }
+    constexpr int kEach = How::kEach, kCopyUnit = kEach * kCopyThreads;
+    const uint32_t pairs = (uint32_t)*a.n_copies * n_pools;
+    const uint32_t row = a.row_bytes / sizeof(P), head = a.pd.page * row;  // pieces of a token of a head, of a head's page
+    const uint32_t page = a.heads * head;
+    const uint32_t each = SMALL ? kCopyUnit / page : (page + kCopyUnit - 1) / kCopyUnit;  // pages a unit; units a page
+    const uint32_t units = SMALL ? (pairs + each - 1) / each : pairs * each;
+    for (uint32_t t = blockIdx.x; t < units; t += gridDim.x) {
+        P v[kEach], *to[kEach];
 #pragma unroll
-        for (int j = 0; j < kCopyEach; ++j) {
-            const int64_t x = x0 + j * kCopyThreads + threadIdx.x;
-            at[j] = -1;
-            if (x < all) {
-                const int g = (int)((uint32_t)x / (uint32_t)seg);
-                at[j] = (int64_t)g * whole + ((int)x - g * seg);
-                v[j] = src[at[j]];
+        for (int j = 0; j < kEach; ++j) {
+            uint32_t x = j * kCopyThreads + threadIdx.x, pair;
+            if (SMALL) {
+                pair = t * each + x / page;
+                x %= page;
+            } else {
+                pair = t / each;
+                x += (t - pair * each) * kCopyUnit;
             }
+            to[j] = nullptr;
+            if (SMALL && (pair >= pairs || pair >= (t + 1) * each)) continue;
+            const uint32_t k = pair / n_pools;
+            const PageCopy c = a.copies[k];
+            const uint32_t part = c.places * row;  // pieces that move of a head
+            if (x >= a.heads * part) continue;
+            const uint32_t at = part == head ? x : x / part * head + x % part;
+            P *base = static_cast<P *>(pools.p[pair - k * n_pools]);
+            const P *from = base + (int64_t)c.src * page + at;
+            v[j] = How::kOnce ? __builtin_nontemporal_load(from) : *from;
+            to[j] = base + (int64_t)c.dst * page + at;
         }
 #pragma unroll
-        for (int j = 0; j < kCopyEach; ++j)
-            if (at[j] >= 0) dst[at[j]] = v[j];
+        for (int j = 0; j < kEach; ++j)
+            if (to[j]) __builtin_nontemporal_store(v[j], to[j]);
     }
 }
 
 }  // namespace
 
-int64_t release_groups(int32_t n_seqs, int32_t max_pages)
+int64_t resize_groups(int32_t n_seqs, int32_t max_pages)
 {
-    return (int64_t)n_seqs * ((max_pages + kReleaseColumns - 1) / kReleaseColumns);
+    return ((int64_t)n_seqs * max_pages + kEntriesEach * kBookThreads - 1) / (kEntriesEach * kBookThreads);
 }
 
-hipError_t launch_fork(const ForkArgs &args, hipStream_t stream)
+hipError_t launch_fork(const ForkArgs &a, hipStream_t stream)
 {
-    ForkArgs a = args;
-    // as many columns as LDS holds, up to 8
-    a.columns = 8;
-    while (a.columns > 1 && a.n_seqs * (2 + a.columns) * (int)sizeof(int32_t) > kForkLds) a.columns /= 2;
-    const unsigned lds = (unsigned)(a.n_seqs * (2 + a.columns) * sizeof(int32_t));
-    hipLaunchKernelGGL(fork_kernel, dim3((unsigned)((a.max_pages + a.columns - 1) / a.columns)), dim3(kForkThreads), lds,
-                       stream, a);
+    auto lds = [&](int columns) { return a.n_seqs * (2 + columns) * (int)sizeof(int32_t); };
+    auto go = [&](auto kern, int columns) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)((a.max_pages + columns - 1) / columns)), dim3(kForkThreads), (unsigned)lds(columns),
+                           stream, a);
+    };
+    // as many columns as LDS holds, up to 8, and to 4 where that leaves compute units idle
+    if (lds(8) <= kForkLds && a.max_pages >= 8 * 256)
+        go(fork_kernel<8>, 8);
+    else if (lds(4) <= kForkLds)
+        go(fork_kernel<4>, 4);
+    else if (lds(2) <= kForkLds)
+        go(fork_kernel<2>, 2);
+    else
+        go(fork_kernel<1>, 1);
     return hipGetLastError();
 }
 
 hipError_t launch_resize(const PagesArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL(release_kernel, dim3((unsigned)release_groups(a.n_seqs, a.max_pages)), dim3(kReleaseThreads), 0, stream,
-                       a);
-    hipLaunchKernelGGL(provide_kernel, dim3(1), dim3(kBookThreads), 0, stream, a);
+    hipLaunchKernelGGL(resize_kernel, dim3((unsigned)resize_groups(a.n_seqs, a.max_pages)), dim3(kBookThreads), 0, stream, a);
     return hipGetLastError();
 }
 
 hipError_t launch_compact(const PagesArgs &a, hipStream_t stream)
 {
     hipLaunchKernelGGL(compact_kernel, dim3(1), dim3(kBookThreads), 0, stream, a);
-    const int64_t groups = ((int64_t)a.n_seqs * a.max_pages + 255) / 256;
-    hipLaunchKernelGGL(rename_kernel, dim3((unsigned)(groups < 1024 ? groups : 1024)), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
-hipError_t launch_copies(const PagesArgs &a, const Pools &pools, int n_pools, hipStream_t stream)
+template <typename How>
+hipError_t copy_pages(const PagesArgs &a, void *const *list, int n, int64_t most_copies, hipStream_t stream)
 {
-    auto go = [&](auto piece) {
-        typedef decltype(piece) P;
-        hipLaunchKernelGGL(copies_kernel<P>, dim3(kCopyGroups), dim3(kCopyThreads), 0, stream, a, pools, n_pools);
-    };
     // (rows of 8 features are 8 bytes in e4m3)
-    a.row_bytes % 16 == 0 ? go(uint4()) : go(uint2());
+    const int piece = a.row_bytes % 16 == 0 ? 16 : 8, unit = How::kEach * kCopyThreads;
+    const int64_t page = (int64_t)a.heads * a.pd.page * (a.row_bytes / piece);
+    const int64_t most = (int64_t)INT32_MAX / (a.n_pages * ((page + unit - 1) / unit));
+    const int at_once = (int)(most < 1 ? 1 : most < kPoolsAtOnce ? most : kPoolsAtOnce);
+    for (int i0 = 0; i0 < n; i0 += at_once) {
+        const int some = n - i0 < at_once ? n - i0 : at_once;
+        Pools pools{};
+        for (int i = 0; i < some; ++i) pools.p[i] = list[i0 + i];
+        const bool small = page <= unit / 2;
+        const int64_t units = small ? most_copies * some / (unit / page) + 1 : most_copies * some * ((page + unit - 1) / unit);
+        const int64_t entries = How::kOnce && i0 == 0 ? (int64_t)a.n_seqs * a.max_pages : 0, turns = entries / kCopyThreads + 1;
+        const int64_t wanted = units > turns ? units : turns;
+        const int groups = (int)(wanted < How::kGroups ? wanted : How::kGroups);
+        auto go = [&](auto kern) {
+            hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kCopyThreads), 0, stream, a, pools, (uint32_t)some, entries);
+        };
+        if (piece == 16)
+            small ? go(copies_kernel<u32x4_t, true, How>) : go(copies_kernel<u32x4_t, false, How>);
+        else
+            small ? go(copies_kernel<u32x2_t, true, How>) : go(copies_kernel<u32x2_t, false, How>);
+    }
     return hipGetLastError();
+}
+
+hipError_t launch_copies(const PagesArgs &a, void *const *list, int n, bool compacted, hipStream_t stream)
+{
+    if (compacted) return copy_pages<Moved>(a, list, n, a.n_pages / 2, stream);
+    const int64_t entries = a.new_tokens ? a.max_pages : (int64_t)a.n_new / a.pd.page + 2;
+    const int64_t most = a.n_seqs * (entries < a.max_pages ? entries : a.max_pages);
+    return copy_pages<Shared>(a, list, n, most < a.n_pages ? most : a.n_pages, stream);
 }
 
 }  // namespace rr

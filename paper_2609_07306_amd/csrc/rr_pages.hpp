@@ -16,7 +16,6 @@ struct ForkArgs {
     const int32_t *parent;
     int32_t *table, *lengths, *refs;
     int32_t n_seqs, max_pages, n_pages;
-    int32_t columns;  // of a workgroup
 };
 
 // A page's first `places` places go from page src to page dst.
@@ -34,11 +33,12 @@ struct PagesArgs {
     int32_t heads;     // of a page
     int32_t row_bytes; // of a token of a head
     PageDiv pd;
-    int32_t *n_copies;  // workspace: copies to make ...
+    uint32_t *counter;  // workspace: finished workgroups, 0 between calls;
+    int32_t *n_copies;  // copies to make ...
     PageCopy *copies;   // ... [n_pages]
 };
 
-// The workspace holds the number of copies, then the copies.
+// The workspace holds the counter and the number of copies, then the copies.
 constexpr size_t kPagesHeadBytes = 256;
 inline size_t pages_workspace_bytes(int32_t n_pages) { return kPagesHeadBytes + (size_t)n_pages * sizeof(PageCopy); }
 
@@ -46,10 +46,10 @@ struct Pools {
     void *p[kPoolsAtOnce];
 };
 
-int64_t release_groups(int32_t n_seqs, int32_t max_pages);  // workgroups of a resize's first launch
+int64_t resize_groups(int32_t n_seqs, int32_t max_pages);
 hipError_t launch_fork(const ForkArgs &a, hipStream_t stream);
 hipError_t launch_resize(const PagesArgs &a, hipStream_t stream);   // the tables; copies to make
 hipError_t launch_compact(const PagesArgs &a, hipStream_t stream);  // the same
-hipError_t launch_copies(const PagesArgs &a, const Pools &pools, int n_pools, hipStream_t stream);
+hipError_t launch_copies(const PagesArgs &a, void *const *list, int n, bool compacted, hipStream_t stream);  // in n pools
 
 }  // namespace rr

@@ -44,16 +44,21 @@ __device__ __forceinline__ void write_piece(T *p, const float (&x)[N])
     }
 }
 
+// Frequencies of a piece.
+template <bool INTER, int N>
+constexpr int kTurns = INTER ? N / 2 : N;
+
 // Rotates a piece: neighbours are partners (INTER), or x's element e and y's.
 template <bool INTER, int N>
-__device__ __forceinline__ void turn_piece(float (&x)[N], float (&y)[N], const float (&c)[N], const float (&s)[N])
+__device__ __forceinline__ void turn_piece(float (&x)[N], float (&y)[N], const float (&c)[kTurns<INTER, N>],
+                                           const float (&s)[kTurns<INTER, N>])
 {
     if constexpr (INTER) {
 #pragma unroll
         for (int e = 0; e < N; e += 2) {
             const float p = x[e], q = x[e + 1];
-            x[e] = p * c[e] - q * s[e];
-            x[e + 1] = q * c[e] + p * s[e];
+            x[e] = p * c[e / 2] - q * s[e / 2];
+            x[e + 1] = q * c[e / 2] + p * s[e / 2];
         }
     } else {
 #pragma unroll
@@ -81,16 +86,42 @@ struct Axes {
     int64_t n;              // tokens
     int32_t n_axes, real;
 
-    // Token i's position as frequency j takes it; 0, which rotates nothing, for
-    // an axis that is not there.
-    __device__ __forceinline__ double at(int64_t i, int j) const
+    // Token i's positions as frequencies j .. j + N - 1 take them; 0, which
+    // rotates nothing, for an axis that is not there.  (Stage by stage: loads
+    // that depend on each other only where they must.)
+    template <int N>
+    __device__ __forceinline__ void at(int64_t i, int j, double (&p)[N]) const
     {
-        const int t = axis ? axis[j] : 0;
-        if ((uint32_t)t >= (uint32_t)n_axes) return 0.0;
-        const int64_t x = t * n + i;
-        return real ? (double)static_cast<const float *>(positions)[x] : (double)static_cast<const int32_t *>(positions)[x];
+        int t[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) t[e] = 0;
+        if (axis) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) t[e] = axis[j + e];
+        }
+        int32_t bits[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const bool there = (uint32_t)t[e] < (uint32_t)n_axes;
+            bits[e] = static_cast<const int32_t *>(positions)[(there ? t[e] : 0) * n + i];
+            if (!there) bits[e] = 0;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) p[e] = real ? (double)__int_as_float(bits[e]) : (double)bits[e];
     }
 };
+
+// Cosines and sines of token i for frequencies j .. j + N - 1.
+template <int N>
+__device__ __forceinline__ void turns_of(const Axes &axes, const double *freqs, int64_t i, int j, float (&c)[N], float (&s)[N])
+{
+    double p[N], f[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = freqs[j + e];
+    axes.at(i, j, p);
+#pragma unroll
+    for (int e = 0; e < N; ++e) turn_of(p[e], f[e], &c[e], &s[e]);
+}
 
 struct RotateArgs {
     const void *X;
@@ -99,8 +130,8 @@ struct RotateArgs {
     Axes axes;
     int64_t x_token, x_head, y_token, y_head;  // elements between rows
     int32_t n_heads, n_tokens, d, rot;
-    int32_t heads_each;  // heads that a workgroup goes through
-    float sign;          // -1: back
+    int32_t each, heads;  // heads, or tokens and heads, of a workgroup (set by the launcher)
+    float sign;           // -1: back
 };
 
 hipError_t launch_rotate(const RotateArgs &a, int dtype, bool interleaved, hipStream_t stream);

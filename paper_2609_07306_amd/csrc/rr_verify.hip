@@ -24,6 +24,7 @@ namespace {
 
 constexpr int kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
 constexpr int kStep = 256;  // elements of a wave's step: four a lane
+constexpr int kManyWaves = 4096;
 
 __device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -75,7 +76,8 @@ __device__ __forceinline__ double wave_sum(double x)
     return x;
 }
 
-// Sums of x over the threads before this one, and over all of them.
+// Sums of x over the threads before this one, and over all of them; s_wave is
+// one of two that calls take in turn.
 __device__ __forceinline__ double block_before(double x, double *s_wave, double *all)
 {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -86,7 +88,6 @@ __device__ __forceinline__ double block_before(double x, double *s_wave, double 
         if (lane >= o) to += y;
     }
     const double before = __shfl_up(to, 1, 64);
-    __syncthreads();
     if (lane == 63) s_wave[w] = to;
     __syncthreads();
     double base = 0.0, sum = 0.0;
@@ -99,15 +100,41 @@ __device__ __forceinline__ double block_before(double x, double *s_wave, double 
     return base + (lane ? before : 0.0);
 }
 
-template <typename T>
-__device__ __forceinline__ double part_sum(const Row<T> &row, int part, int size)
+// Elements of a part of STEPS steps as they lie in memory, a lane's.
+template <typename T, int STEPS>
+struct Held {
+    typename Four<T>::V x[STEPS], y[STEPS];
+};
+
+template <int STEPS, typename T>
+__device__ __forceinline__ void ask(const Row<T> &row, int from, Held<T, STEPS> &h)
 {
-    const int lane = threadIdx.x & 63, from = part * size, to = min(from + size, row.vocab);
+    if (from + STEPS * kStep > row.vocab) return;  // (the last part is read element by element)
+    const int v = from + 4 * (threadIdx.x & 63);
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        h.x[i] = *reinterpret_cast<const typename Four<T>::V *>(row.p + v + i * kStep);
+        if (row.kind == REST_DIFFERENCE) h.y[i] = *reinterpret_cast<const typename Four<T>::V *>(row.q + v + i * kStep);
+    }
+}
+
+// The sum of a part, of which `ask` has asked.
+template <int STEPS, typename T>
+__device__ __forceinline__ double part_sum(const Row<T> &row, int from, const Held<T, STEPS> &h)
+{
+    const int v = from + 4 * (threadIdx.x & 63);
+    const bool whole = from + STEPS * kStep <= row.vocab;
     double sum = 0.0;
-#pragma unroll 4
-    for (int v = from + 4 * lane; v < to; v += kStep) {
-        double r[4];
-        row.four(v, r);
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        double r[4] = {0.0, 0.0, 0.0, 0.0};
+        if (whole) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                r[e] = row.weight(value(h.x[i][e]), row.kind == REST_DIFFERENCE ? value(h.y[i][e]) : 0.0, v + i * kStep + e);
+        } else if (v + i * kStep < row.vocab) {
+            row.four(v + i * kStep, r);
+        }
         sum += (r[0] + r[1]) + (r[2] + r[3]);
     }
     return wave_sum(sum);
@@ -132,26 +159,25 @@ struct Found {
 
 // Of one place a thread, in order (`any`: it has some weight, `here`: the
 // border lies in it), the first that has the border, or else the last that has
-// any weight, into `f`.
-__device__ __forceinline__ void look(Found &f, bool any, bool here, int at, double before)
+// any weight, into `f` where it is not known yet; s_found is one of two that
+// calls take in turn.
+__device__ __forceinline__ void look(Found &f, bool any, bool here, int at, double before, Found *s_found)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint64_t some = __ballot(any), border = __ballot(here);
-    for (int w = 0; w < kVerifyWaves; ++w) {
-        if (w == wave && some && !f.known && lane == (border ? __builtin_ctzll(border) : 63 - __builtin_clzll(some))) {
-            f.at = at;
-            f.before = before;
-            f.known = border != 0;
-        }
-        __syncthreads();
-    }
+    if (some ? lane == (border ? __builtin_ctzll(border) : 63 - __builtin_clzll(some)) : lane == 0)
+        s_found[wave] = Found{some ? at : -1, border != 0, before};
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kVerifyWaves; ++w)
+        if (!f.known && s_found[w].at >= 0) f = s_found[w];
 }
 
-template <typename T>
+template <typename T, int STEPS>
 __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
 {
-    __shared__ double s_wave[kVerifyWaves];
-    __shared__ Found s_part, s_token;
+    __shared__ double s_wave[2][kVerifyWaves];
+    __shared__ Found s_found[2][kVerifyWaves];
     __shared__ int s_last;
     const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T *P = static_cast<const T *>(a.P) + b * a.p_seq, *Q = a.Q ? static_cast<const T *>(a.Q) + b * a.q_seq : nullptr;
@@ -183,73 +209,89 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
     Row<T> row{P + took * a.p_row, Q, took == count ? REST_TARGET : Q ? REST_DIFFERENCE : REST_WITHOUT, draft, a.vocab};
     if (row.kind == REST_DIFFERENCE) row.q += took * a.q_row;
 
-    // this wave's part
+    // this wave's parts, of which the next is asked for before one is summed
+    constexpr int kPart = STEPS * kStep;
     double *sums = a.sums + (int64_t)b * a.n_parts;
-    const int own = blockIdx.x * kVerifyWaves + wave;
-    if (own < a.n_parts) {
-        const double sum = part_sum(row, own, a.part);
-        if (lane == 0) store_sum(sums + own, sum);
+    const int own = (blockIdx.x * kVerifyWaves + wave) * a.each, end = min(own + a.each, a.n_parts);
+    Held<T, STEPS> held, next;
+    if (own < end) ask(row, own * kPart, held);
+    for (int i = own; i < end; ++i) {
+        if (i + 1 < end) ask(row, (i + 1) * kPart, next);
+        const double sum = part_sum(row, i * kPart, held);
+        if (lane == 0) store_sum(sums + i, sum);
+        held = next;
     }
-    wait_vm();        // this wave's sum has been stored ...
+    wait_vm();        // this wave's sums have been stored ...
     __syncthreads();  // ... and the other waves'
     if (tid == 0) {
         const uint32_t before = __hip_atomic_fetch_add(a.counters + b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         s_last = before == gridDim.x - 1;
         if (s_last) __hip_atomic_store(a.counters + b, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_part = s_token = Found{-1, 0, 0.0};
     }
     __syncthreads();
     if (!s_last) return;
 
-    // the workgroup that comes last: the whole sum ...
-    double total = 0.0;
+    // The workgroup that comes last: the whole sum, and the part in which the
+    // border lies (past all of them, the last one) ...
+    Found found{-1, 0, 0.0};
+    double border = 0.0;
+    const double at_border = (double)u[a.n];
     for (int again = 0;; ++again) {
-        double x = 0.0;
-        for (int i = tid; i < a.n_parts; i += kVerifyThreads) x += load_sum(sums + i);
-        block_before(x, s_wave, &total);
+        double x = tid < a.n_parts ? load_sum(sums + tid) : 0.0, total;
+        double from = block_before(x, s_wave[0], &total);
+        if (a.n_parts > kVerifyThreads) {
+            double more = 0.0, rest;
+            for (int i = tid + kVerifyThreads; i < a.n_parts; i += kVerifyThreads) more += load_sum(sums + i);
+            block_before(more, s_wave[1], &rest);
+            double first = total;
+            total += rest;
+            border = at_border * total;
+            look(found, x > 0.0, x > 0.0 && from + x > border, tid, from, s_found[0]);
+            for (int i0 = kVerifyThreads, turn = 0; i0 < a.n_parts && !found.known; i0 += kVerifyThreads, turn ^= 1) {
+                x = i0 + tid < a.n_parts ? load_sum(sums + i0 + tid) : 0.0;
+                from = first + block_before(x, s_wave[turn], &rest);
+                look(found, x > 0.0, x > 0.0 && from + x > border, i0 + tid, from, s_found[turn ^ 1]);
+                first += rest;
+            }
+        } else {
+            border = at_border * total;
+            look(found, x > 0.0, x > 0.0 && from + x > border, tid, from, s_found[0]);
+        }
         if (total > 0.0 || again || row.kind == REST_TARGET) break;
         // (the drafts cover all that the target has: drawn from the target)
         row.kind = REST_TARGET;
         for (int i = wave; i < a.n_parts; i += kVerifyWaves) {
-            const double sum = part_sum(row, i, a.part);
+            ask(row, i * kPart, held);
+            const double sum = part_sum(row, i * kPart, held);
             if (lane == 0) store_sum(sums + i, sum);
         }
         wait_vm();
         __syncthreads();
     }
-    // ... the part in which the border lies (past all of them, the last one) ...
-    const double border = (double)u[a.n] * total;
-    double before = 0.0;
-    for (int i0 = 0; i0 < a.n_parts && !s_part.known; i0 += kVerifyThreads) {
-        const int i = i0 + tid;
-        const double x = i < a.n_parts ? load_sum(sums + i) : 0.0;
-        double all;
-        const double from = before + block_before(x, s_wave, &all);
-        look(s_part, x > 0.0, x > 0.0 && from + x > border, i, from);
-        before += all;
-    }
     // ... and in it the token, in the same way
-    if (s_part.at >= 0) {
-        const int from = s_part.at * a.part, to = min(from + a.part, a.vocab);
-        before = s_part.before;
-        for (int v0 = from; v0 < to && !s_token.known; v0 += 4 * kVerifyThreads) {
+    Found token{-1, 0, 0.0};
+    if (found.at >= 0) {
+        const int first = found.at * kPart, end = min(first + kPart, a.vocab);
+        double before = found.before;
+        int turn = 1;
+        for (int v0 = first; v0 < end && !token.known; v0 += 4 * kVerifyThreads, turn ^= 1) {
             const int v = v0 + 4 * tid;
             double r[4] = {0.0, 0.0, 0.0, 0.0}, all;
-            if (v < to) row.four(v, r);
-            double at = before + block_before((r[0] + r[1]) + (r[2] + r[3]), s_wave, &all);
+            if (v < end) row.four(v, r);
+            double to = before + block_before((r[0] + r[1]) + (r[2] + r[3]), s_wave[turn], &all);
             int here = -1, any = -1;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                at += r[e];
+                to += r[e];
                 if (r[e] > 0.0) any = v + e;
-                if (r[e] > 0.0 && here < 0 && at > border) here = v + e;
+                if (r[e] > 0.0 && here < 0 && to > border) here = v + e;
             }
-            look(s_token, any >= 0, here >= 0, here >= 0 ? here : any, 0.0);
+            look(token, any >= 0, here >= 0, here >= 0 ? here : any, 0.0, s_found[turn]);
             before += all;
         }
     }
     for (int i = tid; i <= a.n; i += kVerifyThreads)
-        a.tokens[(int64_t)b * (a.n + 1) + i] = i < took ? drafts[i] : i == took ? s_token.at : -1;
+        a.tokens[(int64_t)b * (a.n + 1) + i] = i < took ? drafts[i] : i == took ? token.at : -1;
     if (tid == 0) {
         a.accepted[b] = took;
         if (a.lengths) a.lengths[b] -= count - took;
@@ -260,11 +302,14 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
 
 void verify_schedule(VerifyArgs &a)
 {
-    // a wave's part of a row: 256 elements, or up to 2048 where that still
-    // leaves some 8192 waves
-    a.part = kStep;
-    while (a.part < 8 * kStep && (int64_t)a.n_seqs * (a.vocab / a.part) > 16384) a.part *= 2;
-    a.n_parts = (a.vocab + a.part - 1) / a.part;
+    // A part is what the last workgroup reads again at once; a quarter of that
+    // where the parts would not fill the card.  A wave takes as many as leave some
+    // 4096 waves, four a SIMD: each begins with a chain of loads (draft,
+    // probability, row) that the others' reads cover.
+    a.steps = (int64_t)a.n_seqs * a.vocab < 4096 * 4 * kStep ? 1 : 4;
+    a.n_parts = (a.vocab + a.steps * kStep - 1) / (a.steps * kStep);
+    const int64_t each = (int64_t)a.n_seqs * a.n_parts / kManyWaves;
+    a.each = (int)(each < 1 ? 1 : each < 16 ? each : 16);
 }
 
 size_t verify_workspace_bytes(const VerifyArgs &a)
@@ -279,12 +324,16 @@ hipError_t launch_verify(const VerifyArgs &args, int dtype, void *workspace, hip
     a.counters = static_cast<uint32_t *>(workspace);
     a.sums = reinterpret_cast<double *>(static_cast<char *>(workspace) + kVerifyCounterBytes);
     const size_t size = dtype == 0 ? 4 : 2;
-    const unsigned groups = (unsigned)((a.n_parts + kVerifyWaves - 1) / kVerifyWaves);
+    const int each = kVerifyWaves * a.each;
+    const unsigned groups = (unsigned)((a.n_parts + each - 1) / each);
     // (as many sequences at a time as there are counters)
     for (int left = a.n_seqs; left > 0; left -= kVerifySeqs) {
         const int n = left < kVerifySeqs ? left : kVerifySeqs;
         auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(groups, (unsigned)n), dim3(kVerifyThreads), 0, stream, a); };
-        dtype == 0 ? go(verify_kernel<float>) : go(verify_kernel<__bf16>);
+        if (a.steps == 1)
+            dtype == 0 ? go(verify_kernel<float, 1>) : go(verify_kernel<__bf16, 1>);
+        else
+            dtype == 0 ? go(verify_kernel<float, 4>) : go(verify_kernel<__bf16, 4>);
         a.P = static_cast<const char *>(a.P) + (int64_t)n * a.p_seq * size;
         if (a.Q) a.Q = static_cast<const char *>(a.Q) + (int64_t)n * a.q_seq * size;
         a.drafts += (int64_t)n * a.n;

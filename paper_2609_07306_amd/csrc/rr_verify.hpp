@@ -18,8 +18,9 @@ struct VerifyArgs {
     int32_t *accepted, *tokens;        // [B], [B, n + 1]
     int64_t p_seq, p_row, q_seq, q_row;  // elements between rows
     int32_t n_seqs, n, vocab;
-    int32_t part;     // elements that a wave sums
+    int32_t steps;    // of a part of a row
     int32_t n_parts;  // of a row
+    int32_t each;     // parts of a wave
     uint32_t *counters;  // [n_seqs] finished workgroups, 0 between calls
     double *sums;        // [n_seqs, n_parts]
 };

@@ -773,13 +773,13 @@ class Pools:
 
 
 def pages_workspace(pools):
-    """A workspace (uint8 device tensor) for cache_resize and cache_compact calls
-    on these pools, one after the other.  Calls that may run at the same time,
+    """A workspace (uint8 device tensor, zeros) for cache_resize and cache_compact
+    calls on these pools, one after the other.  Calls that may run at the same time,
     captured graphs that are replayed side by side among them, need one each."""
     n = lib.rr_pages_workspace_bytes(pools.shape[0])
     if n == 0:
         _check(RR_ERR_INVALID)
-    return torch.empty(n, dtype=torch.uint8, device=pools.tensors[0].device)
+    return torch.zeros(n, dtype=torch.uint8, device=pools.tensors[0].device)
 
 
 def _workspace_of(workspace, make, stream):

@@ -100,10 +100,10 @@ def _pages_call(rr, compact, cfg="some", pools=(0x1000, 0x2000, 0x3000), lengths
 @pytest.mark.parametrize("compact", [False, True])
 @pytest.mark.parametrize("kw,status", [
     ({"cfg": None}, -1), ({"n_kv_heads": 0}, -1), ({"d": 4}, -1), ({"d": 2048}, -1), ({"page": 0}, -1), ({"n_pages": 0}, -1),
-    ({"n_pages": (1 << 30) + 1}, -1), ({"cache_dtype": 3}, -1), ({"n_pools": 0}, -1), ({"n_pools": 4097}, -1),
+    ({"n_pages": (1 << 28) + 1}, -1), ({"cache_dtype": 3}, -1), ({"n_pools": 0}, -1), ({"n_pools": 4097}, -1),
     ({"max_pages": 0}, -1), ({"max_pages": 1 << 27}, -1), ({"n_seqs": 0}, -1), ({"n_new": -1}, -1), ({"reserved": 1}, -1),
     ({"n_kv_heads": 1 << 18, "page": 1 << 9}, -5), ({"n_kv_heads": 2 ** 31 - 1}, -5),
-    ({"n_seqs": 1 << 23, "max_pages": 1025}, -5), ({"pools": None}, -1), ({"pools": (0x1000, 0, 0x3000)}, -1),
+    ({"n_seqs": 1 << 20, "max_pages": 1 << 14}, -5), ({"pools": None}, -1), ({"pools": (0x1000, 0, 0x3000)}, -1),
     ({"pools": (0x1000, 0x2008, 0x3000)}, -1), ({"table": None}, -1), ({"refs": None}, -1), ({"ws": None}, -1), ({"ws": ODD}, -1),
     ({"size": 0}, -1),
 ])
@@ -117,14 +117,14 @@ def test_pages_workspace():
     rr = _rr()
     assert _pages_call(rr, False, lengths=None) == -1
     assert _pages_call(rr, True, ids=None) == -1 and _pages_call(rr, True, used=None) == -1
-    for n in (0, -1, (1 << 30) + 1):
+    for n in (0, -1, (1 << 28) + 1):
         assert rr.lib.rr_pages_workspace_bytes(n) == 0 and rr.lib.rr_last_error()
     need = rr.lib.rr_pages_workspace_bytes(100)
     assert 1200 <= need < 2048
     for compact in (False, True):
         assert _pages_call(rr, compact, size=need - 1) == -1
         assert b"workspace" in rr.lib.rr_last_error()
-    assert rr.lib.rr_pages_workspace_bytes(1 << 30) > 12 << 30
+    assert rr.lib.rr_pages_workspace_bytes(1 << 28) > 12 << 28
 
 
 # ------------------------------------------------------------------ drafts
