@@ -1345,7 +1345,7 @@ rr_status verify_args(const rr_verify_config *cfg, rr::VerifyArgs *out)
     a.p_row = c.p_row;
     a.q_seq = c.q_seq;
     a.q_row = c.q_row;
-    rr::verify_schedule(a);
+    rr::verify_schedule(a, c.dtype);
     *out = a;
     return RR_OK;
 }

@@ -23,9 +23,9 @@ namespace {
 constexpr int kRotateThreads = 256;
 constexpr int kManyGroups = 1024;  // workgroups that fill the card
 
-// Pieces of a row: INTER: N / 2 pairs of neighbours each; otherwise a rotated
-// unit is a piece of the first half and its partner.  What is not rotated
-// follows in single pieces.
+// Units of a row that a thread takes.  INTER: pieces of N / 2 pairs of
+// neighbours; otherwise a rotated unit is a piece of the first half and its
+// partner.  What is not rotated follows in single pieces.
 struct Units {
     int turned, all;
 };
@@ -34,7 +34,7 @@ template <bool INTER, int N>
 __host__ __device__ __forceinline__ Units units_of(int d, int rot)
 {
     const int turned = INTER ? rot / N : rot / (2 * N);
-    return Units{turned, INTER ? d / N : turned + (d - rot) / N};
+    return Units{turned, turned + (d - rot) / N};
 }
 
 // First element of unit u.
@@ -44,34 +44,38 @@ __device__ __forceinline__ int unit_at(const RotateArgs &a, const Units &un, int
     return INTER || u < un.turned ? u * N : a.rot + (u - un.turned) * N;
 }
 
-template <typename T, int N, bool VEC>
-__device__ __forceinline__ void read_once(const T *p, float (&x)[N])
+// How rows are read and written: element by element, in vectors, or in vectors
+// past the caches.
+enum Way : int { WAY_EACH, WAY_VEC, WAY_ONCE };
+
+template <typename T, int N, Way W>
+__device__ __forceinline__ void read_row(const T *p, float (&x)[N])
 {
-    if constexpr (VEC) {
+    if constexpr (W == WAY_ONCE) {
         const auto v = __builtin_nontemporal_load(reinterpret_cast<const typename Piece<T, N>::V *>(p));
 #pragma unroll
         for (int e = 0; e < N; ++e) x[e] = widen(v[e]);
     } else {
-        read_piece<T, N, false>(p, x);
+        read_piece<T, N, W == WAY_VEC>(p, x);
     }
 }
 
-template <typename T, int N, bool VEC>
-__device__ __forceinline__ void write_once(T *p, const float (&x)[N])
+template <typename T, int N, Way W>
+__device__ __forceinline__ void write_row(T *p, const float (&x)[N])
 {
-    if constexpr (VEC) {
+    if constexpr (W == WAY_ONCE) {
         typename Piece<T, N>::V v;
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = (T)x[e];
         __builtin_nontemporal_store(v, reinterpret_cast<typename Piece<T, N>::V *>(p));
     } else {
-        write_piece<T, N, false>(p, x);
+        write_piece<T, N, W == WAY_VEC>(p, x);
     }
 }
 
 // Tokens of a head follow each other: a thread takes the same unit of one token
 // over a few heads and keeps its angles.
-template <typename T, bool INTER, int N, bool VEC>
+template <typename T, bool INTER, int N, Way W>
 __global__ __launch_bounds__(kRotateThreads) void rotate_heads_kernel(RotateArgs a)
 {
     const Units un = units_of<INTER, N>(a.d, a.rot);
@@ -89,8 +93,8 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_heads_kernel(RotateArgs
         T *dst = static_cast<T *>(a.Y) + i * a.y_token + h0 * a.y_head + f0;
         constexpr int NT = kTurns<INTER, N>;
         float c[NT], s[NT], x[N], y[N], next_x[N], next_y[N];
-        read_once<T, N, VEC>(src, next_x);
-        if (!INTER && turn) read_once<T, N, VEC>(src + half, next_y);
+        read_row<T, N, W>(src, next_x);
+        if (!INTER && turn) read_row<T, N, W>(src + half, next_y);
         if (turn) {
             turns_of(a.axes, a.freqs, i, INTER ? f0 >> 1 : f0, c, s);
 #pragma unroll
@@ -104,12 +108,12 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_heads_kernel(RotateArgs
             }
             if (h + 1 < h1) {
                 src += a.x_head;
-                read_once<T, N, VEC>(src, next_x);
-                if (!INTER && turn) read_once<T, N, VEC>(src + half, next_y);
+                read_row<T, N, W>(src, next_x);
+                if (!INTER && turn) read_row<T, N, W>(src + half, next_y);
             }
             if (turn) turn_piece<INTER, N>(x, y, c, s);
-            write_once<T, N, VEC>(dst, x);
-            if (!INTER && turn) write_once<T, N, VEC>(dst + half, y);
+            write_row<T, N, W>(dst, x);
+            if (!INTER && turn) write_row<T, N, W>(dst + half, y);
         }
     }
 }
@@ -118,7 +122,7 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_heads_kernel(RotateArgs
 // tokens in the order of memory, and its threads share the angles in LDS.
 constexpr int kMostAngles = 2048;  // of a workgroup
 
-template <typename T, bool INTER, int N, bool VEC>
+template <typename T, bool INTER, int N, Way W>
 __global__ __launch_bounds__(kRotateThreads) void rotate_tokens_kernel(RotateArgs a)
 {
     __shared__ float s_cos[kMostAngles], s_sin[kMostAngles];
@@ -147,14 +151,14 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_tokens_kernel(RotateArg
             h -= heads;
             ++t;
         }
-        for (; t < tokens;) {
+        while (t < tokens) {
             const int64_t i = i0 + t;
             const T *src = static_cast<const T *>(a.X) + i * a.x_token + (h0 + h) * a.x_head + f0;
             T *dst = static_cast<T *>(a.Y) + i * a.y_token + (h0 + h) * a.y_head + f0;
             float x[N], y[N];
-            read_once<T, N, VEC>(src, x);
+            read_row<T, N, W>(src, x);
+            if (!INTER && turn) read_row<T, N, W>(src + half, y);
             if (turn) {
-                if constexpr (!INTER) read_once<T, N, VEC>(src + half, y);
                 constexpr int NT = kTurns<INTER, N>;
                 float c[NT], s[NT];
                 const int at = t * half + (INTER ? f0 >> 1 : f0);
@@ -165,8 +169,8 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_tokens_kernel(RotateArg
                 }
                 turn_piece<INTER, N>(x, y, c, s);
             }
-            write_once<T, N, VEC>(dst, x);
-            if (!INTER && turn) write_once<T, N, VEC>(dst + half, y);
+            write_row<T, N, W>(dst, x);
+            if (!INTER && turn) write_row<T, N, W>(dst + half, y);
             h += rows;
             while (h >= heads) {
                 h -= heads;
@@ -184,17 +188,24 @@ hipError_t launch_rotate(const RotateArgs &args, int dtype, bool interleaved, hi
     const int n = dtype == 0 ? 4 : 8;
     const bool vec = ((reinterpret_cast<uintptr_t>(a.X) | reinterpret_cast<uintptr_t>(a.Y)) & 15) == 0 && a.x_token % n == 0 &&
                      a.x_head % n == 0 && a.y_token % n == 0 && a.y_head % n == 0 && a.rot % (interleaved ? n : 2 * n) == 0;
+    // Past the caches only what is read and written in whole lines of 128 bytes: a
+    // row of pairs of neighbours, or halves of that size.
+    const int size = dtype == 0 ? 4 : 2;
+    const bool lines = interleaved ? a.d * size % 128 == 0 : a.rot / 2 * size % 128 == 0 && (a.d - a.rot) * size % 128 == 0;
     // which rows follow each other
     const bool by_token = a.n_heads > 1 && (a.n_tokens == 1 || a.y_head < a.y_token);
     auto go = [&](auto by_heads, auto by_tokens, Units un) {
         if (by_token) {
-            // tokens a workgroup: about 64 KB in 32 rows at a time, as long as there
-            // are workgroups for the card; then heads are shared out too
+            // Tokens a workgroup: two turns of its threads (32768 tokens of 32 heads:
+            // two tokens 87 us, four 90, eight 98; of 2 heads of 64: 16 tokens 10 us,
+            // four 18), as long as there are workgroups for the card; then heads are
+            // shared out too.
+            const int lanes = un.all < kRotateThreads ? un.all : kRotateThreads, rows = kRotateThreads / lanes;
             const int half = a.rot / 2 > 0 ? a.rot / 2 : 1;
-            int each = 8 < kMostAngles / half ? 8 : kMostAngles / half;
+            int each = 2 * rows / (a.n_heads < rows ? a.n_heads : rows);
+            if (each > kMostAngles / half) each = kMostAngles / half;
             while (each > 1 && (a.n_tokens + each - 1) / each < kManyGroups) each /= 2;
             const int tiles = (a.n_tokens + each - 1) / each, parts = tiles >= kManyGroups ? 1 : kManyGroups / tiles;
-            const int lanes = un.all < kRotateThreads ? un.all : kRotateThreads, rows = kRotateThreads / lanes;
             int heads = (a.n_heads + parts - 1) / parts;
             if (heads < rows) heads = rows;
             if (heads > a.n_heads) heads = a.n_heads;
@@ -215,19 +226,24 @@ hipError_t launch_rotate(const RotateArgs &args, int dtype, bool interleaved, hi
         hipLaunchKernelGGL(by_heads, dim3((unsigned)tiles, (unsigned)((a.n_heads + each - 1) / each)), dim3(kRotateThreads), 0,
                            stream, a);
     };
-    auto any = [&](auto type, auto width) {
+    auto ways = [&](auto type, auto inter, auto width, auto way) {
         typedef decltype(type) T;
-        constexpr int W = decltype(width)::value;
-        if (vec)
-            interleaved ? go(rotate_heads_kernel<T, true, W, true>, rotate_tokens_kernel<T, true, W, true>,
-                             units_of<true, W>(a.d, a.rot))
-                        : go(rotate_heads_kernel<T, false, W, true>, rotate_tokens_kernel<T, false, W, true>,
-                             units_of<false, W>(a.d, a.rot));
-        else  // (interleaved partners go together)
-            interleaved ? go(rotate_heads_kernel<T, true, 2, false>, rotate_tokens_kernel<T, true, 2, false>,
-                             units_of<true, 2>(a.d, a.rot))
-                        : go(rotate_heads_kernel<T, false, 1, false>, rotate_tokens_kernel<T, false, 1, false>,
-                             units_of<false, 1>(a.d, a.rot));
+        constexpr bool I = decltype(inter)::value;
+        constexpr int N = decltype(width)::value;
+        constexpr Way W = decltype(way)::value;
+        go(rotate_heads_kernel<T, I, N, W>, rotate_tokens_kernel<T, I, N, W>, units_of<I, N>(a.d, a.rot));
+    };
+    auto any = [&](auto type, auto width) {
+        typedef std::integral_constant<Way, WAY_EACH> Each;
+        typedef std::integral_constant<Way, WAY_VEC> Vec;
+        typedef std::integral_constant<Way, WAY_ONCE> Once;
+        if (!vec)  // (interleaved partners go together)
+            interleaved ? ways(type, std::true_type(), std::integral_constant<int, 2>(), Each())
+                        : ways(type, std::false_type(), std::integral_constant<int, 1>(), Each());
+        else if (lines)
+            interleaved ? ways(type, std::true_type(), width, Once()) : ways(type, std::false_type(), width, Once());
+        else
+            interleaved ? ways(type, std::true_type(), width, Vec()) : ways(type, std::false_type(), width, Vec());
     };
     if (dtype == 0)
         any(float(), std::integral_constant<int, 4>());

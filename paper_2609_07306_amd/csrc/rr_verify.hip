@@ -23,7 +23,6 @@ namespace rr {
 namespace {
 
 constexpr int kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
-constexpr int kStep = 256;  // elements of a wave's step: four a lane
 constexpr int kManyWaves = 4096;
 
 __device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
@@ -31,10 +30,12 @@ __device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(0)" ::
 __device__ __forceinline__ double value(float x) { return (double)x; }
 __device__ __forceinline__ double value(__bf16 x) { return (double)(float)x; }
 
-// Four elements from an address that is a multiple of an element's size.
+// Sixteen bytes of a row, from an address that is a multiple of an element's
+// size; a wave's step takes 64 of them.
 template <typename T>
-struct Four {
-    typedef T V __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+struct Some {
+    static constexpr int N = 16 / sizeof(T), STEP = 64 * N;
+    typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
 
 enum Rest : int { REST_TARGET, REST_DIFFERENCE, REST_WITHOUT };  // p; max(p - q, 0); p but for the draft
@@ -45,27 +46,12 @@ struct Row {
     const T *p, *q;
     int kind, draft, vocab;
 
-    // Not a positive number: nothing.
-    __device__ __forceinline__ double weight(double x, double y, int v) const
+    // Of v, which is in the vocabulary.  Not a positive finite number: nothing.
+    __device__ __forceinline__ double weight(int v) const
     {
-        const double r = kind == REST_DIFFERENCE ? x - y : (kind == REST_WITHOUT && v == draft) ? 0.0 : x;
+        const double x = value(p[v]);
+        const double r = kind == REST_DIFFERENCE ? x - value(q[v]) : (kind == REST_WITHOUT && v == draft) ? 0.0 : x;
         return r > 0.0 && r < (double)INFINITY ? r : 0.0;
-    }
-
-    // The weights of v .. v + 3.
-    __device__ __forceinline__ void four(int v, double (&r)[4]) const
-    {
-        if (v + 4 <= vocab) {
-            const auto x = *reinterpret_cast<const typename Four<T>::V *>(p + v);
-            typename Four<T>::V y = {};
-            if (kind == REST_DIFFERENCE) y = *reinterpret_cast<const typename Four<T>::V *>(q + v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[e] = weight(value(x[e]), value(y[e]), v + e);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                r[e] = v + e < vocab ? weight(value(p[v + e]), kind == REST_DIFFERENCE ? value(q[v + e]) : 0.0, v + e) : 0.0;
-        }
     }
 };
 
@@ -100,43 +86,48 @@ __device__ __forceinline__ double block_before(double x, double *s_wave, double 
     return base + (lane ? before : 0.0);
 }
 
-// Elements of a part of STEPS steps as they lie in memory, a lane's.
+// A lane's elements of a part of STEPS steps, as they lie in memory.
 template <typename T, int STEPS>
 struct Held {
-    typename Four<T>::V x[STEPS], y[STEPS];
+    typename Some<T>::V x[STEPS], y[STEPS];
 };
 
 template <int STEPS, typename T>
 __device__ __forceinline__ void ask(const Row<T> &row, int from, Held<T, STEPS> &h)
 {
-    if (from + STEPS * kStep > row.vocab) return;  // (the last part is read element by element)
-    const int v = from + 4 * (threadIdx.x & 63);
+    typedef typename Some<T>::V V;
+    if (from + STEPS * Some<T>::STEP > row.vocab) return;  // (the last part is read element by element)
+    const int v = from + Some<T>::N * (threadIdx.x & 63);
+    // (past the caches: 45 us against 49 for 192 sequences' drafts)
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
-        h.x[i] = *reinterpret_cast<const typename Four<T>::V *>(row.p + v + i * kStep);
-        if (row.kind == REST_DIFFERENCE) h.y[i] = *reinterpret_cast<const typename Four<T>::V *>(row.q + v + i * kStep);
+        h.x[i] = __builtin_nontemporal_load(reinterpret_cast<const V *>(row.p + v + i * Some<T>::STEP));
+        if (row.kind == REST_DIFFERENCE)
+            h.y[i] = __builtin_nontemporal_load(reinterpret_cast<const V *>(row.q + v + i * Some<T>::STEP));
     }
 }
 
-// The sum of a part, of which `ask` has asked.
+// The sum of a part, of which `ask` has asked.  max(r, 0) is 0 for a NaN, and an
+// infinite r shows in the sum: a part that has one is read again, as are those
+// with the draft to leave out and the end of the vocabulary.
 template <int STEPS, typename T>
 __device__ __forceinline__ double part_sum(const Row<T> &row, int from, const Held<T, STEPS> &h)
 {
-    const int v = from + 4 * (threadIdx.x & 63);
-    const bool whole = from + STEPS * kStep <= row.vocab;
+    const int to = from + STEPS * Some<T>::STEP, lane = threadIdx.x & 63;
     double sum = 0.0;
+    if (to <= row.vocab && !(row.kind == REST_WITHOUT && row.draft >= from && row.draft < to)) {
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        double r[4] = {0.0, 0.0, 0.0, 0.0};
-        if (whole) {
+        for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                r[e] = row.weight(value(h.x[i][e]), row.kind == REST_DIFFERENCE ? value(h.y[i][e]) : 0.0, v + i * kStep + e);
-        } else if (v + i * kStep < row.vocab) {
-            row.four(v + i * kStep, r);
-        }
-        sum += (r[0] + r[1]) + (r[2] + r[3]);
+            for (int e = 0; e < Some<T>::N; ++e) {
+                const double x = value(h.x[i][e]);
+                sum += fmax(row.kind == REST_DIFFERENCE ? x - value(h.y[i][e]) : x, 0.0);
+            }
+        sum = wave_sum(sum);
+        if (sum < (double)INFINITY) return sum;
+        sum = 0.0;
     }
+    for (int v = from + lane; v < min(to, row.vocab); v += 64) sum += row.weight(v);
     return wave_sum(sum);
 }
 
@@ -210,7 +201,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
     if (row.kind == REST_DIFFERENCE) row.q += took * a.q_row;
 
     // this wave's parts, of which the next is asked for before one is summed
-    constexpr int kPart = STEPS * kStep;
+    constexpr int kPart = STEPS * Some<T>::STEP, kEach = kPart / kVerifyThreads;
     double *sums = a.sums + (int64_t)b * a.n_parts;
     const int own = (blockIdx.x * kVerifyWaves + wave) * a.each, end = min(own + a.each, a.n_parts);
     Held<T, STEPS> held, next;
@@ -271,24 +262,22 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
     // ... and in it the token, in the same way
     Found token{-1, 0, 0.0};
     if (found.at >= 0) {
-        const int first = found.at * kPart, end = min(first + kPart, a.vocab);
-        double before = found.before;
-        int turn = 1;
-        for (int v0 = first; v0 < end && !token.known; v0 += 4 * kVerifyThreads, turn ^= 1) {
-            const int v = v0 + 4 * tid;
-            double r[4] = {0.0, 0.0, 0.0, 0.0}, all;
-            if (v < end) row.four(v, r);
-            double to = before + block_before((r[0] + r[1]) + (r[2] + r[3]), s_wave[turn], &all);
-            int here = -1, any = -1;
+        const int first = found.at * kPart + tid * kEach;
+        double r[kEach], all, sum = 0.0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                to += r[e];
-                if (r[e] > 0.0) any = v + e;
-                if (r[e] > 0.0 && here < 0 && to > border) here = v + e;
-            }
-            look(token, any >= 0, here >= 0, here >= 0 ? here : any, 0.0, s_found[turn]);
-            before += all;
+        for (int e = 0; e < kEach; ++e) {
+            r[e] = first + e < a.vocab ? row.weight(first + e) : 0.0;
+            sum += r[e];
         }
+        double to = found.before + block_before(sum, s_wave[1], &all);
+        int here = -1, any = -1;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            to += r[e];
+            if (r[e] > 0.0) any = first + e;
+            if (r[e] > 0.0 && here < 0 && to > border) here = first + e;
+        }
+        look(token, any >= 0, here >= 0, here >= 0 ? here : any, 0.0, s_found[1]);
     }
     for (int i = tid; i <= a.n; i += kVerifyThreads)
         a.tokens[(int64_t)b * (a.n + 1) + i] = i < took ? drafts[i] : i == took ? token.at : -1;
@@ -300,16 +289,21 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
 
 }  // namespace
 
-void verify_schedule(VerifyArgs &a)
+void verify_schedule(VerifyArgs &a, int dtype)
 {
-    // A part is what the last workgroup reads again at once; a quarter of that
-    // where the parts would not fill the card.  A wave takes as many as leave some
-    // 4096 waves, four a SIMD: each begins with a chain of loads (draft,
-    // probability, row) that the others' reads cover.
-    a.steps = (int64_t)a.n_seqs * a.vocab < 4096 * 4 * kStep ? 1 : 4;
-    a.n_parts = (a.vocab + a.steps * kStep - 1) / (a.steps * kStep);
-    const int64_t each = (int64_t)a.n_seqs * a.n_parts / kManyWaves;
-    a.each = (int)(each < 1 ? 1 : each < 16 ? each : 16);
+    // Parts of one, two or four steps, so that the last workgroup finds the
+    // border's with one sum a thread; a wave takes as many, a power of two, as
+    // leave some 4096 waves, four a SIMD.  (Fewer parts a wave are more chains of
+    // loads -- draft, probability, row -- before the first sum, and more counters
+    // to add to; four steps take registers that leave two waves.  192 sequences,
+    // 131072 tokens, binary32, steps and parts: 2 and 8 42 us, 2 and 4 44, 4 and 8
+    // 43, 1 and 8 47, 4 and 1 61.)
+    const int step = dtype == 0 ? Some<float>::STEP : Some<__bf16>::STEP;
+    a.steps = 1;
+    while (a.steps < 4 && a.vocab > kVerifyThreads * a.steps * step) a.steps *= 2;
+    a.n_parts = (a.vocab + a.steps * step - 1) / (a.steps * step);
+    a.each = 1;
+    while (a.each < 16 && (int64_t)a.n_seqs * a.n_parts >= 2 * a.each * kManyWaves) a.each *= 2;
 }
 
 size_t verify_workspace_bytes(const VerifyArgs &a)
@@ -332,6 +326,8 @@ hipError_t launch_verify(const VerifyArgs &args, int dtype, void *workspace, hip
         auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(groups, (unsigned)n), dim3(kVerifyThreads), 0, stream, a); };
         if (a.steps == 1)
             dtype == 0 ? go(verify_kernel<float, 1>) : go(verify_kernel<__bf16, 1>);
+        else if (a.steps == 2)
+            dtype == 0 ? go(verify_kernel<float, 2>) : go(verify_kernel<__bf16, 2>);
         else
             dtype == 0 ? go(verify_kernel<float, 4>) : go(verify_kernel<__bf16, 4>);
         a.P = static_cast<const char *>(a.P) + (int64_t)n * a.p_seq * size;

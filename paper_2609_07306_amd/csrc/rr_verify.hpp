@@ -26,7 +26,7 @@ struct VerifyArgs {
 };
 
 // Fills in the split of a row, from n_seqs and vocab.
-void verify_schedule(VerifyArgs &a);
+void verify_schedule(VerifyArgs &a, int dtype);
 size_t verify_workspace_bytes(const VerifyArgs &a);
 hipError_t launch_verify(const VerifyArgs &a, int dtype, void *workspace, hipStream_t stream);
 
