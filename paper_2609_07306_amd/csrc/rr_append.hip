@@ -89,18 +89,49 @@ __device__ __forceinline__ int find_sequence(const int32_t *start, int n_seqs, i
 }
 
 // AXES: rotated by the token's positions on several axes, not by its place in the
-// sequence.
-template <typename T, bool E4, bool INTER, int N, bool VEC, bool AXES>
+// sequence.  AHEAD: the first rows of a thread (up to AHEAD of them) and its
+// first values are asked for before the token's place is known.
+template <typename T, bool E4, bool INTER, int N, bool VEC, bool AXES, int AHEAD>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
 {
+    typedef typename Raw<T, N>::V V;
     __shared__ float s_cos[kMostRot / 2], s_sin[kMostRot / 2];
     const int tid = threadIdx.x, half = a.rot >> 1;
+    const int64_t i = blockIdx.x;
+
+    // Rows of queries and keys.  INTER: a piece is N / 2 pairs of neighbours;
+    // otherwise a rotated unit is a piece of the first half and its partner,
+    // and what is not rotated follows in single pieces.
+    const int turned = INTER ? a.rot / N : half / N, units = INTER ? a.d / N : turned + (a.d - a.rot) / N;
+    const int n_rows = a.n_kv_heads + (a.Q ? a.n_heads : 0);
+    const int lanes = min(units, kAppendThreads), rows_at_once = kAppendThreads / lanes;
+    const int u0 = tid % lanes, r0 = tid < lanes * rows_at_once ? tid / lanes : n_rows;
+    auto piece_at = [&](int u) { return INTER || u < turned ? u * N : a.rot + (u - turned) * N; };
+    auto row_at = [&](int r) {
+        return r < a.n_kv_heads ? static_cast<const T *>(a.K) + i * a.ldk + r * a.d
+                                : static_cast<const T *>(a.Q) + i * a.ldq + (r - a.n_kv_heads) * a.d;
+    };
+    const int pieces = a.d / N, n_values = a.n_kv_heads * pieces;
+    auto value_at = [&](int x) {
+        const int r = x / pieces;
+        return static_cast<const T *>(a.V) + i * a.ldv + r * a.d + (x - r * pieces) * N;
+    };
+    V first_x[AHEAD + 1], first_y[AHEAD + 1], first_v;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+        const int r = r0 + k * rows_at_once;
+        if (r < n_rows) {
+            const T *src = row_at(r) + piece_at(u0);
+            first_x[k] = read_raw<T, N, VEC>(src);
+            if (!INTER && u0 < turned) first_y[k] = read_raw<T, N, VEC>(src + half);
+        }
+    }
+    if (AHEAD && tid < n_values) first_v = read_raw<T, N, VEC>(value_at(tid));
 
     // where the token goes: sequence, position, page.  (Loads that wait for each
     // other; with their addresses in vector registers, as the scalar loads that
     // the compiler would make of them take longer: 3.3 us against 3.7 for a
     // token)
-    const int64_t i = blockIdx.x;
     int b, left;  // tokens of the sequence's new ones from this one on
     if (a.seq_start) {
         b = find_sequence(a.seq_start, a.n_seqs, in_vector((int)i));
@@ -122,60 +153,59 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
     }
     __syncthreads();
 
-    // Rows of queries and keys.  INTER: a piece is N / 2 pairs of neighbours;
-    // otherwise a rotated unit is a piece of the first half and its partner,
-    // and what is not rotated follows in single pieces.
-    const int turned = INTER ? a.rot / N : half / N, units = INTER ? a.d / N : turned + (a.d - a.rot) / N;
-    const int n_rows = a.n_kv_heads + (a.Q ? a.n_heads : 0);
-    const int lanes = min(units, kAppendThreads), rows_at_once = kAppendThreads / lanes;
-    if (tid < lanes * rows_at_once) {
-        for (int u = tid % lanes; u < units; u += lanes) {
-            const bool turn = u < turned;
-            // first element of the piece, and of its partner
-            const int f0 = INTER ? u * N : turn ? u * N : a.rot + (u - turned) * N, f1 = f0 + half;
-            constexpr int NT = kTurns<INTER, N>;
-            float c[NT], s[NT];
-            if (turn) {
+    constexpr int NT = kTurns<INTER, N>;
+    auto put_row = [&](int r, int u, const float (&c)[NT], const float (&s)[NT], V raw_x, V raw_y) {
+        const bool key = r < a.n_kv_heads, turn = u < turned;
+        const int f0 = piece_at(u), f1 = f0 + half;
+        if (key && phys < 0) return;
+        float x[N], y[N];
+        widen_piece<T, N>(raw_x, x);
+        if (turn) {
+            if constexpr (!INTER) widen_piece<T, N>(raw_y, y);
+            turn_piece<INTER, N>(x, y, c, s);
+        }
+        if (key) {
+            const int64_t at = pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d);
+            const float scale = E4 ? a.k_scale[r] : 1.f;
+            write_cache<T, E4, N, VEC>(a.Kc, at + f0, x, scale);
+            if (!INTER && turn) write_cache<T, E4, N, VEC>(a.Kc, at + f1, y, scale);
+        } else {
+            T *dst = static_cast<T *>(a.Q_out) + (i * a.n_heads + (r - a.n_kv_heads)) * a.d;
+            write_piece<T, N, VEC>(dst + f0, x);
+            if (!INTER && turn) write_piece<T, N, VEC>(dst + f1, y);
+        }
+    };
+    for (int u = u0; u < units; u += lanes) {
+        const bool turn = u < turned;
+        const int f0 = piece_at(u);
+        float c[NT], s[NT];
+        if (turn) {
 #pragma unroll
-                for (int e = 0; e < NT; ++e) {
-                    c[e] = s_cos[(INTER ? f0 >> 1 : f0) + e];
-                    s[e] = s_sin[(INTER ? f0 >> 1 : f0) + e];
-                }
+            for (int e = 0; e < NT; ++e) {
+                c[e] = s_cos[(INTER ? f0 >> 1 : f0) + e];
+                s[e] = s_sin[(INTER ? f0 >> 1 : f0) + e];
             }
-            for (int r = tid / lanes; r < n_rows; r += rows_at_once) {
-                const bool key = r < a.n_kv_heads;
-                if (key && phys < 0) continue;
-                const T *src = key ? static_cast<const T *>(a.K) + i * a.ldk + r * a.d
-                                   : static_cast<const T *>(a.Q) + i * a.ldq + (r - a.n_kv_heads) * a.d;
-                float x[N], y[N];
-                read_piece<T, N, VEC>(src + f0, x);
-                if (turn) {
-                    if constexpr (!INTER) read_piece<T, N, VEC>(src + f1, y);
-                    turn_piece<INTER, N>(x, y, c, s);
-                }
-                if (key) {
-                    const int64_t at = pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d);
-                    const float scale = E4 ? a.k_scale[r] : 1.f;
-                    write_cache<T, E4, N, VEC>(a.Kc, at + f0, x, scale);
-                    if (!INTER && turn) write_cache<T, E4, N, VEC>(a.Kc, at + f1, y, scale);
-                } else {
-                    T *dst = static_cast<T *>(a.Q_out) + (i * a.n_heads + (r - a.n_kv_heads)) * a.d;
-                    write_piece<T, N, VEC>(dst + f0, x);
-                    if (!INTER && turn) write_piece<T, N, VEC>(dst + f1, y);
-                }
-            }
+        }
+        int r = r0;
+        if (u == u0) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k, r += rows_at_once)
+                if (r < n_rows) put_row(r, u, c, s, first_x[k], first_y[k]);
+        }
+        for (; r < n_rows; r += rows_at_once) {
+            const T *src = row_at(r) + f0;
+            V x = read_raw<T, N, VEC>(src), y = x;
+            if (!INTER && turn) y = read_raw<T, N, VEC>(src + half);
+            put_row(r, u, c, s, x, y);
         }
     }
     // values
-    if (phys >= 0) {
-        const int pieces = a.d / N;
-        for (int x = tid; x < a.n_kv_heads * pieces; x += kAppendThreads) {
-            const int r = x / pieces, f = (x - r * pieces) * N;
-            float v[N];
-            read_piece<T, N, VEC>(static_cast<const T *>(a.V) + i * a.ldv + r * a.d + f, v);
-            write_cache<T, E4, N, VEC>(a.Vc, pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d) + f, v,
-                                  E4 ? a.v_scale[r] : 1.f);
-        }
+    if (phys < 0) return;
+    for (int x = tid; x < n_values; x += kAppendThreads) {
+        const int r = x / pieces, f = (x - r * pieces) * N;
+        float v[N];
+        widen_piece<T, N>(AHEAD && x == tid ? first_v : read_raw<T, N, VEC>(value_at(x)), v);
+        write_cache<T, E4, N, VEC>(a.Vc, pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d) + f, v, E4 ? a.v_scale[r] : 1.f);
     }
 }
 
@@ -189,22 +219,32 @@ hipError_t launch_append(const AppendArgs &a, int dtype, int cache, bool interle
     const bool vec = aligned(a.K, a.ldk) && aligned(a.V, a.ldv) && aligned(a.Q, a.Q ? a.ldq : 0) && aligned(a.Q_out, 0) &&
                      aligned(a.Kc, 0) && aligned(a.Vc, 0) && a.rot % (interleaved ? n : 2 * n) == 0;
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)a.n_tokens), dim3(kAppendThreads), 0, stream, a); };
-    auto any = [&](auto type, auto e4, auto width, auto axes) {
+    // Rows are asked for before their place is known (one token 3.8 -> 3.2 us on the
+    // device, 192 into an 8-bit cache 5.7 -> 5.1, 28000 of ragged prompts into one
+    // 152 -> 135), but for large calls of a bf16 cache: the registers that hold them
+    // leave half of the waves, and waves are what keeps the memory busy there (32768
+    // tokens 144 against 151).
+    const bool ahead = !(dtype == 1 && cache == CACHE_BF16 && a.n_tokens >= 4096);
+    auto any = [&](auto type, auto e4, auto width, auto axes, auto rows) {
         typedef decltype(type) T;
         constexpr bool E4 = decltype(e4)::value, AX = decltype(axes)::value;
-        constexpr int W = decltype(width)::value;
+        constexpr int W = decltype(width)::value, A = decltype(rows)::value;
         if (vec)
-            interleaved ? go(append_kernel<T, E4, true, W, true, AX>) : go(append_kernel<T, E4, false, W, true, AX>);
+            interleaved ? go(append_kernel<T, E4, true, W, true, AX, A>) : go(append_kernel<T, E4, false, W, true, AX, A>);
         else  // (interleaved partners go together)
-            interleaved ? go(append_kernel<T, E4, true, 2, false, AX>) : go(append_kernel<T, E4, false, 1, false, AX>);
+            interleaved ? go(append_kernel<T, E4, true, 2, false, AX, A>) : go(append_kernel<T, E4, false, 1, false, AX, A>);
     };
     auto types = [&](auto axes) {
+        typedef std::integral_constant<int, 0> None;
+        typedef std::integral_constant<int, 2> Two;
         if (dtype == 0)
-            any(float(), std::false_type(), std::integral_constant<int, 4>(), axes);
-        else if (cache == CACHE_BF16)
-            any(__bf16(), std::false_type(), std::integral_constant<int, 8>(), axes);
+            any(float(), std::false_type(), std::integral_constant<int, 4>(), axes, Two());
+        else if (cache == CACHE_E4M3)
+            any(__bf16(), std::true_type(), std::integral_constant<int, 8>(), axes, Two());
+        else if (ahead)
+            any(__bf16(), std::false_type(), std::integral_constant<int, 8>(), axes, Two());
         else
-            any(__bf16(), std::true_type(), std::integral_constant<int, 8>(), axes);
+            any(__bf16(), std::false_type(), std::integral_constant<int, 8>(), axes, None());
     };
     a.axes.positions ? types(std::true_type()) : types(std::false_type());
     return hipGetLastError();

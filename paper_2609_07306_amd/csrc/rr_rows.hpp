@@ -15,19 +15,46 @@ struct Piece {
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(__bf16 x) { return (float)x; }
 
-// N consecutive elements of a row as binary32: one vector, or (VEC = false,
-// where rows are not aligned to one) element by element.
+// N consecutive elements of a row as they lie in memory, in as many registers as
+// they have words (a vector of __bf16 would take one an element).
+template <typename T, int N>
+struct Raw {
+    static constexpr int kWords = (N * (int)sizeof(T) + 3) / 4;
+    typedef uint32_t V __attribute__((ext_vector_type(kWords)));
+};
+
+// One vector, or (VEC = false, where rows are not aligned to one) element by
+// element.
+template <typename T, int N, bool VEC>
+__device__ __forceinline__ typename Raw<T, N>::V read_raw(const T *p)
+{
+    typedef typename Raw<T, N>::V V;
+    if constexpr (VEC) return *reinterpret_cast<const V *>(p);
+    V v;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = reinterpret_cast<const uint32_t *>(p)[e];
+    } else {
+        const uint16_t *q = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+        for (int e = 0; e < N; e += 2) v[e / 2] = q[e] | (e + 1 < N ? (uint32_t)q[e + 1] << 16 : 0u);
+    }
+    return v;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void widen_piece(typename Raw<T, N>::V v, float (&x)[N])
+{
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        x[e] = sizeof(T) == 4 ? __uint_as_float(v[e / (4 / (int)sizeof(T))])
+                              : __uint_as_float(e % 2 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
+}
+
 template <typename T, int N, bool VEC>
 __device__ __forceinline__ void read_piece(const T *p, float (&x)[N])
 {
-    if constexpr (VEC) {
-        const auto v = *reinterpret_cast<const typename Piece<T, N>::V *>(p);
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = widen(v[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = widen(p[e]);
-    }
+    widen_piece<T, N>(read_raw<T, N, VEC>(p), x);
 }
 
 template <typename T, int N, bool VEC>
