@@ -33,6 +33,27 @@ namespace {
 constexpr int kAppendThreads = 256;
 constexpr int kMostRot = 1024;
 
+// x / scale, correctly rounded, for many x: with r the correctly rounded 1 /
+// scale, q = x r is off by an ulp at most, x - q scale is exact, and q + (x - q
+// scale) r rounds to the quotient (Markstein's theorem).  That takes four
+// instructions where a division takes ten, of which appending has more than of
+// anything else.  Quotients past 1024, which clamp in any case, are not refined
+// (an infinite one would make a NaN of the remainder); scales so far from one that
+// a remainder could leave the range of normal numbers divide.
+struct Quotient {
+    float scale, r;
+    bool direct;
+
+    __device__ __forceinline__ explicit Quotient(float s) : scale(s), r(1.f / s), direct(!(s > 0x1p-60f && s < 0x1p60f)) {}
+
+    __device__ __forceinline__ float operator()(float x) const
+    {
+        if (direct) return x / scale;
+        const float q = __builtin_amdgcn_fmed3f(x * r, -1024.f, 1024.f);
+        return __builtin_fmaf(-__builtin_fmaf(q, scale, -x), r, q);  // (so that -0 stays -0)
+    }
+};
+
 // What e4m3 holds of x: beyond the largest finite value, that one.
 __device__ __forceinline__ float clamp_e4m3(float x)
 {
@@ -40,7 +61,7 @@ __device__ __forceinline__ float clamp_e4m3(float x)
 }
 
 template <int N, bool VEC>
-__device__ __forceinline__ void write_e4m3(uint8_t *p, const float (&x)[N], float scale)
+__device__ __forceinline__ void write_e4m3(uint8_t *p, const float (&x)[N], const Quotient &over)
 {
     if constexpr (VEC) {
         uint32_t o[N / 4];
@@ -48,7 +69,7 @@ __device__ __forceinline__ void write_e4m3(uint8_t *p, const float (&x)[N], floa
         for (int q = 0; q < N / 4; ++q) {
             float y[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = clamp_e4m3(x[4 * q + e] / scale);
+            for (int e = 0; e < 4; ++e) y[e] = clamp_e4m3(over(x[4 * q + e]));
             const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
             o[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
         }
@@ -56,15 +77,15 @@ __device__ __forceinline__ void write_e4m3(uint8_t *p, const float (&x)[N], floa
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e)
-            p[e] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp_e4m3(x[e] / scale), 0.f, 0, false);
+            p[e] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp_e4m3(over(x[e])), 0.f, 0, false);
     }
 }
 
 template <typename T, bool E4, int N, bool VEC>
-__device__ __forceinline__ void write_cache(void *pool, int64_t at, const float (&x)[N], float scale)
+__device__ __forceinline__ void write_cache(void *pool, int64_t at, const float (&x)[N], const Quotient &over)
 {
     if constexpr (E4)
-        write_e4m3<N, VEC>(static_cast<uint8_t *>(pool) + at, x, scale);
+        write_e4m3<N, VEC>(static_cast<uint8_t *>(pool) + at, x, over);
     else
         write_piece<T, N, VEC>(static_cast<T *>(pool) + at, x);
 }
@@ -104,17 +125,16 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
     // and what is not rotated follows in single pieces.
     const int turned = INTER ? a.rot / N : half / N, units = INTER ? a.d / N : turned + (a.d - a.rot) / N;
     const int n_rows = a.n_kv_heads + (a.Q ? a.n_heads : 0);
-    const int lanes = min(units, kAppendThreads), rows_at_once = kAppendThreads / lanes;
-    const int u0 = tid % lanes, r0 = tid < lanes * rows_at_once ? tid / lanes : n_rows;
+    const int lanes = a.lanes, rows_at_once = a.rows_at_once, row0 = tid * a.lanes_mul >> 16;  // (tid / lanes)
+    const int u0 = tid - row0 * lanes, r0 = row0 < rows_at_once ? row0 : n_rows;
     auto piece_at = [&](int u) { return INTER || u < turned ? u * N : a.rot + (u - turned) * N; };
     auto row_at = [&](int r) {
         return r < a.n_kv_heads ? static_cast<const T *>(a.K) + i * a.ldk + r * a.d
                                 : static_cast<const T *>(a.Q) + i * a.ldq + (r - a.n_kv_heads) * a.d;
     };
-    const int pieces = a.d / N, n_values = a.n_kv_heads * pieces;
-    auto value_at = [&](int x) {
-        const int r = x / pieces;
-        return static_cast<const T *>(a.V) + i * a.ldv + r * a.d + (x - r * pieces) * N;
+    const int n_values = a.n_kv_heads * a.pieces.page;
+    auto value_at = [&](int x) {  // (heads follow each other)
+        return static_cast<const T *>(a.V) + i * a.ldv + x * N;
     };
     V first_x[AHEAD + 1], first_y[AHEAD + 1], first_v;
 #pragma unroll
@@ -166,9 +186,9 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
         }
         if (key) {
             const int64_t at = pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d);
-            const float scale = E4 ? a.k_scale[r] : 1.f;
-            write_cache<T, E4, N, VEC>(a.Kc, at + f0, x, scale);
-            if (!INTER && turn) write_cache<T, E4, N, VEC>(a.Kc, at + f1, y, scale);
+            const Quotient over(E4 ? a.k_scale[r] : 1.f);
+            write_cache<T, E4, N, VEC>(a.Kc, at + f0, x, over);
+            if (!INTER && turn) write_cache<T, E4, N, VEC>(a.Kc, at + f1, y, over);
         } else {
             T *dst = static_cast<T *>(a.Q_out) + (i * a.n_heads + (r - a.n_kv_heads)) * a.d;
             write_piece<T, N, VEC>(dst + f0, x);
@@ -202,10 +222,11 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
     // values
     if (phys < 0) return;
     for (int x = tid; x < n_values; x += kAppendThreads) {
-        const int r = x / pieces, f = (x - r * pieces) * N;
+        const int r = a.pieces.div(x), f = (x - r * a.pieces.page) * N;
         float v[N];
         widen_piece<T, N>(AHEAD && x == tid ? first_v : read_raw<T, N, VEC>(value_at(x)), v);
-        write_cache<T, E4, N, VEC>(a.Vc, pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d) + f, v, E4 ? a.v_scale[r] : 1.f);
+        write_cache<T, E4, N, VEC>(a.Vc, pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d) + f, v,
+                                      Quotient(E4 ? a.v_scale[r] : 1.f));
     }
 }
 
@@ -218,7 +239,17 @@ hipError_t launch_append(const AppendArgs &a, int dtype, int cache, bool interle
     // (cache rows of 8 values are 8 bytes in e4m3)
     const bool vec = aligned(a.K, a.ldk) && aligned(a.V, a.ldv) && aligned(a.Q, a.Q ? a.ldq : 0) && aligned(a.Q_out, 0) &&
                      aligned(a.Kc, 0) && aligned(a.Vc, 0) && a.rot % (interleaved ? n : 2 * n) == 0;
-    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)a.n_tokens), dim3(kAppendThreads), 0, stream, a); };
+    // Quotients that the threads of a workgroup would form: with m = ceil(2^16 /
+    // lanes), tid * m >> 16 = tid / lanes for tid and lanes of at most 256.
+    auto go = [&](auto kern, int n) {
+        AppendArgs b = a;
+        const int turned = interleaved ? a.rot / n : a.rot / 2 / n, units = interleaved ? a.d / n : turned + (a.d - a.rot) / n;
+        b.lanes = units < kAppendThreads ? units : kAppendThreads;
+        b.lanes_mul = (65536 + b.lanes - 1) / b.lanes;
+        b.rows_at_once = kAppendThreads / b.lanes;
+        b.pieces = page_div(a.d / n);
+        hipLaunchKernelGGL(kern, dim3((unsigned)a.n_tokens), dim3(kAppendThreads), 0, stream, b);
+    };
     // Rows are asked for before their place is known (one token 3.8 -> 3.2 us on the
     // device, 192 into an 8-bit cache 5.7 -> 5.1, 28000 of ragged prompts into one
     // 152 -> 135), but for large calls of a bf16 cache: the registers that hold them
@@ -230,9 +261,9 @@ hipError_t launch_append(const AppendArgs &a, int dtype, int cache, bool interle
         constexpr bool E4 = decltype(e4)::value, AX = decltype(axes)::value;
         constexpr int W = decltype(width)::value, A = decltype(rows)::value;
         if (vec)
-            interleaved ? go(append_kernel<T, E4, true, W, true, AX, A>) : go(append_kernel<T, E4, false, W, true, AX, A>);
+            interleaved ? go(append_kernel<T, E4, true, W, true, AX, A>, W) : go(append_kernel<T, E4, false, W, true, AX, A>, W);
         else  // (interleaved partners go together)
-            interleaved ? go(append_kernel<T, E4, true, 2, false, AX, A>) : go(append_kernel<T, E4, false, 1, false, AX, A>);
+            interleaved ? go(append_kernel<T, E4, true, 2, false, AX, A>, 2) : go(append_kernel<T, E4, false, 1, false, AX, A>, 1);
     };
     auto types = [&](auto axes) {
         typedef std::integral_constant<int, 0> None;

@@ -87,6 +87,10 @@ struct AppendArgs {
     int32_t n_heads, n_kv_heads, d, n_pages, max_pages, n_seqs, n_tokens, rot;
     int32_t per_seq;   // new tokens of each sequence where seq_start is null
     PageDiv pd;
+    // set by the launcher: lanes of a row, 2^16 / lanes rounded up, rows that a
+    // workgroup takes at once, pieces of a row of values
+    int32_t lanes, lanes_mul, rows_at_once;
+    PageDiv pieces;
 };
 
 struct PagedArgs {

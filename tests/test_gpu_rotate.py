@@ -288,3 +288,34 @@ def test_positions_of_the_places_are_the_append():
         got.append((out, *pools))
     for other in got[1:]:
         assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.02, 3.1e-3, float.fromhex("0x1.fffffep-7"), 1e-30, 2e30, 7.0 / 3])
+def test_values_of_an_8_bit_cache_are_quotients(scale):
+    """What an e4m3 cache holds is x / scale, rounded to binary32 and then once
+    more, as a division gives it: bits equal, for values that are not finite, past
+    448, and near every border of the type too."""
+    rr = rrmod()
+    note("append e4m3 quotients", scale)
+    rng = np.random.default_rng(11)
+    s = np.float32(scale)
+    borders = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    mid = ((borders[:-1] + borders[1:]) / 2).nan_to_num(0.0)
+    x = torch.cat((borders.nan_to_num(0.0) * s, mid * s, torch.from_numpy(rng.standard_normal(40000).astype(np.float32) * 60 * s),
+                   torch.tensor([float("inf"), -float("inf"), float("nan"), 3e38, -3e38, 1e-38, 0.0, -0.0]) * 1.0))
+    x = torch.cat((x, -x))
+    n, d = -(-x.numel() // 128), 64
+    rows = torch.zeros(n * 128)
+    rows[:x.numel()] = x
+    K = rows.view(n, 2, d).bfloat16().to(DEV)
+    pools = [torch.zeros((n, 2, 1, d), dtype=torch.float8_e4m3fn, device=DEV) for _ in range(2)]
+    table = torch.arange(n, dtype=torch.int32, device=DEV).view(1, n)
+    scales = torch.tensor([s, s], device=DEV)
+    rr.cache_append(K, K, *pools, table, torch.tensor([n], dtype=torch.int32, device=DEV), k_scale=scales, v_scale=scales)
+    y = (K.float().cpu() / torch.tensor(s))
+    y = torch.where(y.isnan(), y, y.clamp(-448, 448)).to(torch.float8_e4m3fn).view(torch.uint8)
+    for pool in pools:
+        got = pool.view(torch.uint8).cpu()[:, :, 0]
+        nan = K.isnan().cpu()
+        assert torch.equal(got[~nan], y[~nan])
+        assert bool(((got[nan] & 0x7f) == 0x7f).all())
