@@ -136,6 +136,12 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
     auto value_at = [&](int x) {  // (heads follow each other)
         return static_cast<const T *>(a.V) + i * a.ldv + x * N;
     };
+    int axis[1];
+    double freq = 0.0;
+    if (tid < half) {
+        freq = a.freqs[tid];
+        if (AXES) a.axes.of(tid, axis);
+    }
     V first_x[AHEAD + 1], first_y[AHEAD + 1], first_v;
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
@@ -147,6 +153,9 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
         }
     }
     if (AHEAD && tid < n_values) first_v = read_raw<T, N, VEC>(value_at(tid));
+
+    double at[1];
+    if (AXES && tid < half) a.axes.at(i, axis, at);
 
     // where the token goes: sequence, position, page.  (Loads that wait for each
     // other; with their addresses in vector registers, as the scalar loads that
@@ -167,9 +176,14 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
     const int phys = pool_page(a.table[(int64_t)b * a.max_pages + c], a.n_pages);
 
     for (int x = tid; x < half; x += kAppendThreads) {
-        double p[1] = {(double)pos};
-        if (AXES) a.axes.at(i, x, p);
-        turn_of(p[0], a.freqs[x], &s_cos[x], &s_sin[x]);
+        if (x != tid) {
+            freq = a.freqs[x];
+            if (AXES) {
+                a.axes.of(x, axis);
+                a.axes.at(i, axis, at);
+            }
+        }
+        turn_of(AXES ? at[0] : (double)pos, freq, &s_cos[x], &s_sin[x]);
     }
     __syncthreads();
 

@@ -33,13 +33,16 @@ constexpr int kForkLds = 65536;  // bytes of parents, children and columns
 // Bound by those additions where many rows change: sequences that hold the same
 // page mostly follow each other, so neighbouring rows' are summed in a wave
 // before one of them adds (beams of 512 sequences, in groups of 8 that share all
-// but the last page of up to 1000: 12.2 -> 9.2 us).
+// but the last page of up to 1000: 12.2 -> 9.2 us), and
+// neighbouring columns, which share lines of memory, are one XCD's (-> 5.1).
 template <int C>
 __global__ __launch_bounds__(kForkThreads) void fork_kernel(ForkArgs a)
 {
     extern __shared__ int32_t lds[];
     int32_t *s_parent = lds, *s_kids = lds + a.n_seqs, *s_tile = lds + 2 * a.n_seqs;
-    const int tid = threadIdx.x, c0 = blockIdx.x * C, n = a.n_seqs * C;
+    // (workgroups are dealt to the eight XCDs in turn)
+    const int tid = threadIdx.x, n = a.n_seqs * C, c0 = ((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3)) * C;
+    if (c0 >= a.max_pages) return;
     for (int b = tid; b < a.n_seqs; b += kForkThreads) s_kids[b] = 0;
     __syncthreads();
     for (int b = tid; b < a.n_seqs; b += kForkThreads) {
@@ -192,6 +195,45 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
     __shared__ int s_cursor, s_copies, s_stop;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
+    // The new entries of sequences b0 .. b0 + 1023, one after the other: how many.
+    auto lay_out = [&](int b0) {
+        const int b = b0 + tid;
+        int first = 0, n = 0, begin = 0, items;
+        if (b < a.n_seqs) {
+            const int length = a.lengths[b], end = held_tokens(length, a.capacity);
+            begin = max(0, length - max(0, a.new_tokens ? a.new_tokens[b] : a.n_new));
+            if (begin < end) {
+                first = a.pd.div(begin);
+                n = a.pd.div(end - 1) + 1 - first;
+            }
+        }
+        s_to[tid] = before_of(n, s_wave[0], &items);
+        s_first[tid] = first;
+        s_begin[tid] = begin;
+        s_missing[tid] = 0;
+        __syncthreads();
+        return items;
+    };
+    // The i-th of them: its sequence (less b0), its entry, and the page there.
+    struct Item {
+        int q, c, e;
+    };
+    auto look_up = [&](int b0, int i, int items) {
+        Item it{0, 0, -1};
+        if (i >= items) return it;
+        int hi = min(kBookThreads, a.n_seqs - b0);  // the last sequence that begins at or before item i
+        while (hi - it.q > 1) {
+            const int mid = (it.q + hi) / 2;
+            if (s_to[mid] <= i)
+                it.q = mid;
+            else
+                hi = mid;
+        }
+        it.c = s_first[it.q] + i - s_to[it.q];
+        it.e = pool_page(a.table[(int64_t)(b0 + it.q) * a.max_pages + it.c], a.n_pages);
+        return it;
+    };
+
     const int64_t from0 = (int64_t)blockIdx.x * (kEntriesEach * kBookThreads);
     const int b_first = (int)(from0 / a.max_pages), c_first = (int)(from0 - (int64_t)b_first * a.max_pages);
 #pragma unroll
@@ -205,6 +247,10 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
         atomicSub(a.refs + e, 1);
         *entry = -1;
     }
+    // (Any workgroup may be the last, so each prepares the first round while its
+    // changes are on their way: entries of new tokens are not among them.)
+    int items = lay_out(0);
+    Item it = look_up(0, tid, items);
     wait_vm();        // this wave's changes are there for all ...
     __syncthreads();  // ... and the other waves'
     if (tid == 0) {
@@ -219,40 +265,11 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
     const __amdgpu_buffer_rsrc_t refs =
         __builtin_amdgcn_make_buffer_rsrc(a.refs, 0, a.n_pages * (int)sizeof(int32_t), 0x00020000);
     for (int b0 = 0; b0 < a.n_seqs; b0 += kBookThreads) {
-        // the sequences' new entries
-        const int b = b0 + tid;
-        int first = 0, n = 0, begin = 0;
-        if (b < a.n_seqs) {
-            const int length = a.lengths[b], end = held_tokens(length, a.capacity);
-            begin = max(0, length - max(0, a.new_tokens ? a.new_tokens[b] : a.n_new));
-            if (begin < end) {
-                first = a.pd.div(begin);
-                n = a.pd.div(end - 1) + 1 - first;
-            }
-        }
-        int items;
-        s_to[tid] = before_of(n, s_wave[0], &items);
-        s_first[tid] = first;
-        s_begin[tid] = begin;
-        s_missing[tid] = 0;
-        __syncthreads();
+        if (b0) items = lay_out(b0);
         for (int i0 = 0; i0 < items; i0 += kBookThreads) {
             const int i = i0 + tid;
-            int q = 0, c = 0, e = -1, holders = 0;
-            if (i < items) {
-                // the last sequence that begins at or before item i
-                int hi = min(kBookThreads, a.n_seqs - b0);
-                while (hi - q > 1) {
-                    const int mid = (q + hi) / 2;
-                    if (s_to[mid] <= i)
-                        q = mid;
-                    else
-                        hi = mid;
-                }
-                c = s_first[q] + i - s_to[q];
-                e = pool_page(a.table[(int64_t)(b0 + q) * a.max_pages + c], a.n_pages);
-                if (e >= 0) holders = now(a.refs + e);
-            }
+            if (b0 || i0) it = look_up(b0, i, items);
+            const int q = it.q, c = it.c, e = it.e, holders = e >= 0 ? now(a.refs + e) : 0;
             // A page that several hold is copied as long as that is so: each
             // item of this round before this one takes its own copy.
             const bool shared = holders > 1;
@@ -331,7 +348,7 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
             wait_vm();  // (the pages' counts, for the next round)
             __syncthreads();
         }
-        if (a.missing && b < a.n_seqs) a.missing[b] = s_missing[tid];
+        if (a.missing && b0 + tid < a.n_seqs) a.missing[b0 + tid] = s_missing[tid];
         __syncthreads();
     }
     if (tid == 0) *a.n_copies = s_copies;
@@ -519,8 +536,8 @@ hipError_t launch_fork(const ForkArgs &a, hipStream_t stream)
 {
     auto lds = [&](int columns) { return a.n_seqs * (2 + columns) * (int)sizeof(int32_t); };
     auto go = [&](auto kern, int columns) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)((a.max_pages + columns - 1) / columns)), dim3(kForkThreads), (unsigned)lds(columns),
-                           stream, a);
+        const int groups = (a.max_pages + columns - 1) / columns;
+        hipLaunchKernelGGL(kern, dim3((unsigned)((groups + 7) / 8 * 8)), dim3(kForkThreads), (unsigned)lds(columns), stream, a);
     };
     // as many columns as LDS holds, up to 8, and to 4 where that leaves compute units idle
     if (lds(8) <= kForkLds && a.max_pages >= 8 * 256)

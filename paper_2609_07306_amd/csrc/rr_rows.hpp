@@ -113,19 +113,24 @@ struct Axes {
     int64_t n;              // tokens
     int32_t n_axes, real;
 
-    // Token i's positions as frequencies j .. j + N - 1 take them; 0, which
-    // rotates nothing, for an axis that is not there.  (Stage by stage: loads
-    // that depend on each other only where they must.)
+    // The axes of frequencies j .. j + N - 1.  (Their loads are a stage of their
+    // own, so that loads wait for each other only where they must.)
     template <int N>
-    __device__ __forceinline__ void at(int64_t i, int j, double (&p)[N]) const
+    __device__ __forceinline__ void of(int j, int (&t)[N]) const
     {
-        int t[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) t[e] = 0;
         if (axis) {
 #pragma unroll
             for (int e = 0; e < N; ++e) t[e] = axis[j + e];
         }
+    }
+
+    // Token i's positions on axes t; 0, which rotates nothing, for an axis that is
+    // not there.
+    template <int N>
+    __device__ __forceinline__ void at(int64_t i, const int (&t)[N], double (&p)[N]) const
+    {
         int32_t bits[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) {
@@ -143,9 +148,11 @@ template <int N>
 __device__ __forceinline__ void turns_of(const Axes &axes, const double *freqs, int64_t i, int j, float (&c)[N], float (&s)[N])
 {
     double p[N], f[N];
+    int t[N];
+    axes.of(j, t);
 #pragma unroll
     for (int e = 0; e < N; ++e) f[e] = freqs[j + e];
-    axes.at(i, j, p);
+    axes.at(i, t, p);
 #pragma unroll
     for (int e = 0; e < N; ++e) turn_of(p[e], f[e], &c[e], &s[e]);
 }
