@@ -46,11 +46,19 @@ struct Quotient {
 
     __device__ __forceinline__ explicit Quotient(float s) : scale(s), r(1.f / s), direct(!(s > 0x1p-60f && s < 0x1p60f)) {}
 
-    __device__ __forceinline__ float operator()(float x) const
+    template <int N>
+    __device__ __forceinline__ void operator()(const float (&x)[N], float (&y)[N]) const
     {
-        if (direct) return x / scale;
-        const float q = __builtin_amdgcn_fmed3f(x * r, -1024.f, 1024.f);
-        return __builtin_fmaf(-__builtin_fmaf(q, scale, -x), r, q);  // (so that -0 stays -0)
+        if (direct) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = x[e] / scale;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float q = __builtin_amdgcn_fmed3f(x[e] * r, -1024.f, 1024.f);
+            y[e] = __builtin_fmaf(-__builtin_fmaf(q, scale, -x[e]), r, q);  // (so that -0 stays -0)
+        }
     }
 };
 
@@ -63,21 +71,21 @@ __device__ __forceinline__ float clamp_e4m3(float x)
 template <int N, bool VEC>
 __device__ __forceinline__ void write_e4m3(uint8_t *p, const float (&x)[N], const Quotient &over)
 {
+    float y[N];
+    over(x, y);
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] = clamp_e4m3(y[e]);
     if constexpr (VEC) {
         uint32_t o[N / 4];
 #pragma unroll
         for (int q = 0; q < N / 4; ++q) {
-            float y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = clamp_e4m3(over(x[4 * q + e]));
-            const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-            o[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
+            const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * q], y[4 * q + 1], 0, false);
+            o[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * q + 2], y[4 * q + 3], lo, true);
         }
         __builtin_memcpy(__builtin_assume_aligned(p, N), o, N);
     } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-            p[e] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp_e4m3(over(x[e])), 0.f, 0, false);
+        for (int e = 0; e < N; ++e) p[e] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[e], 0.f, 0, false);
     }
 }
 
@@ -172,8 +180,9 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
     if (b < 0) return;
     const int64_t p = (int64_t)a.lengths[b] - left;
     if (p < 0 || p >= (int64_t)a.max_pages * a.pd.page) return;
-    const int pos = (int)p, c = a.pd.div(pos), place = pos - c * a.pd.page;
-    const int phys = pool_page(a.table[(int64_t)b * a.max_pages + c], a.n_pages);
+    const int pos = (int)p, c = a.pd.div(pos), place = __builtin_amdgcn_readfirstlane(pos - c * a.pd.page);
+    const int phys = __builtin_amdgcn_readfirstlane(pool_page(a.table[(int64_t)b * a.max_pages + c], a.n_pages));
+    const int64_t at0 = pool_row(phys, a.n_kv_heads, 0, a.pd.page, place, a.d), head = (int64_t)a.pd.page * a.d;
 
     for (int x = tid; x < half; x += kAppendThreads) {
         if (x != tid) {
@@ -199,7 +208,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
             turn_piece<INTER, N>(x, y, c, s);
         }
         if (key) {
-            const int64_t at = pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d);
+            const int64_t at = at0 + r * head;
             const Quotient over(E4 ? a.k_scale[r] : 1.f);
             write_cache<T, E4, N, VEC>(a.Kc, at + f0, x, over);
             if (!INTER && turn) write_cache<T, E4, N, VEC>(a.Kc, at + f1, y, over);
@@ -239,8 +248,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
         const int r = a.pieces.div(x), f = (x - r * a.pieces.page) * N;
         float v[N];
         widen_piece<T, N>(AHEAD && x == tid ? first_v : read_raw<T, N, VEC>(value_at(x)), v);
-        write_cache<T, E4, N, VEC>(a.Vc, pool_row(phys, a.n_kv_heads, r, a.pd.page, place, a.d) + f, v,
-                                      Quotient(E4 ? a.v_scale[r] : 1.f));
+        write_cache<T, E4, N, VEC>(a.Vc, at0 + r * head + f, v, Quotient(E4 ? a.v_scale[r] : 1.f));
     }
 }
 
