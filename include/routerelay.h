@@ -592,7 +592,7 @@ size_t rr_pages_workspace_bytes(int32_t n_pages);
  *   pools   host array of n_pools device pointers, 16-byte aligned
  * Returns RR_ERR_INVALID for bad sizes, types, NULL or unaligned pointers or a
  * workspace too small, RR_ERR_UNSUPPORTED for pages of more than 2^30 bytes, or
- * where n_seqs * max_pages comes to 2^34. */
+ * where n_seqs * max_pages comes to 2^31. */
 rr_status rr_cache_resize(const rr_pages_config *cfg, void *const *pools, const int32_t *new_tokens, const int32_t *lengths,
                           int32_t *page_table, int32_t *refs, int32_t *missing, void *workspace, size_t workspace_bytes,
                           void *hip_stream);
@@ -648,6 +648,7 @@ size_t rr_verify_workspace_bytes(const rr_verify_config *cfg);
  *   tokens    [n_seqs, n_drafts + 1] int32: those, then the drawn one, then -1
  *   lengths   optional [n_seqs] int32, changed in place: less the drafts that
  *             were not taken (as a cache counts them to which all were appended)
+ * accepted, tokens and lengths overlap nothing else.
  * Returns RR_ERR_INVALID for bad sizes, types, strides, NULL pointers or a
  * workspace too small, RR_ERR_UNSUPPORTED for a vocabulary of 2^24 or more. */
 rr_status rr_verify_drafts(const rr_verify_config *cfg, const void *P, const void *Q, const int32_t *drafts,

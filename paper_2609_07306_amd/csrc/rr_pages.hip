@@ -234,8 +234,8 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
         return it;
     };
 
-    const int64_t from0 = (int64_t)blockIdx.x * (kEntriesEach * kBookThreads);
-    const int b_first = (int)(from0 / a.max_pages), c_first = (int)(from0 - (int64_t)b_first * a.max_pages);
+    const uint32_t from0 = blockIdx.x * (kEntriesEach * kBookThreads);  // (a table has less than 2^31 entries)
+    const int b_first = (int)(from0 / (uint32_t)a.max_pages), c_first = (int)(from0 % (uint32_t)a.max_pages);
 #pragma unroll
     for (int j = 0; j < kEntriesEach; ++j) {
         const int x = c_first + j * kBookThreads + tid, b = b_first + x / a.max_pages, c = x % a.max_pages;
@@ -527,11 +527,6 @@ __global__ __launch_bounds__(kCopyThreads) void copies_kernel(PagesArgs a, Pools
 
 }  // namespace
 
-int64_t resize_groups(int32_t n_seqs, int32_t max_pages)
-{
-    return ((int64_t)n_seqs * max_pages + kEntriesEach * kBookThreads - 1) / (kEntriesEach * kBookThreads);
-}
-
 hipError_t launch_fork(const ForkArgs &a, hipStream_t stream)
 {
     auto lds = [&](int columns) { return a.n_seqs * (2 + columns) * (int)sizeof(int32_t); };
@@ -553,7 +548,9 @@ hipError_t launch_fork(const ForkArgs &a, hipStream_t stream)
 
 hipError_t launch_resize(const PagesArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL(resize_kernel, dim3((unsigned)resize_groups(a.n_seqs, a.max_pages)), dim3(kBookThreads), 0, stream, a);
+    constexpr int kEntries = kEntriesEach * kBookThreads;
+    const int64_t groups = ((int64_t)a.n_seqs * a.max_pages + kEntries - 1) / kEntries;
+    hipLaunchKernelGGL(resize_kernel, dim3((unsigned)groups), dim3(kBookThreads), 0, stream, a);
     return hipGetLastError();
 }
 

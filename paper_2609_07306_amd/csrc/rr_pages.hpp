@@ -46,7 +46,6 @@ struct Pools {
     void *p[kPoolsAtOnce];
 };
 
-int64_t resize_groups(int32_t n_seqs, int32_t max_pages);
 hipError_t launch_fork(const ForkArgs &a, hipStream_t stream);
 hipError_t launch_resize(const PagesArgs &a, hipStream_t stream);   // the tables; copies to make
 hipError_t launch_compact(const PagesArgs &a, hipStream_t stream);  // the same

@@ -782,17 +782,19 @@ def pages_workspace(pools):
     return torch.zeros(n, dtype=torch.uint8, device=pools.tensors[0].device)
 
 
-def _workspace_of(workspace, make, stream):
-    """The workspace's address and bytes, and itself (one of this call's own: None given)."""
-    if workspace is None:
-        if stream is not None:
-            with torch.cuda.stream(stream):
-                workspace = make()
-        else:
-            workspace = make()
-    elif workspace.dtype != torch.uint8 or workspace.dim() != 1 or not workspace.is_contiguous():
+def _on(stream, make):
+    """make() with the given stream current (None: as it is)."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
+
+
+def _workspace(workspace):
+    """A workspace's address and bytes."""
+    if workspace.dtype != torch.uint8 or workspace.dim() != 1 or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous one-dimensional uint8 tensor")
-    return workspace.data_ptr(), workspace.numel(), workspace
+    return workspace.data_ptr(), workspace.numel()
 
 
 def _refs(refs, n_pages):
@@ -826,9 +828,10 @@ def cache_resize(pools, page_table, lengths, refs, new_tokens, missing=None, wor
     if missing is None:
         missing = _empty((B,), torch.int32, page_table, stream)
     out = _of("missing", missing, (B,), torch.int32)
-    ws, size, workspace = _workspace_of(workspace, lambda: pages_workspace(pools), stream)
+    if workspace is None:
+        workspace = _on(stream, lambda: pages_workspace(pools))
     _launch(dev, stream, _resize, pools._config(most, B, 0 if many else new_tokens), pools._addresses, new, lens, table, r, out,
-            ws, size)
+            *_workspace(workspace))
     return missing
 
 
@@ -849,32 +852,34 @@ def cache_compact(pools, page_table, refs, new_ids=None, n_used=None, workspace=
     if n_used is None:
         n_used = _empty((1,), torch.int32, page_table, stream)
     ids, used = _of("new_ids", new_ids, (n_pages,), torch.int32), _of("n_used", n_used, (1,), torch.int32)
-    ws, size, workspace = _workspace_of(workspace, lambda: pages_workspace(pools), stream)
-    _launch(dev, stream, _compact, pools._config(most, B), pools._addresses, table, r, ids, used, ws, size)
+    if workspace is None:
+        workspace = _on(stream, lambda: pages_workspace(pools))
+    _launch(dev, stream, _compact, pools._config(most, B), pools._addresses, table, r, ids, used, *_workspace(workspace))
     return new_ids, n_used
 
 
 # --------------------------------------------------------- drafted tokens
 
-def _rows_3d(name, t, shape, dtype):
-    """The strides of rows [B, n, V] that are contiguous (views of padded ones)."""
-    if t.shape != shape or t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype} of shape {list(shape)}")
-    seq, row, one = t.stride()
-    if shape[2] > 1 and one != 1:
-        raise ValueError(f"{name}: rows must be contiguous")
-    return seq, row
-
-
 def _verify_config(P, n_drafts, Q=None):
-    if P.dim() != 3 or P.dtype not in (torch.float32, torch.bfloat16):
+    """The configuration of P [B, n_drafts + 1, V] and Q [B, n_drafts, V], whose rows
+    are contiguous but may lie apart (views of padded ones)."""
+    kind, shape = P.dtype, P.shape
+    if len(shape) != 3 or kind not in (torch.float32, torch.bfloat16):
         raise TypeError("P must be a [B, n_drafts + 1, V] float32 or bfloat16 tensor")
-    B, rows, V = P.shape
+    B, rows, V = shape
     if rows != n_drafts + 1:
         raise ValueError(f"P has {rows} rows a sequence, one more than the {n_drafts} drafts is wanted")
-    p = _rows_3d("P", P, P.shape, P.dtype)
-    q = (0, 0) if Q is None else _rows_3d("draft_probs", Q, (B, n_drafts, V), P.dtype)
-    return _VerifyConfig(B, n_drafts, V, _DTYPES[P.dtype], *p, *q)
+    p_seq, p_row, one = P.stride()
+    q_seq = q_row = 0
+    if Q is not None:
+        if Q.dtype != kind or Q.shape != (B, n_drafts, V):
+            raise ValueError(f"draft_probs must be {kind} of shape {[B, n_drafts, V]}")
+        q_seq, q_row, q_one = Q.stride()
+        if q_one != 1 and V > 1:
+            raise ValueError("draft_probs: rows must be contiguous")
+    if one != 1 and V > 1:
+        raise ValueError("P: rows must be contiguous")
+    return _VerifyConfig(B, n_drafts, V, _DTYPES[kind], p_seq, p_row, q_seq, q_row)
 
 
 def verify_workspace(P):
@@ -905,15 +910,21 @@ def verify_drafts(P, drafts, uniforms, draft_probs=None, n_drafts=None, lengths=
     dev = _device_of((P, drafts, uniforms, draft_probs, n_drafts, lengths, accepted, tokens, workspace))
     cfg = _verify_config(P, n, draft_probs)
     i32 = torch.int32
-    d, u = _of("drafts", drafts, (P.shape[0], n), i32), _of("uniforms", uniforms, (B, n + 1), torch.float32)
+    d, u = _of("drafts", drafts, (cfg.n_seqs, n), i32), _of("uniforms", uniforms, (B, n + 1), torch.float32)
     count = None if n_drafts is None else _of("n_drafts", n_drafts, (B,), i32)
     lens = None if lengths is None else _of("lengths", lengths, (B,), i32)
     if accepted is None:
-        accepted = _empty((B,), i32, P, stream)
+        accepted = _empty((B,), i32, drafts, stream)
+        took = accepted.data_ptr()
+    else:
+        took = _of("accepted", accepted, (B,), i32)
     if tokens is None:
-        tokens = _empty((B, n + 1), i32, P, stream)
-    took, out = _of("accepted", accepted, (B,), i32), _of("tokens", tokens, (B, n + 1), i32)
-    ws, size, workspace = _workspace_of(workspace, lambda: verify_workspace(P), stream)
+        tokens = _empty((B, n + 1), i32, drafts, stream)
+        out = tokens.data_ptr()
+    else:
+        out = _of("tokens", tokens, (B, n + 1), i32)
+    if workspace is None:
+        workspace = _on(stream, lambda: verify_workspace(P))
     _launch(dev, stream, _verify, cfg, P.data_ptr(), None if draft_probs is None else draft_probs.data_ptr(), d, count, u, lens,
-            took, out, ws, size)
+            took, out, *_workspace(workspace))
     return accepted, tokens

@@ -67,7 +67,8 @@ def _check(rr, P, Q, drafts, u, count=None, **kw):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("B,n,V", [(1, 0, 1), (1, 1, 2), (5, 3, 3), (7, 4, 255), (3, 2, 256), (3, 5, 257), (2, 70, 40),
-                                   (64, 4, 1000), (1, 4, 32000), (3, 2, 50001), (2, 1, 131072), (40, 3, 20011)])
+                                   (64, 4, 1000), (1, 4, 32000), (3, 2, 50001), (2, 1, 131072), (40, 3, 20011),
+                                   (2, 2, 300001), (30, 1, 131071)])
 @pytest.mark.parametrize("given", [True, False])
 @pytest.mark.parametrize("ragged", [False, True])
 def test_verify(dtype, B, n, V, given, ragged):
@@ -149,11 +150,12 @@ def test_borders():
         assert rr.verify_drafts(P, drafts, u)[1].tolist() == t.tolist()
 
 
-def test_nothing_left_and_no_probabilities():
+@pytest.mark.parametrize("V", [3000, 300001])
+def test_nothing_left_and_no_probabilities(V):
     rr = rrmod()
-    note("verify nothing left")
+    note("verify nothing left", V)
     inf, nan = float("inf"), float("nan")
-    V = 3000
+    last = V - 1
 
     def row(**at):
         x = torch.zeros(V)
@@ -166,7 +168,7 @@ def test_nothing_left_and_no_probabilities():
         (row(v5=0.5, v2000=0.5), row(v5=0.6, v2000=0.6, v7=0.1), 7, [0.9, 0.6], 2000, 0),
         (row(), row(v5=1.0), 5, [0.0, 0.5], -1, 0),                                      # the target has none
         (row(v3=nan, v4=inf, v9=-1.0), row(v5=1.0), 5, [0.0, 0.5], -1, 0),               # ... that counts
-        (row(v3=nan, v4=inf, v9=-1.0, v2999=0.1), row(v5=1.0), 5, [0.0, 0.0], 2999, 0),
+        (row(v3=nan, v4=inf, v9=-1.0, **{f"v{last}": 0.1}), row(v5=1.0), 5, [0.0, 0.0], last, 0),
         (row(v8=1.0), row(v8=nan), 8, [0.0, 0.5], 8, 0),                                 # p - NaN: nothing, so from p
         (row(v8=1.0, v9=0.5), row(v8=1.0), -1, [0.0, 0.5], 9, 0),                        # no such draft
         (row(v8=1.0, v9=0.5), row(v8=1.0), V, [0.0, 0.5], 9, 0),

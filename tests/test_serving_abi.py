@@ -103,7 +103,7 @@ def _pages_call(rr, compact, cfg="some", pools=(0x1000, 0x2000, 0x3000), lengths
     ({"n_pages": (1 << 28) + 1}, -1), ({"cache_dtype": 3}, -1), ({"n_pools": 0}, -1), ({"n_pools": 4097}, -1),
     ({"max_pages": 0}, -1), ({"max_pages": 1 << 27}, -1), ({"n_seqs": 0}, -1), ({"n_new": -1}, -1), ({"reserved": 1}, -1),
     ({"n_kv_heads": 1 << 18, "page": 1 << 9}, -5), ({"n_kv_heads": 2 ** 31 - 1}, -5),
-    ({"n_seqs": 1 << 20, "max_pages": 1 << 14}, -5), ({"pools": None}, -1), ({"pools": (0x1000, 0, 0x3000)}, -1),
+    ({"n_seqs": 1 << 17, "max_pages": 1 << 14}, -5), ({"pools": None}, -1), ({"pools": (0x1000, 0, 0x3000)}, -1),
     ({"pools": (0x1000, 0x2008, 0x3000)}, -1), ({"table": None}, -1), ({"refs": None}, -1), ({"ws": None}, -1), ({"ws": ODD}, -1),
     ({"size": 0}, -1),
 ])
