@@ -10,14 +10,16 @@
 // a token and shared by all of its heads through LDS.
 //
 // Measured: 32768 tokens of that size in 143 us, 5.6 TB/s read and written (a
-// copy of 1 GiB: 5.1).  Small calls are a chain of loads -- length, page,
-// rows -- and the launch: one token 3.3 us, 192 tokens of as many sequences
-// into an 8-bit cache 5.4, 24 ragged binary32 prompts (3147 tokens, 16 MB) 7.4.
+// copy of 1 GiB: 5.1); 22600 tokens of ragged prompts into an 8-bit cache, rotated
+// by axes, 119 (3.4 TB/s: chains of loads -- start, length, page -- and vector
+// instructions, half of a SIMD's time each).  Small calls are a chain and the
+// launch: one token 3.1 us, 64 by axes 4.4, 192 tokens of as many sequences into an
+// 8-bit cache 4.8, 24 ragged binary32 prompts (3147 tokens, 16 MB) 8.0.
 //
 // A workgroup takes a token.  A thread keeps the same features of a row over
 // the heads that it goes through, so it reads its sines and cosines once; a
-// vector piece is 16 bytes of input (one element where rows are not aligned to
-// that).
+// vector piece is 8 or 16 bytes of input (an element, or two interleaved ones,
+// where rows are not aligned to that).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -272,12 +274,13 @@ hipError_t launch_append(const AppendArgs &a, int dtype, int cache, bool interle
         b.pieces = page_div(a.d / n);
         hipLaunchKernelGGL(kern, dim3((unsigned)a.n_tokens), dim3(kAppendThreads), 0, stream, b);
     };
-    // Rows are asked for before their place is known (one token 3.8 -> 3.2 us on the
-    // device, 192 into an 8-bit cache 5.7 -> 5.1, 28000 of ragged prompts into one
-    // 152 -> 135), but for large calls of a bf16 cache: the registers that hold them
-    // leave half of the waves, and waves are what keeps the memory busy there (32768
-    // tokens 144 against 151).
-    const bool ahead = !(dtype == 1 && cache == CACHE_BF16 && a.n_tokens >= 4096);
+    // Rows are asked for before their place is known (one token 3.8 -> 3.1 us on the
+    // device, 192 into an 8-bit cache 5.7 -> 4.8).  In pieces of 8 bytes, which leave
+    // registers for more waves than those of 16 (22600 tokens of ragged prompts into
+    // an 8-bit cache 152 -> 119 us; 128 in those of 16).  Not so for large calls of a
+    // bf16 cache by place, whose angles cost little: 32768 tokens 144 us as they
+    // come, in pieces of 16 bytes, 148 so; by axes 161 and 156.
+    const bool ahead = a.n_tokens < 4096;
     auto any = [&](auto type, auto e4, auto width, auto axes, auto rows) {
         typedef decltype(type) T;
         constexpr bool E4 = decltype(e4)::value, AX = decltype(axes)::value;
@@ -287,17 +290,21 @@ hipError_t launch_append(const AppendArgs &a, int dtype, int cache, bool interle
         else  // (interleaved partners go together)
             interleaved ? go(append_kernel<T, E4, true, 2, false, AX, A>, 2) : go(append_kernel<T, E4, false, 1, false, AX, A>, 1);
     };
+    typedef std::integral_constant<int, 0> Zero;
+    typedef std::integral_constant<int, 2> Two;
+    typedef std::integral_constant<int, 3> Three;
+    typedef std::integral_constant<int, 4> Four;
+    typedef std::integral_constant<int, 8> Eight;
     auto types = [&](auto axes) {
-        typedef std::integral_constant<int, 0> None;
-        typedef std::integral_constant<int, 2> Two;
+        constexpr bool AX = decltype(axes)::value;
         if (dtype == 0)
-            any(float(), std::false_type(), std::integral_constant<int, 4>(), axes, Two());
+            any(float(), std::false_type(), Four(), axes, Two());
         else if (cache == CACHE_E4M3)
-            any(__bf16(), std::true_type(), std::integral_constant<int, 8>(), axes, Two());
-        else if (ahead)
-            any(__bf16(), std::false_type(), std::integral_constant<int, 8>(), axes, Two());
-        else
-            any(__bf16(), std::false_type(), std::integral_constant<int, 8>(), axes, None());
+            any(__bf16(), std::true_type(), Four(), axes, Three());
+        else if (AX || ahead)
+            any(__bf16(), std::false_type(), Four(), axes, Three());
+        else if constexpr (!AX)
+            any(__bf16(), std::false_type(), Eight(), axes, Zero());
     };
     a.axes.positions ? types(std::true_type()) : types(std::false_type());
     return hipGetLastError();
