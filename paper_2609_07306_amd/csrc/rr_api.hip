@@ -1283,9 +1283,7 @@ rr_status pages_args(const rr_pages_config *cfg, void *const *pools, int32_t *pa
     a.heads = c.n_kv_heads;
     a.row_bytes = (int32_t)row_bytes;
     a.pd = rr::page_div(c.page);
-    a.counter = static_cast<uint32_t *>(workspace);
-    a.n_copies = static_cast<int32_t *>(workspace) + 1;
-    a.copies = reinterpret_cast<rr::PageCopy *>(static_cast<char *>(workspace) + rr::kPagesHeadBytes);
+    rr::pages_layout(a, workspace);
     *out = a;
     return RR_OK;
 }

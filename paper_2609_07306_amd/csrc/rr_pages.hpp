@@ -36,11 +36,29 @@ struct PagesArgs {
     uint32_t *counter;  // workspace: finished workgroups, 0 between calls;
     int32_t *n_copies;  // copies to make ...
     PageCopy *copies;   // ... [n_pages]
+    int32_t *spans;     // compaction of more than a round of pages: used ones of each round,
+    int32_t *rank;      // which of the pages that move a used page past the others is; else null
 };
 
-// The workspace holds the counter and the number of copies, then the copies.
+constexpr int kRoundPages = 16384;  // pages that a workgroup counts at once
+
+// The workspace holds the counter and the number of copies, the copies, and
+// numbers of rounds.  No more than half of the pages move: the ranks take the
+// copies' second half.
 constexpr size_t kPagesHeadBytes = 256;
-inline size_t pages_workspace_bytes(int32_t n_pages) { return kPagesHeadBytes + (size_t)n_pages * sizeof(PageCopy); }
+inline size_t pages_workspace_bytes(int32_t n_pages)
+{
+    return kPagesHeadBytes + (size_t)n_pages * sizeof(PageCopy) + ((size_t)n_pages / kRoundPages + 1) * sizeof(int32_t);
+}
+
+inline void pages_layout(PagesArgs &a, void *workspace)
+{
+    a.counter = static_cast<uint32_t *>(workspace);
+    a.n_copies = static_cast<int32_t *>(workspace) + 1;
+    a.copies = reinterpret_cast<PageCopy *>(static_cast<char *>(workspace) + kPagesHeadBytes);
+    a.spans = reinterpret_cast<int32_t *>(a.copies + a.n_pages);
+    a.rank = a.n_pages > kRoundPages ? reinterpret_cast<int32_t *>(a.copies + (a.n_pages + 1) / 2) : nullptr;
+}
 
 struct Pools {
     void *p[kPoolsAtOnce];
