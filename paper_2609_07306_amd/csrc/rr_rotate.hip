@@ -4,11 +4,11 @@
 //
 // Bound by the bytes, every row read once and written once; how near to that it
 // comes goes by the order: workgroups that follow each other in memory, each
-// with a stretch of its own, reach 6.1 TB/s on 32768 tokens of 32 heads (128
-// bf16 features), a workgroup that takes 32 tokens of every head in turn 4.4.
-// So there is a kernel for each layout.  Angles are formed in binary64, once a
-// token and frequency where the layout lets a workgroup share them.  Loads and
-// stores go past the caches (the rows are 268 MB each way there; 88 -> XX us).
+// with a short stretch of its own, move 32768 tokens of 32 heads (128 bf16
+// features, 268 MB each way) in 92 us heads first and 89 tokens first, 5.8 and
+// 6.0 TB/s; a workgroup that takes 32 tokens of every head in turn in 122.  So
+// there is a kernel for each layout.  Loads and stores go past the caches.  A
+// small call (196 tokens, 6 heads) is a launch and a chain, 3.1 us.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
