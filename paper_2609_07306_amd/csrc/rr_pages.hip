@@ -265,9 +265,15 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
         *entry = -1;
     }
     // (Any workgroup may be the last, so each prepares the first round while its
-    // changes are on their way: entries of new tokens are not among them.)
-    int items = lay_out(0);
-    Item it = look_up(0, 0, items);
+    // changes are on their way: entries of new tokens are not among them.  Where
+    // they do not all run at once, only the last does.)
+    const bool early = gridDim.x <= 256;
+    int items = 0;
+    Item it{0, 0, -1};
+    if (early) {
+        items = lay_out(0);
+        it = look_up(0, 0, items);
+    }
     wait_vm();        // this wave's changes are there for all ...
     __syncthreads();  // ... and the other waves'
     if (tid == 0) {
@@ -284,7 +290,7 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
         __builtin_amdgcn_make_buffer_rsrc(a.refs, 0, a.n_pages * (int)sizeof(int32_t), 0x00020000);
     int round = 0, head = 0, held = 0, cursor = 0, turn = 0;  // (head, held) of s_free; pages before `cursor` have been looked at
     for (int b0 = 0; b0 < a.n_seqs; b0 += kBookThreads) {
-        if (b0) {
+        if (b0 || !early) {
             items = lay_out(b0);
             it = look_up(b0, 0, items);
         }

@@ -173,7 +173,7 @@ def test_resize_with_too_few_pages(seed):
 
 
 @pytest.mark.parametrize("B,width,n_new,page", [(3000, 2, 1, 16), (2, 1500, 5000, 4), (1025, 4, 9, 4), (64, 40, 100, 3),
-                                                (1, 5000, 5000, 1), (2000, 6, 3, 2), (4, 9000, 20000, 3)])
+                                                (1, 5000, 5000, 1), (2000, 6, 3, 2), (4, 9000, 20000, 3), (1200, 1100, 20, 8)])
 @pytest.mark.parametrize("group", [1, 4])
 @pytest.mark.parametrize("spare", [0.5, 1.0])
 def test_resize_of_many(B, width, n_new, page, group, spare):
