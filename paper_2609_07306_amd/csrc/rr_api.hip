@@ -1283,6 +1283,7 @@ rr_status pages_args(const rr_pages_config *cfg, void *const *pools, int32_t *pa
     a.heads = c.n_kv_heads;
     a.row_bytes = (int32_t)row_bytes;
     a.pd = rr::page_div(c.page);
+    a.row = rr::page_div(c.max_pages);
     rr::pages_layout(a, workspace);
     *out = a;
     return RR_OK;

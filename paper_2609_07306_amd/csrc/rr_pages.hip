@@ -197,8 +197,8 @@ constexpr int kSlots = 2 * kBookThreads;  // of the table of shared pages
 // one, and those whose page others hold too get a copy of it.
 //
 // Bound by the chain of a round of 1024 entries (count, table, holders, free
-// pages, each a load and a sum over the workgroup): 8.5 us for a decode step's 64
-// sequences, 8.4 for 128 just forked, 45 for prompts of 16800 pages.
+// pages, each a load and a sum over the workgroup): 8.0 us for a decode step's 64
+// sequences, 9.2 for 128 just forked, 45 for prompts of 16800 pages.
 __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
 {
     __shared__ int s_first[kBookThreads], s_begin[kBookThreads], s_to[kBookThreads], s_missing[kBookThreads];
@@ -251,18 +251,16 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
         return it;
     };
 
-    const uint32_t from0 = blockIdx.x * (kEntriesEach * kBookThreads);  // (a table has less than 2^31 entries)
-    const int b_first = (int)(from0 / (uint32_t)a.max_pages), c_first = (int)(from0 % (uint32_t)a.max_pages);
 #pragma unroll
     for (int j = 0; j < kEntriesEach; ++j) {
-        const int x = c_first + j * kBookThreads + tid, b = b_first + x / a.max_pages, c = x % a.max_pages;
-        if (b >= a.n_seqs) continue;
-        int32_t *entry = a.table + (int64_t)b * a.max_pages + c;
-        const int e = pool_page(*entry, a.n_pages);
+        const uint32_t x = (blockIdx.x * kEntriesEach + j) * kBookThreads + tid;  // (a table has less than 2^31 entries)
+        if (x >= (uint32_t)(a.n_seqs * a.max_pages)) continue;
+        const int b = a.row.div((int)x), c = (int)x - b * a.max_pages;
+        const int e = pool_page(a.table[x], a.n_pages);
         const int end = a.pd.div(held_tokens(a.lengths[b], a.capacity) + a.pd.page - 1);
         if (c < end || e < 0) continue;
         atomicSub(a.refs + e, 1);
-        *entry = -1;
+        a.table[x] = -1;
     }
     // (Any workgroup may be the last, so each prepares the first round while its
     // changes are on their way: entries of new tokens are not among them.  Where
@@ -277,17 +275,32 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
     wait_vm();        // this wave's changes are there for all ...
     __syncthreads();  // ... and the other waves'
     if (tid == 0) {
-        const uint32_t before = __hip_atomic_fetch_add(a.counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_stop = before == gridDim.x - 1;
-        if (s_stop) __hip_atomic_store(a.counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s_stop = 1;
+        if (gridDim.x > 1) {
+            const uint32_t before = __hip_atomic_fetch_add(a.counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_stop = before == gridDim.x - 1;
+            if (s_stop) __hip_atomic_store(a.counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
         s_cursor = s_copies = 0;
         s_any = 0;
     }
     __syncthreads();
     if (!s_stop) return;
 
+    // A round of counts, from page `from` on.  The first is asked for now: between
+    // here and its use no count falls to 0, and none leaves 0 unseen.
     const __amdgpu_buffer_rsrc_t refs =
         __builtin_amdgcn_make_buffer_rsrc(a.refs, 0, a.n_pages * (int)sizeof(int32_t), 0x00020000);
+    i32x4_t r[kScan];
+    auto ask = [&](int from) {
+        const int p0 = from + wave * kWavePages;
+        if (p0 >= a.n_pages) return;
+#pragma unroll
+        for (int k = 0; k < kScan; ++k)
+            r[k] = __builtin_bit_cast(i32x4_t, __builtin_amdgcn_raw_buffer_load_b128(refs, 4 * (p0 + 4 * lane + 256 * k), 0,
+                                                                                    kDeviceScope));
+    };
+    ask(0);
     int round = 0, head = 0, held = 0, cursor = 0, turn = 0;  // (head, held) of s_free; pages before `cursor` have been looked at
     for (int b0 = 0; b0 < a.n_seqs; b0 += kBookThreads) {
         if (b0 || !early) {
@@ -328,12 +341,8 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
             while (held < wanted && cursor < a.n_pages) {
                 const int p0 = cursor + wave * kWavePages + 4 * lane, room = kFreeHeld - held;
                 int free = 0, at[kScan];
-                i32x4_t r[kScan];
+                if (cursor) ask(cursor);
                 if (p0 - 4 * lane < a.n_pages) {
-#pragma unroll
-                    for (int k = 0; k < kScan; ++k)
-                        r[k] = __builtin_bit_cast(
-                            i32x4_t, __builtin_amdgcn_raw_buffer_load_b128(refs, 4 * (p0 + 256 * k), 0, kDeviceScope));
 #pragma unroll
                     for (int k = 0; k < kScan; ++k) {
                         int mine = 0;

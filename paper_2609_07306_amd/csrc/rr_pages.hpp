@@ -33,6 +33,7 @@ struct PagesArgs {
     int32_t heads;     // of a page
     int32_t row_bytes; // of a token of a head
     PageDiv pd;
+    PageDiv row;  // quotients by max_pages
     uint32_t *counter;  // workspace: finished workgroups, 0 between calls;
     int32_t *n_copies;  // copies to make ...
     PageCopy *copies;   // ... [n_pages]
