@@ -480,7 +480,7 @@ def _empty(shape, dtype, like, stream, zeros=False):
     if stream is not None:
         with torch.cuda.stream(stream):
             return _empty(shape, dtype, like, None, zeros)
-    return (torch.zeros if zeros else torch.empty)(shape, dtype=dtype, device=like.device)
+    return (like.new_zeros if zeros else like.new_empty)(shape, dtype=dtype)
 
 
 def _of(name, t, shape, dtype):
