@@ -301,7 +301,7 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
                                                                                     kDeviceScope));
     };
     ask(0);
-    int round = 0, head = 0, held = 0, cursor = 0, turn = 0;  // (head, held) of s_free; pages before `cursor` have been looked at
+    int round = 0, head = 0, held = 0, cursor = 0;  // (head, held) of s_free; pages before `cursor` have been looked at
     for (int b0 = 0; b0 < a.n_seqs; b0 += kBookThreads) {
         if (b0 || !early) {
             items = lay_out(b0);
@@ -357,8 +357,7 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
                     }
                 }
                 int all;
-                const int before = waves_before(free, s_wave[turn], &all);
-                turn ^= 1;
+                const int before = waves_before(free, s_wave[0], &all);  // (others may still read s_wave[1])
                 if (free) {
 #pragma unroll
                     for (int k = 0; k < kScan; ++k) {
