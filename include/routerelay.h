@@ -592,7 +592,7 @@ size_t rr_pages_workspace_bytes(int32_t n_pages);
  *   pools   host array of n_pools device pointers, 16-byte aligned
  * Returns RR_ERR_INVALID for bad sizes, types, NULL or unaligned pointers or a
  * workspace too small, RR_ERR_UNSUPPORTED for pages of more than 2^30 bytes, or
- * where n_seqs * max_pages comes to 2^31. */
+ * where n_seqs * max_pages comes to 2^30. */
 rr_status rr_cache_resize(const rr_pages_config *cfg, void *const *pools, const int32_t *new_tokens, const int32_t *lengths,
                           int32_t *page_table, int32_t *refs, int32_t *missing, void *workspace, size_t workspace_bytes,
                           void *hip_stream);

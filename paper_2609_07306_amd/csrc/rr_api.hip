@@ -1262,7 +1262,8 @@ rr_status pages_args(const rr_pages_config *cfg, void *const *pools, int32_t *pa
     const int64_t row_bytes = (int64_t)c.d * (c.cache_dtype == RR_F32 ? 4 : c.cache_dtype == RR_BF16 ? 2 : 1);
     if (c.n_kv_heads > (1 << 30) / row_bytes / c.page)
         return fail(RR_ERR_UNSUPPORTED, "a page must be at most 2^30 bytes");
-    if ((int64_t)c.n_seqs * c.max_pages > INT32_MAX) return fail(RR_ERR_UNSUPPORTED, "n_seqs * max_pages must be below 2^31");
+    // (rounds of entries are counted in 32 bits)
+    if ((int64_t)c.n_seqs * c.max_pages >= 1 << 30) return fail(RR_ERR_UNSUPPORTED, "n_seqs * max_pages must be below 2^30");
     if (!pools || !page_table || !refs || !workspace)
         return fail(RR_ERR_INVALID, "pools, page_table, refs and workspace must be pointers");
     for (int i = 0; i < c.n_pools; ++i)

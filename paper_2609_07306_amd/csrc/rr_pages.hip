@@ -253,7 +253,7 @@ __global__ __launch_bounds__(kBookThreads) void resize_kernel(PagesArgs a)
 
 #pragma unroll
     for (int j = 0; j < kEntriesEach; ++j) {
-        const uint32_t x = (blockIdx.x * kEntriesEach + j) * kBookThreads + tid;  // (a table has less than 2^31 entries)
+        const uint32_t x = (blockIdx.x * kEntriesEach + j) * kBookThreads + tid;  // (a table has less than 2^30 entries)
         if (x >= (uint32_t)(a.n_seqs * a.max_pages)) continue;
         const int b = a.row.div((int)x), c = (int)x - b * a.max_pages;
         const int e = pool_page(a.table[x], a.n_pages);

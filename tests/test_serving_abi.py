@@ -113,6 +113,16 @@ def test_resize_and_compact_refuse(compact, kw, status):
     assert rr.lib.rr_last_error()
 
 
+@pytest.mark.parametrize("compact", [False, True])
+def test_tables_past_the_count_of_rounds(compact):
+    """Entries are counted on in rounds of 1024, in 32 bits: the largest tables
+    that 31 bits hold leave that count no room."""
+    rr = _rr()
+    for n_seqs, max_pages in ((1 << 16, 1 << 14), (2 ** 31 - 1, 1), (127, 2 ** 24)):
+        assert _pages_call(rr, compact, n_seqs=n_seqs, max_pages=max_pages, page=1) == -5
+        assert b"2^30" in rr.lib.rr_last_error()
+
+
 def test_pages_workspace():
     rr = _rr()
     assert _pages_call(rr, False, lengths=None) == -1
