@@ -437,7 +437,7 @@ rr_status rr_cache_append_axes(const rr_append_config *cfg, const void *K, const
                                void *hip_stream);
 
 typedef struct {
-    int32_t n_heads;
+    int32_t n_heads;      /* below 2^24 */
     int32_t n_tokens;     /* (0: nothing to do), below 2^24 */
     int32_t d;            /* a multiple of 8, at most 1024 */
     int32_t rot;          /* leading features that are rotated: even, 0 .. d */
@@ -457,7 +457,7 @@ typedef struct {
  * = d.  With inverse = 1 rows are turned back, which is also the gradient of
  * the rotation.  Y may be X where its strides are X's, and must not overlap it
  * otherwise.  Returns RR_ERR_INVALID for bad sizes, types, strides or NULL
- * pointers, RR_ERR_UNSUPPORTED for 2^24 tokens or more. */
+ * pointers, RR_ERR_UNSUPPORTED for 2^24 tokens or heads or more. */
 rr_status rr_rotate(const rr_rotate_config *cfg, const void *X, const double *freqs, const rr_axes *axes, void *Y,
                     void *hip_stream);
 

@@ -1179,6 +1179,7 @@ rr_status rr_rotate(const rr_rotate_config *cfg, const void *X, const double *fr
     if (!cfg) return fail(RR_ERR_INVALID, "config is NULL");
     const rr_rotate_config &c = *cfg;
     if (c.n_heads < 1) return fail(RR_ERR_INVALID, "n_heads must be >= 1");
+    if (c.n_heads > kMostGroups) return fail(RR_ERR_UNSUPPORTED, "n_heads must be below 2^24");
     if (c.n_tokens < 0) return fail(RR_ERR_INVALID, "n_tokens must be >= 0");
     if (c.n_tokens > kMostGroups) return fail(RR_ERR_UNSUPPORTED, "n_tokens must be below 2^24");
     if (c.d < 8 || c.d > 1024 || c.d % 8 != 0) return fail(RR_ERR_INVALID, "d must be a multiple of 8 in [8, 1024]");

@@ -53,6 +53,14 @@ def test_rotate_refuses(kw, status):
     assert status == 0 or rr.lib.rr_last_error()
 
 
+def test_rotate_of_too_many_heads():
+    """(shares of them are rounded up in 32 bits)"""
+    rr = _rr()
+    for heads in (1 << 24, 2 ** 31 - 1):
+        assert _rotate(rr, n_heads=heads, x_head=0) == -5
+        assert b"n_heads" in rr.lib.rr_last_error()
+
+
 @pytest.mark.parametrize("kw", [{"n_axes": 0}, {"n_axes": -3}, {"real": 2}, {"positions": None}])
 def test_bad_axes(kw):
     rr = _rr()
