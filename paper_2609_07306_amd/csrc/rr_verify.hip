@@ -59,11 +59,32 @@ struct Row {
     }
 };
 
+// By data-parallel moves; a lane that nothing comes to gets 0.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double x)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// Sums over lanes 0 .. this one.
+__device__ __forceinline__ double wave_up_to(double x)
+{
+    x += moved<0x111, 0xf>(x);  // from 1, 2, 4 and 8 lanes before, of the row of 16
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    x += moved<0x118, 0xf>(x);
+    x += moved<0x142, 0xa>(x);         // row 0 to row 1, row 2 to row 3
+    return x + moved<0x143, 0xc>(x);   // the first two rows to the others
+}
+
 __device__ __forceinline__ double wave_sum(double x)
 {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o, 64);
-    return x;
+    const uint64_t b = __builtin_bit_cast(uint64_t, wave_up_to(x));
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, 63), hi = __builtin_amdgcn_readlane((int)(b >> 32), 63);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
 // Sums of x over the threads before this one, and over all of them; s_wave is
@@ -71,13 +92,7 @@ __device__ __forceinline__ double wave_sum(double x)
 __device__ __forceinline__ double block_before(double x, double *s_wave, double *all)
 {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    double to = x;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const double y = __shfl_up(to, o, 64);
-        if (lane >= o) to += y;
-    }
-    const double before = __shfl_up(to, 1, 64);
+    const double to = wave_up_to(x), before = moved<0x138, 0xf>(to);  // (the lane before's)
     if (lane == 63) s_wave[w] = to;
     __syncthreads();
     double base = 0.0, sum = 0.0;
@@ -87,7 +102,7 @@ __device__ __forceinline__ double block_before(double x, double *s_wave, double 
         sum += s_wave[i];
     }
     *all = sum;
-    return base + (lane ? before : 0.0);
+    return base + before;
 }
 
 // A lane's elements of a part of STEPS steps, as they lie in memory.
