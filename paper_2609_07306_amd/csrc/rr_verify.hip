@@ -14,10 +14,10 @@
 // are not read).  A row is split into parts, one or several a wave, that sum r;
 // the workgroup of a sequence that comes last finds the part in which the border
 // lies and reads that part again.  192 sequences of five drafts over 131072
-// tokens, binary32 (182 MB): 40 us, 4.5 TB/s.  What is missing to the 6.5 that
+// tokens, binary32 (182 MB): 38.6 us, 4.7 TB/s; bf16 25.  What is missing to the 6.5 that
 // reads reach are a chain of loads before the first sum (draft, probability, row:
 // about 4 us) and one after the last (counter, sums, part: about 5), which all
-// sequences meet at once; one sequence over 32000 tokens is these chains, 6.7 us.
+// sequences meet at once; one sequence over 32000 tokens is these chains, 6.1 us.
 #include <hip/hip_runtime.h>
 
 #include "rr_device.hpp"
@@ -222,6 +222,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
     // this wave's parts, of which the next is asked for before one is summed
     constexpr int kPart = STEPS * Some<T>::STEP, kEach = kPart / kVerifyThreads;
     double *sums = a.sums + (int64_t)b * a.n_parts;
+    uint32_t *counter = a.counters + b * kVerifyApart;
     const int own = (blockIdx.x * kVerifyWaves + wave) * a.each, end = min(own + a.each, a.n_parts);
     Held<T, STEPS> held, next;
     if (own < end) ask(row, own * kPart, held);
@@ -234,9 +235,9 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
     wait_vm();        // this wave's sums have been stored ...
     __syncthreads();  // ... and the other waves'
     if (tid == 0) {
-        const uint32_t before = __hip_atomic_fetch_add(a.counters + b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         s_last = before == gridDim.x - 1;
-        if (s_last) __hip_atomic_store(a.counters + b, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (s_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
     if (!s_last) return;
@@ -314,9 +315,9 @@ void verify_schedule(VerifyArgs &a, int dtype)
     // border's with one sum a thread; a wave takes as many, a power of two, as
     // leave some 4096 waves, four a SIMD.  (Fewer parts a wave are more chains of
     // loads -- draft, probability, row -- before the first sum, and more counters
-    // to add to; four steps take registers that leave two waves.  192 sequences,
-    // 131072 tokens, binary32, steps and parts: 2 and 8 42 us, 2 and 4 44, 4 and 8
-    // 43, 1 and 8 47, 4 and 1 61.)
+    // to add to; four steps take registers that leave five waves.  192 sequences,
+    // 131072 tokens, two steps: binary32 in 8 parts a wave 38.7 us, 4 37.7, 16 38.9;
+    // bf16 in 4 25.2, 2 27.5, 8 26.5; one step 41.2 and 25.2.)
     const int step = dtype == 0 ? Some<float>::STEP : Some<__bf16>::STEP;
     a.steps = 1;
     while (a.steps < 4 && a.vocab > kVerifyThreads * a.steps * step) a.steps *= 2;

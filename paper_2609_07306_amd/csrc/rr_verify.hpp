@@ -7,8 +7,11 @@
 
 namespace rr {
 
-constexpr int kVerifySeqs = 16384;  // sequences of a launch: each has a counter
-constexpr size_t kVerifyCounterBytes = kVerifySeqs * sizeof(uint32_t);
+// Sequences of a launch: each has a counter, in 64 bytes of its own (those of one
+// line are added to one after the other: 32 sequences in 32 workgroups each 15.7
+// us side by side, 7.9 so).
+constexpr int kVerifySeqs = 1024, kVerifyApart = 16;
+constexpr size_t kVerifyCounterBytes = kVerifySeqs * kVerifyApart * sizeof(uint32_t);
 
 struct VerifyArgs {
     const void *P, *Q;  // [B, n + 1, V] and [B, n, V] with strides; Q or null
@@ -21,7 +24,7 @@ struct VerifyArgs {
     int32_t steps;    // of a part of a row
     int32_t n_parts;  // of a row
     int32_t each;     // parts of a wave
-    uint32_t *counters;  // [n_seqs] finished workgroups, 0 between calls
+    uint32_t *counters;  // [n_seqs] kVerifyApart apart, finished workgroups, 0 between calls
     double *sums;        // [n_seqs, n_parts]
 };
 
