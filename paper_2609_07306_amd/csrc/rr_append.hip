@@ -9,17 +9,19 @@
 // to a fraction of a turn in binary64, and its sine and cosine are taken once
 // a token and shared by all of its heads through LDS.
 //
-// Measured: 32768 tokens of that size in 143 us, 5.6 TB/s read and written (a
+// Measured: 32768 tokens of that size in 135 us, 5.8 TB/s read and written (a
 // copy of 1 GiB: 5.1); 22600 tokens of ragged prompts into an 8-bit cache, rotated
-// by axes, 119 (3.4 TB/s: chains of loads -- start, length, page -- and vector
-// instructions, half of a SIMD's time each).  Small calls are a chain and the
-// launch: one token 3.1 us, 64 by axes 4.4, 192 tokens of as many sequences into an
-// 8-bit cache 4.8, 24 ragged binary32 prompts (3147 tokens, 16 MB) 8.0.
+// by axes, 90 (5.6 TB/s).  Small calls are a chain of loads -- start, length, page
+// -- and the launch: one token 2.6 us, 64 by axes 3.9, 192 tokens of as many
+// sequences into an 8-bit cache 4.4, 24 ragged binary32 prompts (3147 tokens, 16
+// MB) 7.2.
 //
 // A workgroup takes a token.  A thread keeps the same features of a row over
 // the heads that it goes through, so it reads its sines and cosines once; a
-// vector piece is 8 or 16 bytes of input (an element, or two interleaved ones,
-// where rows are not aligned to that).
+// piece is 16 bytes of input (an element, or two interleaved ones, where rows
+// are not aligned to that).  What hides the chain are many waves and rows that
+// are asked for before it: a kernel of 44 to 66 registers and pieces of 16 bytes
+// takes 98 us for the ragged prompts where one of 87 and pieces of 8 took 121.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -34,6 +36,8 @@ namespace {
 
 constexpr int kAppendThreads = 256;
 constexpr int kMostRot = 1024;
+constexpr int kAhead = 2;              // rows that a thread asks for first
+constexpr int64_t kCaches = 32 << 20;  // bytes of the XCDs' caches together
 
 // x / scale, correctly rounded, for many x: with r the correctly rounded 1 /
 // scale, q = x r is off by an ulp at most, x - q scale is exact, and q + (x - q
@@ -91,13 +95,37 @@ __device__ __forceinline__ void write_e4m3(uint8_t *p, const float (&x)[N], cons
     }
 }
 
-template <typename T, bool E4, int N, bool VEC>
+// Pieces of rows, past the caches (ONCE) or not.
+template <typename T, int N, bool VEC, bool ONCE>
+__device__ __forceinline__ typename Raw<T, N>::V read_input(const T *p)
+{
+    if constexpr (ONCE)
+        return __builtin_nontemporal_load(reinterpret_cast<const typename Raw<T, N>::V *>(p));
+    else
+        return read_raw<T, N, VEC>(p);
+}
+
+template <typename T, int N, bool VEC, bool ONCE>
+__device__ __forceinline__ void write_output(T *p, const float (&x)[N])
+{
+    if constexpr (ONCE) {
+        typename Piece<T, N>::V v;
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = (T)x[e];
+        __builtin_nontemporal_store(v, reinterpret_cast<typename Piece<T, N>::V *>(p));
+    } else {
+        write_piece<T, N, VEC>(p, x);
+    }
+}
+
+// (8-bit rows are written in parts of lines, which the caches put together)
+template <typename T, bool E4, int N, bool VEC, bool ONCE>
 __device__ __forceinline__ void write_cache(void *pool, int64_t at, const float (&x)[N], const Quotient &over)
 {
     if constexpr (E4)
         write_e4m3<N, VEC>(static_cast<uint8_t *>(pool) + at, x, over);
     else
-        write_piece<T, N, VEC>(static_cast<T *>(pool) + at, x);
+        write_output<T, N, VEC, ONCE>(static_cast<T *>(pool) + at, x);
 }
 
 // The same number, in a vector register.
@@ -120,9 +148,10 @@ __device__ __forceinline__ int find_sequence(const int32_t *start, int n_seqs, i
 }
 
 // AXES: rotated by the token's positions on several axes, not by its place in the
-// sequence.  AHEAD: the first rows of a thread (up to AHEAD of them) and its
-// first values are asked for before the token's place is known.
-template <typename T, bool E4, bool INTER, int N, bool VEC, bool AXES, int AHEAD>
+// sequence.  ONCE: past the caches.  The first rows of a thread and its first
+// values are asked for before the token's place is known (one token 2.6 us, none
+// ahead 3.1; ragged prompts into an 8-bit cache 98 and 113).
+template <typename T, bool E4, bool INTER, int N, bool VEC, bool AXES, bool ONCE>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
 {
     typedef typename Raw<T, N>::V V;
@@ -152,17 +181,17 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
         freq = a.freqs[tid];
         if (AXES) a.axes.of(tid, axis);
     }
-    V first_x[AHEAD + 1], first_y[AHEAD + 1], first_v;
+    V first_x[kAhead], first_y[kAhead], first_v;
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
+    for (int k = 0; k < kAhead; ++k) {
         const int r = r0 + k * rows_at_once;
         if (r < n_rows) {
             const T *src = row_at(r) + piece_at(u0);
-            first_x[k] = read_raw<T, N, VEC>(src);
-            if (!INTER && u0 < turned) first_y[k] = read_raw<T, N, VEC>(src + half);
+            first_x[k] = read_input<T, N, VEC, ONCE>(src);
+            if (!INTER && u0 < turned) first_y[k] = read_input<T, N, VEC, ONCE>(src + half);
         }
     }
-    if (AHEAD && tid < n_values) first_v = read_raw<T, N, VEC>(value_at(tid));
+    if (tid < n_values) first_v = read_input<T, N, VEC, ONCE>(value_at(tid));
 
     double at[1];
     if (AXES && tid < half) a.axes.at(i, axis, at);
@@ -212,15 +241,15 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
         if (key) {
             const int64_t at = at0 + r * head;
             const Quotient over(E4 ? a.k_scale[r] : 1.f);
-            write_cache<T, E4, N, VEC>(a.Kc, at + f0, x, over);
-            if (!INTER && turn) write_cache<T, E4, N, VEC>(a.Kc, at + f1, y, over);
+            write_cache<T, E4, N, VEC, ONCE>(a.Kc, at + f0, x, over);
+            if (!INTER && turn) write_cache<T, E4, N, VEC, ONCE>(a.Kc, at + f1, y, over);
         } else {
             T *dst = static_cast<T *>(a.Q_out) + (i * a.n_heads + (r - a.n_kv_heads)) * a.d;
-            write_piece<T, N, VEC>(dst + f0, x);
-            if (!INTER && turn) write_piece<T, N, VEC>(dst + f1, y);
+            write_output<T, N, VEC, ONCE>(dst + f0, x);
+            if (!INTER && turn) write_output<T, N, VEC, ONCE>(dst + f1, y);
         }
     };
-    for (int u = u0; u < units; u += lanes) {
+    auto put_rows = [&](int u, auto first) {
         const bool turn = u < turned;
         const int f0 = piece_at(u);
         float c[NT], s[NT];
@@ -232,25 +261,30 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
             }
         }
         int r = r0;
-        if (u == u0) {
+        if constexpr (decltype(first)::value) {
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k, r += rows_at_once)
+            for (int k = 0; k < kAhead; ++k, r += rows_at_once)
                 if (r < n_rows) put_row(r, u, c, s, first_x[k], first_y[k]);
         }
         for (; r < n_rows; r += rows_at_once) {
             const T *src = row_at(r) + f0;
-            V x = read_raw<T, N, VEC>(src), y = x;
-            if (!INTER && turn) y = read_raw<T, N, VEC>(src + half);
+            V x = read_input<T, N, VEC, ONCE>(src), y = x;
+            if (!INTER && turn) y = read_input<T, N, VEC, ONCE>(src + half);
             put_row(r, u, c, s, x, y);
         }
-    }
+    };
+    put_rows(u0, std::true_type());
+    // (a row has no more than 256 vectors, and a loop over them would cost the
+    // registers of three waves: ragged prompts 121 us against 109)
+    if constexpr (!VEC)
+        for (int u = u0 + lanes; u < units; u += lanes) put_rows(u, std::false_type());
     // values
     if (phys < 0) return;
     for (int x = tid; x < n_values; x += kAppendThreads) {
         const int r = a.pieces.div(x), f = (x - r * a.pieces.page) * N;
         float v[N];
-        widen_piece<T, N>(AHEAD && x == tid ? first_v : read_raw<T, N, VEC>(value_at(x)), v);
-        write_cache<T, E4, N, VEC>(a.Vc, at0 + r * head + f, v, Quotient(E4 ? a.v_scale[r] : 1.f));
+        widen_piece<T, N>(x == tid ? first_v : read_input<T, N, VEC, ONCE>(value_at(x)), v);
+        write_cache<T, E4, N, VEC, ONCE>(a.Vc, at0 + r * head + f, v, Quotient(E4 ? a.v_scale[r] : 1.f));
     }
 }
 
@@ -274,37 +308,35 @@ hipError_t launch_append(const AppendArgs &a, int dtype, int cache, bool interle
         b.pieces = page_div(a.d / n);
         hipLaunchKernelGGL(kern, dim3((unsigned)a.n_tokens), dim3(kAppendThreads), 0, stream, b);
     };
-    // Rows are asked for before their place is known (one token 3.8 -> 3.1 us on the
-    // device, 192 into an 8-bit cache 5.7 -> 4.8).  In pieces of 8 bytes, which leave
-    // registers for more waves than those of 16 (22600 tokens of ragged prompts into
-    // an 8-bit cache 152 -> 119 us; 128 in those of 16).  Not so for large calls of a
-    // bf16 cache by place, whose angles cost little: 32768 tokens 144 us as they
-    // come, in pieces of 16 bytes, 148 so; by axes 161 and 156.
-    const bool ahead = a.n_tokens < 4096;
-    auto any = [&](auto type, auto e4, auto width, auto axes, auto rows) {
+    // What is written does not stay in the caches until it is read: past them, and
+    // what is read too.  (Measured alone, calls of a few MB gain as well: but what
+    // they write is read soon.  4500 tokens by axes, heads as above: e4m3 21.2 us
+    // against 24.8, bf16 22.0 and 26.7, binary32 of half the heads 23.1 and 26.7;
+    // 32768 by place, bf16, 135 and 143; the ragged prompts 90 and 98.)
+    const int64_t bytes = a.n_tokens * (int64_t)a.d *
+                          (size * (a.Q ? a.n_heads : 0) + (cache == CACHE_E4M3 ? 1 : size) * 2 * (int64_t)a.n_kv_heads);
+    const bool once = vec && bytes > kCaches;
+    auto any = [&](auto type, auto e4, auto axes) {
         typedef decltype(type) T;
         constexpr bool E4 = decltype(e4)::value, AX = decltype(axes)::value;
-        constexpr int W = decltype(width)::value, A = decltype(rows)::value;
-        if (vec)
-            interleaved ? go(append_kernel<T, E4, true, W, true, AX, A>, W) : go(append_kernel<T, E4, false, W, true, AX, A>, W);
+        constexpr int W = 16 / sizeof(T);
+        if (once)
+            interleaved ? go(append_kernel<T, E4, true, W, true, AX, true>, W)
+                        : go(append_kernel<T, E4, false, W, true, AX, true>, W);
+        else if (vec)
+            interleaved ? go(append_kernel<T, E4, true, W, true, AX, false>, W)
+                        : go(append_kernel<T, E4, false, W, true, AX, false>, W);
         else  // (interleaved partners go together)
-            interleaved ? go(append_kernel<T, E4, true, 2, false, AX, A>, 2) : go(append_kernel<T, E4, false, 1, false, AX, A>, 1);
+            interleaved ? go(append_kernel<T, E4, true, 2, false, AX, false>, 2)
+                        : go(append_kernel<T, E4, false, 1, false, AX, false>, 1);
     };
-    typedef std::integral_constant<int, 0> Zero;
-    typedef std::integral_constant<int, 2> Two;
-    typedef std::integral_constant<int, 3> Three;
-    typedef std::integral_constant<int, 4> Four;
-    typedef std::integral_constant<int, 8> Eight;
     auto types = [&](auto axes) {
-        constexpr bool AX = decltype(axes)::value;
         if (dtype == 0)
-            any(float(), std::false_type(), Four(), axes, Two());
+            any(float(), std::false_type(), axes);
         else if (cache == CACHE_E4M3)
-            any(__bf16(), std::true_type(), Four(), axes, Three());
-        else if (AX || ahead)
-            any(__bf16(), std::false_type(), Four(), axes, Three());
-        else if constexpr (!AX)
-            any(__bf16(), std::false_type(), Eight(), axes, Zero());
+            any(__bf16(), std::true_type(), axes);
+        else
+            any(__bf16(), std::false_type(), axes);
     };
     a.axes.positions ? types(std::true_type()) : types(std::false_type());
     return hipGetLastError();
