@@ -579,15 +579,21 @@ constexpr int kCopyThreads = 256;
 // 125.  Copies of a page that several sequences share read it again, from the
 // caches; most calls have none to make, and fewer workgroups are sooner through
 // (an empty launch of 4096 takes 2.3 us, of 8192 3.9): half a page of 16 pools,
-// three times each for 32 groups (31 MB read, 92 written), in 28 us, 4.4 TB/s;
-// with stores through the caches 49, four pieces a thread 31.
+// three times each for 32 groups (31 MB read, 92 written), in 23.5 us, 5.2 TB/s;
+// with stores through the caches some 20 more.  Units of a page are an odd number
+// (kOdd): where a page is copied in part, the units of its end have nothing to do,
+// and an even number would leave them to the same XCDs page after page (four
+// units 27.7 us).  Small pages take fewer pieces a thread, which need no more
+// registers than leave five waves (2 KB in 8 pools: 4.5 us, eight pieces 7.5).
 struct Moved {
-    static constexpr int kEach = 2, kGroups = 16384;  // pieces of a thread's turn
+    static constexpr int kEach = 2, kEachSmall = 2, kGroups = 16384;  // pieces of a thread's turn
     static constexpr bool kOnce = true;
+    static constexpr uint32_t kOdd = 0;
 };
 struct Shared {
-    static constexpr int kEach = 8, kGroups = 4096;
+    static constexpr int kEach = 8, kEachSmall = 4, kGroups = 4096;
     static constexpr bool kOnce = false;
+    static constexpr uint32_t kOdd = 1;
 };
 
 // Pages of all pools, a piece (a vector P) at a time.  A unit of a workgroup's
@@ -611,11 +617,11 @@ __global__ __launch_bounds__(kCopyThreads) void copies_kernel(PagesArgs a, Pools
         if (a.rank && n_entries)
             for (int k = first; k < *a.n_copies; k += all) settle(a, a.copies[k].src, a.copies[k].dst);
     }
-    constexpr int kEach = How::kEach, kCopyUnit = kEach * kCopyThreads;
+    constexpr int kEach = SMALL ? How::kEachSmall : How::kEach, kCopyUnit = kEach * kCopyThreads;
     const uint32_t pairs = (uint32_t)*a.n_copies * n_pools;
     const uint32_t row = a.row_bytes / sizeof(P), head = a.pd.page * row;  // pieces of a token of a head, of a head's page
     const uint32_t page = a.heads * head;
-    const uint32_t each = SMALL ? kCopyUnit / page : (page + kCopyUnit - 1) / kCopyUnit;  // pages a unit; units a page
+    const uint32_t each = SMALL ? kCopyUnit / page : (page + kCopyUnit - 1) / kCopyUnit | How::kOdd;  // pages a unit; units a page
     const uint32_t units = SMALL ? (pairs + each - 1) / each : pairs * each;
     for (uint32_t t = blockIdx.x; t < units; t += gridDim.x) {
         P v[kEach], *to[kEach];
@@ -692,16 +698,18 @@ template <typename How>
 hipError_t copy_pages(const PagesArgs &a, void *const *list, int n, int64_t most_copies, hipStream_t stream)
 {
     // (rows of 8 features are 8 bytes in e4m3)
-    const int piece = a.row_bytes % 16 == 0 ? 16 : 8, unit = How::kEach * kCopyThreads;
+    const int piece = a.row_bytes % 16 == 0 ? 16 : 8;
     const int64_t page = (int64_t)a.heads * a.pd.page * (a.row_bytes / piece);
-    const int64_t most = (int64_t)INT32_MAX / (a.n_pages * ((page + unit - 1) / unit));
+    const bool small = page <= How::kEachSmall * kCopyThreads / 2;
+    const int unit = (small ? How::kEachSmall : How::kEach) * kCopyThreads;
+    const int64_t each = small ? unit / page : (page + unit - 1) / unit | How::kOdd;  // as in the kernel
+    const int64_t most = (int64_t)INT32_MAX / (a.n_pages * (small ? 1 : each));
     const int at_once = (int)(most < 1 ? 1 : most < kPoolsAtOnce ? most : kPoolsAtOnce);
     for (int i0 = 0; i0 < n; i0 += at_once) {
         const int some = n - i0 < at_once ? n - i0 : at_once;
         Pools pools{};
         for (int i = 0; i < some; ++i) pools.p[i] = list[i0 + i];
-        const bool small = page <= unit / 2;
-        const int64_t units = small ? most_copies * some / (unit / page) + 1 : most_copies * some * ((page + unit - 1) / unit);
+        const int64_t units = small ? most_copies * some / each + 1 : most_copies * some * each;
         const int64_t entries = How::kOnce && i0 == 0 ? (int64_t)a.n_seqs * a.max_pages : 0, turns = entries / kCopyThreads + 1;
         const int64_t wanted = units > turns ? units : turns;
         const int groups = (int)(wanted < How::kGroups ? wanted : How::kGroups);
