@@ -320,3 +320,58 @@ def test_profiled_kinds_of_these_calls():
     got = {k: n for k, (ms, n) in rr.profile_stop().items() if n}
     join = got.pop("join", 0)
     assert got == {"append": LAYERS, "paged": LAYERS, "verify": 1, "pages": 3, "copy": 2, "rotate": 1} and join <= LAYERS
+
+
+@pytest.mark.parametrize("heads,kv,d,rot", [(32, 8, 128, 128), (24, 4, 160, 96), (5, 3, 1024, 1024), (6, 2, 1024, 0),
+                                            (40, 1, 72, 48)])
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("by_axes", [False, True])
+def test_large_appends_are_small_ones(heads, kv, d, rot, dtype, cache, inter, by_axes):
+    """A call that writes more than the caches hold goes past them: every bit as a
+    call for each sequence gives it, in place too; behind the last sequence and
+    beyond the table nothing is written."""
+    rr = rrmod()
+    note("append large", heads, kv, d, rot, dtype, cache, inter, by_axes)
+    T = {"f32": torch.float32, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}
+    g = torch.Generator(device=DEV).manual_seed(heads + d)
+    token = d * (heads * T[dtype].itemsize + 2 * kv * T[cache].itemsize)
+    # (the last sequence has some tokens beyond its pages, and some follow it)
+    n0 = 33 * (1 << 20) // token // 2 + 9
+    n, page = 2 * n0 + 40, 16
+    width = -(-(n0 + 30) // page)
+    beyond = n0 + 30 + 10 - width * page
+    start = torch.tensor([0, n0 + 10, 2 * n0 + 20], dtype=torch.int32, device=DEV)
+    lengths = torch.tensor([n0 + 17, n0 + 40], dtype=torch.int32, device=DEV)
+    table = torch.randperm(2 * width, generator=g, device=DEV).to(torch.int32).view(2, width)
+    qkv = torch.randn((n, heads + 2 * kv, d), generator=g, device=DEV).to(T[dtype])
+    Q, K, V = qkv[:, :heads], qkv[:, heads:heads + kv], qkv[:, heads + kv:]
+    scales = [torch.rand(kv, generator=g, device=DEV) + 0.1 for _ in range(2)] if cache == "e4m3" else [None, None]
+    freqs = 10000.0 ** (-torch.arange(rot // 2, dtype=torch.float64, device=DEV) / max(1, rot // 2))
+    positions = axis = None
+    if by_axes:
+        positions = torch.randint(0, 5000, (3, n), generator=g, device=DEV).to(torch.int32)
+        axis = torch.randint(0, 3, (rot // 2,), generator=g, device=DEV).to(torch.int32)
+    pools = [[torch.zeros((2 * width, kv, page, d), device=DEV).to(T[cache]) for _ in range(2)] for _ in range(2)]
+    outs = [torch.full((n, heads, d), 7.0, dtype=T[dtype], device=DEV) for _ in range(3)]
+    common = dict(freqs=freqs, interleaved=inter, k_scale=scales[0], v_scale=scales[1])
+    rr.cache_append(K, V, *pools[0], table, lengths, seq_start=start, Q=Q, Q_out=outs[0], positions=positions, axis=axis, **common)
+    step = n0 // 6
+    for b in range(2):
+        i0, i1 = int(start[b]), int(start[b + 1])
+        for i in range(i0, i1, step):
+            j = min(i + step, i1)
+            part = None if positions is None else positions[:, i:j].contiguous()
+            rr.cache_append(K[i:j], V[i:j], *pools[1], table[b:b + 1], lengths[b:b + 1] - (i1 - j), Q=Q[i:j],
+                            Q_out=outs[1][i:j], positions=part, axis=axis, **common)
+    bits = lambda t: t.view({1: torch.uint8, 2: torch.int16, 4: torch.int32}[t.element_size()])
+    assert torch.equal(bits(outs[0]), bits(outs[1]))
+    for a, b in zip(*pools):
+        assert torch.equal(bits(a), bits(b))
+    kept = int(start[2])
+    assert bool((outs[0][kept:] == 7.0).all()) and bool((outs[0][kept - max(0, beyond):kept] == 7.0).all())
+    assert float(outs[0][:kept - max(0, beyond)].float().std()) > 0.5
+    outs[2].copy_(Q)
+    rr.cache_append(K, V, *pools[1], table, lengths, seq_start=start, Q=outs[2], Q_out=outs[2], positions=positions, axis=axis,
+                    **common)
+    assert torch.equal(bits(outs[2][:kept - max(0, beyond)]), bits(outs[0][:kept - max(0, beyond)]))
