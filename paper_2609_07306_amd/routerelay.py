@@ -543,7 +543,7 @@ def _axes_of(positions, axis, rot, n):
     if kind not in (torch.int32, torch.float32):
         raise TypeError("positions must be int32 or float32")
     shape = positions.shape
-    if shape[-1:] != (n,) or len(shape) > 2 or not shape[0]:
+    if not shape or shape[-1] != n or len(shape) > 2 or (len(shape) == 2 and not shape[0]):
         raise ValueError(f"positions must be [n_axes, {n}]: got {list(shape)}")
     if not positions.is_contiguous():
         raise ValueError("positions must be contiguous")

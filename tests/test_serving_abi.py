@@ -267,3 +267,18 @@ def test_profile_stop_fills_the_kinds_of_the_header_before():
         assert rr.lib.rr_profile_stop(ms, cnt, size) == -1
     assert rr.lib.rr_profile_stop(ms, cnt, 11) == 0
     assert list(ms) == [0.0] * 11 + [-7.0] * (n - 11) and list(cnt) == [0] * 11 + [-7] * (n - 11)
+
+
+@pytest.mark.parametrize("shape,n,fits", [((), 0, False), ((), 1, False), ((0,), 0, True), ((0,), 4, False), ((3, 0), 0, True),
+                                          ((0, 4), 4, False), ((4,), 4, True), ((3, 4), 4, True), ((4, 3), 4, False),
+                                          ((1, 3, 4), 4, False)])
+def test_shapes_of_positions(shape, n, fits):
+    """One axis without a dimension of its own, or some; no tokens are none to place."""
+    rr = _rr()
+    positions = torch.zeros(shape, dtype=torch.int32)
+    if fits:
+        axes = rr._axes_of(positions, None, 4, n)
+        assert axes.n_axes == (shape[0] if len(shape) == 2 else 1)
+    else:
+        with pytest.raises(ValueError, match="positions must be"):
+            rr._axes_of(positions, None, 4, n)
