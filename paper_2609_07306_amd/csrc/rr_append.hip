@@ -36,8 +36,7 @@ namespace {
 
 constexpr int kAppendThreads = 256;
 constexpr int kMostRot = 1024;
-constexpr int kAhead = 2;              // rows that a thread asks for first
-constexpr int64_t kCaches = 32 << 20;  // bytes of the XCDs' caches together
+constexpr int kAhead = 2;  // rows that a thread asks for first
 
 // x / scale, correctly rounded, for many x: with r the correctly rounded 1 /
 // scale, q = x r is off by an ulp at most, x - q scale is exact, and q + (x - q
@@ -308,14 +307,14 @@ hipError_t launch_append(const AppendArgs &a, int dtype, int cache, bool interle
         b.pieces = page_div(a.d / n);
         hipLaunchKernelGGL(kern, dim3((unsigned)a.n_tokens), dim3(kAppendThreads), 0, stream, b);
     };
-    // What is written does not stay in the caches until it is read: past them, and
-    // what is read too.  (Measured alone, calls of a few MB gain as well: but what
-    // they write is read soon.  4500 tokens by axes, heads as above: e4m3 21.2 us
-    // against 24.8, bf16 22.0 and 26.7, binary32 of half the heads 23.1 and 26.7;
-    // 32768 by place, bf16, 135 and 143; the ragged prompts 90 and 98.)
-    const int64_t bytes = a.n_tokens * (int64_t)a.d *
-                          (size * (a.Q ? a.n_heads : 0) + (cache == CACHE_E4M3 ? 1 : size) * 2 * (int64_t)a.n_kv_heads);
-    const bool once = vec && bytes > kCaches;
+    // What is read and written does not fit the last cache together: past the
+    // caches.  Between a call that writes the rows and one that reads the queries
+    // (bf16, heads as above, by place; append and reader, through the caches and
+    // past them): 8000 tokens 34 + 22 us and 33 + 27, 12000 52 + 49 and 48 + 37,
+    // 32768 147 + 106 and 144 + 95, into an 8-bit cache 133 + 104 and 118 + 99.
+    const int64_t rows = a.n_tokens * (int64_t)a.d, heads = a.Q ? a.n_heads : 0;
+    const int64_t bytes = rows * (size * 2 * (heads + a.n_kv_heads) + (cache == CACHE_E4M3 ? 1 : size) * 2 * (int64_t)a.n_kv_heads);
+    const bool once = vec && bytes >= kLastCache;
     auto any = [&](auto type, auto e4, auto axes) {
         typedef decltype(type) T;
         constexpr bool E4 = decltype(e4)::value, AX = decltype(axes)::value;

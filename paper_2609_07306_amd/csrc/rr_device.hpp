@@ -8,6 +8,8 @@
 
 namespace rr {
 
+constexpr int64_t kLastCache = 256 << 20;  // bytes of the cache before the memory, all XCDs'
+
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));

@@ -7,8 +7,8 @@
 // with a short stretch of its own, move 32768 tokens of 32 heads (128 bf16
 // features, 268 MB each way) in 92 us heads first and 89 tokens first, 5.8 and
 // 6.0 TB/s; a workgroup that takes 32 tokens of every head in turn in 122.  So
-// there is a kernel for each layout.  Loads and stores go past the caches.  A
-// small call (196 tokens, 6 heads) is a launch and a chain, 3.1 us.
+// there is a kernel for each layout.  Loads and stores of such calls go past the
+// caches.  A small call (196 tokens, 6 heads) is a launch and a chain, 3.1 us.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -188,10 +188,16 @@ hipError_t launch_rotate(const RotateArgs &args, int dtype, bool interleaved, hi
     const int n = dtype == 0 ? 4 : 8;
     const bool vec = ((reinterpret_cast<uintptr_t>(a.X) | reinterpret_cast<uintptr_t>(a.Y)) & 15) == 0 && a.x_token % n == 0 &&
                      a.x_head % n == 0 && a.y_token % n == 0 && a.y_head % n == 0 && a.rot % (interleaved ? n : 2 * n) == 0;
-    // Past the caches only what is read and written in whole lines of 128 bytes: a
-    // row of pairs of neighbours, or halves of that size.
+    // Past the caches what does not fit the last one, input and output together, so
+    // that a reader finds what is left there (between a call that writes the rows and
+    // one that reads them, bf16, 32 heads of 128, out of place, through the caches and
+    // past them: 12000 tokens 33 + 33 us and 33 + 37, 16384 46 + 57 and 44 + 49,
+    // 32768 99 + 103 and 100 + 95; in place 16384 44 + 40 and 43 + 49, 32768 86 + 113
+    // and 95 + 95), and only in whole lines of 128 bytes: a row of pairs of
+    // neighbours, or halves of that size.
     const int size = dtype == 0 ? 4 : 2;
     const bool lines = interleaved ? a.d * size % 128 == 0 : a.rot / 2 * size % 128 == 0 && (a.d - a.rot) * size % 128 == 0;
+    const bool once = lines && (int64_t)a.n_tokens * a.n_heads * a.d * size >= kLastCache / (a.X == a.Y ? 1 : 2);
     // which rows follow each other
     const bool by_token = a.n_heads > 1 && (a.n_tokens == 1 || a.y_head < a.y_token);
     auto go = [&](auto by_heads, auto by_tokens, Units un) {
@@ -240,7 +246,7 @@ hipError_t launch_rotate(const RotateArgs &args, int dtype, bool interleaved, hi
         if (!vec)  // (interleaved partners go together)
             interleaved ? ways(type, std::true_type(), std::integral_constant<int, 2>(), Each())
                         : ways(type, std::false_type(), std::integral_constant<int, 1>(), Each());
-        else if (lines)
+        else if (once)
             interleaved ? ways(type, std::true_type(), width, Once()) : ways(type, std::false_type(), width, Once());
         else
             interleaved ? ways(type, std::true_type(), width, Vec()) : ways(type, std::false_type(), width, Vec());

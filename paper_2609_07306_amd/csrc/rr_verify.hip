@@ -14,8 +14,8 @@
 // are not read).  A row is split into parts, one or several a wave, that sum r;
 // the workgroup of a sequence that comes last finds the part in which the border
 // lies and reads that part again.  192 sequences of five drafts over 131072
-// tokens, binary32 (182 MB): 38.6 us, 4.7 TB/s; bf16 25.  What is missing to the 6.5 that
-// reads reach are a chain of loads before the first sum (draft, probability, row:
+// tokens, binary32 (182 MB): 37 us, 4.9 TB/s; bf16 23.  What is missing to the 6.5
+// that reads reach are a chain of loads before the first sum (draft, probability, row:
 // about 4 us) and one after the last (counter, sums, part: about 5), which all
 // sequences meet at once; one sequence over 32000 tokens is these chains, 6.1 us.
 #include <hip/hip_runtime.h>
@@ -49,6 +49,7 @@ template <typename T>
 struct Row {
     const T *p, *q;
     int kind, draft, vocab;
+    bool once;  // read past the caches
 
     // Of v, which is in the vocabulary.  Not a positive finite number: nothing.
     __device__ __forceinline__ double weight(int v) const
@@ -117,13 +118,17 @@ __device__ __forceinline__ void ask(const Row<T> &row, int from, Held<T, STEPS> 
     typedef typename Some<T>::V V;
     if (from + STEPS * Some<T>::STEP > row.vocab) return;  // (the last part is read element by element)
     const int v = from + Some<T>::N * (threadIdx.x & 63);
-    // (past the caches: 45 us against 49 for 192 sequences' drafts)
+    auto read = [&](auto get) {
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        h.x[i] = __builtin_nontemporal_load(reinterpret_cast<const V *>(row.p + v + i * Some<T>::STEP));
-        if (row.kind == REST_DIFFERENCE)
-            h.y[i] = __builtin_nontemporal_load(reinterpret_cast<const V *>(row.q + v + i * Some<T>::STEP));
-    }
+        for (int i = 0; i < STEPS; ++i) {
+            h.x[i] = get(reinterpret_cast<const V *>(row.p + v + i * Some<T>::STEP));
+            if (row.kind == REST_DIFFERENCE) h.y[i] = get(reinterpret_cast<const V *>(row.q + v + i * Some<T>::STEP));
+        }
+    };
+    if (row.once)
+        read([](const V *p) { return __builtin_nontemporal_load(p); });
+    else
+        read([](const V *p) { return *p; });
 }
 
 // The sum of a part, of which `ask` has asked.  max(r, 0) is 0 for a NaN, and an
@@ -216,7 +221,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
             break;
         }
     }
-    Row<T> row{P + took * a.p_row, Q, took == count ? REST_TARGET : Q ? REST_DIFFERENCE : REST_WITHOUT, draft, a.vocab};
+    Row<T> row{P + took * a.p_row, Q, took == count ? REST_TARGET : Q ? REST_DIFFERENCE : REST_WITHOUT, draft, a.vocab, a.once};
     if (row.kind == REST_DIFFERENCE) row.q += took * a.q_row;
 
     // this wave's parts, of which the next is asked for before one is summed
@@ -338,6 +343,10 @@ hipError_t launch_verify(const VerifyArgs &args, int dtype, void *workspace, hip
     a.counters = static_cast<uint32_t *>(workspace);
     a.sums = reinterpret_cast<double *>(static_cast<char *>(workspace) + kVerifyCounterBytes);
     const size_t size = dtype == 0 ? 4 : 2;
+    // Past the caches what the last one has not kept of the call that wrote it (right
+    // behind that call, three drafts, binary32, 128 sequences of 64000: 21.0 us through
+    // the caches, 22.7 past them; 192 of 131072 and five drafts 42 and 37).
+    a.once = (double)a.n_seqs * (a.Q ? 2 * a.n + 1 : a.n + 1) * a.vocab * size >= (double)kLastCache;
     const int each = kVerifyWaves * a.each;
     const unsigned groups = (unsigned)((a.n_parts + each - 1) / each);
     // (as many sequences at a time as there are counters)

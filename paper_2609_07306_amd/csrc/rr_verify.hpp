@@ -24,6 +24,7 @@ struct VerifyArgs {
     int32_t steps;    // of a part of a row
     int32_t n_parts;  // of a row
     int32_t each;     // parts of a wave
+    bool once;        // rows are read past the caches
     uint32_t *counters;  // [n_seqs] kVerifyApart apart, finished workgroups, 0 between calls
     double *sums;        // [n_seqs, n_parts]
 };

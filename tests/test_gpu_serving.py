@@ -335,9 +335,9 @@ def test_large_appends_are_small_ones(heads, kv, d, rot, dtype, cache, inter, by
     note("append large", heads, kv, d, rot, dtype, cache, inter, by_axes)
     T = {"f32": torch.float32, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}
     g = torch.Generator(device=DEV).manual_seed(heads + d)
-    token = d * (heads * T[dtype].itemsize + 2 * kv * T[cache].itemsize)
+    token = 2 * d * ((heads + kv) * T[dtype].itemsize + kv * T[cache].itemsize)  # read and written
     # (the last sequence has some tokens beyond its pages, and some follow it)
-    n0 = 33 * (1 << 20) // token // 2 + 9
+    n0 = 260 * (1 << 20) // token // 2 + 9
     n, page = 2 * n0 + 40, 16
     width = -(-(n0 + 30) // page)
     beyond = n0 + 30 + 10 - width * page
