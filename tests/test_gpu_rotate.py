@@ -319,3 +319,31 @@ def test_values_of_an_8_bit_cache_are_quotients(scale):
         nan = K.isnan().cpu()
         assert torch.equal(got[~nan], y[~nan])
         assert bool(((got[nan] & 0x7f) == 0x7f).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens", [0, 1])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("heads,d,rot", [(17, 128, 128), (5, 256, 128), (3, 1024, 1024)])
+def test_large_rotations_are_small_ones(dtype, tokens, inter, heads, d, rot):
+    """What does not fit the last cache goes past it: every bit as a few tokens at a
+    time give it, in place too."""
+    rr = rrmod()
+    note("rotate large", dtype, tokens, inter, heads, d, rot)
+    g = torch.Generator(device=DEV).manual_seed(heads)
+    n = (260 << 20) // (heads * d * dtype.itemsize) + 3
+    shape = (n, heads, d) if tokens == 0 else (heads, n, d)
+    X = torch.randn(shape, generator=g, device=DEV).to(dtype)
+    positions = torch.randint(0, 9000, (2, n), generator=g, device=DEV).to(torch.int32)
+    axis = torch.randint(0, 2, (rot // 2,), generator=g, device=DEV).to(torch.int32)
+    freqs = 10000.0 ** (-torch.arange(rot // 2, dtype=torch.float64, device=DEV) / (rot // 2))
+    kw = dict(axis=axis, tokens=tokens, interleaved=inter)
+    whole = rr.rotate(X, positions, freqs, **kw)
+    parts = torch.empty_like(X)
+    step = n // 5 + 1
+    for i in range(0, n, step):
+        j = min(i + step, n)
+        rr.rotate(X.narrow(tokens, i, j - i), positions[:, i:j].contiguous(), freqs, out=parts.narrow(tokens, i, j - i), **kw)
+    assert torch.equal(whole, parts)
+    rr.rotate(X, positions, freqs, out=X, **kw)
+    assert torch.equal(whole, X)

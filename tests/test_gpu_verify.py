@@ -244,3 +244,22 @@ def test_rows_past_2_31_elements():
     want = rr.verify_drafts(P, drafts, u, draft_probs=Q)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     _check(rr, P[-2:], Q[-2:], drafts[-2:], u[-2:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("given", [True, False])
+def test_large_batches_are_small_ones(dtype, given):
+    """Probabilities that do not fit the last cache are read past it."""
+    rr = rrmod()
+    note("verify large", dtype, given)
+    n, V = 3, 50003
+    B = (270 << 20) // ((2 * n + 1 if given else n + 1) * V * (4 if dtype == "f32" else 2)) + 1
+    P, Q, drafts, u = _inputs(31, B, n, V, dtype)
+    Q = Q if given else None
+    accepted, tokens = rr.verify_drafts(P, drafts, u, draft_probs=Q)
+    step = B // 3 + 1
+    for i in range(0, B, step):
+        s = slice(i, min(i + step, B))
+        a, t = rr.verify_drafts(P[s], drafts[s], u[s], draft_probs=None if Q is None else Q[s])
+        assert torch.equal(a, accepted[s])
+        assert torch.equal(t, tokens[s])
