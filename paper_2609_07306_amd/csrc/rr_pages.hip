@@ -580,7 +580,8 @@ constexpr int kCopyThreads = 256;
 // caches; most calls have none to make, and fewer workgroups are sooner through
 // (an empty launch of 4096 takes 2.3 us, of 8192 3.9): half a page of 16 pools,
 // three times each for 32 groups (31 MB read, 92 written), in 23.5 us, 5.2 TB/s;
-// with stores through the caches some 20 more.  Units of a page are an odd number
+// with stores through the caches 30, and the attention that follows is no faster
+// (eight layers 828 us, 837 so).  Units of a page are an odd number
 // (kOdd): where a page is copied in part, the units of its end have nothing to do,
 // and an even number would leave them to the same XCDs page after page (four
 // units 27.7 us).  Small pages take fewer pieces a thread, which need no more
