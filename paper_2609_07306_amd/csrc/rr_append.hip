@@ -223,6 +223,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
             }
         }
         turn_of(AXES ? at[0] : (double)pos, freq, &s_cos[x], &s_sin[x]);
+        if (AXES && !a.axes.there(axis[0])) s_cos[x] = kStays;
     }
     __syncthreads();
 
@@ -235,7 +236,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
         widen_piece<T, N>(raw_x, x);
         if (turn) {
             if constexpr (!INTER) widen_piece<T, N>(raw_y, y);
-            turn_piece<INTER, N>(x, y, c, s);
+            turn_piece<INTER, N, AXES>(x, y, c, s);
         }
         if (key) {
             const int64_t at = at0 + r * head;

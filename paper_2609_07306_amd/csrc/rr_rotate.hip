@@ -111,7 +111,7 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_heads_kernel(RotateArgs
                 read_row<T, N, W>(src, next_x);
                 if (!INTER && turn) read_row<T, N, W>(src + half, next_y);
             }
-            if (turn) turn_piece<INTER, N>(x, y, c, s);
+            if (turn) turn_piece<INTER, N, true>(x, y, c, s);
             write_row<T, N, W>(dst, x);
             if (!INTER && turn) write_row<T, N, W>(dst + half, y);
         }
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_tokens_kernel(RotateArg
                     c[e] = s_cos[at + e];
                     s[e] = s_sin[at + e];
                 }
-                turn_piece<INTER, N>(x, y, c, s);
+                turn_piece<INTER, N, true>(x, y, c, s);
             }
             write_row<T, N, W>(dst, x);
             if (!INTER && turn) write_row<T, N, W>(dst + half, y);

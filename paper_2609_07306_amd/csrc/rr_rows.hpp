@@ -75,25 +75,29 @@ __device__ __forceinline__ void write_piece(T *p, const float (&x)[N])
 template <bool INTER, int N>
 constexpr int kTurns = INTER ? N / 2 : N;
 
+// The cosine, which no angle has, of a frequency whose axis is not there: its
+// partners stay as they are.  (Turned by an angle of 0, an infinite one would make
+// the other a NaN, and a -0 could lose its sign.)
+constexpr float kStays = 2.f;
+
 // Rotates a piece: neighbours are partners (INTER), or x's element e and y's.
-template <bool INTER, int N>
+// SOME: but for those that kStays stands for.
+template <bool INTER, int N, bool SOME>
 __device__ __forceinline__ void turn_piece(float (&x)[N], float (&y)[N], const float (&c)[kTurns<INTER, N>],
                                            const float (&s)[kTurns<INTER, N>])
 {
+    auto turn = [](float &x, float &y, float c, float s) {
+        const float p = x, q = y;
+        const bool stays = SOME && c == kStays;
+        x = stays ? p : p * c - q * s;
+        y = stays ? q : q * c + p * s;
+    };
     if constexpr (INTER) {
 #pragma unroll
-        for (int e = 0; e < N; e += 2) {
-            const float p = x[e], q = x[e + 1];
-            x[e] = p * c[e / 2] - q * s[e / 2];
-            x[e + 1] = q * c[e / 2] + p * s[e / 2];
-        }
+        for (int e = 0; e < N; e += 2) turn(x[e], x[e + 1], c[e / 2], s[e / 2]);
     } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float p = x[e], q = y[e];
-            x[e] = p * c[e] - q * s[e];
-            y[e] = q * c[e] + p * s[e];
-        }
+        for (int e = 0; e < N; ++e) turn(x[e], y[e], c[e], s[e]);
     }
 }
 
@@ -126,24 +130,21 @@ struct Axes {
         }
     }
 
-    // Token i's positions on axes t; 0, which rotates nothing, for an axis that is
-    // not there.
+    __device__ __forceinline__ bool there(int t) const { return (uint32_t)t < (uint32_t)n_axes; }
+
+    // Token i's positions on axes t; the first one's for an axis that is not there.
     template <int N>
     __device__ __forceinline__ void at(int64_t i, const int (&t)[N], double (&p)[N]) const
     {
         int32_t bits[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const bool there = (uint32_t)t[e] < (uint32_t)n_axes;
-            bits[e] = static_cast<const int32_t *>(positions)[(there ? t[e] : 0) * n + i];
-            if (!there) bits[e] = 0;
-        }
+        for (int e = 0; e < N; ++e) bits[e] = static_cast<const int32_t *>(positions)[(there(t[e]) ? t[e] : 0) * n + i];
 #pragma unroll
         for (int e = 0; e < N; ++e) p[e] = real ? (double)__int_as_float(bits[e]) : (double)bits[e];
     }
 };
 
-// Cosines and sines of token i for frequencies j .. j + N - 1.
+// Cosines (or kStays) and sines of token i for frequencies j .. j + N - 1.
 template <int N>
 __device__ __forceinline__ void turns_of(const Axes &axes, const double *freqs, int64_t i, int j, float (&c)[N], float (&s)[N])
 {
@@ -154,7 +155,10 @@ __device__ __forceinline__ void turns_of(const Axes &axes, const double *freqs, 
     for (int e = 0; e < N; ++e) f[e] = freqs[j + e];
     axes.at(i, t, p);
 #pragma unroll
-    for (int e = 0; e < N; ++e) turn_of(p[e], f[e], &c[e], &s[e]);
+    for (int e = 0; e < N; ++e) {
+        turn_of(p[e], f[e], &c[e], &s[e]);
+        if (!axes.there(t[e])) c[e] = kStays;
+    }
 }
 
 struct RotateArgs {

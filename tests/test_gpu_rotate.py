@@ -347,3 +347,91 @@ def test_large_rotations_are_small_ones(dtype, tokens, inter, heads, d, rot):
     assert torch.equal(whole, parts)
     rr.rotate(X, positions, freqs, out=X, **kw)
     assert torch.equal(whole, X)
+
+
+NOT_THERE = [2, 7, -1, 2 ** 31 - 1, -2 ** 31]
+
+
+def _without_axes(rng, half, n):
+    """Axes of frequencies, some of them not there, whose frequencies are whatever they are."""
+    axis = rng.integers(0, 2, half).astype(np.int32)
+    still = rng.random(half) < 0.5
+    still[:5] = True
+    axis[still] = rng.choice(NOT_THERE, int(still.sum()))
+    f = _freqs(half)
+    f[still] = rng.choice([np.nan, np.inf, -np.inf, 0.0, 1e300, 1.0], int(still.sum()))
+    return axis, f, still
+
+
+def _any_values(rng, shape, still, rot, inter, dtype):
+    """Rows that are ordinary but for the features that stay: infinities, NaN, zeros of both signs, the largest there are."""
+    x = torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(TYPE[dtype])
+    at = np.nonzero(still)[0]
+    both = np.concatenate((2 * at, 2 * at + 1) if inter else (at, at + rot // 2))
+    big = torch.finfo(TYPE[dtype]).max
+    some = torch.tensor([float("inf"), -float("inf"), float("nan"), -0.0, 0.0, big, -big, 1.0], dtype=torch.float32).to(TYPE[dtype])
+    x[..., both] = some[torch.from_numpy(rng.integers(0, len(some), (*shape[:-1], len(both))))]
+    return x.to(DEV), both
+
+
+def _same_bits(a, b):
+    kind = torch.int32 if a.dtype == torch.float32 else torch.int16 if a.dtype == torch.bfloat16 else torch.uint8
+    return torch.equal(a.contiguous().view(kind), b.contiguous().view(kind))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,H,d,rot,tokens", [(1, 1, 64, 64, 0), (40, 4, 64, 64, 0), (40, 4, 64, 32, 1), (40, 4, 72, 72, 0),
+                                              (40, 4, 72, 72, 1), (9001, 64, 128, 128, 0), (9001, 64, 128, 128, 1)])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_an_axis_that_is_not_there_leaves_its_partners(dtype, n, H, d, rot, tokens, inter, inverse):
+    """Whatever they are, and whatever its frequency is, by bits: a partner of an
+    infinity or a NaN, zeros below 0.  (The largest go past the caches.)"""
+    rr = rrmod()
+    note("rotate no axis", dtype, n, H, d, rot, tokens, inter, inverse)
+    rng = np.random.default_rng(n + rot)
+    axis, f, still = _without_axes(rng, rot // 2, n)
+    X, both = _any_values(rng, (n, H, d) if tokens == 0 else (H, n, d), still, rot, inter, dtype)
+    dev = [torch.from_numpy(a).to(DEV) for a in (_positions(rng, 2, n, False), f, axis)]
+    got = rr.rotate(X, dev[0], dev[1], axis=dev[2], tokens=tokens, interleaved=inter, inverse=inverse)
+    assert _same_bits(got[..., both], X[..., both])
+    assert _same_bits(got[..., rot:], X[..., rot:])
+    others = np.setdiff1d(np.arange(rot), both)
+    assert bool(got[..., others].isfinite().all())
+    assert len(others) == 0 or n == 1 or not _same_bits(got[..., others], X[..., others])
+    Y = X.clone()
+    rr.rotate(Y, dev[0], dev[1], axis=dev[2], tokens=tokens, interleaved=inter, inverse=inverse, out=Y)
+    assert _same_bits(Y, got)
+
+
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("H,Hkv,d,rot,n", [(6, 2, 64, 64, 50), (6, 2, 72, 72, 50), (3, 1, 1024, 1024, 33), (60, 4, 128, 128, 9001)])
+@pytest.mark.parametrize("inter", [False, True])
+def test_append_by_an_axis_that_is_not_there(dtype, cache, H, Hkv, d, rot, n, inter):
+    rr = rrmod()
+    note("append no axis", dtype, cache, H, Hkv, d, rot, n, inter)
+    rng = np.random.default_rng(n + rot)
+    axis, f, still = _without_axes(rng, rot // 2, n)
+    X, both = _any_values(rng, (n, H + 2 * Hkv, d), still, rot, inter, dtype)
+    Q, K, V = X[:, :H], X[:, H:H + Hkv], X[:, H + Hkv:]
+    pools = [torch.zeros((n, Hkv, 1, d), dtype=TYPE[cache], device=DEV) for _ in range(2)]
+    scales = {}
+    if cache == "e4m3":
+        scales = {k: torch.full((Hkv,), 0.0625, device=DEV) for k in ("k_scale", "v_scale")}
+    dev = [torch.from_numpy(a).to(DEV) for a in (_positions(rng, 2, n, False), f, axis)]
+    table = torch.randperm(n, generator=torch.Generator().manual_seed(n)).to(torch.int32).to(DEV)
+    out = rr.cache_append(K, V, *pools, table.view(1, n), torch.tensor([n], dtype=torch.int32, device=DEV), freqs=dev[1],
+                          interleaved=inter, Q=Q, positions=dev[0], axis=dev[2], **scales)
+    assert _same_bits(out[..., both], Q[..., both])
+    got, values = (p[table.long(), :, 0] if cache != "e4m3" else p.view(torch.uint8)[table.long(), :, 0] for p in pools)
+    want, values_want = K[..., both], V
+    if cache == "e4m3":  # (16 x is exact, NaN is any of that type's two)
+        want, values_want = ((16 * x.float()).clamp(-448.0, 448.0).to(TYPE[cache]).view(torch.uint8) for x in (want, values_want))
+        k_nan, v_nan = K[..., both].isnan(), V.isnan()
+        assert bool(((got[..., both][k_nan] & 0x7f) == 0x7f).all()) and bool(((values[v_nan] & 0x7f) == 0x7f).all())
+        assert torch.equal(got[..., both][~k_nan], want[~k_nan]) and torch.equal(values[~v_nan], values_want[~v_nan])
+    else:
+        assert _same_bits(got[..., both], want) and _same_bits(values, values_want)
+    others = np.setdiff1d(np.arange(rot), both)
+    assert bool(out[..., others].isfinite().all()) and bool((got.float() if cache != "e4m3" else got.view(TYPE[cache]).float())
+                                                            [..., others].isfinite().all())
