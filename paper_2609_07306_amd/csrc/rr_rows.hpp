@@ -81,7 +81,9 @@ constexpr int kTurns = INTER ? N / 2 : N;
 constexpr float kStays = 2.f;
 
 // Rotates a piece: neighbours are partners (INTER), or x's element e and y's.
-// SOME: but for those that kStays stands for.
+// SOME: but for those that kStays stands for.  Of two products one is rounded before
+// they are added; which one is written down, as the compiler would choose it kernel
+// by kernel: every call gives a row the same bits.
 template <bool INTER, int N, bool SOME>
 __device__ __forceinline__ void turn_piece(float (&x)[N], float (&y)[N], const float (&c)[kTurns<INTER, N>],
                                            const float (&s)[kTurns<INTER, N>])
@@ -89,8 +91,8 @@ __device__ __forceinline__ void turn_piece(float (&x)[N], float (&y)[N], const f
     auto turn = [](float &x, float &y, float c, float s) {
         const float p = x, q = y;
         const bool stays = SOME && c == kStays;
-        x = stays ? p : p * c - q * s;
-        y = stays ? q : q * c + p * s;
+        x = stays ? p : __builtin_fmaf(p, c, -(q * s));
+        y = stays ? q : INTER ? __builtin_fmaf(p, s, q * c) : __builtin_fmaf(q, c, p * s);
     };
     if constexpr (INTER) {
 #pragma unroll

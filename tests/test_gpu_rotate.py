@@ -435,3 +435,60 @@ def test_append_by_an_axis_that_is_not_there(dtype, cache, H, Hkv, d, rot, n, in
     others = np.setdiff1d(np.arange(rot), both)
     assert bool(out[..., others].isfinite().all()) and bool((got.float() if cache != "e4m3" else got.view(TYPE[cache]).float())
                                                             [..., others].isfinite().all())
+
+
+def _either(x):
+    """What binary32 may hold of a sum of two numbers that binary64 has rounded to x."""
+    return [torch.from_numpy((x * (1 + e)).astype(np.float32)) for e in (-2.0 ** -52, 2.0 ** -52)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("d,rot,shift", [(64, 64, 0), (128, 64, 0), (72, 40, 0), (64, 64, 1)])
+@pytest.mark.parametrize("heads", [3, 40])
+def test_every_call_rounds_the_same_product_first(dtype, inter, d, rot, shift, heads):
+    """x c - (q s rounded), and the partner's own product last of two halves, first
+    of two neighbours: the same bits from the rotation of either layout, from the
+    append by place and by axes, of few tokens and (40 heads) of what goes past the
+    caches.  Cosines and sines are those that the rotation gives 1 and 0."""
+    rr = rrmod()
+    note("rotate product", dtype, inter, d, rot, shift, heads)
+    rng = np.random.default_rng(d + rot)
+    few = 70
+    n = few if heads == 3 else (260 << 20) // (heads * d * TYPE[dtype].itemsize) + 1
+    half = rot // 2
+    a, b = (np.arange(0, rot, 2), np.arange(1, rot, 2)) if inter else (np.arange(half), np.arange(half, rot))
+    wide = torch.zeros((n, heads, d + 8 * shift), dtype=TYPE[dtype], device=DEV)
+    wide.normal_(generator=torch.Generator(device=DEV).manual_seed(d))
+    X = wide[:, :, shift:shift + d]
+    f = torch.from_numpy(_freqs(half)).to(DEV)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)
+    one = torch.zeros((few, 1, d), device=DEV)
+    one[..., a] = 1.0
+    turn = _np(rr.rotate(one, pos[:few].contiguous(), f, interleaved=inter))
+    c, s, x = turn[..., a], turn[..., b], _np(X[:few])
+    p, q = x[..., a], x[..., b]
+
+    def once(v):
+        return v.astype(np.float32).astype(np.float64)
+
+    first = _either(p * c - once(q * s))
+    second = _either(p * s + once(q * c) if inter else q * c + once(p * s))
+    got = rr.rotate(X, pos, f, interleaved=inter)
+    for at, want in ((a, first), (b, second)):
+        y = got[:few].cpu()[..., at]
+        assert bool(((y == want[0].to(TYPE[dtype])) | (y == want[1].to(TYPE[dtype]))).all())
+    turned = rr.rotate(wide.transpose(0, 1).contiguous()[:, :, shift:shift + d], pos, f, tokens=1, interleaved=inter)
+    assert torch.equal(turned.transpose(0, 1), got)
+    del turned
+    assert torch.equal(rr.rotate(X[:few], pos[:few].contiguous(), f, interleaved=inter), got[:few])
+    table, lens = pos.view(1, n), torch.tensor([n], dtype=torch.int32, device=DEV)
+    flat = X.contiguous() if not shift else None
+    if shift:  # (rows of a token lie together: as many elements off as a vector has not)
+        flat = torch.empty(n * heads * d + 1, dtype=TYPE[dtype], device=DEV)[1:].view(n, heads, d)
+        flat.copy_(X)
+    for more in ({}, dict(positions=pos)):
+        pools = [torch.zeros((n, 1, 1, d), dtype=TYPE[dtype], device=DEV) for _ in range(2)]
+        out = rr.cache_append(flat[:, :1], flat[:, :1], *pools, table, lens, freqs=f, interleaved=inter, Q=flat, **more)
+        assert torch.equal(out, got)
+        assert torch.equal(pools[0][:, :, 0], got[:, :1])
