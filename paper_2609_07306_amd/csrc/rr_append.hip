@@ -313,9 +313,15 @@ hipError_t launch_append(const AppendArgs &a, int dtype, int cache, bool interle
     // (bf16, heads as above, by place; append and reader, through the caches and
     // past them): 8000 tokens 34 + 22 us and 33 + 27, 12000 52 + 49 and 48 + 37,
     // 32768 147 + 106 and 144 + 95, into an 8-bit cache 133 + 104 and 118 + 99.
+    // But only in whole lines of 128 bytes, as in a rotation: parts of lines that
+    // the caches do not put together are slower by more than the reader gains
+    // (32768 tokens of 64 heads on 8: of 64 features 123 + 93 and 163 + 81, of 96
+    // 190 + 135 and 274 + 120; 32 heads of 128, of which 64 are rotated, 144 + 93 and
+    // 156 + 81, rows of a fused projection 146 + 92 and 147 + 80).
     const int64_t rows = a.n_tokens * (int64_t)a.d, heads = a.Q ? a.n_heads : 0;
     const int64_t bytes = rows * (size * 2 * (heads + a.n_kv_heads) + (cache == CACHE_E4M3 ? 1 : size) * 2 * (int64_t)a.n_kv_heads);
-    const bool once = vec && bytes >= kLastCache;
+    const bool lines = interleaved ? a.d * size % 128 == 0 : a.rot / 2 * size % 128 == 0 && (a.d - a.rot) * size % 128 == 0;
+    const bool once = vec && lines && bytes >= kLastCache;
     auto any = [&](auto type, auto e4, auto axes) {
         typedef decltype(type) T;
         constexpr bool E4 = decltype(e4)::value, AX = decltype(axes)::value;

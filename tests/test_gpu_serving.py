@@ -375,3 +375,57 @@ def test_large_appends_are_small_ones(heads, kv, d, rot, dtype, cache, inter, by
     rr.cache_append(K, V, *pools[1], table, lengths, seq_start=start, Q=outs[2], Q_out=outs[2], positions=positions, axis=axis,
                     **common)
     assert torch.equal(bits(outs[2][:kept - max(0, beyond)]), bits(outs[0][:kept - max(0, beyond)]))
+
+
+@pytest.mark.parametrize("heads,kv,d,rot", [(32, 8, 128, 128), (9, 4, 256, 128), (5, 3, 1024, 1024), (6, 2, 1024, 0),
+                                            (40, 3, 64, 64), (24, 4, 160, 96)])
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("by_axes", [False, True])
+def test_appends_past_the_last_cache(heads, kv, d, rot, dtype, cache, inter, by_axes):
+    """More than the last cache holds, read and written together: what is made of
+    whole lines goes past it, and every bit is as calls for a part of the tokens
+    give it; rows behind the last sequence are left, tokens beyond the table too."""
+    rr = rrmod()
+    note("append past the last cache", heads, kv, d, rot, dtype, cache, inter, by_axes)
+    T = {"f32": torch.float32, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}
+    g = torch.Generator(device=DEV).manual_seed(heads + d)
+    n0 = (270 << 20) // (2 * d * ((heads + kv) * T[dtype].itemsize + kv * T[cache].itemsize)) // 2 + 7
+    n, page = 2 * n0 + 40, 16
+    width = -(-(n0 + 30) // page)
+    start = torch.tensor([0, n0 + 10, 2 * n0 + 20], dtype=torch.int32, device=DEV)
+    lengths = torch.tensor([n0 + 17, n0 + 40], dtype=torch.int32, device=DEV)  # (the second passes its pages)
+    table = torch.randperm(2 * width, generator=g, device=DEV).to(torch.int32).view(2, width)
+    qkv = torch.empty((n, heads + 2 * kv, d), dtype=T[dtype], device=DEV).normal_(generator=g)
+    Q, K, V = qkv[:, :heads], qkv[:, heads:heads + kv], qkv[:, heads + kv:]
+    scales = [torch.rand(kv, generator=g, device=DEV) + 0.1 for _ in range(2)] if cache == "e4m3" else [None, None]
+    freqs = 10000.0 ** (-torch.arange(rot // 2, dtype=torch.float64, device=DEV) / max(1, rot // 2))
+    positions = axis = None
+    if by_axes:
+        positions = torch.randint(0, 5000, (3, n), generator=g, device=DEV).to(torch.int32)
+        axis = torch.randint(-1, 4, (rot // 2,), generator=g, device=DEV).to(torch.int32)
+    pools = [[torch.zeros((2 * width, kv, page, d), device=DEV).to(T[cache]) for _ in range(2)] for _ in range(2)]
+    outs = [torch.full((n, heads, d), 7.0, dtype=T[dtype], device=DEV) for _ in range(2)]
+    common = dict(freqs=freqs, interleaved=inter, k_scale=scales[0], v_scale=scales[1])
+    rr.cache_append(K, V, *pools[0], table, lengths, seq_start=start, Q=Q, Q_out=outs[0], positions=positions, axis=axis, **common)
+    step = n0 // 3
+    for b in range(2):
+        i0, i1 = int(start[b]), int(start[b + 1])
+        for i in range(i0, i1, step):
+            j = min(i + step, i1)
+            part = None if positions is None else positions[:, i:j].contiguous()
+            rr.cache_append(K[i:j], V[i:j], *pools[1], table[b:b + 1], lengths[b:b + 1] - (i1 - j), Q=Q[i:j],
+                            Q_out=outs[1][i:j], positions=part, axis=axis, **common)
+    bits = {1: torch.uint8, 2: torch.int16, 4: torch.int32}
+    for a, b in ((outs[0], outs[1]), *zip(*pools)):
+        assert torch.equal(a.view(bits[a.element_size()]), b.view(bits[b.element_size()]))
+    assert bool((outs[0][2 * n0 + 20:] == 7.0).all())
+    assert not bool((outs[0][0] == 7.0).all()) and bool(pools[0][0].float().any())
+    # in place, where rows of queries follow each other
+    q = Q.contiguous()
+    again = [torch.zeros_like(p) for p in pools[0]]
+    rr.cache_append(K, V, *again, table, lengths, seq_start=start, Q=q, Q_out=q, positions=positions, axis=axis, **common)
+    end = 2 * n0 + 10  # (the last ones of the second sequence's tokens have no pages, and keep what Q_out held)
+    assert torch.equal(q[:end].view(bits[q.element_size()]), outs[0][:end].view(bits[q.element_size()]))
+    for a, b in zip(again, pools[0]):
+        assert torch.equal(a.view(bits[a.element_size()]), b.view(bits[b.element_size()]))
