@@ -40,6 +40,18 @@ class RRError(RuntimeError):
         self.status = status
 
 
+_MOST = 2 ** 31 - 1
+
+
+def _fits(*sizes):
+    """Numbers that the library takes in 32 bits, to which ctypes would cut others
+    without a word.  (Where only a tensor's sizes can be large, and time counts, a
+    call tests them itself: their bits together, as none is below 0.)"""
+    for n in sizes:
+        if not -_MOST - 1 <= n <= _MOST:
+            raise ValueError(f"{n} does not fit 32 bits")
+
+
 class _Config(ctypes.Structure):
     _fields_ = [
         ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("n_q", ctypes.c_int32),
@@ -182,6 +194,8 @@ class Config:
         return self.m + self.r + self.n_sink + self.n_recent
 
     def c(self) -> _Config:
+        _fits(self.n_heads, self.n_kv_heads, self.n_q, self.n_k, self.d, self.k, self.m, self.r, self.n_sink, self.n_recent,
+              self.min_reuse)
         g = None
         if self.gamma_rows is not None:
             t = self.gamma_rows
@@ -261,6 +275,7 @@ def unconverged_rows() -> int:
 
 def set_sweep_cap(cap: int):
     """Test hook: collection sweeps allowed per route tile (0: default)."""
+    _fits(cap)
     _check(lib.rr_set_sweep_cap(int(cap)))
 
 
@@ -281,6 +296,7 @@ def relay_static(cfg: Config, layer: int, Q, K, ledger, routes=None, mask=None, 
     """rr_relay_layer_static: a relay layer on a caller-owned ledger (a dict of
     int32 device tensors as Ledger.export returns), updated in place; the
     library allocates nothing."""
+    _fits(layer)
     q, k = _inputs(cfg, Q, K)
     c = cfg
     _check(lib.rr_relay_layer_static(
@@ -322,12 +338,14 @@ class Ledger:
         return self._h
 
     def anchor(self, layer: int, Q, K, routes=None, pairs=None, stream=None):
+        _fits(layer)
         q, k = _inputs(self.cfg, Q, K)
         c = self.cfg
         _check(lib.rr_anchor_route(self._h, layer, q, k, _out(routes, (c.rows, c.k), torch.int32),
                                    _out(pairs, (1,), torch.int64), _stream(stream)))
 
     def relay(self, layer: int, Q, K, routes=None, mask=None, pairs=None, n_rerouted=None, stream=None):
+        _fits(layer)
         q, k = _inputs(self.cfg, Q, K)
         c = self.cfg
         _check(lib.rr_relay_layer(self._h, layer, q, k, _out(routes, (c.rows, c.k), torch.int32),
@@ -352,6 +370,7 @@ class Ledger:
         return out
 
     def import_(self, layer: int, routes, sent, build, age, stream=None):
+        _fits(layer)
         c = self.cfg
         _check(lib.rr_ledger_import(self._h, layer, _out(routes, (c.rows, c.k), torch.int32),
                                     _out(sent, (c.rows, c.sent_width), torch.int32) if c.sent_width else None,
@@ -390,6 +409,7 @@ def pool_chunks(X, chunk: int, out=None, stream=None):
     if X.dim() != 3 or X.dtype not in (torch.float32, torch.bfloat16):
         raise TypeError("X must be a [H, n_tokens, d] float32 or bfloat16 tensor")
     H, n, d = X.shape
+    _fits(H, n, d, chunk)
     shape = (H, n_chunks(n, chunk), d)
     if out is None:
         out = torch.empty(shape, dtype=X.dtype, device=X.device)
@@ -403,6 +423,7 @@ def expand_tokens(routes, chunk: int, n_tokens: int, out=None, stream=None):
     if routes.dim() != 2 or routes.dtype != torch.int32:
         raise TypeError("routes must be a [rows, k] int32 tensor")
     rows, k = routes.shape
+    _fits(k, chunk, n_tokens)
     shape = (rows, k * chunk)
     if out is None:
         out = torch.empty(shape, dtype=torch.int32, device=routes.device)
@@ -421,6 +442,7 @@ def sparse_attention(Q, K, V, routes, chunk: int, causal: bool, scale: float = 0
     Hkv = K.shape[0]
     if tuple(K.shape) != (Hkv, n, d) or tuple(V.shape) != (Hkv, n, d):
         raise ValueError("K and V must be [H_kv, n_tokens, d]")
+    _fits(H, Hkv, n, d, chunk, *routes.shape[1:])
     nc = n_chunks(n, chunk)
     if routes.dim() != 2 or routes.dtype != torch.int32 or routes.shape[0] != H * nc:
         raise ValueError("routes must be [H * n_chunks, k] int32")
@@ -547,6 +569,8 @@ def _axes_of(positions, axis, rot, n):
         raise ValueError(f"positions must be [n_axes, {n}]: got {list(shape)}")
     if not positions.is_contiguous():
         raise ValueError("positions must be contiguous")
+    if shape[0] > _MOST:
+        _fits(shape[0])
     return _Axes(positions.data_ptr(), None if axis is None else _of("axis", axis, (rot // 2,), torch.int32),
                  shape[0] if len(shape) == 2 else 1, 1 if kind == torch.float32 else 0)
 
@@ -566,8 +590,8 @@ def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, fr
     if len(shape) != 3 or kind not in (torch.float32, torch.bfloat16):
         raise TypeError("K must be a [n_tokens, H_kv, d] float32 or bfloat16 tensor")
     (n_pages, Hkv, page, d), cache, kc, vc, ks, vs = _cache_of(K_cache, V_cache, kind, k_scale, v_scale)
-    dev = _device_of((K, V, K_cache, V_cache, page_table, lengths, seq_start, freqs, Q, Q_out, k_scale, v_scale, positions,
-                      axis))
+    tensors = (K, V, K_cache, V_cache, page_table, lengths, seq_start, freqs, Q, Q_out, k_scale, v_scale)
+    dev = _device_of(tensors if positions is None else (*tensors, positions, axis))
     n = shape[0]
     rows = (n, Hkv, d)
     ldk, ldv = _rows_of("K", K, rows, kind), _rows_of("V", V, rows, kind)
@@ -580,9 +604,10 @@ def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, fr
     if seq_start is not None:
         start = _of("seq_start", seq_start, (B + 1,), torch.int32)
     if Q is not None:
-        if Q.dim() != 3:
+        heads = Q.shape
+        if len(heads) != 3:
             raise TypeError("Q must be a [n_tokens, H, d] tensor")
-        H = Q.shape[1]
+        H = heads[1]
         rows = (n, H, d)
         ldq = _rows_of("Q", Q, rows, kind)
         if Q_out is None:
@@ -590,6 +615,8 @@ def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, fr
         q, out = Q.data_ptr(), _of("Q_out", Q_out, rows, kind)
     elif Q_out is not None:
         raise ValueError("Q_out without Q")
+    if n | n_pages | Hkv | page | d | B | most | H | rot > _MOST:
+        _fits(n, n_pages, Hkv, page, d, B, most, H, rot)
     cfg = _AppendConfig(H, Hkv, d, page, n_pages, most, B, n, rot, 1 if interleaved else 0, _DTYPES[kind], cache, ldq, ldk,
                         ldv, ks, vs)
     if positions is None:
@@ -632,7 +659,10 @@ def rotate(X, positions, freqs, axis=None, tokens=0, interleaved=False, inverse=
         out = _empty(shape, kind, X, stream)
     elif out.shape != shape or out.dtype != kind:
         raise ValueError(f"out must be {kind} of shape {list(shape)}")
-    cfg = _RotateConfig(shape[1 - tokens], n, shape[2], rot, 1 if interleaved else 0, 1 if inverse else 0, _DTYPES[kind], 0,
+    H, d = shape[1 - tokens], shape[2]
+    if n | H | d | rot > _MOST:
+        _fits(n, H, d, rot)
+    cfg = _RotateConfig(H, n, d, rot, 1 if interleaved else 0, 1 if inverse else 0, _DTYPES[kind], 0,
                         *_strides("X", X, tokens), *_strides("out", out, tokens))
     _launch(dev, stream, _rotate, cfg, X.data_ptr(), f, axes, out.data_ptr())
     return out
@@ -647,9 +677,9 @@ def _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, n_p
     B, nq, H, dq = Q.shape
     if dq != d:
         raise ValueError(f"Q has rows of {dq} features, the cache of {d}")
-    if page_table.dim() != 2 or page_table.shape[0] != B:
+    table, lens, rows, most = _lists(page_table, lengths)
+    if rows != B:
         raise ValueError("page_table must be [B, max_pages]")
-    table, lens, _, most = _lists(page_table, lengths)
     k = 0
     if routes is not None:
         if routes.dim() != 2 or routes.shape[0] != B * H * nq:
@@ -657,6 +687,10 @@ def _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, n_p
         k = routes.shape[1]
         if k == n_sink == n_recent == 0:
             k = 1  # (a slot that names no page, _some_routes: the library takes k = 0 alone for no routes)
+    if n_sink or n_recent or n_prefix:
+        _fits(n_sink, n_recent, n_prefix)
+    if n_pages | Hkv | page | d | B | most | nq | H | k > _MOST:
+        _fits(n_pages, Hkv, page, d, B, most, nq, H, k)
     cfg = _PagedConfig(H, Hkv, d, page, n_pages, most, B, nq, k, n_sink, n_recent, n_prefix, _DTYPES[Q.dtype], cache, scale, 0,
                        ks, vs)
     return cfg, kc, vc, table, lens
@@ -764,6 +798,7 @@ class Pools:
                 raise ValueError("caches must have one shape and one type")
             if not t.is_contiguous():
                 raise ValueError("caches must be contiguous")
+        _fits(len(self.tensors), *self.shape)
         self.dev = _device_of(self.tensors)
         self._addresses = (ctypes.c_void_p * len(self.tensors))(*(t.data_ptr() for t in self.tensors))
 
@@ -810,6 +845,8 @@ def cache_fork(page_table, lengths, refs, parent, stream=None):
     if refs.dim() != 1:
         raise ValueError("refs must be [n_pages]")
     n_pages = refs.shape[0]
+    if n_pages | B | most > _MOST:
+        _fits(n_pages, B, most)
     _launch(dev, stream, _fork, B, most, n_pages, _of("parent", parent, (B,), torch.int32), table, lens, _refs(refs, n_pages))
 
 
@@ -823,7 +860,12 @@ def cache_resize(pools, page_table, lengths, refs, new_tokens, missing=None, wor
     many = isinstance(new_tokens, torch.Tensor)
     dev = _device_of((pools.tensors[0], page_table, lengths, refs, new_tokens if many else None, missing, workspace))
     table, lens, B, most = _lists(page_table, lengths)
-    new = _of("new_tokens", new_tokens, (B,), torch.int32) if many else None
+    new = None
+    if many:
+        new = _of("new_tokens", new_tokens, (B,), torch.int32)
+        _fits(B, most)
+    elif not 0 <= new_tokens <= _MOST or B | most > _MOST:
+        _fits(new_tokens, B, most)
     r = _refs(refs, pools.shape[0])
     if missing is None:
         missing = _empty((B,), torch.int32, page_table, stream)
@@ -844,6 +886,7 @@ def cache_compact(pools, page_table, refs, new_ids=None, n_used=None, workspace=
     if page_table.dim() != 2:
         raise ValueError("page_table must be [B, max_pages]")
     B, most = page_table.shape
+    _fits(B, most)
     table = _of("page_table", page_table, (B, most), torch.int32)
     n_pages = pools.shape[0]
     r = _refs(refs, n_pages)
@@ -879,6 +922,8 @@ def _verify_config(P, n_drafts, Q=None):
             raise ValueError("draft_probs: rows must be contiguous")
     if one != 1 and V > 1:
         raise ValueError("P: rows must be contiguous")
+    if B | n_drafts | V > _MOST:
+        _fits(B, n_drafts, V)
     return _VerifyConfig(B, n_drafts, V, _DTYPES[kind], p_seq, p_row, q_seq, q_row)
 
 
