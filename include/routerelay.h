@@ -621,7 +621,8 @@ typedef struct {
     int64_t q_seq, q_row;
 } rr_verify_config;
 
-/* Bytes of workspace of rr_verify_drafts (0: the config is not valid).  It is
+/* Bytes of workspace of rr_verify_drafts (0: the config is not valid): no fewer
+ * for more sequences, a larger vocabulary, or RR_F32 in place of RR_BF16.  It is
  * filled with zeros before its first use, and calls leave the part of it that
  * has to be zero (the first 65536 bytes) at zero, so that it serves any calls
  * that follow one another.  Calls that may run at the same time need one each. */

@@ -333,8 +333,11 @@ void verify_schedule(VerifyArgs &a, int dtype)
 
 size_t verify_workspace_bytes(const VerifyArgs &a)
 {
-    const int seqs = a.n_seqs < kVerifySeqs ? a.n_seqs : kVerifySeqs;
-    return kVerifyCounterBytes + (size_t)seqs * a.n_parts * sizeof(double);
+    // Rows of two or four steps a part have fewer parts than some shorter ones (65536
+    // tokens 256, 65537 129): for as many as any row up to this one's length has.
+    const int seqs = a.n_seqs < kVerifySeqs ? a.n_seqs : kVerifySeqs, step = Some<float>::STEP;
+    const int shorter = (a.vocab + step - 1) / step < kVerifyThreads ? (a.vocab + step - 1) / step : kVerifyThreads;
+    return kVerifyCounterBytes + (size_t)seqs * (a.n_parts > shorter ? a.n_parts : shorter) * sizeof(double);
 }
 
 hipError_t launch_verify(const VerifyArgs &args, int dtype, void *workspace, hipStream_t stream)

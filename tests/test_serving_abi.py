@@ -282,3 +282,21 @@ def test_shapes_of_positions(shape, n, fits):
     else:
         with pytest.raises(ValueError, match="positions must be"):
             rr._axes_of(positions, None, 4, n)
+
+
+def test_a_verification_s_workspace_serves_smaller_ones():
+    """Fewer sequences, a smaller vocabulary (whose rows may have more parts) and
+    the shorter type need no more bytes."""
+    rr = _rr()
+
+    def need(n_seqs, vocab, dtype):
+        return rr.lib.rr_verify_workspace_bytes(rr._VerifyConfig(n_seqs, 3, vocab, dtype, 0, 0, 0, 0))
+
+    edges = [e + x for k in range(24) for e in (1 << k, 3 << k) for x in (-1, 0, 1)]
+    sizes = sorted({v for v in edges + [1000, 32000, 50257, 128256, 151936, 262144, 300001] if 1 <= v < 1 << 24})
+    for n_seqs in (1, 7, 1024, 5000):
+        for dtype in (rr.RR_F32, rr.RR_BF16):
+            got = [need(n_seqs, v, dtype) for v in sizes]
+            assert got == sorted(got) and got[0] > 65536
+    for v in sizes:
+        assert need(7, v, rr.RR_BF16) <= need(7, v, rr.RR_F32) <= need(8, v, rr.RR_F32)
