@@ -24,6 +24,7 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
 constexpr int kForkThreads = 512, kForkAtOnce = 4;
 constexpr int kForkLds = 65536;  // bytes of parents, children and columns
+static_assert(kForkSeqs * (2 + 2) * sizeof(int32_t) <= kForkLds, "two columns of any call");
 
 // Row b becomes what row parent[b] was; no such row: empty.  A workgroup takes
 // C columns of all rows, through LDS, so that rows change in place.  A row that
@@ -668,10 +669,8 @@ hipError_t launch_fork(const ForkArgs &a, hipStream_t stream)
         go(fork_kernel<8>, 8);
     else if (lds(4) <= kForkLds)
         go(fork_kernel<4>, 4);
-    else if (lds(2) <= kForkLds)
-        go(fork_kernel<2>, 2);
     else
-        go(fork_kernel<1>, 1);
+        go(fork_kernel<2>, 2);
     return hipGetLastError();
 }
 

@@ -92,6 +92,49 @@ def test_fork(B, width, n_pages, kind):
         assert t.tolist() == table and r.tolist() == refs
 
 
+@pytest.mark.parametrize("B,width,n_pages", [(5, 2049, 12000), (1, 2048, 2100), (64, 2500, 60000), (130, 2065, 90000),
+                                             (1638, 2051, 400000), (1639, 2051, 400000), (2731, 65, 40000)])
+@pytest.mark.parametrize("kind", ["any", "groups", "ends", "stay", "swap"])
+def test_fork_of_wide_tables(B, width, n_pages, kind):
+    """Eight columns a workgroup where they are many, with some left over and numbers
+    of workgroups that the XCDs do not share evenly; the most sequences that eight and
+    four columns take, and one more."""
+    rr = rrmod()
+    note("fork wide", B, width, n_pages, kind)
+    rng = np.random.default_rng(B * width)
+    # rows of their own pages or an earlier row's, of any length, as counted
+    table, lengths = np.full((B, width), -1, np.int64), np.zeros(B, np.int64)
+    order, at = rng.permutation(n_pages), 0
+    for b in range(B):
+        n = int(rng.integers(0, width + 1)) if b % 7 else width
+        if b and rng.random() < 0.6:
+            o = int(rng.integers(max(0, b - 3), b))
+            n = min(n, int(lengths[o]))
+            table[b, :n] = table[o, :n]
+        else:
+            n = min(n, n_pages - at, max(width // 9, n_pages // B))
+            table[b, :n] = order[at:at + n]
+            at += n
+        lengths[b] = n
+        if n < width:
+            table[b, n] = rng.choice(BAD)
+    counts = np.bincount(table[(table >= 0) & (table < n_pages)], minlength=n_pages)
+    parent = {"any": rng.integers(0, B, B), "groups": np.arange(B) // 4 * 4, "stay": np.arange(B),
+              "ends": np.where(rng.random(B) < 0.5, np.arange(B), rng.choice([-1, B, 2 ** 31 - 1, -2 ** 31], B)),
+              "swap": np.arange(B)[::-1].copy()}[kind]
+    there = (parent >= 0) & (parent < B)
+    rows = np.where(there[:, None], table[np.where(there, parent, 0)], -1)
+    refs = np.bincount(rows[(rows >= 0) & (rows < n_pages)], minlength=n_pages) + 3  # (three held apart)
+    t, n, r = _i32(table), _i32(lengths * 5), _i32(counts + 3)
+    rr.cache_fork(t, n, r, _i32(parent))
+    assert np.array_equal(t.cpu().numpy(), rows)
+    assert np.array_equal(n.cpu().numpy(), np.where(there, 5 * lengths[np.where(there, parent, 0)], 0))
+    assert np.array_equal(r.cpu().numpy(), refs)
+    if B * width < 20000:
+        want = serving.fork(table.tolist(), (5 * lengths).tolist(), (counts + 3).tolist(), [int(p) for p in parent])
+        assert want[0] == rows.tolist() and want[2] == refs.tolist()
+
+
 # ----------------------------------------------------------------- resize
 
 def _resize(rr, table, lengths, refs, new, pools, page, missing=True, workspace=None):
