@@ -321,6 +321,85 @@ def test_compact_of_large_pages():
                 assert torch.equal(p[new, -1, -1], m[old]) and torch.equal(p[new, 0, 0], f[old])
 
 
+def _random_pools(seed, n_pools, shape, dtype):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    size = int(np.prod(shape)) * TYPE[dtype].itemsize
+    return [torch.empty(size, dtype=torch.uint8, device=DEV).random_(0, 256, generator=g).view(TYPE[dtype]).view(shape)
+            for _ in range(n_pools)]
+
+
+@pytest.mark.parametrize("dtype,Hkv,page,d,n_pages,n_pools", [
+    ("bf16", 1, 16, 128, 90, 2),      # 256 pieces of 16 bytes: two pages a turn of a workgroup's threads
+    ("bf16", 1, 17, 128, 90, 2),      # just over that: a page a turn
+    ("f32", 2, 16, 64, 90, 4),        # a whole turn
+    ("f32", 2, 16, 72, 90, 4),        # a turn and a part of one
+    ("bf16", 3, 43, 136, 90, 6),      # some of them and a part
+    ("e4m3", 2, 15, 72, 90, 2),       # rows of an odd number of 8 bytes: the same in pieces of these
+    ("e4m3", 4, 16, 72, 90, 2),
+    ("e4m3", 8, 64, 72, 40, 4),
+    ("e4m3", 3, 50, 200, 40, 66),     # more pools than a launch takes
+    ("bf16", 3, 43, 136, 40, 130),
+    ("bf16", 1, 3, 8, 300, 130),
+    ("bf16", 1, 17, 128, 20000, 2),   # more pages than a workgroup counts
+    ("e4m3", 2, 31, 72, 33000, 4),
+    ("bf16", 1, 17, 128, 17000, 66),
+    ("bf16", 8, 4096, 128, 300, 2),   # past 2^31 bytes into a pool
+])
+@pytest.mark.parametrize("used", [0.05, 0.5, 0.9])
+def test_compact_moves_whole_pages(dtype, Hkv, page, d, n_pages, n_pools, used):
+    """Every byte of every pool, pages of all sizes of the copies."""
+    rr = rrmod()
+    note("compact whole", dtype, Hkv, page, d, n_pages, n_pools, used)
+    rng = np.random.default_rng(n_pages + page)
+    refs = (rng.random(n_pages) < used) * rng.integers(1, 5, n_pages)
+    refs[-1] = 2
+    held = np.nonzero(refs)[0]
+    table = rng.choice(held, (25, 9))
+    table[rng.random(table.shape) < 0.3] = -1
+    pools = _random_pools(page, n_pools, (n_pages, Hkv, page, d), dtype)
+    t, r = _i32(table), _i32(refs)
+    handle = rr.Pools(pools[0::2], pools[1::2])
+    before = [p.view(torch.uint8).clone() for p in pools]
+    ids, n = rr.cache_compact(handle, t, r)
+    wt, wr, wids, wn = serving.compact(table.tolist(), refs.tolist())
+    assert n.tolist() == [wn] and ids.tolist() == wids and t.tolist() == wt and r.tolist() == wr
+    src = [p for p, to in enumerate(wids) if to >= 0 and to != p]
+    assert src
+    dst = torch.tensor([wids[p] for p in src], device=DEV)
+    for p, old in zip(pools, before):
+        old[dst] = old[torch.tensor(src, device=DEV)]  # (sources lie behind all destinations)
+        assert torch.equal(p.view(torch.uint8), old)
+
+
+@pytest.mark.parametrize("dtype,Hkv,page,d,n_pools", [
+    ("e4m3", 2, 28, 72, 2), ("e4m3", 2, 29, 72, 2),    # 504 and 522 pieces of 8 bytes: pages together, and one a unit
+    ("e4m3", 8, 64, 72, 4), ("e4m3", 16, 64, 72, 2),   # three units, five
+    ("bf16", 3, 61, 136, 66), ("bf16", 2, 16, 128, 130), ("f32", 8, 64, 128, 2), ("bf16", 1, 33, 128, 2),
+])
+@pytest.mark.parametrize("group", [2, 5])
+def test_resize_copies_parts_of_large_pages(dtype, Hkv, page, d, n_pools, group):
+    """Groups just forked write their first tokens behind any number of places."""
+    rr = rrmod()
+    note("resize parts", dtype, Hkv, page, d, n_pools, group)
+    rng = np.random.default_rng(page * group)
+    places = [1, page - 1, page // 2, page, 3, 2 * page, page + 1, 2 * page - 1]  # tokens of the groups
+    B, width = group * len(places), 4
+    table, refs, at = [], [], 0
+    for n in places:
+        held = -(-n // page)
+        row = list(range(at, at + held)) + [-1] * (width - held)
+        at += held
+        refs += [group] * held
+        table += [list(row) for _ in range(group)]
+    n_pages = at + 2 * B
+    refs += [0] * (n_pages - at)
+    new = rng.integers(1, page + 2, B)
+    lengths = [n + int(m) for n, m in zip(np.repeat(places, group), new)]
+    pools = _random_pools(page, n_pools, (n_pages, Hkv, page, d), dtype)
+    copies = _resize(rr, table, lengths, refs, new, pools, page)[3]
+    assert len(copies) == 6 * (group - 1)  # (of the groups whose last page is not full)
+
+
 # -------------------------------------------------------------- all of it
 
 def test_a_long_life_of_a_cache():

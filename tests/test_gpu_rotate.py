@@ -492,3 +492,35 @@ def test_every_call_rounds_the_same_product_first(dtype, inter, d, rot, shift, h
         out = rr.cache_append(flat[:, :1], flat[:, :1], *pools, table, lens, freqs=f, interleaved=inter, Q=flat, **more)
         assert torch.equal(out, got)
         assert torch.equal(pools[0][:, :, 0], got[:, :1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens", [0, 1])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("heads,d,rot", [(17, 128, 64), (9, 256, 128), (5, 512, 128), (40, 96, 32), (3, 1024, 0)])
+def test_large_rotations_of_a_part_of_each_row(dtype, tokens, inter, heads, d, rot):
+    """What is not rotated is copied past the last cache too, and left where it is
+    in place."""
+    rr = rrmod()
+    note("rotate large, a part", dtype, tokens, inter, heads, d, rot)
+    g = torch.Generator(device=DEV).manual_seed(heads + d)
+    n = (260 << 20) // (heads * d * dtype.itemsize) + 3
+    shape = (n, heads, d) if tokens == 0 else (heads, n, d)
+    X = torch.empty(shape, dtype=dtype, device=DEV).normal_(generator=g)
+    positions = torch.randint(0, 9000, (2, n), generator=g, device=DEV).to(torch.int32)
+    axis = torch.randint(0, 2, (rot // 2,), generator=g, device=DEV).to(torch.int32)
+    freqs = 10000.0 ** (-torch.arange(rot // 2, dtype=torch.float64, device=DEV) / max(1, rot // 2))
+    kw = dict(axis=axis, tokens=tokens, interleaved=inter)
+    whole = rr.rotate(X, positions, freqs, **kw)
+    parts = torch.empty_like(X)
+    step = n // 5 + 1
+    for i in range(0, n, step):
+        j = min(i + step, n)
+        rr.rotate(X.narrow(tokens, i, j - i), positions[:, i:j].contiguous(), freqs, out=parts.narrow(tokens, i, j - i), **kw)
+    assert torch.equal(whole, parts)
+    assert torch.equal(whole[..., rot:], X[..., rot:])
+    assert rot == 0 or not torch.equal(whole[..., :rot], X[..., :rot])
+    back = rr.rotate(whole, positions, freqs, inverse=True, **kw)
+    assert torch.equal(back[..., rot:], X[..., rot:])
+    rr.rotate(X, positions, freqs, out=X, **kw)
+    assert torch.equal(whole, X)

@@ -263,3 +263,56 @@ def test_large_batches_are_small_ones(dtype, given):
         a, t = rr.verify_drafts(P[s], drafts[s], u[s], draft_probs=None if Q is None else Q[s])
         assert torch.equal(a, accepted[s])
         assert torch.equal(t, tokens[s])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,n,V", [(33, 1, 131071), (90, 1, 100003), (170, 1, 100500), (340, 1, 100500), (60, 1, 300001),
+                                   (700, 2, 20011), (1100, 1, 9000)])
+@pytest.mark.parametrize("given", [True, False])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_waves_that_sum_several_parts(dtype, B, n, V, given, ragged):
+    """Two to sixteen parts a wave, the last waves with fewer or none, of one, two
+    and four steps; and the same sequences in calls of one part a wave."""
+    rr = rrmod()
+    note("verify several parts", dtype, B, n, V, given, ragged)
+    P, Q, drafts, u = _inputs(B + V, B, n, V, dtype)
+    count = torch.randint(-1, n + 3, (B,), device=DEV).to(torch.int32) if ragged else None
+    Q = Q if given else None
+    accepted, tokens = _check(rr, P, Q, drafts, u, count)
+    step = max(1, 8000 // max(1, -(-V // 256)))
+    for i in range(0, B, step):
+        s = slice(i, min(i + step, B))
+        a, t = rr.verify_drafts(P[s], drafts[s], u[s], draft_probs=None if Q is None else Q[s],
+                                n_drafts=None if count is None else count[s])
+        assert torch.equal(a, accepted[s]) and torch.equal(t, tokens[s])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_past_the_last_cache_as_one_part_a_wave(dtype):
+    rr = rrmod()
+    note("verify past the last cache", dtype)
+    n, V = 3, 50003
+    B = (270 << 20) // ((2 * n + 1) * V * (4 if dtype == "f32" else 2)) + 1
+    P, Q, drafts, u = _inputs(32, B, n, V, dtype)
+    accepted, tokens = rr.verify_drafts(P, drafts, u, draft_probs=Q)
+    for i in range(0, B, 40):  # (of 196 parts, or 98)
+        s = slice(i, min(i + 40, B))
+        a, t = rr.verify_drafts(P[s], drafts[s], u[s], draft_probs=Q[s])
+        assert torch.equal(a, accepted[s]) and torch.equal(t, tokens[s])
+    _check(rr, P[-9:], Q[-9:], drafts[-9:], u[-9:])
+
+
+def test_looked_up_drafts_are_taken_as_often_as_the_target_says():
+    """Each within six standard deviations of its probability."""
+    rr = rrmod()
+    note("verify looked up")
+    B, V = 1 << 17, 8
+    g = torch.Generator(device=DEV).manual_seed(6)
+    p = _probabilities(g, (1, 2, V), "f32", sharp=1.0)
+    drafts = (torch.arange(B, device=DEV) % V).to(torch.int32)
+    u = torch.rand((B, 2), generator=g, device=DEV)
+    a, t = rr.verify_drafts(p.expand(B, 2, V), drafts[:, None].contiguous(), u)
+    for x in range(V):
+        want, k = float(p[0, 0, x]), B // V
+        assert abs(float(a[drafts == x].double().mean()) - want) <= 6 * (want * (1 - want) / k) ** 0.5
+        assert not bool((t[(drafts == x) & (a == 0), 0] == x).any())
