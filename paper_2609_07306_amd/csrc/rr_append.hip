@@ -38,11 +38,17 @@ constexpr int kAppendThreads = 256;
 constexpr int kMostRot = 1024;
 constexpr int kAhead = 2;  // rows that a thread asks for first
 
-// x / scale, correctly rounded, for many x: with r the correctly rounded 1 /
-// scale, q = x r is off by an ulp at most, x - q scale is exact, and q + (x - q
-// scale) r rounds to the quotient (Markstein's theorem).  That takes four
-// instructions where a division takes ten, of which appending has more than of
-// anything else.  Quotients past 1024, which clamp in any case, are not refined
+// x / scale for many x, on the same side of every border between two 8-bit numbers
+// as a division's quotient, in four instructions where a division takes ten, of
+// which appending has more than of anything else.  With r the rounded 1 / scale, q =
+// x r is off by less than 1.5 of its steps; r and the remainder x - q scale are off
+// by 2^-24 relative each, so that q + (x - q scale) r before its own rounding is off
+// by less than 2^-22 steps.  It can then leave a division's side only where x is one
+// of the two binary32 numbers around scale times a border, or scale times half a step
+// beside one.  Borders have 16 significands, and powers of two change nothing within
+// the scales that are not divided by: for all 2^23 significands of scale, those x and
+// the one beyond on either side give a division's quotient bit for bit (1.2e9 pairs,
+// gone through once).  Quotients past 1024, which clamp in any case, are not refined
 // (an infinite one would make a NaN of the remainder); scales so far from one that
 // a remainder could leave the range of normal numbers divide.
 struct Quotient {

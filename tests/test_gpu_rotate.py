@@ -524,3 +524,40 @@ def test_large_rotations_of_a_part_of_each_row(dtype, tokens, inter, heads, d, r
     assert torch.equal(back[..., rot:], X[..., rot:])
     rr.rotate(X, positions, freqs, out=X, **kw)
     assert torch.equal(whole, X)
+
+
+def _at_borders(rng, x):
+    """Scales, one for each number of x, that bring it to a border between two e4m3
+    numbers or as near as binary32 comes: three for each of some borders."""
+    values = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy()
+    t = rng.choice((values[:-1].astype(np.float64) + values[1:]) / 2, x.shape)
+    s = (np.abs(x) / t).astype(np.float32)
+    way = rng.integers(-1, 2, x.shape)
+    return np.where(way < 0, np.nextafter(s, np.float32(0)), np.where(way > 0, np.nextafter(s, np.float32(np.inf)), s))
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("axes", [False, True])
+@pytest.mark.parametrize("d,size", [(64, 1.0), (72, 1e-6), (128, 3e4)])
+def test_quotients_at_the_borders_of_8_bits(inter, axes, d, size):
+    """Keys that are rotated (all 24 bits of a numerator) and values, under scales
+    that bring one of each row next to a border: the bits of a division.  (What a
+    key is before its quotient is what the rotation gives in binary32.)"""
+    rr = rrmod()
+    note("append e4m3 borders", inter, axes, d, size)
+    rng = np.random.default_rng(d)
+    heads, n = 3000, 5
+    K, V = (torch.from_numpy(rng.standard_normal((n, heads, d)).astype(np.float32) * size).bfloat16().to(DEV) for _ in range(2))
+    f = torch.from_numpy(_freqs(d // 2)).to(DEV)
+    pos = torch.arange(100, 100 + n, dtype=torch.int32, device=DEV)
+    keys = rr.rotate(K.float(), pos, f, interleaved=inter).cpu()
+    scales = [torch.from_numpy(_at_borders(rng, x[rng.integers(0, n, heads), np.arange(heads), rng.integers(0, d, heads)].numpy()))
+              for x in (keys, V.float().cpu())]
+    assert bool((torch.cat(scales) > 2.0 ** -60).all())
+    pools = [torch.zeros((105, heads, 1, d), dtype=TYPE["e4m3"], device=DEV) for _ in range(2)]
+    table = torch.arange(105, dtype=torch.int32, device=DEV).view(1, 105)
+    rr.cache_append(K, V, *pools, table, torch.tensor([100 + n], dtype=torch.int32, device=DEV), freqs=f, interleaved=inter,
+                    positions=pos if axes else None, k_scale=scales[0].to(DEV), v_scale=scales[1].to(DEV))
+    for pool, x, s in zip(pools, (keys, V.float().cpu()), scales):
+        want = (x / s[:, None]).clamp(-448.0, 448.0).to(TYPE["e4m3"]).view(torch.uint8)
+        assert torch.equal(pool.view(torch.uint8)[100:, :, 0].cpu(), want)
