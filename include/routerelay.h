@@ -456,8 +456,9 @@ typedef struct {
  * of this library, [n_heads, n_tokens, d], has x_head = n_tokens * d and x_token
  * = d.  With inverse = 1 rows are turned back, which is also the gradient of
  * the rotation.  Y may be X where its strides are X's, and must not overlap it
- * otherwise.  Returns RR_ERR_INVALID for bad sizes, types, strides or NULL
- * pointers, RR_ERR_UNSUPPORTED for 2^24 tokens or heads or more. */
+ * otherwise.  Returns RR_ERR_INVALID for bad sizes, types, strides (rows of Y that
+ * overlap each other among them) or NULL pointers, RR_ERR_UNSUPPORTED for 2^24
+ * tokens or heads or more. */
 rr_status rr_rotate(const rr_rotate_config *cfg, const void *X, const double *freqs, const rr_axes *axes, void *Y,
                     void *hip_stream);
 

@@ -8,6 +8,7 @@
 #include <cstring>
 #include <mutex>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "routerelay.h"
@@ -986,6 +987,24 @@ rr_status check_axes(const rr_axes *axes, int32_t n_tokens)
     return RR_OK;
 }
 
+// Whether two rows of d elements, of those at i * a + h * b for i < na and h < nb,
+// share one (a and b at least d, where there are several).
+bool rows_overlap(int64_t a, int32_t na, int64_t b, int32_t nb, int32_t d)
+{
+    if (na < 2 || nb < 2) return false;
+    if (a > b) {
+        std::swap(a, b);
+        std::swap(na, nb);
+    }
+    // (the rows of a step of b lie behind all those of the step before it in most layouts)
+    const __int128 span = (__int128)(na - 1) * a + d;
+    for (__int128 at = b; at < span && at <= (__int128)(nb - 1) * b; at += b) {
+        const int64_t before = (int64_t)(at / a), off = (int64_t)(at % a);
+        if ((before < na && off < d) || (before + 1 < na && a - off < d)) return true;
+    }
+    return false;
+}
+
 rr::Axes axes_of(const rr_axes *axes, int32_t n_tokens)
 {
     return rr::Axes{axes->positions, axes->axis, n_tokens, axes->n_axes, axes->real};
@@ -1191,6 +1210,8 @@ rr_status rr_rotate(const rr_rotate_config *cfg, const void *X, const double *fr
     if (c.x_token < 0 || c.x_head < 0) return fail(RR_ERR_INVALID, "x_token and x_head must be >= 0");
     if ((c.n_tokens > 1 && c.y_token < c.d) || (c.n_heads > 1 && c.y_head < c.d))
         return fail(RR_ERR_INVALID, "rows of Y must be at least d elements apart");
+    if (rows_overlap(c.y_token, c.n_tokens, c.y_head, c.n_heads, c.d))
+        return fail(RR_ERR_INVALID, "rows of Y must not overlap");
     if (c.rot > 0) {
         if (!freqs) return fail(RR_ERR_INVALID, "freqs must hold rot / 2 frequencies");
         if (!axes) return fail(RR_ERR_INVALID, "axes must be given");

@@ -300,3 +300,25 @@ def test_a_verification_s_workspace_serves_smaller_ones():
             assert got == sorted(got) and got[0] > 65536
     for v in sizes:
         assert need(7, v, rr.RR_BF16) <= need(7, v, rr.RR_F32) <= need(8, v, rr.RR_F32)
+
+
+def test_rotate_refuses_rows_that_overlap():
+    """Each element of Y is of one row at most: against the rows laid out (where they
+    are not, no tokens or a NULL pointer ends the call before anything is launched)."""
+    rr = _rr()
+    d = 8
+    for tokens in (1, 2, 3, 5):
+        for heads in (1, 2, 4):
+            for y_token in range(d, 5 * d + 2):
+                for y_head in range(d, 5 * d + 2, 1 if tokens * heads < 9 else 3):
+                    at = [i * y_token + h * y_head + e for i in range(tokens) for h in range(heads) for e in range(d)]
+                    status = _rotate(rr, X=None, n_tokens=tokens, n_heads=heads, d=d, rot=d, y_token=y_token, y_head=y_head)
+                    assert status == -1
+                    overlap = b"overlap" in rr.lib.rr_last_error()
+                    assert overlap == (len(set(at)) < len(at)), (tokens, heads, y_token, y_head)
+    # the largest calls: one after the other, and shifted by less than a row
+    many = (1 << 24) - 1
+    for y_token, y_head, overlap in ((128, 128 * many, False), (128 * many, 128, False), (128, 128 * many - 1, True),
+                                     (1 << 62, 1 << 62, True), ((1 << 62) - 64, 1 << 62, True), (129, 129 * 2, True)):
+        assert _rotate(rr, X=None, n_tokens=many, n_heads=many, y_token=y_token, y_head=y_head) == -1
+        assert (b"overlap" in rr.lib.rr_last_error()) == overlap, (y_token, y_head)
