@@ -515,9 +515,10 @@ def _of(name, t, shape, dtype):
 
 def _lists(page_table, lengths):
     """The addresses of page_table [B, max_pages] and lengths [B], and their sizes."""
-    if page_table.dim() != 2:
+    shape = page_table.shape
+    if len(shape) != 2:
         raise ValueError("page_table must be [B, max_pages]")
-    B, most = page_table.shape
+    B, most = shape
     if page_table.dtype != torch.int32 or lengths.dtype != torch.int32 or lengths.shape != (B,):
         raise ValueError(f"page_table [B, max_pages] and lengths [B] must be int32: got {page_table.dtype} of shape "
                          f"{list(page_table.shape)}, {lengths.dtype} of shape {list(lengths.shape)}")
@@ -562,7 +563,7 @@ def _rows_of(name, t, shape, dtype):
 def _axes_of(positions, axis, rot, n):
     """rr_axes of positions [n_axes, n] (or [n]) int32 or float32 and axis [rot / 2] int32."""
     kind = positions.dtype
-    if kind not in (torch.int32, torch.float32):
+    if kind != torch.int32 and kind != torch.float32:
         raise TypeError("positions must be int32 or float32")
     shape = positions.shape
     if not shape or shape[-1] != n or len(shape) > 2 or (len(shape) == 2 and not shape[0]):
@@ -590,8 +591,11 @@ def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, fr
     if len(shape) != 3 or kind not in (torch.float32, torch.bfloat16):
         raise TypeError("K must be a [n_tokens, H_kv, d] float32 or bfloat16 tensor")
     (n_pages, Hkv, page, d), cache, kc, vc, ks, vs = _cache_of(K_cache, V_cache, kind, k_scale, v_scale)
-    tensors = (K, V, K_cache, V_cache, page_table, lengths, seq_start, freqs, Q, Q_out, k_scale, v_scale)
-    dev = _device_of(tensors if positions is None else (*tensors, positions, axis))
+    if positions is None:
+        dev = _device_of((K, V, K_cache, V_cache, page_table, lengths, seq_start, freqs, Q, Q_out, k_scale, v_scale))
+    else:
+        dev = _device_of((K, V, K_cache, V_cache, page_table, lengths, seq_start, freqs, Q, Q_out, k_scale, v_scale, positions,
+                          axis))
     n = shape[0]
     rows = (n, Hkv, d)
     ldk, ldv = _rows_of("K", K, rows, kind), _rows_of("V", V, rows, kind)
@@ -599,8 +603,9 @@ def cache_append(K, V, K_cache, V_cache, page_table, lengths, seq_start=None, fr
     H = ldq = rot = 0
     f = q = out = start = None
     if freqs is not None:
-        rot = 2 * freqs.numel()
-        f = _of("freqs", freqs, (rot // 2,), torch.float64)
+        half = freqs.numel()
+        rot = 2 * half
+        f = _of("freqs", freqs, (half,), torch.float64)
     if seq_start is not None:
         start = _of("seq_start", seq_start, (B + 1,), torch.int32)
     if Q is not None:
@@ -652,8 +657,9 @@ def rotate(X, positions, freqs, axis=None, tokens=0, interleaved=False, inverse=
     if tokens not in (0, 1):
         raise ValueError("tokens must be 0 or 1")
     dev = _device_of((X, positions, freqs, axis, out))
-    n, rot = shape[tokens], 2 * freqs.numel()
-    f = _of("freqs", freqs, (rot // 2,), torch.float64)
+    n, half = shape[tokens], freqs.numel()
+    rot = 2 * half
+    f = _of("freqs", freqs, (half,), torch.float64)
     axes = _axes_of(positions, axis, rot, n)
     if out is None:
         out = _empty(shape, kind, X, stream)
@@ -687,7 +693,7 @@ def _paged_config(Q, K_cache, V_cache, page_table, routes, n_sink, n_recent, n_p
         k = routes.shape[1]
         if k == n_sink == n_recent == 0:
             k = 1  # (a slot that names no page, _some_routes: the library takes k = 0 alone for no routes)
-    if n_sink or n_recent or n_prefix:
+    if not 0 <= n_sink | n_recent | n_prefix <= _MOST:
         _fits(n_sink, n_recent, n_prefix)
     if n_pages | Hkv | page | d | B | most | nq | H | k > _MOST:
         _fits(n_pages, Hkv, page, d, B, most, nq, H, k)
@@ -886,7 +892,8 @@ def cache_compact(pools, page_table, refs, new_ids=None, n_used=None, workspace=
     if page_table.dim() != 2:
         raise ValueError("page_table must be [B, max_pages]")
     B, most = page_table.shape
-    _fits(B, most)
+    if B | most > _MOST:
+        _fits(B, most)
     table = _of("page_table", page_table, (B, most), torch.int32)
     n_pages = pools.shape[0]
     r = _refs(refs, n_pages)
@@ -949,9 +956,10 @@ def verify_drafts(P, drafts, uniforms, draft_probs=None, n_drafts=None, lengths=
     1]) int32: how many were taken; they, the token drawn after them, then -1.
     P and draft_probs may be views whose rows lie apart.  workspace:
     verify_workspace(P), or None for one of this call's own."""
-    if drafts.dim() != 2:
+    shape = drafts.shape
+    if len(shape) != 2:
         raise ValueError("drafts must be [B, n_drafts]")
-    B, n = drafts.shape
+    B, n = shape
     dev = _device_of((P, drafts, uniforms, draft_probs, n_drafts, lengths, accepted, tokens, workspace))
     cfg = _verify_config(P, n, draft_probs)
     i32 = torch.int32
