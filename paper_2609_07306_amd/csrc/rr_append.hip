@@ -20,7 +20,7 @@
 // the heads that it goes through, so it reads its sines and cosines once; a
 // piece is 16 bytes of input (an element, or two interleaved ones, where rows
 // are not aligned to that).  What hides the chain are many waves and rows that
-// are asked for before it: a kernel of 44 to 66 registers and pieces of 16 bytes
+// are asked for before it: a kernel of 37 to 66 registers and pieces of 16 bytes
 // takes 98 us for the ragged prompts where one of 87 and pieces of 8 took 121.
 #include <hip/hip_runtime.h>
 

@@ -575,9 +575,9 @@ constexpr int kCopyThreads = 256;
 
 // How pages are copied.  Compaction reads every page once and leaves little to
 // other calls, so both ways go past the caches, and workgroups are many: 600
-// pages of 128 KB in four pools (629 MB) in 111 us, 5.6 TB/s; four pieces a
-// thread and 8192 workgroups 117, with stores alone past the caches 120, none
-// 125.  Copies of a page that several sequences share read it again, from the
+// pages of 128 KB in four pools (629 MB) in 111 us, 5.6 TB/s (116 in a trace); four
+// pieces a thread and 8192 workgroups 117, with stores alone past the caches 120,
+// none 125.  Copies of a page that several sequences share read it again, from the
 // caches; most calls have none to make, and fewer workgroups are sooner through
 // (an empty launch of 4096 takes 2.3 us, of 8192 3.9): half a page of 16 pools,
 // three times each for 32 groups (31 MB read, 92 written), in 23.5 us, 5.2 TB/s;

@@ -5,7 +5,7 @@
 // Bound by the bytes, every row read once and written once; how near to that it
 // comes goes by the order: workgroups that follow each other in memory, each
 // with a short stretch of its own, move 32768 tokens of 32 heads (128 bf16
-// features, 268 MB each way) in 92 us heads first and 89 tokens first, 5.8 and
+// features, 268 MB each way) in 92 us heads first and 90 tokens first, 5.8 and
 // 6.0 TB/s; a workgroup that takes 32 tokens of every head in turn in 122.  So
 // there is a kernel for each layout.  Loads and stores of such calls go past the
 // caches.  A small call (196 tokens, 6 heads) is a launch and a chain, 3.1 us.
@@ -203,7 +203,7 @@ hipError_t launch_rotate(const RotateArgs &args, int dtype, bool interleaved, hi
     auto go = [&](auto by_heads, auto by_tokens, Units un) {
         if (by_token) {
             // Tokens a workgroup: two turns of its threads (32768 tokens of 32 heads:
-            // two tokens 87 us, four 90, eight 98; of 2 heads of 64: 16 tokens 10 us,
+            // two tokens 90 us, four 91, eight 103; of 2 heads of 64: 16 tokens 9 us,
             // four 18), as long as there are workgroups for the card; then heads are
             // shared out too.
             const int lanes = un.all < kRotateThreads ? un.all : kRotateThreads, rows = kRotateThreads / lanes;
