@@ -194,8 +194,10 @@ class Config:
         return self.m + self.r + self.n_sink + self.n_recent
 
     def c(self) -> _Config:
-        _fits(self.n_heads, self.n_kv_heads, self.n_q, self.n_k, self.d, self.k, self.m, self.r, self.n_sink, self.n_recent,
-              self.min_reuse)
+        sizes = (self.n_heads, self.n_kv_heads, self.n_q, self.n_k, self.d, self.k, self.m, self.r, self.n_sink,
+                 self.n_recent, self.min_reuse)
+        if min(sizes) < 0 or max(sizes) > _MOST:
+            _fits(*sizes)
         g = None
         if self.gamma_rows is not None:
             t = self.gamma_rows
